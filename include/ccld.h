@@ -26,7 +26,7 @@
  *    capacity CAP starts at table + c*CAP.  Unsigned fields (seq, bytes) are
  *    stored bit-for-bit.  When a table is too small its list is truncated, its
  *    count is still exact, and the status is CCLD_W_TRUNCATED.
- *  - All arithmetic is 64-bit integer; products are compared in 128 bits.
+ *  - All arithmetic of the analysis is 64-bit integer; products are compared in 128 bits.
  */
 #ifndef CCLD_H
 #define CCLD_H
@@ -400,6 +400,44 @@ enum { CCLD_PROF_INGEST, CCLD_PROF_SORT_HIST, CCLD_PROF_SORT_SCAN, CCLD_PROF_SOR
        CCLD_PROF_NCLASS = 16 };
 ccld_status ccld_profile_enable(ccld_ctx *ctx, int32_t on);
 ccld_status ccld_profile_read(ccld_ctx *ctx, double *ms, uint64_t *launches, uint64_t *sort_passes);
+
+/* ---- The computation between collectives -----------------------------------------------------------
+ * What a rank of a training job computes between two collectives, as operators to run on the card that
+ * the analysis names: a rank is computation-slow (Section 2.2, S1) because its card is slow or because it
+ * was given more work, and these are the kinds of work that are uneven by design (experts with different
+ * numbers of rows, the loss that only the last pipeline stage has) or that only memory bounds (norms).
+ *
+ * They need no context.  Arguments are checked before anything is enqueued; work goes to `stream` (a
+ * hipStream_t) of the current device and the call returns before it is done.  Nothing is allocated: where a
+ * workspace is needed its size comes from the query beside the call, and it may be reused as soon as the
+ * stream has passed the call.  Matrices are row-major with unit stride within a row; ld* is the number of
+ * elements between rows.  Elements are CCLD_BF16 or CCLD_FP16; sums are held in 32
+ * bits and rounded once.  Results do not depend on the order in which workgroups run. */
+enum { CCLD_BF16 = 0, CCLD_FP16 = 1 };
+
+/* Products grouped by expert: rows offsets[e] .. offsets[e + 1) - 1 of x belong to expert e.
+ *   y[r] = x[r] w[e]^T      dx[r] = dy[r] w[e]      dw[e] = sum over its rows of dy[r]^T x[r]
+ * Rows before offsets[0] and from offsets[n_experts] on belong to nobody: their y and dx are zero and they
+ * have no part in dw, whatever they hold.  dw of an expert without rows is zero.  Offsets are read on the
+ * device (no host wait); they must not decrease, and are clamped to [0, rows]. */
+typedef struct {
+  int32_t dtype;
+  int32_t offsets_bits;              /* 32 or 64: signed integers                                       */
+  int64_t rows, k, n, n_experts;     /* rows may be 0; each below 2^31, and k, n < 2^22                 */
+  const void *x;                     /* [rows][k]                                                       */
+  const void *w;                     /* [n_experts][n][k], expert_stride elements between experts       */
+  const void *offsets;               /* [n_experts + 1]                                                 */
+  const void *dy;                    /* [rows][n]: gradient of y (grad call)                            */
+  void *y;                           /* [rows][n] out (product call)                                    */
+  void *dx;                          /* [rows][k] out, or NULL (grad call)                              */
+  void *dw;                          /* [n_experts][n][k] contiguous, out, or NULL (grad call)          */
+  int64_t ldx, ldw, expert_stride, lddy, ldy, lddx;
+  void *workspace;                   /* aligned to 256 bytes; may be NULL where the query gives 0       */
+  uint64_t workspace_bytes;
+} ccld_expert_args;
+ccld_status ccld_expert_workspace(const ccld_expert_args *a, int32_t grad, uint64_t *bytes);
+ccld_status ccld_expert_product(const ccld_expert_args *a, void *stream);
+ccld_status ccld_expert_product_grad(const ccld_expert_args *a, void *stream);
 
 const char *ccld_status_str(ccld_status s);
 

@@ -114,7 +114,8 @@ EXPORTS = ("ccld_profile_enable", "ccld_profile_read", "ccld_default_params", "c
            "ccld_reset_window", "ccld_analyze_window", "ccld_flag_chains", "ccld_rank_blame", "ccld_locate_hang",
            "ccld_locate_hang_static",
            "ccld_progress_rates",
-           "ccld_decode_frames", "ccld_reset_frames", "ccld_status_str")
+           "ccld_decode_frames", "ccld_reset_frames", "ccld_status_str",
+           "ccld_expert_workspace", "ccld_expert_product", "ccld_expert_product_grad")
 
 
 def lib() -> C.CDLL:
@@ -142,6 +143,9 @@ def lib() -> C.CDLL:
         L.ccld_reset_frames.argtypes = [vp]
         L.ccld_profile_enable.argtypes = [vp, C.c_int32]
         L.ccld_profile_read.argtypes = [vp, vp, vp, vp]
+        L.ccld_expert_workspace.argtypes = [vp, C.c_int32, vp]
+        L.ccld_expert_product.argtypes = [vp, vp]
+        L.ccld_expert_product_grad.argtypes = [vp, vp]
         L.ccld_status_str.argtypes = [C.c_int32]
         L.ccld_status_str.restype = C.c_char_p
         for name in EXPORTS:

@@ -1,0 +1,334 @@
+// Matrix products grouped by expert, with ragged numbers of rows, and their gradients (ccld_expert_*).
+//
+//   y[r] = x[r] w_e^T      dx[r] = dy[r] w_e      dw_e = sum over e's rows of dy[r]^T x[r]
+//
+// One launch for all experts: the host knows how many rows there are but not whose, so it launches as many workgroups as the
+// worst division of the rows needs and each finds its tile in the offsets (a prefix sum over the experts' tile counts by a
+// wavefront); those beyond the last tile end at once.  What bounds the kernels: the matrix cores from about 128 rows for
+// an expert on, reading the experts' weights below that.
+#include <algorithm>
+
+#include "ccld_internal.h"
+#include "products.h"
+#include "tiles.h"
+
+using namespace ccld;
+
+namespace {
+
+extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+
+struct Offsets {
+  const void* at; int bits; int rows; u32 n_experts;
+  __device__ __forceinline__ int get(u32 e) const {
+    const i64 v = bits == 64 ? static_cast<const i64*>(at)[e] : (i64)static_cast<const i32*>(at)[e];
+    return v < 0 ? 0 : v > rows ? rows : (int)v;
+  }
+  // rows of a part: the experts, then the rows before the first and after the last one, which are nobody's
+  __device__ __forceinline__ int2 range(u32 e) const {
+    if (e < n_experts) { const int a = get(e), b = get(e + 1); return make_int2(a, b > a ? b : a); }
+    return e == n_experts ? make_int2(0, get(0)) : make_int2(get(n_experts), rows);
+  }
+};
+
+struct RowJob {              // y or dx
+  const void *a, *w;         // x or dy; the weights
+  void* out;
+  float* part;               // [splits][rows][cols] sums of the splits, or null: `out` is written
+  Offsets off;
+  i64 lda, ldw, estride, ldo;
+  int cols, depth, split_depth;
+  u32 col_tiles;
+  bool wide;
+};
+
+struct WeightJob {           // dw
+  const void *dy, *x;
+  void* out;
+  float* part;               // [splits][n_experts][n][k]
+  Offsets off;
+  i64 lddy, ldx;
+  int n, k;
+  u32 n_tiles, k_tiles;
+};
+
+// The tile of a workgroup: the part that it belongs to, that part's first m-tile (of BM rows, counted over all parts), number of m-tiles and
+// rows, and the tile's number within it.  part is n_experts + 2 for workgroups beyond the last tile.  Every wavefront finds it by
+// itself, 64 parts at a time: once for the number of tiles, which the XCDs share evenly, and once for its own.
+struct Place { u32 part, at, tiles; int2 range; };
+template <int BM>
+__device__ __forceinline__ Place find_tile(const Offsets& off, u32 block, u32 col_tiles) {
+  const u32 parts = off.n_experts + 2, lane = lane_id();
+  auto part_tiles = [&](u32 e, int2& r) {
+    r = e < parts ? off.range(e) : make_int2(0, 0);
+    return (u32)(r.y - r.x + BM - 1) / BM;
+  };
+  int2 r;
+  u32 total = 0;
+  for (u32 base = 0; base < parts; base += CCLD_WAVE)
+    total += __builtin_amdgcn_readlane((int)wave_inclusive_sum(part_tiles(base + lane, r)), CCLD_WAVE - 1);
+  const Place none{parts, 0, 0, make_int2(0, 0)};
+  if (block >= total * col_tiles) return none;
+  const u32 id = xcd_order(block, total * col_tiles);
+  u32 before = 0;
+  for (u32 base = 0; base < parts; base += CCLD_WAVE) {
+    const u32 t = part_tiles(base + lane, r), incl = before + wave_inclusive_sum(t);
+    const u64 hit = ballot64(id < incl * col_tiles);
+    if (hit) {
+      const int src = __builtin_ctzll(hit);
+      Place p;
+      p.part = base + src;
+      p.tiles = __builtin_amdgcn_readlane((int)t, src);
+      p.at = id - (__builtin_amdgcn_readlane((int)incl, src) - p.tiles) * col_tiles;
+      p.range = make_int2(__builtin_amdgcn_readlane(r.x, src), __builtin_amdgcn_readlane(r.y, src));
+      return p;
+    }
+    before = __builtin_amdgcn_readlane((int)incl, CCLD_WAVE - 1);
+  }
+  return none;
+}
+
+template <class C, class T, bool W_ACROSS, bool DIRECT>
+__global__ __launch_bounds__(C::THREADS) void k_expert_rows(RowJob j) {
+  const Place p = find_tile<C::BM>(j.off, blockIdx.x, j.col_tiles);
+  if (p.part >= j.off.n_experts + 2) return;
+  const uint2 t = grouped_order(p.at, p.tiles, j.col_tiles, 8);
+  const int row0 = p.range.x + (int)t.x * C::BM, col0 = (int)t.y * C::BN;
+  const int c0 = (int)blockIdx.y * j.split_depth;
+  int depth = min(j.split_depth, j.depth - c0);
+  if (p.part >= j.off.n_experts || depth < 0) depth = 0;       // nobody's rows: zeros
+  const u32 e = p.part < j.off.n_experts ? p.part : 0;
+  const int rows = min(C::BM, p.range.y - row0), cols = min(C::BN, j.cols - col0);
+  const T* w = static_cast<const T*>(j.w) + (i64)e * j.estride + (W_ACROSS ? (i64)c0 * j.ldw + col0 : (i64)col0 * j.ldw + c0);
+  TileProduct<C, T, false, W_ACROSS, DIRECT> prod;
+  prod.run(lds, static_cast<const T*>(j.a) + (i64)row0 * j.lda + c0, j.lda, rows, w, j.ldw, cols, depth);
+  if (j.part) {
+    float* o = j.part + ((i64)blockIdx.y * j.off.rows + row0) * j.cols + col0;
+    prod.each([&](u32 m, u32 n, f32x4 v) { if ((int)m < rows) store4(o + (i64)m * j.cols + n, v, cols - (int)n, j.cols % 4 == 0); });
+  } else {
+    T* o = static_cast<T*>(j.out) + (i64)row0 * j.ldo + col0;
+    prod.each([&](u32 m, u32 n, f32x4 v) { if ((int)m < rows) store4(o + (i64)m * j.ldo + n, v, cols - (int)n, j.wide); });
+  }
+}
+
+template <class C, class T, bool DIRECT>
+__global__ __launch_bounds__(C::THREADS) void k_expert_weights(WeightJob j) {
+  const u32 id = xcd_order(blockIdx.x, gridDim.x), each = j.n_tiles * j.k_tiles, e = id / each;
+  const uint2 t = grouped_order(id - e * each, j.n_tiles, j.k_tiles, 8);
+  const int n0 = (int)t.x * C::BM, k0 = (int)t.y * C::BN;
+  const int2 r = j.off.range(e);
+  // this split's rows: an equal share, in whole stages
+  const int share = ((r.y - r.x + (int)gridDim.y - 1) / (int)gridDim.y + DEPTH - 1) / DEPTH * DEPTH;
+  const i64 first = r.x + (i64)blockIdx.y * share;
+  const int depth = (int)max((i64)0, min((i64)share, r.y - first));
+  const i64 at = depth ? first : 0;
+  const int ns = min(C::BM, j.n - n0), ks = min(C::BN, j.k - k0);
+  TileProduct<C, T, true, true, DIRECT> prod;
+  prod.run(lds, static_cast<const T*>(j.dy) + at * j.lddy + n0, j.lddy, ns, static_cast<const T*>(j.x) + at * j.ldx + k0, j.ldx,
+           ks, depth);
+  const i64 o = ((i64)e * j.n + n0) * j.k + k0;
+  if (j.part) {
+    float* q = j.part + (i64)blockIdx.y * j.off.n_experts * j.n * j.k + o;
+    prod.each([&](u32 m, u32 n, f32x4 v) { if ((int)m < ns) store4(q + (i64)m * j.k + n, v, ks - (int)n, j.k % 4 == 0); });
+  } else {
+    T* q = static_cast<T*>(j.out) + o;
+    prod.each([&](u32 m, u32 n, f32x4 v) { if ((int)m < ns) store4(q + (i64)m * j.k + n, v, ks - (int)n, j.k % 4 == 0); });
+  }
+}
+
+using Large = Tiling<256, 256, 2, 4, 2>;
+using Medium = Tiling<128, 128, 2, 2, 2>;
+using Few = Tiling<32, 128, 1, 4, 4>;
+
+u64 div_up(u64 a, u64 b) { return (a + b - 1) / b; }
+
+// How the rows' products are cut: tile size by the rows that an expert has on average, and the contraction in several parts
+// where the tiles alone leave compute units idle.
+struct RowPlan { int bm, bn; u32 col_tiles; u64 groups; u32 splits; int split_depth; };
+RowPlan plan_rows(u64 rows, u64 experts, int cols, int depth) {
+  RowPlan p;
+  const u64 busy = std::min(rows, experts), mean = rows / std::max<u64>(experts, 1);
+  p.bm = mean >= 512 ? 256 : mean >= 48 ? 128 : 32;
+  p.bn = p.bm == 256 ? 256 : 128;
+  p.col_tiles = (u32)div_up(cols, p.bn);
+  // tiles of the worst division: every part may end in a tile of its own
+  p.groups = (rows / p.bm + std::min(rows, experts + 2)) * p.col_tiles;
+  const u64 tiles = std::max<u64>(div_up(rows, p.bm), busy) * p.col_tiles, steps = div_up(depth, DEPTH);
+  u64 s = 1;
+  while (tiles * s < COMPUTE_UNITS && steps / (2 * s) >= 8) s *= 2;
+  p.split_depth = (int)(div_up(steps, s) * DEPTH);
+  p.splits = (u32)div_up(steps, div_up(steps, s));
+  return p;
+}
+
+struct WeightPlan { int bm, bn; u32 n_tiles, k_tiles, splits; };
+WeightPlan plan_weights(u64 rows, u64 experts, int n, int k) {
+  WeightPlan p;
+  p.bm = p.bn = experts * div_up(n, 256) * div_up(k, 256) >= COMPUTE_UNITS ? 256 : 128;
+  p.n_tiles = (u32)div_up(n, p.bm);
+  p.k_tiles = (u32)div_up(k, p.bn);
+  const u64 tiles = experts * p.n_tiles * p.k_tiles, steps = div_up(rows, experts * DEPTH);
+  u32 s = 1;
+  while (tiles * s < COMPUTE_UNITS && steps / (2 * s) >= 8) s *= 2;
+  p.splits = s;
+  return p;
+}
+
+// 16-byte pieces lie wholly inside or outside the operands, and start on 16 bytes
+bool direct(const ccld_expert_args* a, const void* rows_at, i64 ld) {
+  return a->k % 8 == 0 && a->n % 8 == 0 && a->ldw % 8 == 0 && a->expert_stride % 8 == 0 && ld % 8 == 0 && aligned(a->w, 16) &&
+         aligned(rows_at, 16);
+}
+
+ccld_status check(const ccld_expert_args* a, bool grad) {
+  if (!a) return CCLD_E_NULL;
+  if ((a->dtype != CCLD_BF16 && a->dtype != CCLD_FP16) || (a->offsets_bits != 32 && a->offsets_bits != 64)) return CCLD_E_BAD_ARG;
+  if (a->rows < 0 || a->k < 1 || a->n < 1 || a->n_experts < 1) return CCLD_E_BAD_ARG;
+  if (a->rows >= MAX_ROWS || a->n_experts >= MAX_EXPERTS || a->k >= MAX_WIDTH || a->n >= MAX_WIDTH) return CCLD_E_CAPACITY;
+  if (a->ldw < a->k || a->expert_stride < 0 || a->ldx < a->k) return CCLD_E_BAD_ARG;
+  if (a->ldw >= MAX_LD || a->ldx >= MAX_LD) return CCLD_E_CAPACITY;
+  if (grad) {
+    if (a->lddy < a->n || (a->dx && a->lddx < a->k)) return CCLD_E_BAD_ARG;
+    if (a->lddy >= MAX_LD) return CCLD_E_CAPACITY;
+  } else if (a->ldy < a->n) return CCLD_E_BAD_ARG;
+  // a launch has less than 2^32 threads
+  const bool rows_product = !grad || a->dx;
+  if (rows_product && plan_rows(a->rows, a->n_experts, (int)(grad ? a->k : a->n), (int)(grad ? a->n : a->k)).groups >= MAX_GROUPS) return CCLD_E_CAPACITY;
+  if (grad && a->dw) {
+    const WeightPlan p = plan_weights(a->rows, a->n_experts, (int)a->n, (int)a->k);
+    if ((u64)a->n_experts * p.n_tiles * p.k_tiles >= MAX_GROUPS) return CCLD_E_CAPACITY;
+  }
+  return CCLD_OK;
+}
+
+ccld_status check_pointers(const ccld_expert_args* a, bool grad) {
+  if (!a->offsets || !a->w) return CCLD_E_NULL;
+  if (a->rows && (grad ? !a->dy || (a->dw && !a->x) : !a->x || !a->y)) return CCLD_E_NULL;
+  if (!aligned(a->offsets, a->offsets_bits / 8)) return CCLD_E_BAD_ARG;
+  for (const void* p : {a->x, a->w, a->dy, (const void*)a->y, (const void*)a->dx, (const void*)a->dw})
+    if (!aligned(p, 2)) return CCLD_E_BAD_ARG;
+  uint64_t need = 0;
+  const ccld_status s = ccld_expert_workspace(a, grad, &need);
+  if (s != CCLD_OK) return s;
+  if (need && (!a->workspace || !aligned(a->workspace, 256) || a->workspace_bytes < need)) return CCLD_E_WORKSPACE;
+  return CCLD_OK;
+}
+
+u64 row_part_bytes(const RowPlan& p, u64 rows, u64 cols) { return p.splits > 1 ? 4 * p.splits * rows * cols : 0; }
+u64 weight_part_bytes(const WeightPlan& p, u64 experts, u64 n, u64 k) { return p.splits > 1 ? 4 * p.splits * experts * n * k : 0; }
+
+template <class C, class T, bool W_ACROSS, bool DIRECT>
+void launch_rows(const RowJob& j, const RowPlan& p, hipStream_t stream) {
+  k_expert_rows<C, T, W_ACROSS, DIRECT><<<dim3((u32)p.groups, p.splits), C::THREADS, C::LDS_BYTES, stream>>>(j);
+}
+template <class T, bool W_ACROSS, bool DIRECT>
+void launch_rows(const RowJob& j, const RowPlan& p, hipStream_t stream) {
+  if (p.bm == 256) launch_rows<Large, T, W_ACROSS, DIRECT>(j, p, stream);
+  else if (p.bm == 128) launch_rows<Medium, T, W_ACROSS, DIRECT>(j, p, stream);
+  else launch_rows<Few, T, W_ACROSS, DIRECT>(j, p, stream);
+}
+
+template <class T>
+ccld_status product_of_rows(const ccld_expert_args* a, bool grad, hipStream_t stream) {
+  const int cols = (int)(grad ? a->k : a->n), depth = (int)(grad ? a->n : a->k);
+  const RowPlan p = plan_rows(a->rows, a->n_experts, cols, depth);
+  RowJob j{};
+  j.a = grad ? a->dy : a->x;
+  j.lda = grad ? a->lddy : a->ldx;
+  j.w = a->w;
+  j.out = grad ? a->dx : a->y;
+  j.ldo = grad ? a->lddx : a->ldy;
+  j.part = p.splits > 1 ? static_cast<float*>(a->workspace) : nullptr;
+  j.off = Offsets{a->offsets, a->offsets_bits, (int)a->rows, (u32)a->n_experts};
+  j.ldw = a->ldw; j.estride = a->expert_stride;
+  j.cols = cols; j.depth = depth; j.split_depth = p.split_depth; j.col_tiles = p.col_tiles;
+  j.wide = j.ldo % 4 == 0 && aligned(j.out, 8);
+  const bool d = direct(a, j.a, j.lda);
+  if (grad) d ? launch_rows<T, true, true>(j, p, stream) : launch_rows<T, true, false>(j, p, stream);
+  else d ? launch_rows<T, false, true>(j, p, stream) : launch_rows<T, false, false>(j, p, stream);
+  if (j.part) launch_join(j.part, p.splits, (u64)a->rows, (u64)cols, j.out, j.ldo, a->dtype, stream);
+  return launched();
+}
+
+template <class C, class T>
+void launch_weights(const WeightJob& j, const WeightPlan& p, bool d, hipStream_t stream) {
+  const dim3 grid((u32)(j.off.n_experts * (u64)p.n_tiles * p.k_tiles), p.splits);
+  if (d) k_expert_weights<C, T, true><<<grid, C::THREADS, C::LDS_BYTES, stream>>>(j);
+  else k_expert_weights<C, T, false><<<grid, C::THREADS, C::LDS_BYTES, stream>>>(j);
+}
+
+template <class T>
+ccld_status product_of_weights(const ccld_expert_args* a, hipStream_t stream) {
+  const WeightPlan p = plan_weights(a->rows, a->n_experts, (int)a->n, (int)a->k);
+  WeightJob j{};
+  j.dy = a->dy; j.x = a->x; j.out = a->dw;
+  j.part = p.splits > 1 ? static_cast<float*>(a->workspace) : nullptr;
+  j.off = Offsets{a->offsets, a->offsets_bits, (int)a->rows, (u32)a->n_experts};
+  j.lddy = a->lddy; j.ldx = a->ldx; j.n = (int)a->n; j.k = (int)a->k;
+  j.n_tiles = p.n_tiles; j.k_tiles = p.k_tiles;
+  const bool d = direct(a, a->dy, a->lddy) && a->ldx % 8 == 0 && aligned(a->x, 16) && aligned(a->dw, 16);
+  if (p.bm == 256) launch_weights<Large, T>(j, p, d, stream);
+  else launch_weights<Medium, T>(j, p, d, stream);
+  if (j.part) launch_join(j.part, p.splits, (u64)a->n_experts * a->n, (u64)a->k, j.out, a->k, a->dtype, stream);
+  return launched();
+}
+
+template <class T>
+hipError_t allow_tiles() {
+  hipError_t e = hipSuccess;
+  auto allow = [&](auto k, int bytes) { if (e == hipSuccess) e = allow_lds(reinterpret_cast<const void*>(k), bytes); };
+  allow(&k_expert_rows<Large, T, false, true>, Large::LDS_BYTES);
+  allow(&k_expert_rows<Large, T, false, false>, Large::LDS_BYTES);
+  allow(&k_expert_rows<Large, T, true, true>, Large::LDS_BYTES);
+  allow(&k_expert_rows<Large, T, true, false>, Large::LDS_BYTES);
+  allow(&k_expert_rows<Few, T, false, true>, Few::LDS_BYTES);
+  allow(&k_expert_rows<Few, T, false, false>, Few::LDS_BYTES);
+  allow(&k_expert_rows<Few, T, true, true>, Few::LDS_BYTES);
+  allow(&k_expert_rows<Few, T, true, false>, Few::LDS_BYTES);
+  allow(&k_expert_weights<Large, T, true>, Large::LDS_BYTES);
+  allow(&k_expert_weights<Large, T, false>, Large::LDS_BYTES);
+  return e;
+}
+
+}  // namespace
+
+namespace ccld {
+hipError_t allow_lds_experts() {
+  const hipError_t e = allow_tiles<__bf16>();
+  return e != hipSuccess ? e : allow_tiles<_Float16>();
+}
+}  // namespace ccld
+
+extern "C" ccld_status ccld_expert_workspace(const ccld_expert_args* a, int32_t grad, uint64_t* bytes) {
+  if (!bytes) return CCLD_E_NULL;
+  const ccld_status s = check(a, grad != 0);
+  if (s != CCLD_OK) return s;
+  u64 need = 0;
+  if (!grad || a->dx)
+    need = row_part_bytes(plan_rows(a->rows, a->n_experts, (int)(grad ? a->k : a->n), (int)(grad ? a->n : a->k)), a->rows, grad ? a->k : a->n);
+  if (grad && a->dw)     // the two gradients follow one another: one workspace serves both
+    need = std::max(need, weight_part_bytes(plan_weights(a->rows, a->n_experts, (int)a->n, (int)a->k), a->n_experts, a->n, a->k));
+  *bytes = (need + 255) & ~(u64)255;
+  return CCLD_OK;
+}
+
+extern "C" ccld_status ccld_expert_product(const ccld_expert_args* a, void* stream) {
+  ccld_status s = check(a, false);
+  if (s == CCLD_OK) s = check_pointers(a, false);
+  if (s == CCLD_OK) s = ccld_device_init();
+  if (s != CCLD_OK || a->rows == 0) return s;
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  return a->dtype == CCLD_BF16 ? product_of_rows<__bf16>(a, false, st) : product_of_rows<_Float16>(a, false, st);
+}
+
+extern "C" ccld_status ccld_expert_product_grad(const ccld_expert_args* a, void* stream) {
+  ccld_status s = check(a, true);
+  if (s == CCLD_OK) s = check_pointers(a, true);
+  if (s == CCLD_OK) s = ccld_device_init();
+  if (s != CCLD_OK) return s;
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  const bool bf = a->dtype == CCLD_BF16;
+  if (a->dx && a->rows) s = bf ? product_of_rows<__bf16>(a, true, st) : product_of_rows<_Float16>(a, true, st);
+  if (s == CCLD_OK && a->dw) s = bf ? product_of_weights<__bf16>(a, st) : product_of_weights<_Float16>(a, st);
+  return s;
+}

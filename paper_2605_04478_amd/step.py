@@ -1,0 +1,149 @@
+"""The computation of a training step between its collectives, on the GPU.
+
+A rank that the analysis calls computation-slow (Section 2.2, S1) has a slow card, or was given more work than its peers.
+These operators are the work to run on such a card, and the kinds of work that are uneven by design: the products of
+a rank's experts, whose rows routing decides.  The HIP library computes them; this module checks arguments and marshals them,
+PyTorch supplies memory and the stream.  Every call goes to the current stream of its tensors' device and returns before it is
+done; outputs and workspaces come from torch's allocator, so calls may be captured into a graph.
+
+Matrices have unit stride within a row and any row stride.  The functions named `*_grad` are the gradients by themselves;
+the classes at the end of each section give the same to automatic differentiation.
+"""
+from __future__ import annotations
+
+import ctypes as C
+
+import torch
+
+from .ccld import CcldError, lib
+
+DTYPES = {torch.bfloat16: 0, torch.float16: 1}
+
+
+class _ExpertArgs(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("offsets_bits", C.c_int32), ("rows", C.c_int64), ("k", C.c_int64), ("n", C.c_int64),
+                ("n_experts", C.c_int64), ("x", C.c_void_p), ("w", C.c_void_p), ("offsets", C.c_void_p), ("dy", C.c_void_p),
+                ("y", C.c_void_p), ("dx", C.c_void_p), ("dw", C.c_void_p), ("ldx", C.c_int64), ("ldw", C.c_int64),
+                ("expert_stride", C.c_int64), ("lddy", C.c_int64), ("ldy", C.c_int64), ("lddx", C.c_int64),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
+
+
+# ---- checks and marshalling -------------------------------------------------------------------------------------
+def _require(ok: bool, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+def _tensor(t, name: str, shape, dtype):
+    """A tensor of this shape (None: any size) and type."""
+    _require(torch.is_tensor(t), f"{name} is no tensor")
+    _require(t.dim() == len(shape) and all(s is None or s == n for s, n in zip(shape, t.shape)),
+             f"{name} has shape {tuple(t.shape)}, expected {tuple('any' if s is None else s for s in shape)}")
+    _require(t.dtype in dtype if isinstance(dtype, (tuple, dict)) else t.dtype == dtype, f"{name} has type {t.dtype}")
+    return t
+
+
+def _on_gpu(**tensors):
+    """All on one GPU."""
+    first = None
+    for name, t in tensors.items():
+        if t is not None:
+            _require(t.is_cuda, f"{name} is not on a GPU: there is no CPU path")
+            first = t if first is None else first
+            _require(t.device == first.device, f"{name} is on {t.device}, not on {first.device}")
+
+
+def _rows(t):
+    """The tensor itself where its last dimension has unit stride and its rows do not overlap, else a copy that does so
+    (expanded and transposed tensors: gradients of broadcast outputs come as the former)."""
+    if t.stride(-1) != 1 and t.shape[-1] > 1 or any(st < t.shape[-1] and n > 1 for st, n in zip(t.stride()[:-1], t.shape[:-1])):
+        return t.contiguous()
+    return t
+
+
+def _ld(t) -> int:
+    """Elements between rows; that of a single row may be anything."""
+    return max(t.stride(-2), t.shape[-1]) if t.shape[-2] > 1 else t.shape[-1]
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _check(status: int, where: str) -> None:
+    if status != 0:
+        raise CcldError(status, where)
+
+
+def _workspace(query, args, device, *extra):
+    """A buffer of the size that the query names, set in the arguments; torch's allocator starts buffers on 512 bytes."""
+    need = C.c_uint64(0)
+    _check(query(C.addressof(args), *extra, C.addressof(need)), query.__name__)
+    ws = torch.empty(need.value, dtype=torch.uint8, device=device) if need.value else None
+    args.workspace, args.workspace_bytes = _ptr(ws), need.value
+    return ws
+
+
+def _call(fn, args, device) -> None:
+    _check(fn(C.addressof(args), torch.cuda.current_stream(device).cuda_stream), fn.__name__)
+
+
+# ---- products grouped by expert ---------------------------------------------------------------------------------------
+def _expert_args(x, w, offsets):
+    _tensor(w, "w", (None, None, None), DTYPES)
+    e, n, k = w.shape
+    _tensor(x, "x", (None, k), w.dtype)
+    _tensor(offsets, "offsets", (e + 1,), (torch.int32, torch.int64))
+    _require(e > 0 and n > 0 and k > 0, f"w has shape {tuple(w.shape)}: no size may be zero")
+    _on_gpu(w=w, x=x, offsets=offsets)
+    x, w, offsets = _rows(x), _rows(w), offsets.contiguous()
+    a = _ExpertArgs(dtype=DTYPES[w.dtype], offsets_bits=8 * offsets.element_size(), rows=x.shape[0], k=k, n=n, n_experts=e,
+                    x=_ptr(x), w=_ptr(w), offsets=_ptr(offsets), ldx=_ld(x), ldw=_ld(w),
+                    expert_stride=w.stride(0) if e > 1 else 0)
+    return a, (x, w, offsets)
+
+
+def expert_product(x, w, offsets):
+    """y[r] = x[r] w[e]^T for the rows offsets[e] .. offsets[e + 1) - 1 of every expert e.
+
+    x [rows, k] and w [experts, n, k] in bfloat16 or float16, offsets [experts + 1] in int32 or int64 -> y [rows, n].
+    Rows that belong to no expert are zero.  The offsets stay on the device; they must not decrease."""
+    a, keep = _expert_args(x, w, offsets)
+    with torch.cuda.device(w.device):
+        y = torch.empty(a.rows, a.n, dtype=w.dtype, device=w.device)
+        a.y, a.ldy = _ptr(y), a.n
+        ws = _workspace(lib().ccld_expert_workspace, a, w.device, 0)
+        _call(lib().ccld_expert_product, a, w.device)
+    del keep, ws
+    return y
+
+
+def expert_product_grad(dy, x, w, offsets, need_dx: bool = True, need_dw: bool = True):
+    """Gradients of expert_product: (dx [rows, k], dw [experts, n, k]); None for one that is not needed."""
+    a, keep = _expert_args(x, w, offsets)
+    _tensor(dy, "dy", (a.rows, a.n), w.dtype)
+    _on_gpu(w=w, dy=dy)
+    dy = _rows(dy)
+    with torch.cuda.device(w.device):
+        dx = torch.empty(a.rows, a.k, dtype=w.dtype, device=w.device) if need_dx else None
+        dw = torch.empty(a.n_experts, a.n, a.k, dtype=w.dtype, device=w.device) if need_dw else None
+        a.dy, a.lddy, a.dx, a.lddx, a.dw = _ptr(dy), _ld(dy), _ptr(dx), a.k, _ptr(dw)
+        ws = _workspace(lib().ccld_expert_workspace, a, w.device, 1)
+        _call(lib().ccld_expert_product_grad, a, w.device)
+    del keep, ws
+    return dx, dw
+
+
+class ExpertProduct(torch.autograd.Function):
+    """expert_product with its gradients: ExpertProduct.apply(x, w, offsets)."""
+
+    @staticmethod
+    def forward(ctx, x, w, offsets):
+        ctx.save_for_backward(x, w, offsets)
+        return expert_product(x, w, offsets)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        dx, dw = expert_product_grad(dy, *ctx.saved_tensors, need_dx=ctx.needs_input_grad[0], need_dw=ctx.needs_input_grad[1])
+        return dx, dw, None

@@ -1,0 +1,76 @@
+"""What the operators of a training step refuse, without a GPU: shapes and types in Python, sizes and pointers at the C ABI."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2605_04478_amd import ccld, step
+
+BF = torch.bfloat16
+BAD_ARG, NULL, CAPACITY, WORKSPACE = -6, -7, -8, -12
+
+
+def _experts(**change):
+    t = dict(x=torch.zeros(4, 8, dtype=BF), w=torch.zeros(2, 16, 8, dtype=BF), offsets=torch.zeros(3, dtype=torch.int32))
+    t.update(change)
+    return t
+
+
+@pytest.mark.parametrize("change,word", [
+    (dict(x=torch.zeros(4, 9, dtype=BF)), "x has shape"),
+    (dict(x=torch.zeros(4, 2, 8, dtype=BF)), "x has shape"),
+    (dict(x=torch.zeros(4, 8, dtype=torch.float16)), "x has type"),
+    (dict(w=torch.zeros(2, 16, 8)), "w has type"),
+    (dict(w=torch.zeros(16, 8, dtype=BF)), "w has shape"),
+    (dict(offsets=torch.zeros(2, dtype=torch.int32)), "offsets has shape"),
+    (dict(offsets=torch.zeros(3)), "offsets has type"),
+    (dict(x=[1.0]), "x is no tensor"),
+    (dict(), "not on a GPU"),
+])
+def test_expert_product_refuses(change, word):
+    with pytest.raises(ValueError, match=word):
+        step.expert_product(**_experts(**change))
+    with pytest.raises(ValueError, match=word):
+        step.expert_product_grad(torch.zeros(4, 16, dtype=BF), **_experts(**change))
+
+
+def _expert_args(**change):
+    """Arguments that are right but for the changes; the pointers are never followed."""
+    at = 1 << 20
+    a = dict(dtype=0, offsets_bits=32, rows=4, k=8, n=16, n_experts=2, x=at, w=at, offsets=at, dy=at, y=at, dx=at, dw=at,
+             ldx=8, ldw=8, expert_stride=128, lddy=16, ldy=16, lddx=8)
+    a.update(change)
+    return step._ExpertArgs(**a)
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(dtype=2), BAD_ARG), (dict(dtype=-1), BAD_ARG), (dict(offsets_bits=16), BAD_ARG), (dict(rows=-1), BAD_ARG),
+    (dict(k=0), BAD_ARG), (dict(n=0), BAD_ARG), (dict(n_experts=0), BAD_ARG), (dict(ldx=7), BAD_ARG), (dict(ldw=7), BAD_ARG),
+    (dict(ldy=15), BAD_ARG), (dict(expert_stride=-1), BAD_ARG), (dict(rows=1 << 31), CAPACITY), (dict(ldx=1 << 40), CAPACITY),
+    (dict(ldw=1 << 40), CAPACITY), (dict(k=1 << 23, ldx=1 << 23, ldw=1 << 23), CAPACITY), (dict(n_experts=1 << 30), CAPACITY),
+    (dict(x=None), NULL), (dict(w=None), NULL), (dict(offsets=None), NULL), (dict(y=None), NULL), (dict(offsets=2), BAD_ARG),
+    (dict(x=1), BAD_ARG), (dict(k=8192, ldx=8192, ldw=8192), WORKSPACE),
+])
+def test_expert_product_status(change, status):
+    assert ccld.lib().ccld_expert_product(C.addressof(_expert_args(**change)), None) == status
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(dy=None), NULL), (dict(x=None), NULL), (dict(lddy=15), BAD_ARG), (dict(lddx=7), BAD_ARG), (dict(dw=3), BAD_ARG),
+    (dict(lddy=1 << 40), CAPACITY), (dict(rows=1 << 20), WORKSPACE),
+])
+def test_expert_gradient_status(change, status):
+    assert ccld.lib().ccld_expert_product_grad(C.addressof(_expert_args(**change)), None) == status
+
+
+def test_null_arguments():
+    L = ccld.lib()
+    need = C.c_uint64(0)
+    assert L.ccld_expert_product(None, None) == NULL and L.ccld_expert_product_grad(None, None) == NULL
+    assert L.ccld_expert_workspace(None, 0, C.addressof(need)) == NULL
+    assert L.ccld_expert_workspace(C.addressof(_expert_args()), 0, None) == NULL
+    assert L.ccld_expert_workspace(C.addressof(_expert_args()), 0, C.addressof(need)) == 0 and need.value == 0
+    a = _expert_args(rows=64, k=8192, ldx=8192, ldw=8192)
+    assert L.ccld_expert_workspace(C.addressof(a), 0, C.addressof(need)) == 0 and need.value >= 2 * 4 * 64 * 16
+    a.workspace, a.workspace_bytes = (1 << 20) + 8, need.value           # misaligned
+    assert L.ccld_expert_product(C.addressof(a), None) == WORKSPACE
