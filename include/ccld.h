@@ -439,6 +439,31 @@ ccld_status ccld_expert_workspace(const ccld_expert_args *a, int32_t grad, uint6
 ccld_status ccld_expert_product(const ccld_expert_args *a, void *stream);
 ccld_status ccld_expert_product_grad(const ccld_expert_args *a, void *stream);
 
+/* Softmax cross entropy over a vocabulary, h [rows][d], w [vocab][d]; the logits z = h w^T are taken in
+ * pieces of the vocabulary and never kept.
+ *   lse[t] = log sum over v of exp z[t, v]      loss[t] = lse[t] - z[t, labels[t]]
+ *   dz = dloss[t] (exp(z - lse[t]) - [v = labels[t]])      dh = dz w      dw = dz^T h
+ * A row whose label is outside [0, vocab) has no target: its loss, lse and dh are zero and it has no part
+ * in dw, whatever its h and dloss hold. */
+typedef struct {
+  int32_t dtype;
+  int32_t label_bits;                /* 32 or 64: signed integers                                       */
+  int64_t rows, d, vocab;            /* rows may be 0; below 2^31, d < 2^22                             */
+  const void *h, *w;
+  const void *labels;                /* [rows]                                                          */
+  const float *dloss;                /* [rows], dloss_stride elements apart (0: one for all) (grad)     */
+  float *loss;                       /* [rows] out (loss call)                                          */
+  float *lse;                        /* [rows] out (loss call), in (grad call)                          */
+  void *dh;                          /* [rows][d] out, or NULL (grad call)                              */
+  void *dw;                          /* [vocab][d] out, or NULL (grad call)                             */
+  int64_t ldh, ldw, dloss_stride, lddh, lddw;
+  void *workspace;
+  uint64_t workspace_bytes;
+} ccld_vocab_args;
+ccld_status ccld_vocab_workspace(const ccld_vocab_args *a, int32_t grad, uint64_t *bytes);
+ccld_status ccld_vocab_loss(const ccld_vocab_args *a, void *stream);
+ccld_status ccld_vocab_loss_grad(const ccld_vocab_args *a, void *stream);
+
 const char *ccld_status_str(ccld_status s);
 
 #ifdef __cplusplus

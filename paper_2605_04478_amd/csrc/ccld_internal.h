@@ -237,6 +237,7 @@ hipError_t allow_lds_grid();
 hipError_t allow_lds_segments();
 hipError_t allow_lds_hang();
 hipError_t allow_lds_experts();
+hipError_t allow_lds_vocab();
 }  // namespace ccld
 
 // what every device needs once, for the current one (hang.hip): kernels with much LDS allowed it, and the device address of

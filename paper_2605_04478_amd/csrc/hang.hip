@@ -1603,7 +1603,8 @@ ccld_status device_scratch(unsigned char** out) {
   std::lock_guard<std::mutex> lock(g_scratch_mutex);
   if (!g_scratch_ptr[dev]) {
     void* p = nullptr;
-    for (hipError_t e : {allow_lds_window(), allow_lds_grid(), allow_lds_segments(), allow_lds_hang(), allow_lds_experts()})
+    for (hipError_t e : {allow_lds_window(), allow_lds_grid(), allow_lds_segments(), allow_lds_hang(), allow_lds_experts(),
+                         allow_lds_vocab()})
       if (e != hipSuccess) { (void)hipGetLastError(); return CCLD_E_HIP; }
     if (hipGetSymbolAddress(&p, HIP_SYMBOL(scratch)) != hipSuccess || !p) { (void)hipGetLastError(); return CCLD_E_HIP; }
     g_scratch_ptr[dev] = static_cast<unsigned char*>(p);

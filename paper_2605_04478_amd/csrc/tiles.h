@@ -43,6 +43,15 @@ constexpr int DEPTH = 64;                      // values of c in a stage
 constexpr u32 OUTSIDE = 0x80000000u;           // an offset beyond every buffer's range
 constexpr u32 BUFFER_RANGE = 0x7FFFFFF0u;
 
+// 16 bytes of every lane, from `offset` bytes behind base, to LDS from p on, the lanes' side by side.  (The host's pass over this file
+// knows no loads of 16 bytes to LDS, which only gfx950 has.)
+__device__ __forceinline__ void load_to_lds(const void* base, unsigned char* p, u32 offset) {
+#ifdef __HIP_DEVICE_COMPILE__
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, BUFFER_RANGE, 0x00027000),
+                                           (__attribute__((address_space(3))) void*)p, 16, offset, 0, 0, 0);
+#endif
+}
+
 // A workgroup's tile of BM x BN, divided among WM x WN wavefronts.
 template <int BM_, int BN_, int WM_, int WN_, int STAGES_>
 struct Tiling {
@@ -100,9 +109,8 @@ struct Operand {
   // Brings the stage that starts at base to LDS and moves on; `depth` values of c are left.  tile: the operand's place in the
   // stage.
   __device__ __forceinline__ void fetch(unsigned char* tile, int depth) {
-    const u32 wave = __builtin_amdgcn_readfirstlane(threadIdx.x / CCLD_WAVE);
     if constexpr (DIRECT) {
-      auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(base), 0, BUFFER_RANGE, 0x00027000);
+      const u32 wave = __builtin_amdgcn_readfirstlane(threadIdx.x / CCLD_WAVE);
 #pragma unroll
       for (int i = 0; i < PIECES; ++i) {
         u32 o = offset[i];
@@ -110,8 +118,7 @@ struct Operand {
           const int c = ACROSS ? (int)(row + i * ROW_STEP) : (int)col;
           o = c < depth ? o : OUTSIDE;
         }
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(
-            rsrc, (__attribute__((address_space(3))) void*)(tile + (i * THREADS + wave * CCLD_WAVE) * 16), 16, o, 0, 0, 0);
+        load_to_lds(base, tile + (i * THREADS + wave * CCLD_WAVE) * 16, o);
       }
     } else {
 #pragma unroll

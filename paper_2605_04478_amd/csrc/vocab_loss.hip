@@ -1,0 +1,608 @@
+// Softmax cross entropy over a large vocabulary and its gradient (ccld_vocab_*), without the matrix of logits.
+//
+//   z = h w^T     lse = log sum_v exp z_v     loss = lse - z_label
+//   dz = g (exp(z - lse) - [v = label])     dh = dz w     dw = dz^T h
+//
+// Loss: every output tile of the product reduces its logits to a running maximum and a sum of exponentials per row, and
+// one kernel joins a row's tiles.  Gradient: the logits of a piece of the vocabulary are taken again, turned into dz where they
+// are, and two more products bring the piece's share of dh and its rows of dw; dz is kept for one piece at a time.
+//
+// Rows without a target are dropped first: the others' h rows are copied side by side, so that what a masked row holds
+// reaches no sum (zero times infinity would) and costs no work.  How many there are is known on the device only: grids are laid
+// out for all rows, and workgroups beyond the last row end at once.
+//
+// Exponentials are 2^(x log2 e) in 32 bits: for x down to -30 off by 30 roundings of 2^-24 at most, a thousandth of a step of the
+// 16-bit types that gradients leave in.  dz is rounded to the operands' type for the matrix cores, after a scaling by the power of two that
+// brings the largest |g| just under 2^15: half-precision gradients of 10^-9 keep their bits.
+#include <algorithm>
+
+#include "ccld_internal.h"
+#include "products.h"
+#include "tiles.h"
+
+using namespace ccld;
+
+namespace {
+
+extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr int USED_THREADS = 1024;
+
+// what the kernels share in the workspace
+struct Rows {
+  u32* count;          // rows with a target; then the exponent of the scaling of dz
+  i32* row;            // [rows] which they are
+  i32* place;          // [rows] a row's place among them, or -1
+  i32* label;          // [rows] of the kept rows, as are the following
+  float* target;       // [rows] z_label
+  float* lse;          // [rows] (gradient)
+  float* scale;        // [rows] dloss (gradient), scaled
+  void* h;             // [rows][dp]
+};
+
+__device__ __forceinline__ i64 label_at(const void* p, int bits, i64 i) {
+  return bits == 64 ? static_cast<const i64*>(p)[i] : (i64)static_cast<const i32*>(p)[i];
+}
+
+// Which rows have a target, in order; zeros for the loss of the others; the largest |dloss|.  One workgroup: the labels of 8,192
+// rows are 64 KB.
+__global__ __launch_bounds__(USED_THREADS) void k_used_rows(Rows w, const void* labels, int bits, i64 rows, i64 vocab, float* loss,
+                                                            float* lse, const float* dloss, i64 dloss_stride) {
+  __shared__ u32 sums[USED_THREADS / CCLD_WAVE];
+  __shared__ float tops[USED_THREADS / CCLD_WAVE];
+  const u32 lane = lane_id(), wave = threadIdx.x / CCLD_WAVE;
+  u32 before = 0;
+  float top = 0;
+  for (i64 base = 0; base < rows; base += USED_THREADS) {
+    const i64 r = base + threadIdx.x;
+    const i64 l = r < rows ? label_at(labels, bits, r) : -1;
+    const bool used = l >= 0 && l < vocab;
+    const u64 mask = ballot64(used);
+    if (lane == 0) sums[wave] = (u32)__popcll(mask);
+    __syncthreads();
+    u32 at = before;
+    for (u32 i = 0; i < USED_THREADS / CCLD_WAVE; ++i) {
+      if (i < wave) at += sums[i];
+      before += sums[i];
+    }
+    __syncthreads();
+    at += mbcnt64(mask);
+    if (used) {
+      w.row[at] = (i32)r;
+      w.label[at] = (i32)l;
+      if (dloss) top = fmaxf(top, fabsf(dloss[r * dloss_stride]));
+    } else if (r < rows && loss) {
+      loss[r] = 0;
+      lse[r] = 0;
+    }
+    if (r < rows) w.place[r] = used ? (i32)at : -1;
+  }
+  for (int m = CCLD_WAVE / 2; m >= 1; m >>= 1) top = fmaxf(top, __shfl_xor(top, m, CCLD_WAVE));
+  if (lane == 0) tops[wave] = top;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (u32 i = 0; i < USED_THREADS / CCLD_WAVE; ++i) top = fmaxf(top, tops[i]);
+    int e = 0;
+    if (top > 0 && top < __builtin_inff()) (void)frexpf(top, &e);
+    w.count[0] = before;
+    // top 2^(15 - e) lies in [2^14, 2^15); the scale and its inverse stay within 32-bit floats
+    reinterpret_cast<i32*>(w.count)[1] = top > 0 && top < __builtin_inff() ? min(15 - e, 120) : 0;
+  }
+}
+
+// The kept rows side by side, padded with zeros to dp columns, and what the gradient needs of each.
+template <class T, int V>
+__global__ __launch_bounds__(256) void k_gather_rows(Rows w, const T* __restrict__ h, i64 ldh, int d, int dp, const float* lse,
+                                                     const float* dloss, i64 dloss_stride) {
+  const i64 n = w.count[0];
+  const int pieces = dp / V;
+  const float scale = ldexpf(1.0f, reinterpret_cast<const i32*>(w.count)[1]);
+  for (i64 i = (i64)blockIdx.x * 256 + threadIdx.x; i < n * pieces; i += (i64)gridDim.x * 256) {
+    const i64 at = i / pieces;
+    const int c = (int)(i - at * pieces) * V;
+    const i64 r = w.row[at];
+    if constexpr (V == 8) {
+      reinterpret_cast<s16x8*>(w.h)[i] = *reinterpret_cast<const s16x8*>(h + r * ldh + c);
+    } else {
+      static_cast<T*>(w.h)[i] = c < d ? h[r * ldh + c] : (T)0.0f;
+    }
+    if (c == 0 && dloss) {
+      w.lse[at] = lse[r];
+      w.scale[at] = dloss[r * dloss_stride] * scale;
+    }
+  }
+}
+
+struct LogitJob {
+  Rows rows;
+  const void* w;           // first row of the piece
+  i64 ldw;
+  int d, dp;
+  int first, cols;         // the piece of the vocabulary
+  u32 col_tiles;
+  float2* part;            // [rows][col_tiles] (maximum, sum of exponentials) of a row's tiles
+  void* dz;                // [rows][lddz] (gradient)
+  i64 lddz;
+};
+
+// the tile of this workgroup among those of the kept rows, or false
+template <class C>
+__device__ __forceinline__ bool logit_tile(u32 kept, u32 col_tiles, int& m0, int& n0) {
+  const u32 tm = (kept + C::BM - 1) / C::BM;
+  if (blockIdx.x >= tm * col_tiles) return false;
+  const uint2 t = grouped_order(xcd_order(blockIdx.x, tm * col_tiles), tm, col_tiles, 8);
+  m0 = (int)t.x * C::BM;
+  n0 = (int)t.y * C::BN;
+  return true;
+}
+
+// (maximum, sum of exp(x - maximum)) of two sets; the maximum is -inf where all are, 0 where one is +inf
+__device__ __forceinline__ float2 join_sums(float2 a, float2 b) {
+  const float top = fmaxf(a.x, b.x);
+  const float ref = top == -__builtin_inff() ? 0 : top;
+  return make_float2(top, a.y * __builtin_amdgcn_exp2f((a.x - ref) * LOG2E) + b.y * __builtin_amdgcn_exp2f((b.x - ref) * LOG2E));
+}
+
+template <class C, class T, bool DIRECT>
+__global__ __launch_bounds__(C::THREADS) void k_logit_sums(LogitJob j) {
+  int m0, n0;
+  const int kept = (int)j.rows.count[0];
+  if (!logit_tile<C>(kept, j.col_tiles, m0, n0)) return;
+  const int rows = min(C::BM, kept - m0), cols = min(C::BN, j.cols - n0);
+  TileProduct<C, T, false, false, DIRECT> prod;
+  prod.run(lds, static_cast<const T*>(j.rows.h) + (i64)m0 * j.dp, j.dp, rows, static_cast<const T*>(j.w) + (i64)n0 * j.ldw, j.ldw,
+           cols, j.d);
+  __syncthreads();                                      // the stages' place is taken over
+  float2* sums = reinterpret_cast<float2*>(lds);        // [WN][BM]
+  const u32 lane = lane_id(), wave = threadIdx.x / CCLD_WAVE;
+  const int left = cols - (int)(prod.wave_n() + 4 * (lane / 16));
+#pragma unroll
+  for (int i = 0; i < C::MI; ++i) {
+    const int m = (int)prod.wave_m() + 16 * i + (int)(lane % 16);
+    const int want = m < rows ? j.rows.label[m0 + m] - j.first - n0 - (int)(prod.wave_n() + 4 * (lane / 16)) : -1;
+    float top = -__builtin_inff();
+#pragma unroll
+    for (int b = 0; b < C::NI; ++b)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (16 * b + r < left) {
+          top = fmaxf(top, prod.acc[i][b][r]);
+          if (16 * b + r == want) j.rows.target[m0 + m] = prod.acc[i][b][r];
+        }
+#pragma unroll
+    for (int x = 16; x < CCLD_WAVE; x *= 2) top = fmaxf(top, __shfl_xor(top, x, CCLD_WAVE));
+    if (top == __builtin_inff()) top = 0;
+    const float ref = top == -__builtin_inff() ? 0 : top;
+    float sum = 0;
+#pragma unroll
+    for (int b = 0; b < C::NI; ++b)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (16 * b + r < left) sum += __builtin_amdgcn_exp2f((prod.acc[i][b][r] - ref) * LOG2E);
+#pragma unroll
+    for (int x = 16; x < CCLD_WAVE; x *= 2) sum += __shfl_xor(sum, x, CCLD_WAVE);
+    if (lane < 16) sums[wave % C::WN * C::BM + m] = make_float2(top, sum);
+  }
+  __syncthreads();
+  for (int m = threadIdx.x; m < rows; m += C::THREADS) {
+    float2 s = sums[m];
+#pragma unroll
+    for (int i = 1; i < C::WN; ++i) s = join_sums(s, sums[i * C::BM + m]);
+    j.part[(i64)(m0 + m) * j.col_tiles + n0 / C::BN] = s;
+  }
+}
+
+// a wavefront to a row: its tiles' sums
+__global__ __launch_bounds__(256) void k_loss(Rows w, const float2* __restrict__ part, u32 col_tiles, float* loss, float* lse) {
+  const i64 n = w.count[0];
+  const i64 at = (i64)blockIdx.x * 4 + threadIdx.x / CCLD_WAVE;
+  if (at >= n) return;
+  float2 s = make_float2(-__builtin_inff(), 0);
+  for (u32 i = lane_id(); i < col_tiles; i += CCLD_WAVE) s = join_sums(s, part[at * col_tiles + i]);
+#pragma unroll
+  for (int x = 1; x < CCLD_WAVE; x *= 2)
+    s = join_sums(s, make_float2(__shfl_xor(s.x, x, CCLD_WAVE), __shfl_xor(s.y, x, CCLD_WAVE)));
+  if (lane_id() == 0) {
+    const float l = (s.x == -__builtin_inff() ? 0 : s.x) + logf(s.y);
+    lse[w.row[at]] = l;
+    loss[w.row[at]] = l - w.target[at];
+  }
+}
+
+template <class C, class T, bool DIRECT>
+__global__ __launch_bounds__(C::THREADS) void k_logit_grad(LogitJob j) {
+  int m0, n0;
+  const int kept = (int)j.rows.count[0];
+  if (!logit_tile<C>(kept, j.col_tiles, m0, n0)) return;
+  const int rows = min(C::BM, kept - m0), cols = min(C::BN, j.cols - n0);
+  TileProduct<C, T, false, false, DIRECT> prod;
+  prod.run(lds, static_cast<const T*>(j.rows.h) + (i64)m0 * j.dp, j.dp, rows, static_cast<const T*>(j.w) + (i64)n0 * j.ldw, j.ldw,
+           cols, j.d);
+  T* dz = static_cast<T*>(j.dz) + (i64)m0 * j.lddz + n0;
+  const u32 lane = lane_id(), n1 = prod.wave_n() + 4 * (lane / 16);
+#pragma unroll
+  for (int i = 0; i < C::MI; ++i) {
+    const int m = (int)prod.wave_m() + 16 * i + (int)(lane % 16);
+    if (m >= rows) continue;
+    const float lse = j.rows.lse[m0 + m], scale = j.rows.scale[m0 + m];
+    const int want = j.rows.label[m0 + m] - j.first - n0 - (int)n1;
+#pragma unroll
+    for (int b = 0; b < C::NI; ++b) {
+      f32x4 v;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float p = __builtin_amdgcn_exp2f((prod.acc[i][b][r] - lse) * LOG2E);
+        if (16 * b + r == want) p -= 1;
+        v[r] = (int)n1 + 16 * b + r < cols ? p * scale : 0;      // columns beyond the piece are zeros that products may read
+      }
+      store4(dz + (i64)m * j.lddz + n1 + 16 * b, v, 4, true);
+    }
+  }
+}
+
+struct InputJob {            // dh: dz [kept][width] times w [width][d]
+  Rows rows;
+  const void *dz, *w;
+  i64 lddz, ldw;
+  int d, width, split_width;
+  u32 col_tiles;
+  float* sum;                // [splits][rows][d]
+  i64 all_rows;
+  bool more;                 // add to what an earlier piece left
+};
+
+template <class C, class T, bool DIRECT>
+__global__ __launch_bounds__(C::THREADS) void k_input_grad(InputJob j) {
+  int m0, n0;
+  const int kept = (int)j.rows.count[0];
+  if (!logit_tile<C>(kept, j.col_tiles, m0, n0)) return;
+  const int c0 = (int)blockIdx.y * j.split_width;
+  const int depth = max(0, min(j.split_width, j.width - c0));
+  const int rows = min(C::BM, kept - m0), cols = min(C::BN, j.d - n0);
+  TileProduct<C, T, false, true, DIRECT> prod;
+  prod.run(lds, static_cast<const T*>(j.dz) + (i64)m0 * j.lddz + c0, j.lddz, rows, static_cast<const T*>(j.w) + (i64)c0 * j.ldw + n0,
+           j.ldw, cols, depth);
+  float* o = j.sum + ((i64)blockIdx.y * j.all_rows + m0) * j.d + n0;
+  prod.each([&](u32 m, u32 n, f32x4 v) {
+    if ((int)m >= rows || (int)n >= cols) return;
+    float* q = o + (i64)m * j.d + n;
+    if (j.d % 4 == 0) {
+      if (j.more) v += *reinterpret_cast<const f32x4*>(q);
+      *reinterpret_cast<f32x4*>(q) = v;
+    } else {
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if ((int)n + r < cols) q[r] = j.more ? q[r] + v[r] : v[r];
+    }
+  });
+}
+
+// dh leaves: the splits' sums in their order, rows back in their places, zeros for rows without a target
+template <class T>
+__global__ __launch_bounds__(256) void k_input_rows(Rows w, const float* __restrict__ sum, u32 splits, i64 rows, int d, T* dh, i64 lddh) {
+  const float back = ldexpf(1.0f, -reinterpret_cast<const i32*>(w.count)[1]);
+  for (i64 i = (i64)blockIdx.x * 256 + threadIdx.x; i < rows * d; i += (i64)gridDim.x * 256) {
+    const i64 r = i / d, c = i - r * d, at = w.place[r];
+    float v = 0;
+    if (at >= 0)
+      for (u32 s = 0; s < splits; ++s) v += sum[((i64)s * rows + at) * d + c];
+    dh[r * lddh + c] = (T)(v * back);
+  }
+}
+
+struct WeightJob {           // dw of a piece: dz^T [width][kept] times h [kept][d]
+  Rows rows;
+  const void* dz;
+  i64 lddz;
+  void* dw;                  // first row of the piece
+  i64 lddw;
+  int d, dp, width;
+  u32 n_tiles, k_tiles;
+  float* part;               // [splits][width][d] or null
+  bool wide;
+};
+
+template <class C, class T>
+__global__ __launch_bounds__(C::THREADS) void k_weight_grad(WeightJob j) {
+  const u32 id = xcd_order(blockIdx.x, gridDim.x);
+  const uint2 t = grouped_order(id, j.n_tiles, j.k_tiles, 8);
+  const int n0 = (int)t.x * C::BM, k0 = (int)t.y * C::BN;
+  const int kept = (int)j.rows.count[0];
+  const int share = ((kept + (int)gridDim.y - 1) / (int)gridDim.y + DEPTH - 1) / DEPTH * DEPTH;
+  const i64 first = (i64)blockIdx.y * share;
+  const int depth = (int)max((i64)0, min((i64)share, kept - first));
+  const i64 at = depth ? first : 0;
+  // dz has whole tiles of columns, h rows padded to 16 bytes
+  const int ns = min(C::BM, j.width - n0), ks = min(C::BN, j.d - k0);
+  TileProduct<C, T, true, true, true> prod;
+  prod.run(lds, static_cast<const T*>(j.dz) + at * j.lddz + n0, j.lddz, C::BM, static_cast<const T*>(j.rows.h) + at * j.dp + k0, j.dp,
+           min(C::BN, j.dp - k0), depth);
+  if (j.part) {
+    float* q = j.part + ((i64)blockIdx.y * j.width + n0) * j.d + k0;
+    prod.each([&](u32 m, u32 n, f32x4 v) { if ((int)m < ns) store4(q + (i64)m * j.d + n, v, ks - (int)n, j.d % 4 == 0); });
+  } else {
+    const float back = ldexpf(1.0f, -reinterpret_cast<const i32*>(j.rows.count)[1]);
+    T* q = static_cast<T*>(j.dw) + (i64)n0 * j.lddw + k0;
+    prod.each([&](u32 m, u32 n, f32x4 v) { if ((int)m < ns) store4(q + (i64)m * j.lddw + n, v * back, ks - (int)n, j.wide); });
+  }
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void k_weight_rows(Rows w, const float* __restrict__ part, u32 splits, i64 width, int d, T* dw, i64 lddw) {
+  const float back = ldexpf(1.0f, -reinterpret_cast<const i32*>(w.count)[1]);
+  for (i64 i = (i64)blockIdx.x * 256 + threadIdx.x; i < width * d; i += (i64)gridDim.x * 256) {
+    const i64 r = i / d, c = i - r * d;
+    float v = 0;
+    for (u32 s = 0; s < splits; ++s) v += part[(i64)s * width * d + i];
+    dw[r * lddw + c] = (T)(v * back);
+  }
+}
+
+using Large = Tiling<256, 256, 2, 4, 2>;
+using Medium = Tiling<128, 128, 2, 2, 2>;
+using Few = Tiling<32, 128, 1, 4, 4>;
+
+i64 div_up(i64 a, i64 b) { return (a + b - 1) / b; }
+i64 round_up(i64 a, i64 b) { return div_up(a, b) * b; }
+
+enum Size { LARGE, MEDIUM, FEW };
+Size tile_size(i64 rows, i64 cols) {
+  if (rows < 48) return FEW;
+  return div_up(rows, 256) * div_up(cols, 256) >= (i64)COMPUTE_UNITS * 3 / 4 ? LARGE : MEDIUM;
+}
+int tile_m(Size s) { return s == LARGE ? Large::BM : s == MEDIUM ? Medium::BM : Few::BM; }
+int tile_n(Size s) { return s == LARGE ? Large::BN : s == MEDIUM ? Medium::BN : Few::BN; }
+
+u32 splits_for(i64 tiles, i64 steps) {
+  u32 s = 1;
+  while (tiles * s < (i64)COMPUTE_UNITS && steps / (2 * s) >= 8) s *= 2;
+  return s;
+}
+
+// dz of a piece is 2^28 values at most (512 MB), but a piece has 4,096 columns at least
+i64 piece_width(const ccld_vocab_args* a) {
+  const i64 w = std::max<i64>(round_up(((i64)1 << 28) / std::max<i64>(a->rows, 1), 256), 4096);
+  const i64 pieces = div_up(a->vocab, w);
+  return round_up(div_up(a->vocab, pieces), 256);
+}
+
+struct Carver {
+  uint8_t* base; u64 off;
+  template <class V> V* take(u64 count) {
+    off = (off + 255) & ~(u64)255;
+    V* p = base ? reinterpret_cast<V*>(base + off) : nullptr;
+    off += count * sizeof(V);
+    return p;
+  }
+};
+
+struct Plan {
+  Rows rows;
+  int dp;
+  // loss
+  Size logits;
+  u32 col_tiles;
+  float2* part;
+  // gradient
+  i64 width;
+  uint16_t* dz;
+  Size input;
+  u32 input_splits; int input_split;
+  float* sum;
+  Size weight;
+  u32 weight_splits;
+  float* weight_part;
+};
+
+Plan make_plan(const ccld_vocab_args* a, bool grad, Carver& c) {
+  Plan p{};
+  const u64 rows = (u64)a->rows;
+  p.dp = (int)round_up(a->d, 8);
+  p.rows.count = c.take<u32>(2);
+  p.rows.row = c.take<i32>(rows);
+  p.rows.place = c.take<i32>(rows);
+  p.rows.label = c.take<i32>(rows);
+  p.rows.target = c.take<float>(rows);
+  p.rows.lse = c.take<float>(rows);
+  p.rows.scale = c.take<float>(rows);
+  p.rows.h = c.take<uint16_t>(rows * p.dp);
+  if (!grad) {
+    p.logits = tile_size(a->rows, a->vocab);
+    p.col_tiles = (u32)div_up(a->vocab, tile_n(p.logits));
+    p.part = c.take<float2>(rows * p.col_tiles);
+    return p;
+  }
+  p.width = piece_width(a);
+  p.logits = tile_size(a->rows, p.width);
+  p.col_tiles = (u32)div_up(p.width, tile_n(p.logits));
+  p.dz = c.take<uint16_t>(rows * p.width);
+  if (a->dh) {
+    p.input = tile_size(a->rows, a->d);
+    const i64 steps = p.width / DEPTH, tiles = div_up(a->rows, tile_m(p.input)) * div_up(a->d, tile_n(p.input));
+    const u32 s = splits_for(tiles, steps);
+    p.input_split = (int)(div_up(steps, s) * DEPTH);
+    p.input_splits = (u32)div_up(p.width, p.input_split);
+    p.sum = c.take<float>((u64)p.input_splits * rows * a->d);
+  }
+  if (a->dw) {
+    p.weight = div_up(p.width, 256) * div_up(a->d, 256) >= (i64)COMPUTE_UNITS * 3 / 4 ? LARGE : MEDIUM;
+    p.weight_splits = splits_for(div_up(p.width, tile_m(p.weight)) * div_up(a->d, tile_n(p.weight)), div_up(a->rows, DEPTH));
+    if (p.weight_splits > 1) p.weight_part = c.take<float>((u64)p.weight_splits * p.width * a->d);
+  }
+  return p;
+}
+
+ccld_status check(const ccld_vocab_args* a, bool grad) {
+  if (!a) return CCLD_E_NULL;
+  if ((a->dtype != CCLD_BF16 && a->dtype != CCLD_FP16) || (a->label_bits != 32 && a->label_bits != 64)) return CCLD_E_BAD_ARG;
+  if (a->rows < 0 || a->d < 1 || a->vocab < 1) return CCLD_E_BAD_ARG;
+  if (a->rows >= MAX_ROWS || a->vocab >= MAX_ROWS - 512 || a->d >= MAX_LD) return CCLD_E_CAPACITY;
+  if (a->ldh < a->d || a->ldw < a->d) return CCLD_E_BAD_ARG;
+  if (a->ldw >= MAX_LD) return CCLD_E_CAPACITY;
+  if (grad && (a->dloss_stride < 0 || (a->dh && a->lddh < a->d) || (a->dw && a->lddw < a->d))) return CCLD_E_BAD_ARG;
+  if ((u64)div_up(a->rows, 32) * div_up(a->vocab, 128) >= MAX_GROUPS && (u64)div_up(a->rows, 256) * div_up(a->vocab, 256) >= MAX_GROUPS)
+    return CCLD_E_CAPACITY;
+  if (grad && (u64)div_up(std::max<i64>(a->rows, piece_width(a)), 256) * div_up(a->d, 256) >= MAX_GROUPS) return CCLD_E_CAPACITY;
+  return CCLD_OK;
+}
+
+ccld_status check_pointers(const ccld_vocab_args* a, bool grad) {
+  if (!a->w || (a->rows && (!a->h || !a->labels))) return CCLD_E_NULL;
+  if (a->rows && (grad ? !a->lse || !a->dloss : !a->loss || !a->lse)) return CCLD_E_NULL;
+  if (!aligned(a->labels, a->label_bits / 8)) return CCLD_E_BAD_ARG;
+  for (const void* p : {a->h, a->w, (const void*)a->dh, (const void*)a->dw})
+    if (!aligned(p, 2)) return CCLD_E_BAD_ARG;
+  for (const void* p : {(const void*)a->dloss, (const void*)a->loss, (const void*)a->lse})
+    if (!aligned(p, 4)) return CCLD_E_BAD_ARG;
+  uint64_t need = 0;
+  const ccld_status s = ccld_vocab_workspace(a, grad, &need);
+  if (s != CCLD_OK) return s;
+  if (!a->workspace || !aligned(a->workspace, 256) || a->workspace_bytes < need) return CCLD_E_WORKSPACE;
+  return CCLD_OK;
+}
+
+u32 stream_groups(i64 threads) { return (u32)std::min<i64>(std::max<i64>(div_up(threads, 256), 1), 4096); }
+
+template <class T>
+void start(const ccld_vocab_args* a, const Plan& p, bool grad, hipStream_t stream) {
+  k_used_rows<<<1, USED_THREADS, 0, stream>>>(p.rows, a->labels, a->label_bits, a->rows, a->vocab, grad ? nullptr : a->loss,
+                                              grad ? nullptr : a->lse, grad ? a->dloss : nullptr, a->dloss_stride);
+  const T* h = static_cast<const T*>(a->h);
+  const float *lse = grad ? a->lse : nullptr, *dloss = grad ? a->dloss : nullptr;
+  if (a->d % 8 == 0 && a->ldh % 8 == 0 && aligned(h, 16))
+    k_gather_rows<T, 8><<<stream_groups(a->rows * (p.dp / 8)), 256, 0, stream>>>(p.rows, h, a->ldh, (int)a->d, p.dp, lse, dloss, a->dloss_stride);
+  else
+    k_gather_rows<T, 1><<<stream_groups(a->rows * p.dp), 256, 0, stream>>>(p.rows, h, a->ldh, (int)a->d, p.dp, lse, dloss, a->dloss_stride);
+}
+
+bool direct(const ccld_vocab_args* a) { return a->d % 8 == 0 && a->ldw % 8 == 0 && aligned(a->w, 16); }
+
+template <class C, class T>
+void launch_logit_sums(const ccld_vocab_args* a, const LogitJob& j, hipStream_t stream) {
+  const u32 grid = (u32)(div_up(a->rows, C::BM) * j.col_tiles);
+  const auto kernel = direct(a) ? &k_logit_sums<C, T, true> : &k_logit_sums<C, T, false>;
+  kernel<<<grid, C::THREADS, C::LDS_BYTES, stream>>>(j);
+}
+template <class C, class T>
+void launch_logit_grad(const ccld_vocab_args* a, LogitJob j, hipStream_t stream) {
+  j.col_tiles = (u32)div_up(j.cols, C::BN);
+  const u32 grid = (u32)(div_up(a->rows, C::BM) * j.col_tiles);
+  const auto kernel = direct(a) ? &k_logit_grad<C, T, true> : &k_logit_grad<C, T, false>;
+  kernel<<<grid, C::THREADS, C::LDS_BYTES, stream>>>(j);
+}
+template <class C, class T>
+void launch_input_grad(const ccld_vocab_args* a, const Plan& p, InputJob j, hipStream_t stream) {
+  j.col_tiles = (u32)div_up(j.d, C::BN);
+  const dim3 grid((u32)(div_up(a->rows, C::BM) * j.col_tiles), p.input_splits);
+  const auto kernel = direct(a) ? &k_input_grad<C, T, true> : &k_input_grad<C, T, false>;
+  kernel<<<grid, C::THREADS, C::LDS_BYTES, stream>>>(j);
+}
+template <class C, class T>
+void launch_weight_grad(const Plan& p, WeightJob j, hipStream_t stream) {
+  j.n_tiles = (u32)div_up(j.width, C::BM);
+  j.k_tiles = (u32)div_up(j.d, C::BN);
+  const auto kernel = &k_weight_grad<C, T>;
+  kernel<<<dim3(j.n_tiles * j.k_tiles, p.weight_splits), C::THREADS, C::LDS_BYTES, stream>>>(j);
+}
+
+template <class T>
+ccld_status loss(const ccld_vocab_args* a, const Plan& p, hipStream_t stream) {
+  start<T>(a, p, false, stream);
+  const LogitJob j{p.rows, a->w, a->ldw, (int)a->d, p.dp, 0, (int)a->vocab, p.col_tiles, p.part, nullptr, 0};
+  if (p.logits == LARGE) launch_logit_sums<Large, T>(a, j, stream);
+  else if (p.logits == MEDIUM) launch_logit_sums<Medium, T>(a, j, stream);
+  else launch_logit_sums<Few, T>(a, j, stream);
+  k_loss<<<(u32)div_up(a->rows, 4), 256, 0, stream>>>(p.rows, p.part, p.col_tiles, a->loss, a->lse);
+  return launched();
+}
+
+template <class T>
+ccld_status gradient(const ccld_vocab_args* a, const Plan& p, hipStream_t stream) {
+  start<T>(a, p, true, stream);
+  for (i64 first = 0; first < a->vocab; first += p.width) {
+    const i64 cols = std::min<i64>(p.width, a->vocab - first);
+    const T* w = static_cast<const T*>(a->w) + first * a->ldw;
+    if (a->rows) {
+      const LogitJob j{p.rows, w, a->ldw, (int)a->d, p.dp, (int)first, (int)cols, 0, nullptr, p.dz, p.width};
+      if (p.logits == LARGE) launch_logit_grad<Large, T>(a, j, stream);
+      else if (p.logits == MEDIUM) launch_logit_grad<Medium, T>(a, j, stream);
+      else launch_logit_grad<Few, T>(a, j, stream);
+    }
+    if (a->dh && a->rows) {
+      const InputJob j{p.rows, p.dz, w, p.width, a->ldw, (int)a->d, (int)cols, p.input_split, 0, p.sum, a->rows, first > 0};
+      if (p.input == LARGE) launch_input_grad<Large, T>(a, p, j, stream);
+      else if (p.input == MEDIUM) launch_input_grad<Medium, T>(a, p, j, stream);
+      else launch_input_grad<Few, T>(a, p, j, stream);
+    }
+    if (a->dw) {
+      T* dw = static_cast<T*>(a->dw) + first * a->lddw;
+      const WeightJob j{p.rows, p.dz, p.width, dw, a->lddw, (int)a->d, p.dp, (int)cols, 0, 0, p.weight_part,
+                        a->lddw % 4 == 0 && aligned(dw, 8)};
+      if (p.weight == LARGE) launch_weight_grad<Large, T>(p, j, stream);
+      else launch_weight_grad<Medium, T>(p, j, stream);
+      if (p.weight_part)
+        k_weight_rows<T><<<stream_groups(cols * a->d), 256, 0, stream>>>(p.rows, p.weight_part, p.weight_splits, cols, (int)a->d, dw, a->lddw);
+    }
+  }
+  if (a->dh && a->rows)
+    k_input_rows<T><<<stream_groups(a->rows * a->d), 256, 0, stream>>>(p.rows, p.sum, p.input_splits, a->rows, (int)a->d, static_cast<T*>(a->dh), a->lddh);
+  return launched();
+}
+
+template <class C, class T>
+hipError_t allow_tiling() {
+  hipError_t e = hipSuccess;
+  auto allow = [&](auto k) { if (e == hipSuccess) e = allow_lds(reinterpret_cast<const void*>(k), C::LDS_BYTES); };
+  allow(&k_logit_sums<C, T, true>);
+  allow(&k_logit_sums<C, T, false>);
+  allow(&k_logit_grad<C, T, true>);
+  allow(&k_logit_grad<C, T, false>);
+  allow(&k_input_grad<C, T, true>);
+  allow(&k_input_grad<C, T, false>);
+  if constexpr (C::BM > 32) allow(&k_weight_grad<C, T>);
+  return e;
+}
+
+}  // namespace
+
+namespace ccld {
+hipError_t allow_lds_vocab() {
+  for (hipError_t e : {allow_tiling<Large, __bf16>(), allow_tiling<Large, _Float16>(), allow_tiling<Few, __bf16>(),
+                       allow_tiling<Few, _Float16>()})
+    if (e != hipSuccess) return e;
+  return hipSuccess;
+}
+}  // namespace ccld
+
+extern "C" ccld_status ccld_vocab_workspace(const ccld_vocab_args* a, int32_t grad, uint64_t* bytes) {
+  if (!bytes) return CCLD_E_NULL;
+  const ccld_status s = check(a, grad != 0);
+  if (s != CCLD_OK) return s;
+  Carver c{nullptr, 0};
+  (void)make_plan(a, grad != 0, c);
+  *bytes = (c.off + 255) & ~(u64)255;
+  return CCLD_OK;
+}
+
+extern "C" ccld_status ccld_vocab_loss(const ccld_vocab_args* a, void* stream) {
+  ccld_status s = check(a, false);
+  if (s == CCLD_OK) s = check_pointers(a, false);
+  if (s == CCLD_OK) s = ccld_device_init();
+  if (s != CCLD_OK || a->rows == 0) return s;
+  Carver c{static_cast<uint8_t*>(a->workspace), 0};
+  const Plan p = make_plan(a, false, c);
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  return a->dtype == CCLD_BF16 ? loss<__bf16>(a, p, st) : loss<_Float16>(a, p, st);
+}
+
+extern "C" ccld_status ccld_vocab_loss_grad(const ccld_vocab_args* a, void* stream) {
+  ccld_status s = check(a, true);
+  if (s == CCLD_OK) s = check_pointers(a, true);
+  if (s == CCLD_OK) s = ccld_device_init();
+  if (s != CCLD_OK) return s;
+  Carver c{static_cast<uint8_t*>(a->workspace), 0};
+  const Plan p = make_plan(a, true, c);
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  return a->dtype == CCLD_BF16 ? gradient<__bf16>(a, p, st) : gradient<_Float16>(a, p, st);
+}

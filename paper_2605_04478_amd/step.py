@@ -2,7 +2,7 @@
 
 A rank that the analysis calls computation-slow (Section 2.2, S1) has a slow card, or was given more work than its peers.
 These operators are the work to run on such a card, and the kinds of work that are uneven by design: the products of
-a rank's experts, whose rows routing decides.  The HIP library computes them; this module checks arguments and marshals them,
+a rank's experts, whose rows routing decides, and the loss over the vocabulary, which the last pipeline stage alone has.  The HIP library computes them; this module checks arguments and marshals them,
 PyTorch supplies memory and the stream.  Every call goes to the current stream of its tensors' device and returns before it is
 done; outputs and workspaces come from torch's allocator, so calls may be captured into a graph.
 
@@ -26,6 +26,14 @@ class _ExpertArgs(C.Structure):
                 ("y", C.c_void_p), ("dx", C.c_void_p), ("dw", C.c_void_p), ("ldx", C.c_int64), ("ldw", C.c_int64),
                 ("expert_stride", C.c_int64), ("lddy", C.c_int64), ("ldy", C.c_int64), ("lddx", C.c_int64),
                 ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
+
+
+class _VocabArgs(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("label_bits", C.c_int32), ("rows", C.c_int64), ("d", C.c_int64), ("vocab", C.c_int64),
+                ("h", C.c_void_p), ("w", C.c_void_p), ("labels", C.c_void_p), ("dloss", C.c_void_p), ("loss", C.c_void_p),
+                ("lse", C.c_void_p), ("dh", C.c_void_p), ("dw", C.c_void_p), ("ldh", C.c_int64), ("ldw", C.c_int64),
+                ("dloss_stride", C.c_int64), ("lddh", C.c_int64), ("lddw", C.c_int64), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_uint64)]
 
 
 # ---- checks and marshalling -------------------------------------------------------------------------------------
@@ -147,3 +155,69 @@ class ExpertProduct(torch.autograd.Function):
     def backward(ctx, dy):
         dx, dw = expert_product_grad(dy, *ctx.saved_tensors, need_dx=ctx.needs_input_grad[0], need_dw=ctx.needs_input_grad[1])
         return dx, dw, None
+
+
+# ---- softmax cross entropy over a vocabulary ----------------------------------------------------------------------------
+def _vocab_args(h, w, labels):
+    _tensor(w, "w", (None, None), DTYPES)
+    v, d = w.shape
+    _tensor(h, "h", (None, d), w.dtype)
+    _tensor(labels, "labels", (h.shape[0],), (torch.int32, torch.int64))
+    _require(v > 0 and d > 0, f"w has shape {tuple(w.shape)}: no size may be zero")
+    _on_gpu(w=w, h=h, labels=labels)
+    h, w, labels = _rows(h), _rows(w), labels.contiguous()
+    a = _VocabArgs(dtype=DTYPES[w.dtype], label_bits=8 * labels.element_size(), rows=h.shape[0], d=d, vocab=v, h=_ptr(h),
+                   w=_ptr(w), labels=_ptr(labels), ldh=_ld(h), ldw=_ld(w))
+    return a, (h, w, labels)
+
+
+def vocab_loss(h, w, labels):
+    """Softmax cross entropy of every row of h [rows, d] over the vocabulary w [vocab, d], whose logits h w^T are never kept.
+
+    h and w in bfloat16 or float16, labels [rows] in int32 or int64 -> (loss [rows], lse [rows]) in float32, lse being the
+    logarithm of the sum of the logits' exponentials.  A row whose label is outside [0, vocab) has no target: both are zero."""
+    a, keep = _vocab_args(h, w, labels)
+    with torch.cuda.device(w.device):
+        loss, lse = torch.empty(2, a.rows, dtype=torch.float32, device=w.device).unbind(0)
+        a.loss, a.lse = _ptr(loss), _ptr(lse)
+        ws = _workspace(lib().ccld_vocab_workspace, a, w.device, 0)
+        _call(lib().ccld_vocab_loss, a, w.device)
+    del keep, ws
+    return loss, lse
+
+
+def vocab_loss_grad(dloss, h, w, labels, lse, need_dh: bool = True, need_dw: bool = True):
+    """Gradients of vocab_loss for dloss [rows], the gradient of each row's loss, and the lse that it returned:
+    (dh [rows, d], dw [vocab, d]) in the type of h and w; None for one that is not needed.  The logits are taken again, in
+    pieces of the vocabulary.  Rows without a target have no gradient, whatever they hold."""
+    a, keep = _vocab_args(h, w, labels)
+    _tensor(dloss, "dloss", (a.rows,), torch.float32)
+    _tensor(lse, "lse", (a.rows,), torch.float32)
+    _on_gpu(w=w, dloss=dloss, lse=lse)
+    lse = lse.contiguous()
+    with torch.cuda.device(w.device):
+        dh = torch.empty(a.rows, a.d, dtype=w.dtype, device=w.device) if need_dh else None
+        dw = torch.empty(a.vocab, a.d, dtype=w.dtype, device=w.device) if need_dw else None
+        a.dloss, a.dloss_stride, a.lse = _ptr(dloss), dloss.stride(0), _ptr(lse)
+        a.dh, a.lddh, a.dw, a.lddw = _ptr(dh), a.d, _ptr(dw), a.d
+        ws = _workspace(lib().ccld_vocab_workspace, a, w.device, 1)
+        _call(lib().ccld_vocab_loss_grad, a, w.device)
+    del keep, ws
+    return dh, dw
+
+
+class VocabLoss(torch.autograd.Function):
+    """vocab_loss with its gradients: VocabLoss.apply(h, w, labels) -> loss [rows]."""
+
+    @staticmethod
+    def forward(ctx, h, w, labels):
+        loss, lse = vocab_loss(h, w, labels)
+        ctx.save_for_backward(h, w, labels, lse)
+        return loss
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dloss):
+        h, w, labels, lse = ctx.saved_tensors
+        dh, dw = vocab_loss_grad(dloss, h, w, labels, lse, need_dh=ctx.needs_input_grad[0], need_dw=ctx.needs_input_grad[1])
+        return dh, dw, None

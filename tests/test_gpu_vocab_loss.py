@@ -1,0 +1,269 @@
+"""Softmax cross entropy over a vocabulary and its gradients against the definition in 64 bits."""
+import pytest
+import torch
+
+from tests.step_check import F32, HALF_STEP, close, rounding
+
+pytestmark = pytest.mark.gpu
+BF, FP = torch.bfloat16, torch.float16
+DEV = "cuda:0"
+
+
+def _inputs(rows, d, vocab, dtype, masked=0.0, seed=0, spread=1.0):
+    g = torch.Generator().manual_seed(seed)
+    w = (torch.randn(vocab, d, generator=g) * d ** -0.5).to(dtype)
+    labels = torch.randint(0, vocab, (rows,), generator=g)
+    h = (spread * torch.randn(rows, d, generator=g) + 8 * torch.rand(rows, 1, generator=g) * w[labels].float()).to(dtype)
+    labels[torch.rand(rows, generator=g) < masked] = -100
+    dloss = 0.25 + torch.rand(rows, generator=g)
+    return h, w, labels, dloss
+
+
+def _mm(a, b):
+    return torch.mm(a.contiguous(), b.contiguous())
+
+
+def _want(h, w, labels, dloss, terms_d):
+    """Results in 64 bits, and how far sums of 32 bits and roundings of dz to the operands' type may be off."""
+    dtype, vocab = h.dtype, w.shape[0]
+    h, w, labels, dloss = h.to(DEV).double(), w.to(DEV).double(), labels.to(DEV), dloss.to(DEV).double()
+    used = (labels >= 0) & (labels < vocab)
+    rows = used.nonzero()[:, 0]
+    at = torch.arange(rows.numel(), device=DEV)
+    hu, lu, g = h[rows], labels[rows].long(), dloss[rows][:, None]
+    z = _mm(hu, w.t())
+    lse = torch.logsumexp(z, 1) if rows.numel() else z.new_zeros(0)
+    # products in 32 bits: a step of the sum of magnitudes for each addition, twice for sums that are cut, not rounded
+    dz_z = 2 * F32 * (terms_d + 8) * _mm(hu.abs(), w.abs().t())
+    # the sum of exponentials: exponents up to 60 (30 roundings each of x log2 e), some 200 additions in a row's longest chain
+    d_lse = dz_z.amax(1) + 300 * F32 + 4 * F32 * (lse.abs() + z.abs().amax(1)) if rows.numel() else lse
+    full = lambda t, shape: torch.zeros(shape, dtype=torch.float64, device=DEV).index_copy_(0, rows, t)
+    n = labels.shape[0]
+    out = {"lse": (full(lse, n), full(d_lse, n)),
+           "loss": (full(lse - z[at, lu], n), full(d_lse + dz_z[at, lu] + 2 * F32 * (lse.abs() + z[at, lu].abs()), n))}
+    p = torch.exp(z - lse[:, None])
+    e = dz_z + d_lse[:, None] + 64 * F32
+    dz = p.clone()
+    dz[at, lu] -= 1
+    dz = dz * g
+    top = float(g.abs().max()) if rows.numel() else 0.0
+    d_dz = g.abs() * (p * e + 4 * F32) + HALF_STEP[dtype] * dz.abs() + 2.0 ** -38 * top
+    dh, dw = _mm(dz, w), _mm(dz.t(), hu)
+    b_dh = _mm(d_dz, w.abs()) + 2 * F32 * (vocab + 16) * _mm(dz.abs(), w.abs()) + rounding(dh, dtype)
+    b_dw = _mm(d_dz.t(), hu.abs()) + 2 * F32 * (rows.numel() + 16) * _mm(dz.abs().t(), hu.abs()) + rounding(dw, dtype)
+    out["dh"] = (full(dh, h.shape), full(b_dh, h.shape))
+    out["dw"] = (dw, b_dw)
+    return out
+
+
+def _run(h, w, labels, dloss):
+    from paper_2605_04478_amd import step
+    loss, lse = step.vocab_loss(h, w, labels)
+    dh, dw = step.vocab_loss_grad(dloss, h, w, labels, lse)
+    return {"loss": loss, "lse": lse, "dh": dh, "dw": dw}
+
+
+def _check(h, w, labels, dloss, got=None, want_from=None):
+    got = got or _run(h.to(DEV), w.to(DEV), labels.to(DEV), dloss.to(DEV))
+    want = _want(*(want_from or (h, w, labels, dloss)), h.shape[1])
+    for k, (v, bound) in want.items():
+        close(got[k], v, bound, k)
+    return got
+
+
+@pytest.mark.parametrize("dtype", [BF, FP], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("masked", [0.0, 0.4])
+@pytest.mark.parametrize("rows,d,vocab", [(1, 8, 1), (1, 64, 1000), (5, 256, 3001), (47, 72, 130), (48, 64, 128), (200, 200, 517),
+                                          (300, 64, 20011), (700, 1032, 1500), (1500, 128, 9000)])
+def test_against_64_bits(rows, d, vocab, masked, dtype):
+    _check(*_inputs(rows, d, vocab, dtype, masked))
+
+
+@pytest.mark.parametrize("rows,d,vocab", [(3, 1, 7), (20, 63, 129), (150, 100, 333), (260, 129, 2050), (600, 37, 25600)])
+def test_odd_widths(rows, d, vocab):
+    _check(*_inputs(rows, d, vocab, BF, 0.2))
+
+
+def test_several_pieces_of_the_vocabulary():
+    """8,192 rows: pieces of up to 32,768 columns, the sums of dh over two of them."""
+    _check(*_inputs(8192, 40, 40001, BF, 0.1))
+
+
+@pytest.mark.parametrize("rows", [1, 5, 1024, 1025, 2500])
+def test_rows_without_a_target(rows):
+    """None, all but one, and all rows masked; labels beyond the vocabulary; NaN and infinities in what is masked."""
+    for keep in (0, 1, rows):
+        h, w, labels, dloss = _inputs(rows, 64, 300, BF)
+        off = torch.ones(rows, dtype=torch.bool)
+        off[rows // 2:rows // 2 + keep] = False
+        if keep == rows:
+            off[:] = False
+        choice = torch.tensor([-1, -100, 300, 2 ** 31 - 1, -2 ** 31])
+        labels[off] = choice[torch.arange(rows)[off] % 5]
+        clean = (h.clone(), w, labels, dloss.clone())
+        clean[0][off], clean[3][off] = 0, 0
+        h[off], dloss[off] = float("nan"), float("inf")
+        got = _check(h, w, labels, dloss, want_from=clean)
+        for k in ("loss", "lse", "dh"):
+            assert not got[k][off.to(DEV)].any(), k
+        if keep == 0:
+            assert not got["dw"].any()
+        again = _run(h.to(DEV), w.to(DEV), labels.int().to(DEV), dloss.to(DEV))
+        assert all(torch.equal(got[k], again[k]) for k in got)
+
+
+def test_no_rows():
+    from paper_2605_04478_amd import step
+    h, w = torch.empty(0, 64, dtype=BF, device=DEV), torch.randn(100, 64, device=DEV).to(BF)
+    labels, empty = torch.empty(0, dtype=torch.int64, device=DEV), torch.empty(0, device=DEV)
+    loss, lse = step.vocab_loss(h, w, labels)
+    dh, dw = step.vocab_loss_grad(empty, h, w, labels, lse)
+    assert loss.shape == lse.shape == (0,) and dh.shape == (0, 64) and dw.shape == w.shape and not dw.any()
+
+
+def test_far_logits():
+    """Logits of some hundreds: a row's probability lies on one word."""
+    _check(*_inputs(90, 128, 700, BF, spread=150.0))
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-9, 65536.0, 0.0])
+def test_small_and_large_loss_gradients(scale):
+    """Half-precision gradients of tiny and huge losses: dz is scaled to its type's range and back."""
+    h, w, labels, dloss = _inputs(130, 64, 500, BF, 0.1)
+    _check(h, w, labels, dloss * scale)
+    if scale in (0.0, 65536.0):
+        h, w, labels, dloss = _inputs(130, 64, 500, FP, 0.1)
+        _check(h, w, labels, dloss * scale / 64)
+
+
+def test_infinite_logits():
+    from paper_2605_04478_amd import step
+    h, w, labels, _ = _inputs(50, 64, 400, BF)
+    h = h.abs() + 0.1
+    labels[labels == 7] = 8
+    for value in (float("inf"), float("-inf")):
+        w[7] = value
+        loss, lse = step.vocab_loss(h.to(DEV), w.to(DEV), labels.to(DEV))
+        if value > 0:
+            assert (lse == value).all() and (loss == value).all()
+        else:
+            rest = torch.cat([w[:7], w[8:]])
+            moved = torch.where(labels > 7, labels - 1, labels)
+            other = step.vocab_loss(h.to(DEV), rest.to(DEV), moved.to(DEV))
+            assert torch.isfinite(loss).all() and (loss - other[0]).abs().max() < 1e-5
+    w[7], h[3, 3] = 0, float("nan")
+    loss, lse = step.vocab_loss(h.to(DEV), w.to(DEV), labels.to(DEV))
+    assert torch.isnan(loss[3]) and torch.isnan(lse[3]) and torch.isfinite(loss).sum() == 49
+    w[:] = float("-inf")
+    loss, lse = step.vocab_loss(h[4:].to(DEV), w.to(DEV), labels[4:].to(DEV))
+    assert (lse == float("-inf")).all()
+
+
+def test_strides_and_orders():
+    h, w, labels, dloss = _inputs(150, 96, 700, BF, 0.3)
+    plain = _check(h, w, labels, dloss)
+
+    def padded(t):
+        big = torch.full((t.shape[0], t.shape[1] + 40), float("nan"), dtype=t.dtype, device=DEV)
+        big[:, :t.shape[1]] = t.to(DEV)
+        return big[:, :t.shape[1]]
+
+    def transposed(t):
+        return t.to(DEV).t().contiguous().t()
+
+    def shifted(t):
+        flat = torch.empty(t.numel() + 1, dtype=t.dtype, device=DEV)
+        flat[1:] = t.to(DEV).flatten()
+        return flat[1:].view(t.shape)
+    every_other = torch.stack([labels, torch.zeros_like(labels)], 1).to(DEV)[:, 0]
+    spaced = torch.stack([dloss, torch.full_like(dloss, float("nan"))], 1).to(DEV)[:, 0]
+    for form in (padded, transposed, shifted):
+        got = _run(form(h), form(w), every_other, spaced)
+        assert all(torch.equal(got[k], plain[k]) for k in plain), form.__name__
+    one = torch.full((1,), 0.125).expand(150)                      # the gradient of a mean
+    _check(h, w, labels, one, got=_run(h.to(DEV), w.to(DEV), labels.to(DEV), torch.full((1,), 0.125, device=DEV).expand(150)))
+
+
+def test_vocabulary_beyond_two_gigabytes():
+    from paper_2605_04478_amd import step
+    v, d = 140000, 16384
+    w = torch.empty(v, d, dtype=BF, device=DEV)
+    assert w.numel() > 1 << 31
+    g = torch.Generator(device=DEV).manual_seed(3)
+    w.normal_(0, d ** -0.5, generator=g)
+    h = torch.randn(3, d, device=DEV, generator=g).to(BF)
+    labels = torch.tensor([0, v - 1, 70000], device=DEV)
+    dloss = torch.tensor([1.0, 0.5, 2.0], device=DEV)
+    loss, lse = step.vocab_loss(h, w, labels)
+    z = torch.cat([(h.float() @ c.float().t()) for c in w.split(20000)], 1).double()
+    want = torch.logsumexp(z, 1)
+    assert (lse.double() - want).abs().max() < 2e-4          # two products of 16,384 terms in 32 bits, of magnitude one
+    dh, dw = step.vocab_loss_grad(dloss, h, w, labels, lse)
+    p = torch.exp(z - want[:, None])
+    p[torch.arange(3), labels] -= 1
+    p = p * dloss.double()[:, None]
+    for rows in (slice(0, 8), slice(v - 8, v), slice(69998, 70003)):
+        ref = _mm(p[:, rows].t(), h.double())
+        bound = rounding(ref, BF) + (HALF_STEP[BF] + 4e-4) * _mm(p[:, rows].abs().t(), h.double().abs()) + 1e-9
+        close(dw[rows], ref, bound, str(rows))
+    ref = sum(_mm(p[:, i:i + 20000], w[i:i + 20000].double()) for i in range(0, v, 20000))
+    size = sum(_mm(p[:, i:i + 20000].abs(), w[i:i + 20000].double().abs()) for i in range(0, v, 20000))
+    close(dh, ref, rounding(ref, BF) + (HALF_STEP[BF] + 4e-4) * size, "dh")
+
+
+def test_automatic_differentiation_and_differences():
+    """The gradient of a weighted mean through VocabLoss: the formula's, and what differences of the loss give."""
+    from paper_2605_04478_amd import step
+    h, w, labels, weight = _inputs(40, 48, 90, FP, 0.25)
+    gh, gw = h.to(DEV).requires_grad_(), w.to(DEV).requires_grad_()
+    kept = int((labels >= 0).sum())
+    (step.VocabLoss.apply(gh, gw, labels.to(DEV)) * weight.to(DEV)).sum().div(kept).backward()
+    want = _want(h, w, labels, weight / kept, 48)
+    close(gh.grad, *want["dh"], "dh")
+    close(gw.grad, *want["dw"], "dw")
+
+    def value(hd, wd):
+        z = hd @ wd.t()
+        used = labels >= 0
+        return float(((torch.logsumexp(z, 1) - z.gather(1, labels.clamp(min=0)[:, None])[:, 0]) * weight.double())[used].sum() / kept)
+    g = torch.Generator().manual_seed(9)
+    for leaf, grad, bound in ((0, gh.grad, want["dh"][1]), (1, gw.grad, want["dw"][1])):
+        d = torch.randn(grad.shape, generator=g).double()
+        args, eps = [h.double(), w.double()], 1e-4
+        hi, lo = list(args), list(args)
+        hi[leaf], lo[leaf] = args[leaf] + eps * d, args[leaf] - eps * d
+        slope = (value(*hi) - value(*lo)) / (2 * eps)
+        got = float((grad.double().cpu() * d).sum())
+        assert abs(got - slope) <= float((d.abs() * bound.cpu()).sum()) + 1e-6 * abs(slope)
+
+
+def test_one_gradient_alone():
+    from paper_2605_04478_amd import step
+    h, w, labels, dloss = (t.to(DEV) for t in _inputs(130, 64, 500, BF, 0.2))
+    both = _run(h, w, labels, dloss)
+    dh, none = step.vocab_loss_grad(dloss, h, w, labels, both["lse"], need_dw=False)
+    assert none is None and torch.equal(dh, both["dh"])
+    none, dw = step.vocab_loss_grad(dloss, h, w, labels, both["lse"], need_dh=False)
+    assert none is None and torch.equal(dw, both["dw"])
+
+
+def test_replayed_graph_and_another_stream():
+    h, w, labels, dloss = (t.to(DEV) for t in _inputs(300, 128, 1100, BF, 0.3))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        on_side = _run(h, w, labels, dloss)
+    torch.cuda.current_stream().wait_stream(side)
+    here = _run(h, w, labels, dloss)
+    assert all(torch.equal(here[k], on_side[k]) for k in here)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = _run(h, w, labels, dloss)
+    for i in range(4):
+        h.normal_()
+        dloss.uniform_()
+        labels.copy_(torch.randint(-200 * i, 1100, (300,)))
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = _run(h, w, labels, dloss)
+        assert all(torch.equal(out[k], eager[k]) for k in eager), i

@@ -74,3 +74,54 @@ def test_null_arguments():
     assert L.ccld_expert_workspace(C.addressof(a), 0, C.addressof(need)) == 0 and need.value >= 2 * 4 * 64 * 16
     a.workspace, a.workspace_bytes = (1 << 20) + 8, need.value           # misaligned
     assert L.ccld_expert_product(C.addressof(a), None) == WORKSPACE
+
+
+# ---- the vocabulary's loss ----------------------------------------------------------------------------------------------
+def _vocab(**change):
+    t = dict(h=torch.zeros(4, 8, dtype=BF), w=torch.zeros(10, 8, dtype=BF), labels=torch.zeros(4, dtype=torch.int64))
+    t.update(change)
+    return t
+
+
+@pytest.mark.parametrize("change,word", [
+    (dict(h=torch.zeros(4, 9, dtype=BF)), "h has shape"),
+    (dict(h=torch.zeros(2, 2, 8, dtype=BF)), "h has shape"),
+    (dict(h=torch.zeros(4, 8)), "h has type"),
+    (dict(w=torch.zeros(10, 8, dtype=torch.float64)), "w has type"),
+    (dict(w=torch.zeros(0, 8, dtype=BF)), "no size may be zero"),
+    (dict(labels=torch.zeros(5, dtype=torch.int64)), "labels has shape"),
+    (dict(labels=torch.zeros(4)), "labels has type"),
+    (dict(), "not on a GPU"),
+])
+def test_vocab_loss_refuses(change, word):
+    with pytest.raises(ValueError, match=word):
+        step.vocab_loss(**_vocab(**change))
+    with pytest.raises(ValueError, match=word):
+        step.vocab_loss_grad(torch.zeros(4), lse=torch.zeros(4), **_vocab(**change))
+
+
+def _vocab_args(**change):
+    at = 1 << 20
+    a = dict(dtype=0, label_bits=64, rows=4, d=8, vocab=10, h=at, w=at, labels=at, dloss=at, loss=at, lse=at, dh=at, dw=at, ldh=8,
+             ldw=8, dloss_stride=1, lddh=8, lddw=8, workspace=at, workspace_bytes=1 << 30)
+    a.update(change)
+    return step._VocabArgs(**a)
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(dtype=2), BAD_ARG), (dict(label_bits=8), BAD_ARG), (dict(rows=-1), BAD_ARG), (dict(d=0), BAD_ARG), (dict(vocab=0), BAD_ARG),
+    (dict(ldh=7), BAD_ARG), (dict(ldw=7), BAD_ARG), (dict(rows=1 << 31), CAPACITY), (dict(vocab=1 << 31), CAPACITY),
+    (dict(ldw=1 << 40), CAPACITY), (dict(rows=1 << 30, vocab=1 << 30), CAPACITY), (dict(h=None), NULL), (dict(w=None), NULL),
+    (dict(labels=None), NULL), (dict(loss=None), NULL), (dict(lse=None), NULL), (dict(labels=4), BAD_ARG), (dict(loss=2), BAD_ARG),
+    (dict(workspace=None), WORKSPACE), (dict(workspace=(1 << 20) + 16), WORKSPACE), (dict(workspace_bytes=100), WORKSPACE),
+])
+def test_vocab_loss_status(change, status):
+    assert ccld.lib().ccld_vocab_loss(C.addressof(_vocab_args(**change)), None) == status
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(dloss=None), NULL), (dict(lse=None), NULL), (dict(dloss_stride=-1), BAD_ARG), (dict(lddh=7), BAD_ARG), (dict(lddw=7), BAD_ARG),
+    (dict(dw=1), BAD_ARG), (dict(dloss=6), BAD_ARG), (dict(workspace_bytes=1000), WORKSPACE),
+])
+def test_vocab_gradient_status(change, status):
+    assert ccld.lib().ccld_vocab_loss_grad(C.addressof(_vocab_args(**change)), None) == status
