@@ -411,9 +411,9 @@ ccld_status ccld_profile_read(ccld_ctx *ctx, double *ms, uint64_t *launches, uin
  * hipStream_t) of the current device and the call returns before it is done.  Nothing is allocated: where a
  * workspace is needed its size comes from the query beside the call, and it may be reused as soon as the
  * stream has passed the call.  Matrices are row-major with unit stride within a row; ld* is the number of
- * elements between rows.  Elements are CCLD_BF16 or CCLD_FP16; sums are held in 32
+ * elements between rows.  Elements are CCLD_BF16 or CCLD_FP16 (norms: CCLD_FP32 too); sums are held in 32
  * bits and rounded once.  Results do not depend on the order in which workgroups run. */
-enum { CCLD_BF16 = 0, CCLD_FP16 = 1 };
+enum { CCLD_BF16 = 0, CCLD_FP16 = 1, CCLD_FP32 = 2 };
 
 /* Products grouped by expert: rows offsets[e] .. offsets[e + 1) - 1 of x belong to expert e.
  *   y[r] = x[r] w[e]^T      dx[r] = dy[r] w[e]      dw[e] = sum over its rows of dy[r]^T x[r]
@@ -463,6 +463,34 @@ typedef struct {
 ccld_status ccld_vocab_workspace(const ccld_vocab_args *a, int32_t grad, uint64_t *bytes);
 ccld_status ccld_vocab_loss(const ccld_vocab_args *a, void *stream);
 ccld_status ccld_vocab_loss_grad(const ccld_vocab_args *a, void *stream);
+
+/* The norms before and after a block with its gate and the scale of the residual stream:
+ *   r1 = 1 / sqrt(mean(b^2) + eps)     h' = scale h + gate (b r1 w_post)
+ *   r2 = 1 / sqrt(mean(h'^2) + eps)    u = h' r2 w_pre
+ * b is the block's output, u the next block's input.  gate has `groups` rows (rows divisible by groups;
+ * consecutive rows / groups rows share one), or is NULL: one.  The norms are taken of 32-bit values. */
+typedef struct {
+  int32_t dtype;
+  float scale, eps;
+  int32_t reserved;
+  int64_t rows, d, groups;           /* d <= CCLD_NORM_MAX                                              */
+  const void *h, *b;                 /* [rows][d]                                                       */
+  const void *gate;                  /* [groups][d] or NULL                                             */
+  const void *w_post, *w_pre;        /* [d]                                                             */
+  void *h_out, *u;                   /* [rows][d] out                                                   */
+  float *rstd_post, *rstd_pre;       /* [rows] r1, r2: out, in of the grad call                         */
+  const void *dh_out, *du;           /* [rows][d]: gradients of h' and u (grad call); NULL: zero        */
+  void *dh, *db;                     /* [rows][d] out                                                   */
+  void *dgate;                       /* [groups][d] out, or NULL                                        */
+  void *dw_post, *dw_pre;            /* [d] out                                                         */
+  int64_t ldh, ldb, ldgate, ldh_out, ldu, lddh_out, lddu, lddh, lddb;
+  void *workspace;
+  uint64_t workspace_bytes;
+} ccld_norm_args;
+#define CCLD_NORM_MAX 16384
+ccld_status ccld_norm_workspace(const ccld_norm_args *a, uint64_t *bytes);      /* of the grad call      */
+ccld_status ccld_norm_residual(const ccld_norm_args *a, void *stream);
+ccld_status ccld_norm_residual_grad(const ccld_norm_args *a, void *stream);
 
 const char *ccld_status_str(ccld_status s);
 

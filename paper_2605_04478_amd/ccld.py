@@ -116,7 +116,8 @@ EXPORTS = ("ccld_profile_enable", "ccld_profile_read", "ccld_default_params", "c
            "ccld_progress_rates",
            "ccld_decode_frames", "ccld_reset_frames", "ccld_status_str",
            "ccld_expert_workspace", "ccld_expert_product", "ccld_expert_product_grad",
-           "ccld_vocab_workspace", "ccld_vocab_loss", "ccld_vocab_loss_grad")
+           "ccld_vocab_workspace", "ccld_vocab_loss", "ccld_vocab_loss_grad",
+           "ccld_norm_workspace", "ccld_norm_residual", "ccld_norm_residual_grad")
 
 
 def lib() -> C.CDLL:
@@ -150,6 +151,9 @@ def lib() -> C.CDLL:
         L.ccld_vocab_workspace.argtypes = [vp, C.c_int32, vp]
         L.ccld_vocab_loss.argtypes = [vp, vp]
         L.ccld_vocab_loss_grad.argtypes = [vp, vp]
+        L.ccld_norm_workspace.argtypes = [vp, vp]
+        L.ccld_norm_residual.argtypes = [vp, vp]
+        L.ccld_norm_residual_grad.argtypes = [vp, vp]
         L.ccld_status_str.argtypes = [C.c_int32]
         L.ccld_status_str.restype = C.c_char_p
         for name in EXPORTS:

@@ -2,7 +2,7 @@
 
 A rank that the analysis calls computation-slow (Section 2.2, S1) has a slow card, or was given more work than its peers.
 These operators are the work to run on such a card, and the kinds of work that are uneven by design: the products of
-a rank's experts, whose rows routing decides, and the loss over the vocabulary, which the last pipeline stage alone has.  The HIP library computes them; this module checks arguments and marshals them,
+a rank's experts, whose rows routing decides, and the loss over the vocabulary, which the last pipeline stage alone has; and the norms around a block, which only memory bounds.  The HIP library computes them; this module checks arguments and marshals them,
 PyTorch supplies memory and the stream.  Every call goes to the current stream of its tensors' device and returns before it is
 done; outputs and workspaces come from torch's allocator, so calls may be captured into a graph.
 
@@ -18,6 +18,8 @@ import torch
 from .ccld import CcldError, lib
 
 DTYPES = {torch.bfloat16: 0, torch.float16: 1}
+NORM_DTYPES = {**DTYPES, torch.float32: 2}
+NORM_MAX = 16384
 
 
 class _ExpertArgs(C.Structure):
@@ -34,6 +36,15 @@ class _VocabArgs(C.Structure):
                 ("lse", C.c_void_p), ("dh", C.c_void_p), ("dw", C.c_void_p), ("ldh", C.c_int64), ("ldw", C.c_int64),
                 ("dloss_stride", C.c_int64), ("lddh", C.c_int64), ("lddw", C.c_int64), ("workspace", C.c_void_p),
                 ("workspace_bytes", C.c_uint64)]
+
+
+class _NormArgs(C.Structure):
+    _fields_ = ([("dtype", C.c_int32), ("scale", C.c_float), ("eps", C.c_float), ("reserved", C.c_int32), ("rows", C.c_int64),
+                 ("d", C.c_int64), ("groups", C.c_int64)]
+                + [(n, C.c_void_p) for n in ("h", "b", "gate", "w_post", "w_pre", "h_out", "u", "rstd_post", "rstd_pre", "dh_out",
+                                             "du", "dh", "db", "dgate", "dw_post", "dw_pre")]
+                + [(n, C.c_int64) for n in ("ldh", "ldb", "ldgate", "ldh_out", "ldu", "lddh_out", "lddu", "lddh", "lddb")]
+                + [("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)])
 
 
 # ---- checks and marshalling -------------------------------------------------------------------------------------
@@ -221,3 +232,88 @@ class VocabLoss(torch.autograd.Function):
         h, w, labels, lse = ctx.saved_tensors
         dh, dw = vocab_loss_grad(dloss, h, w, labels, lse, need_dh=ctx.needs_input_grad[0], need_dw=ctx.needs_input_grad[1])
         return dh, dw, None
+
+
+# ---- the norms around a block, its gate and the residual scale -----------------------------------------------------------
+def _norm_args(h, b, gate, w_post, w_pre, scale, eps):
+    _tensor(h, "h", (None, None), NORM_DTYPES)
+    rows, d = h.shape
+    _tensor(b, "b", (rows, d), h.dtype)
+    _tensor(w_post, "w_post", (d,), h.dtype)
+    _tensor(w_pre, "w_pre", (d,), h.dtype)
+    _require(0 < d <= NORM_MAX, f"h has {d} columns: 1 to {NORM_MAX} are possible")
+    groups = 1
+    if gate is not None:
+        _tensor(gate, "gate", (None, d), h.dtype)
+        groups = gate.shape[0]
+        _require(groups > 0 and rows % groups == 0, f"{rows} rows cannot share {groups} rows of gate evenly")
+    _require(eps >= 0, f"eps is {eps}")
+    _on_gpu(h=h, b=b, gate=gate, w_post=w_post, w_pre=w_pre)
+    h, b, w_post, w_pre = _rows(h), _rows(b), w_post.contiguous(), w_pre.contiguous()
+    gate = None if gate is None else _rows(gate)
+    a = _NormArgs(dtype=NORM_DTYPES[h.dtype], scale=scale, eps=eps, rows=rows, d=d, groups=groups, h=_ptr(h), b=_ptr(b),
+                  gate=_ptr(gate), w_post=_ptr(w_post), w_pre=_ptr(w_pre), ldh=_ld(h), ldb=_ld(b),
+                  ldgate=d if gate is None else _ld(gate))
+    return a, (h, b, gate, w_post, w_pre)
+
+
+def norm_residual(h, b, gate, w_post, w_pre, scale: float = 1.0, eps: float = 1e-6):
+    """A block's end and the next one's beginning: the norm of the block's output b, its gate, the residual stream h with its
+    scale, and the norm that the next block reads.
+
+        h' = scale h + gate (b / rms(b) w_post)          u = h' / rms(h') w_pre          rms(x) = sqrt(mean(x^2) + eps)
+
+    h, b [rows, d] in bfloat16, float16 or float32, w_post and w_pre [d]; gate [g, d], each of whose rows serves rows / g
+    consecutive rows, or None.  -> (h', u, 1 / rms(b), 1 / rms(h')), the last two [rows] in float32."""
+    a, keep = _norm_args(h, b, gate, w_post, w_pre, scale, eps)
+    with torch.cuda.device(h.device):
+        h_out, u = (torch.empty(a.rows, a.d, dtype=h.dtype, device=h.device) for _ in range(2))
+        rstd_post, rstd_pre = torch.empty(2, a.rows, dtype=torch.float32, device=h.device).unbind(0)
+        a.h_out, a.u, a.ldh_out, a.ldu = _ptr(h_out), _ptr(u), a.d, a.d
+        a.rstd_post, a.rstd_pre = _ptr(rstd_post), _ptr(rstd_pre)
+        _call(lib().ccld_norm_residual, a, h.device)
+    del keep
+    return h_out, u, rstd_post, rstd_pre
+
+
+def norm_residual_grad(dh_out, du, h, b, gate, w_post, w_pre, rstd_post, rstd_pre, scale: float = 1.0):
+    """Gradients of norm_residual for those of h' and u (either may be None: zero) and the two vectors that it returned:
+    (dh, db, dgate, dw_post, dw_pre), all in the type of h; dgate is None without a gate."""
+    a, keep = _norm_args(h, b, gate, w_post, w_pre, scale, 0.0)
+    for name, t in (("dh_out", dh_out), ("du", du)):
+        if t is not None:
+            _tensor(t, name, (a.rows, a.d), h.dtype)
+    _tensor(rstd_post, "rstd_post", (a.rows,), torch.float32)
+    _tensor(rstd_pre, "rstd_pre", (a.rows,), torch.float32)
+    _on_gpu(h=h, dh_out=dh_out, du=du, rstd_post=rstd_post, rstd_pre=rstd_pre)
+    dh_out, du = (None if t is None else _rows(t) for t in (dh_out, du))
+    rstd_post, rstd_pre = rstd_post.contiguous(), rstd_pre.contiguous()
+    with torch.cuda.device(h.device):
+        dh, db = (torch.empty(a.rows, a.d, dtype=h.dtype, device=h.device) for _ in range(2))
+        dgate = None if gate is None else torch.empty(a.groups, a.d, dtype=h.dtype, device=h.device)
+        dw_post, dw_pre = (torch.empty(a.d, dtype=h.dtype, device=h.device) for _ in range(2))
+        a.dh_out, a.du, a.dh, a.db, a.dgate, a.dw_post, a.dw_pre = map(_ptr, (dh_out, du, dh, db, dgate, dw_post, dw_pre))
+        a.lddh_out, a.lddu = (a.d if t is None else _ld(t) for t in (dh_out, du))
+        a.lddh, a.lddb = a.d, a.d
+        a.rstd_post, a.rstd_pre = _ptr(rstd_post), _ptr(rstd_pre)
+        ws = _workspace(lib().ccld_norm_workspace, a, h.device)
+        _call(lib().ccld_norm_residual_grad, a, h.device)
+    del keep, ws
+    return dh, db, dgate, dw_post, dw_pre
+
+
+class NormResidual(torch.autograd.Function):
+    """norm_residual with its gradients: NormResidual.apply(h, b, gate, w_post, w_pre, scale, eps) -> (h', u)."""
+
+    @staticmethod
+    def forward(ctx, h, b, gate, w_post, w_pre, scale, eps):
+        h_out, u, rstd_post, rstd_pre = norm_residual(h, b, gate, w_post, w_pre, scale, eps)
+        ctx.set_materialize_grads(False)
+        ctx.scale = scale
+        ctx.save_for_backward(h, b, gate, w_post, w_pre, rstd_post, rstd_pre)
+        return h_out, u
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dh_out, du):
+        return (*norm_residual_grad(dh_out, du, *ctx.saved_tensors, scale=ctx.scale), None, None)

@@ -66,6 +66,8 @@ def test_expert_gradient_status(change, status):
 def test_null_arguments():
     L = ccld.lib()
     need = C.c_uint64(0)
+    assert L.ccld_vocab_loss(None, None) == L.ccld_vocab_loss_grad(None, None) == L.ccld_vocab_workspace(None, 0, C.addressof(need)) == NULL
+    assert L.ccld_norm_residual(None, None) == L.ccld_norm_residual_grad(None, None) == L.ccld_norm_workspace(None, C.addressof(need)) == NULL
     assert L.ccld_expert_product(None, None) == NULL and L.ccld_expert_product_grad(None, None) == NULL
     assert L.ccld_expert_workspace(None, 0, C.addressof(need)) == NULL
     assert L.ccld_expert_workspace(C.addressof(_expert_args()), 0, None) == NULL
@@ -125,3 +127,66 @@ def test_vocab_loss_status(change, status):
 ])
 def test_vocab_gradient_status(change, status):
     assert ccld.lib().ccld_vocab_loss_grad(C.addressof(_vocab_args(**change)), None) == status
+
+
+# ---- the norms ------------------------------------------------------------------------------------------------------------
+def _norm(**change):
+    t = dict(h=torch.zeros(6, 8), b=torch.zeros(6, 8), gate=torch.zeros(3, 8), w_post=torch.zeros(8), w_pre=torch.zeros(8))
+    t.update(change)
+    return t
+
+
+@pytest.mark.parametrize("change,word", [
+    (dict(b=torch.zeros(6, 9)), "b has shape"),
+    (dict(b=torch.zeros(6, 8, dtype=BF)), "b has type"),
+    (dict(h=torch.zeros(6, 8, dtype=torch.float64)), "h has type"),
+    (dict(h=torch.zeros(6, 20000), b=torch.zeros(6, 20000), gate=None, w_post=torch.zeros(20000), w_pre=torch.zeros(20000)), "columns"),
+    (dict(h=torch.zeros(6, 0), b=torch.zeros(6, 0), gate=None, w_post=torch.zeros(0), w_pre=torch.zeros(0)), "columns"),
+    (dict(gate=torch.zeros(4, 8)), "share 4 rows of gate"),
+    (dict(gate=torch.zeros(0, 8)), "share 0 rows of gate"),
+    (dict(gate=torch.zeros(8)), "gate has shape"),
+    (dict(w_post=torch.zeros(1, 8)), "w_post has shape"),
+    (dict(w_pre=torch.zeros(8, dtype=BF)), "w_pre has type"),
+    (dict(), "not on a GPU"),
+])
+def test_norm_residual_refuses(change, word):
+    t = _norm(**change)
+    with pytest.raises(ValueError, match=word):
+        step.norm_residual(**t)
+    with pytest.raises(ValueError, match=word):
+        step.norm_residual_grad(t["h"], t["h"], *t.values(), torch.zeros(6), torch.zeros(6))
+
+
+def test_norm_residual_refuses_a_negative_eps():
+    with pytest.raises(ValueError, match="eps"):
+        step.norm_residual(**_norm(), eps=-1.0)
+
+
+def _norm_args(**change):
+    at = 1 << 20
+    a = dict(dtype=2, scale=1.0, eps=1e-6, rows=6, d=8, groups=3, workspace=at, workspace_bytes=1 << 30)
+    a.update({n: at for n in ("h", "b", "gate", "w_post", "w_pre", "h_out", "u", "rstd_post", "rstd_pre", "dh_out", "du", "dh", "db",
+                              "dgate", "dw_post", "dw_pre")})
+    a.update({n: 8 for n in ("ldh", "ldb", "ldgate", "ldh_out", "ldu", "lddh_out", "lddu", "lddh", "lddb")})
+    a.update(change)
+    return step._NormArgs(**a)
+
+
+SHARED = [
+    (dict(dtype=3), BAD_ARG), (dict(rows=-6), BAD_ARG), (dict(d=0), BAD_ARG), (dict(groups=0), BAD_ARG), (dict(groups=4), BAD_ARG),
+    (dict(d=20000), CAPACITY), (dict(rows=3 << 31), CAPACITY), (dict(eps=-1.0), BAD_ARG), (dict(eps=float("nan")), BAD_ARG),
+    (dict(h=None), NULL), (dict(b=None), NULL), (dict(w_post=None), NULL), (dict(w_pre=None), NULL), (dict(rstd_pre=None), NULL),
+    (dict(ldh=7), BAD_ARG), (dict(ldb=7), BAD_ARG), (dict(ldgate=7), BAD_ARG), (dict(h=2), BAD_ARG), (dict(rstd_post=2), BAD_ARG),
+]
+
+
+@pytest.mark.parametrize("change,status", SHARED + [(dict(h_out=None), NULL), (dict(u=None), NULL), (dict(ldu=7), BAD_ARG), (dict(u=2), BAD_ARG)])
+def test_norm_residual_status(change, status):
+    assert ccld.lib().ccld_norm_residual(C.addressof(_norm_args(**change)), None) == status
+
+
+@pytest.mark.parametrize("change,status", SHARED + [
+    (dict(dh=None), NULL), (dict(dw_pre=None), NULL), (dict(lddh=7), BAD_ARG), (dict(lddu=7), BAD_ARG), (dict(du=2), BAD_ARG),
+    (dict(workspace=None), WORKSPACE), (dict(workspace_bytes=8), WORKSPACE), (dict(workspace=(1 << 20) + 4), WORKSPACE)])
+def test_norm_gradient_status(change, status):
+    assert ccld.lib().ccld_norm_residual_grad(C.addressof(_norm_args(**change)), None) == status
