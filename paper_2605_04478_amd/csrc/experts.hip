@@ -118,7 +118,7 @@ __global__ __launch_bounds__(C::THREADS) void k_expert_weights(WeightJob j) {
   const int n0 = (int)t.x * C::BM, k0 = (int)t.y * C::BN;
   const int2 r = j.off.range(e);
   // this split's rows: an equal share, in whole stages
-  const int share = ((r.y - r.x + (int)gridDim.y - 1) / (int)gridDim.y + DEPTH - 1) / DEPTH * DEPTH;
+  const int share = ((r.y - r.x + (int)gridDim.y - 1) / (int)gridDim.y + C::DEPTH - 1) / C::DEPTH * C::DEPTH;
   const i64 first = r.x + (i64)blockIdx.y * share;
   const int depth = (int)max((i64)0, min((i64)share, r.y - first));
   const i64 at = depth ? first : 0;
@@ -136,9 +136,6 @@ __global__ __launch_bounds__(C::THREADS) void k_expert_weights(WeightJob j) {
   }
 }
 
-using Large = Tiling<256, 256, 2, 4, 2>;
-using Medium = Tiling<128, 128, 2, 2, 2>;
-using Few = Tiling<32, 128, 1, 4, 4>;
 
 u64 div_up(u64 a, u64 b) { return (a + b - 1) / b; }
 

@@ -7,6 +7,7 @@
 
 namespace ccld {
 
+constexpr int DEPTH = 64;              // contractions are divided in whole multiples of it
 constexpr uint64_t COMPUTE_UNITS = 256;
 constexpr uint64_t MAX_GROUPS = (uint64_t)1 << 22;      // workgroups of up to 1,024 threads in a launch
 constexpr int64_t MAX_ROWS = (int64_t)1 << 31, MAX_EXPERTS = (int64_t)1 << 20, MAX_WIDTH = (int64_t)1 << 22;

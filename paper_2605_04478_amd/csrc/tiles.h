@@ -6,11 +6,11 @@
 // A[c * ld + m]).  The forward product of a linear layer has both along, its input's gradient has the weights across, its
 // weights' gradient has both across; no operand is transposed in memory for any of them.
 //
-// A tile of DEPTH values of c is brought to LDS by loads that bypass the registers (16 bytes per lane, a wavefront's 1,024
-// bytes side by side), STAGES - 1 tiles ahead of the one that is multiplied.  Fragments of operands that lie along c are read
-// 16 bytes at a time; those that lie across by the transposing read, which gives a lane four values of c of its own
-// column.  LDS positions are permuted so that neither meets a bank twice: the loads fetch, for a fixed position, the
-// piece that belongs there.
+// A stage of DEPTH values of c is brought to LDS by loads that bypass the registers (16 bytes per lane, a wavefront's 1,024
+// bytes side by side), STAGES - 1 ahead of the one that is multiplied, whose fragments are in registers: while the matrix
+// instructions work on these, the next stage's are read.  Fragments of operands that lie along c are read 16 bytes at a
+// time; those that lie across by the transposing read, which gives a lane four values of c of its own column.  LDS
+// positions are permuted so that neither meets a bank twice: the loads fetch, for a fixed position, the piece that belongs there.
 //
 // The matrix instruction is given B as its first operand, so that a lane ends up with four neighbouring n of one m:
 // value r of block (i, j) in lane l is C[16 i + l % 16, 16 j + 4 (l / 16) + r].
@@ -39,23 +39,26 @@ __device__ __forceinline__ f32x4 mma(s16x8 a, s16x8 b, f32x4 c, _Float16) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
-constexpr int DEPTH = 64;                      // values of c in a stage
 constexpr u32 OUTSIDE = 0x80000000u;           // an offset beyond every buffer's range
 constexpr u32 BUFFER_RANGE = 0x7FFFFFF0u;
 
-// 16 bytes of every lane, from `offset` bytes behind base, to LDS from p on, the lanes' side by side.  (The host's pass over this file
-// knows no loads of 16 bytes to LDS, which only gfx950 has.)
+// 16 bytes of every lane, from `offset` bytes behind base, to LDS from p on, the lanes' side by side.  In assembly, because the compiler
+// waits for all loads to LDS that it knows of before every transposing read; who reads waits in stage_barrier.  No register is
+// written.  (M0 holds the place; what uses it may follow its write after one instruction.)
 __device__ __forceinline__ void load_to_lds(const void* base, unsigned char* p, u32 offset) {
 #ifdef __HIP_DEVICE_COMPILE__
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, BUFFER_RANGE, 0x00027000),
-                                           (__attribute__((address_space(3))) void*)p, 16, offset, 0, 0, 0);
+  typedef __attribute__((ext_vector_type(4))) u32 u32x4;
+  const u64 at = (u64)(uintptr_t)base;
+  const u32x4 buffer = {(u32)at, (u32)(at >> 32) & 0xFFFF, BUFFER_RANGE, 0x00027000};
+  const u32 place = (u32)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)p;
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(place), "v"(offset), "s"(buffer) : "memory");
 #endif
 }
 
-// A workgroup's tile of BM x BN, divided among WM x WN wavefronts.
-template <int BM_, int BN_, int WM_, int WN_, int STAGES_>
+// A workgroup's tile of BM x BN, divided among WM x WN wavefronts, and its stages.
+template <int BM_, int BN_, int WM_, int WN_, int DEPTH_, int STAGES_>
 struct Tiling {
-  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_;
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, DEPTH = DEPTH_, STAGES = STAGES_;
   static constexpr int THREADS = WM * WN * CCLD_WAVE;
   static constexpr int TM = BM / WM, TN = BN / WN;       // a wavefront's share
   static constexpr int MI = TM / 16, NI = TN / 16;
@@ -63,6 +66,10 @@ struct Tiling {
   static constexpr int LDS_BYTES = STAGES * STAGE_BYTES;
   static_assert(TM % 16 == 0 && TN % 16 == 0, "blocks of 16 x 16");
 };
+
+using Large = Tiling<256, 256, 2, 4, 32, 5>;
+using Medium = Tiling<128, 128, 2, 2, 32, 4>;
+using Few = Tiling<32, 128, 1, 4, 64, 4>;
 
 // Which 32-byte piece of an operand that lies across c is kept at a position of row c in LDS: the wavefront's transposing
 // reads touch rows c .. c + 3 and c + 8 .. c + 11 at once, 32 bytes of each.
@@ -73,10 +80,14 @@ __device__ __forceinline__ u32 across_key(u32 c) {
   else return (c >> 3) & 1;
 }
 
+// The same for operands that lie along c: reads touch eight rows at once, 16 bytes of each.
+template <int DEPTH>
+__device__ __forceinline__ u32 along_key(u32 row) { return DEPTH == 64 ? row & 7 : (row >> 1) & 3; }
+
 // One operand's share of the stages: ROWS of its output index by DEPTH of c.
 // DIRECT loads need 16-byte pieces to be aligned and wholly inside or outside the operand; otherwise single values are loaded
 // with a check each and written to LDS from registers.
-template <class T, int ROWS, int THREADS, bool ACROSS, bool DIRECT>
+template <class T, int ROWS, int DEPTH, int THREADS, bool ACROSS, bool DIRECT>
 struct Operand {
   static constexpr int PIECES = ROWS * DEPTH / 8 / THREADS;      // 16-byte pieces per thread and stage
   static_assert(ROWS * DEPTH / 8 % THREADS == 0, "whole pieces");
@@ -95,53 +106,43 @@ struct Operand {
     row = tid / PER_ROW;
     const u32 at = tid % PER_ROW;
     if constexpr (ACROSS) col = 8 * ((((at >> 1) ^ across_key<ROWS>(row)) << 1) | (at & 1));
-    else col = 8 * (at ^ (row & 7));
-    // the permutation is the same for all of a thread's pieces: their rows differ by multiples of 16 or 8
-    static_assert(ACROSS ? ROW_STEP % 16 == 0 || PIECES == 1 : ROW_STEP % 8 == 0, "one permutation per thread");
+    else col = 8 * (at ^ along_key<DEPTH>(row));
+    static_assert(ACROSS ? ROW_STEP % 16 == 0 || PIECES == 1 || (ROW_STEP == 8 && ROWS >= 128) : ROW_STEP % 8 == 0, "column()");
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-      const u32 r = row + i * ROW_STEP;
-      const bool in = ACROSS ? (int)col < left : (int)r < left;
-      offset[i] = in ? (u32)((i64)r * ld + col) * 2 : OUTSIDE;
+      const u32 r = row + i * ROW_STEP, x = column(i);
+      const bool in = ACROSS ? (int)x < left : (int)r < left;
+      offset[i] = in ? (u32)((i64)r * ld + x) * 2 : OUTSIDE;
     }
   }
+  // first value of piece i within its row: a thread's rows are permuted alike, but for those that differ by an odd multiple of 8
+  __device__ __forceinline__ u32 column(int i) const { return ACROSS && ROW_STEP == 8 ? col ^ ((i & 1) * 64) : col; }
 
-  // Brings the stage that starts at base to LDS and moves on; `depth` values of c are left.  tile: the operand's place in the
-  // stage.
-  __device__ __forceinline__ void fetch(unsigned char* tile, int depth) {
+  // Loads one of the thread's pieces of the stage that starts at base to the operand's place in it; `depth` values of c are left.
+  __device__ __forceinline__ void fetch(unsigned char* tile, int i, int depth) const {
     if constexpr (DIRECT) {
       const u32 wave = __builtin_amdgcn_readfirstlane(threadIdx.x / CCLD_WAVE);
-#pragma unroll
-      for (int i = 0; i < PIECES; ++i) {
-        u32 o = offset[i];
-        if (depth < DEPTH) {
-          const int c = ACROSS ? (int)(row + i * ROW_STEP) : (int)col;
-          o = c < depth ? o : OUTSIDE;
-        }
-        load_to_lds(base, tile + (i * THREADS + wave * CCLD_WAVE) * 16, o);
-      }
+      const int c = ACROSS ? (int)(row + i * ROW_STEP) : (int)col;
+      load_to_lds(base, tile + (i * THREADS + wave * CCLD_WAVE) * 16, c < depth ? offset[i] : OUTSIDE);
     } else {
+      const u32 r = row + i * ROW_STEP;
+      s16x8 v;
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i) {
-        const u32 r = row + i * ROW_STEP;
-        s16x8 v;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int x = (int)col + e;
-          const bool in = ACROSS ? x < left && (int)r < depth : (int)r < left && x < depth;
-          v[e] = in ? __builtin_bit_cast(short, base[(i64)r * ld + x]) : (short)0;
-        }
-        *reinterpret_cast<s16x8*>(tile + (i * THREADS + threadIdx.x) * 16) = v;
+      for (int e = 0; e < 8; ++e) {
+        const int x = (int)column(i) + e;
+        const bool in = ACROSS ? x < left && (int)r < depth : (int)r < left && x < depth;
+        v[e] = in ? __builtin_bit_cast(short, base[(i64)r * ld + x]) : (short)0;
       }
+      *reinterpret_cast<s16x8*>(tile + (i * THREADS + threadIdx.x) * 16) = v;
     }
-    base += ACROSS ? ld * DEPTH : (i64)DEPTH;
   }
+  __device__ __forceinline__ void next_stage() { base += ACROSS ? ld * DEPTH : (i64)DEPTH; }
 };
 
-// A wavefront's fragments of an operand: COUNT blocks of 16 from row0 on.
-template <int ROWS, int COUNT, bool ACROSS>
+// Where a wavefront finds its fragments of an operand: COUNT blocks of 16 from row0 on.
+template <int ROWS, int COUNT, int DEPTH, bool ACROSS>
 struct Fragments {
-  u32 at[ACROSS ? COUNT : 2];
+  u32 at[ACROSS ? COUNT : DEPTH / 32];
 
   __device__ __forceinline__ void start(u32 row0) {
     const u32 lane = threadIdx.x % CCLD_WAVE, g = lane / 16, t = lane % 16;
@@ -152,10 +153,10 @@ struct Fragments {
         at[j] = c * (ROWS * 2) + (((row0 / 16 + j) ^ across_key<ROWS>(c)) * 32) + (t % 4) * 8;
     } else {
 #pragma unroll
-      for (int k = 0; k < 2; ++k) at[k] = (row0 + t) * (DEPTH * 2) + (((4 * k + g) ^ (t & 7)) * 16);
+      for (int k = 0; k < DEPTH / 32; ++k) at[k] = (row0 + t) * (DEPTH * 2) + (((4 * k + g) ^ along_key<DEPTH>(t)) * 16);
     }
   }
-  // block j, half k of the stage: eight values of c from 32 k + 8 (lane / 16) on, of row row0 + 16 j + lane % 16
+  // block j, part k of the stage: eight values of c from 32 k + 8 (lane / 16) on, of row row0 + 16 j + lane % 16
   __device__ __forceinline__ s16x8 read(const unsigned char* tile, int j, int k) const {
     if constexpr (ACROSS) {
       typedef __attribute__((address_space(3))) s16x4* lds_ptr;
@@ -169,10 +170,11 @@ struct Fragments {
   }
 };
 
-// waits until all but the newest `newer` of this wavefront's loads are in LDS and its LDS reads are done, then for the others
-template <int NEWER>
+// waits until all but the newest NEWER of this wavefront's loads are in LDS, then for the others; DONE: its LDS accesses too
+template <int NEWER, bool DONE>
 __device__ __forceinline__ void stage_barrier() {
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(NEWER) : "memory");
+  if constexpr (DONE) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(NEWER) : "memory");
+  else asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(NEWER) : "memory");
 }
 
 template <class C, class T, bool A_ACROSS, bool B_ACROSS, bool DIRECT>
@@ -182,52 +184,80 @@ struct TileProduct {
   __device__ __forceinline__ static u32 wave_m() { return (threadIdx.x / CCLD_WAVE) / C::WN * C::TM; }
   __device__ __forceinline__ static u32 wave_n() { return (threadIdx.x / CCLD_WAVE) % C::WN * C::TN; }
 
+  static constexpr int PARTS = C::DEPTH / 32, A_BYTES = C::BM * C::DEPTH * 2;
+  typedef Operand<T, C::BM, C::DEPTH, C::THREADS, A_ACROSS, DIRECT> A;
+  typedef Operand<T, C::BN, C::DEPTH, C::THREADS, B_ACROSS, DIRECT> B;
+  static constexpr int LOADS = A::PIECES + B::PIECES;
   // a, b: the tile's first values; rows_a, rows_b: outputs that the operands have from there on (more than zero); depth: values
-  // of c (zero leaves the sums zero).  All of the workgroup's threads take part; lds has C::LDS_BYTES.
+  // of c (zero leaves the sums zero).  All of the workgroup's threads take part; lds has C::LDS_BYTES, which are free afterwards.
   __device__ __forceinline__ void run(unsigned char* lds, const T* a, i64 lda, int rows_a, const T* b, i64 ldb, int rows_b,
                                       int depth) {
 #pragma unroll
     for (int i = 0; i < C::MI; ++i)
 #pragma unroll
       for (int j = 0; j < C::NI; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
-    Operand<T, C::BM, C::THREADS, A_ACROSS, DIRECT> oa;
-    Operand<T, C::BN, C::THREADS, B_ACROSS, DIRECT> ob;
+    if (depth <= 0) return;
+    A oa;
+    B ob;
     oa.start(a, lda, rows_a);
     ob.start(b, ldb, rows_b);
-    Fragments<C::BM, C::MI, A_ACROSS> fa;
-    Fragments<C::BN, C::NI, B_ACROSS> fb;
+    Fragments<C::BM, C::MI, C::DEPTH, A_ACROSS> fa;
+    Fragments<C::BN, C::NI, C::DEPTH, B_ACROSS> fb;
     fa.start(wave_m());
     fb.start(wave_n());
-    constexpr int A_BYTES = C::BM * DEPTH * 2;
-    constexpr int LOADS = DIRECT ? decltype(oa)::PIECES + decltype(ob)::PIECES : 0;
-    const int steps = (depth + DEPTH - 1) / DEPTH;
-    auto fetch = [&](int step) {
-      unsigned char* s = lds + step % C::STAGES * C::STAGE_BYTES;
-      oa.fetch(s, depth - step * DEPTH);
-      ob.fetch(s + A_BYTES, depth - step * DEPTH);
+    auto fetch = [&](unsigned char* s, int i, int left) {
+      if (i < A::PIECES) oa.fetch(s, i, left);
+      else ob.fetch(s + A_BYTES, i - A::PIECES, left);
     };
 #pragma unroll
-    for (int s = 0; s < C::STAGES - 1; ++s)
-      if (s < steps) fetch(s);
-    for (int step = 0; step < steps; ++step) {
-      // the oldest stage has arrived, and everybody is done with the one before it, whose place the next fetch takes
-      if (step + C::STAGES - 2 < steps) stage_barrier<LOADS * (C::STAGES - 2)>();
-      else stage_barrier<0>();
-      if (step + C::STAGES - 1 < steps) fetch(step + C::STAGES - 1);
-      const unsigned char* s = lds + step % C::STAGES * C::STAGE_BYTES;
+    for (int s = 0; s < C::STAGES - 1; ++s) {
 #pragma unroll
-      for (int k = 0; k < DEPTH / 32; ++k) {
-        s16x8 va[C::MI], vb[C::NI];
-#pragma unroll
-        for (int j = 0; j < C::NI; ++j) vb[j] = fb.read(s + A_BYTES, j, k);
-#pragma unroll
-        for (int i = 0; i < C::MI; ++i) va[i] = fa.read(s, i, k);
-#pragma unroll
-        for (int i = 0; i < C::MI; ++i)
-#pragma unroll
-          for (int j = 0; j < C::NI; ++j) acc[i][j] = mma(vb[j], va[i], acc[i][j], T());
-      }
+      for (int i = 0; i < LOADS; ++i) fetch(lds + s * C::STAGE_BYTES, i, depth - s * C::DEPTH);
+      oa.next_stage();
+      ob.next_stage();
     }
+    int left = depth - (C::STAGES - 1) * C::DEPTH;      // of the stages that are not on their way yet
+    stage_barrier<DIRECT ? LOADS * (C::STAGES - 2) : 0, !DIRECT>();
+    s16x8 va[PARTS][C::MI], even[PARTS][C::NI], odd[PARTS][C::NI];
+#pragma unroll
+    for (int k = 0; k < PARTS; ++k) {
+#pragma unroll
+      for (int j = 0; j < C::NI; ++j) even[k][j] = fb.read(lds + A_BYTES, j, k);
+#pragma unroll
+      for (int i = 0; i < C::MI; ++i) va[k][i] = fa.read(lds, i, k);
+    }
+    // The stage that is multiplied is in registers, and another's place is free: everybody has multiplied the stage before, so has
+    // read it.  The fragments of A are replaced by the next stage's as soon as they have been used, those of B are used until the end.
+    // Stages beyond the last are zeros.
+    u32 free = (C::STAGES - 1) * C::STAGE_BYTES, next = C::STAGE_BYTES;
+    auto step = [&](const s16x8 (&vb)[PARTS][C::NI], s16x8 (&then)[PARTS][C::NI]) {
+      stage_barrier<DIRECT ? LOADS * (C::STAGES - 3) : 0, !DIRECT>();
+      const unsigned char* s = lds + next;
+      constexpr int TURNS = PARTS * C::MI;
+      int loaded = 0, read = 0;
+#pragma unroll
+      for (int turn = 0; turn < TURNS; ++turn) {
+        const int k = turn / C::MI, i = turn % C::MI;
+#pragma unroll
+        for (; read < PARTS * C::NI * (turn + 1) / TURNS; ++read) then[read / C::NI][read % C::NI] = fb.read(s + A_BYTES, read % C::NI, read / C::NI);
+#pragma unroll
+        for (; loaded < LOADS * (turn + 1) / TURNS; ++loaded) fetch(lds + free, loaded, left);
+#pragma unroll
+        for (int j = 0; j < C::NI; ++j) acc[i][j] = mma(vb[k][j], va[k][i], acc[i][j], T());
+        va[k][i] = fa.read(s, i, k);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      oa.next_stage();
+      ob.next_stage();
+      left -= C::DEPTH;
+      free = free + C::STAGE_BYTES == C::LDS_BYTES ? 0 : free + C::STAGE_BYTES;
+      next = next + C::STAGE_BYTES == C::LDS_BYTES ? 0 : next + C::STAGE_BYTES;
+    };
+    for (int done = 0; done < depth; done += 2 * C::DEPTH) {
+      step(even, odd);
+      step(odd, even);
+    }
+    stage_barrier<0, true>();
   }
 
   // f(m, n, four sums of n .. n + 3) for every block, m and n within the tile

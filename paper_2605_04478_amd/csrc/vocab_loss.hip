@@ -309,7 +309,7 @@ __global__ __launch_bounds__(C::THREADS) void k_weight_grad(WeightJob j) {
   const uint2 t = grouped_order(id, j.n_tiles, j.k_tiles, 8);
   const int n0 = (int)t.x * C::BM, k0 = (int)t.y * C::BN;
   const int kept = (int)j.rows.count[0];
-  const int share = ((kept + (int)gridDim.y - 1) / (int)gridDim.y + DEPTH - 1) / DEPTH * DEPTH;
+  const int share = ((kept + (int)gridDim.y - 1) / (int)gridDim.y + C::DEPTH - 1) / C::DEPTH * C::DEPTH;
   const i64 first = (i64)blockIdx.y * share;
   const int depth = (int)max((i64)0, min((i64)share, kept - first));
   const i64 at = depth ? first : 0;
@@ -339,9 +339,6 @@ __global__ __launch_bounds__(256) void k_weight_rows(Rows w, const float* __rest
   }
 }
 
-using Large = Tiling<256, 256, 2, 4, 2>;
-using Medium = Tiling<128, 128, 2, 2, 2>;
-using Few = Tiling<32, 128, 1, 4, 4>;
 
 i64 div_up(i64 a, i64 b) { return (a + b - 1) / b; }
 i64 round_up(i64 a, i64 b) { return div_up(a, b) * b; }
