@@ -39,7 +39,7 @@ struct RowJob {              // y or dx
   i64 lda, ldw, estride, ldo;
   int cols, depth, split_depth;
   u32 col_tiles;
-  bool wide;
+  bool whole;                // rows of out are aligned to 16 bytes
 };
 
 struct WeightJob {           // dw
@@ -50,6 +50,7 @@ struct WeightJob {           // dw
   i64 lddy, ldx;
   int n, k;
   u32 n_tiles, k_tiles;
+  bool whole;
 };
 
 // The tile of a workgroup: the part that it belongs to, that part's first m-tile (of BM rows, counted over all parts), number of m-tiles and
@@ -106,8 +107,7 @@ __global__ __launch_bounds__(C::THREADS) void k_expert_rows(RowJob j) {
     float* o = j.part + ((i64)blockIdx.y * j.off.rows + row0) * j.cols + col0;
     prod.each([&](u32 m, u32 n, f32x4 v) { if ((int)m < rows) store4(o + (i64)m * j.cols + n, v, cols - (int)n, j.cols % 4 == 0); });
   } else {
-    T* o = static_cast<T*>(j.out) + (i64)row0 * j.ldo + col0;
-    prod.each([&](u32 m, u32 n, f32x4 v) { if ((int)m < rows) store4(o + (i64)m * j.ldo + n, v, cols - (int)n, j.wide); });
+    prod.store(lds, static_cast<T*>(j.out) + (i64)row0 * j.ldo + col0, j.ldo, rows, cols, j.whole, 1.0f);
   }
 }
 
@@ -131,8 +131,7 @@ __global__ __launch_bounds__(C::THREADS) void k_expert_weights(WeightJob j) {
     float* q = j.part + (i64)blockIdx.y * j.off.n_experts * j.n * j.k + o;
     prod.each([&](u32 m, u32 n, f32x4 v) { if ((int)m < ns) store4(q + (i64)m * j.k + n, v, ks - (int)n, j.k % 4 == 0); });
   } else {
-    T* q = static_cast<T*>(j.out) + o;
-    prod.each([&](u32 m, u32 n, f32x4 v) { if ((int)m < ns) store4(q + (i64)m * j.k + n, v, ks - (int)n, j.k % 4 == 0); });
+    prod.store(lds, static_cast<T*>(j.out) + o, j.k, ns, ks, j.whole, 1.0f);
   }
 }
 
@@ -239,7 +238,7 @@ ccld_status product_of_rows(const ccld_expert_args* a, bool grad, hipStream_t st
   j.off = Offsets{a->offsets, a->offsets_bits, (int)a->rows, (u32)a->n_experts};
   j.ldw = a->ldw; j.estride = a->expert_stride;
   j.cols = cols; j.depth = depth; j.split_depth = p.split_depth; j.col_tiles = p.col_tiles;
-  j.wide = j.ldo % 4 == 0 && aligned(j.out, 8);
+  j.whole = j.ldo % 8 == 0 && aligned(j.out, 16);
   const bool d = direct(a, j.a, j.lda);
   if (grad) d ? launch_rows<T, true, true>(j, p, stream) : launch_rows<T, true, false>(j, p, stream);
   else d ? launch_rows<T, false, true>(j, p, stream) : launch_rows<T, false, false>(j, p, stream);
@@ -263,27 +262,26 @@ ccld_status product_of_weights(const ccld_expert_args* a, hipStream_t stream) {
   j.off = Offsets{a->offsets, a->offsets_bits, (int)a->rows, (u32)a->n_experts};
   j.lddy = a->lddy; j.ldx = a->ldx; j.n = (int)a->n; j.k = (int)a->k;
   j.n_tiles = p.n_tiles; j.k_tiles = p.k_tiles;
-  const bool d = direct(a, a->dy, a->lddy) && a->ldx % 8 == 0 && aligned(a->x, 16) && aligned(a->dw, 16);
+  j.whole = a->k % 8 == 0 && aligned(a->dw, 16);
+  const bool d = direct(a, a->dy, a->lddy) && a->ldx % 8 == 0 && aligned(a->x, 16);
   if (p.bm == 256) launch_weights<Large, T>(j, p, d, stream);
   else launch_weights<Medium, T>(j, p, d, stream);
   if (j.part) launch_join(j.part, p.splits, (u64)a->n_experts * a->n, (u64)a->k, j.out, a->k, a->dtype, stream);
   return launched();
 }
 
-template <class T>
-hipError_t allow_tiles() {
+template <class C, class T>
+hipError_t allow_tiling() {
   hipError_t e = hipSuccess;
-  auto allow = [&](auto k, int bytes) { if (e == hipSuccess) e = allow_lds(reinterpret_cast<const void*>(k), bytes); };
-  allow(&k_expert_rows<Large, T, false, true>, Large::LDS_BYTES);
-  allow(&k_expert_rows<Large, T, false, false>, Large::LDS_BYTES);
-  allow(&k_expert_rows<Large, T, true, true>, Large::LDS_BYTES);
-  allow(&k_expert_rows<Large, T, true, false>, Large::LDS_BYTES);
-  allow(&k_expert_rows<Few, T, false, true>, Few::LDS_BYTES);
-  allow(&k_expert_rows<Few, T, false, false>, Few::LDS_BYTES);
-  allow(&k_expert_rows<Few, T, true, true>, Few::LDS_BYTES);
-  allow(&k_expert_rows<Few, T, true, false>, Few::LDS_BYTES);
-  allow(&k_expert_weights<Large, T, true>, Large::LDS_BYTES);
-  allow(&k_expert_weights<Large, T, false>, Large::LDS_BYTES);
+  auto allow = [&](auto k) { if (e == hipSuccess) e = allow_lds(reinterpret_cast<const void*>(k), C::LDS_BYTES); };
+  allow(&k_expert_rows<C, T, false, true>);
+  allow(&k_expert_rows<C, T, false, false>);
+  allow(&k_expert_rows<C, T, true, true>);
+  allow(&k_expert_rows<C, T, true, false>);
+  if constexpr (C::BM > 32) {
+    allow(&k_expert_weights<C, T, true>);
+    allow(&k_expert_weights<C, T, false>);
+  }
   return e;
 }
 
@@ -291,8 +289,10 @@ hipError_t allow_tiles() {
 
 namespace ccld {
 hipError_t allow_lds_experts() {
-  const hipError_t e = allow_tiles<__bf16>();
-  return e != hipSuccess ? e : allow_tiles<_Float16>();
+  for (hipError_t e : {allow_tiling<Large, __bf16>(), allow_tiling<Large, _Float16>(), allow_tiling<Medium, __bf16>(),
+                       allow_tiling<Medium, _Float16>(), allow_tiling<Few, __bf16>(), allow_tiling<Few, _Float16>()})
+    if (e != hipSuccess) return e;
+  return hipSuccess;
 }
 }  // namespace ccld
 

@@ -7,10 +7,14 @@
 // weights' gradient has both across; no operand is transposed in memory for any of them.
 //
 // A stage of DEPTH values of c is brought to LDS by loads that bypass the registers (16 bytes per lane, a wavefront's 1,024
-// bytes side by side), STAGES - 1 ahead of the one that is multiplied, whose fragments are in registers: while the matrix
-// instructions work on these, the next stage's are read.  Fragments of operands that lie along c are read 16 bytes at a
-// time; those that lie across by the transposing read, which gives a lane four values of c of its own column.  LDS
-// positions are permuted so that neither meets a bank twice: the loads fetch, for a fixed position, the piece that belongs there.
+// bytes side by side).  The fragments of the stage that is multiplied are in registers, and are replaced by the next stage's as they
+// are used up.  Fragments of operands that lie along c are read 16 bytes at a time; those that lie across by the
+// transposing read, which gives a lane four values of c of its own column.  LDS positions are permuted so that neither meets a
+// bank twice: the loads fetch, for a fixed position, the piece that belongs there.
+//
+// Rows of a stage of 32 values are half a cache line of an operand that lies along c.  Stages are therefore loaded in pairs, both
+// of A's in one step and both of B's in the next: the second half of a line is asked for right after the first, and does not
+// travel from the L2 again.
 //
 // The matrix instruction is given B as its first operand, so that a lane ends up with four neighbouring n of one m:
 // value r of block (i, j) in lane l is C[16 i + l % 16, 16 j + 4 (l / 16) + r].
@@ -20,6 +24,7 @@
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include <type_traits>
 
 #include "device_utils.h"
 
@@ -68,7 +73,7 @@ struct Tiling {
 };
 
 using Large = Tiling<256, 256, 2, 4, 32, 5>;
-using Medium = Tiling<128, 128, 2, 2, 32, 4>;
+using Medium = Tiling<128, 128, 2, 2, 32, 5>;
 using Few = Tiling<32, 128, 1, 4, 64, 4>;
 
 // Which 32-byte piece of an operand that lies across c is kept at a position of row c in LDS: the wavefront's transposing
@@ -170,11 +175,10 @@ struct Fragments {
   }
 };
 
-// waits until all but the newest NEWER of this wavefront's loads are in LDS, then for the others; DONE: its LDS accesses too
-template <int NEWER, bool DONE>
+// waits until all but the newest NEWER of this wavefront's loads are in LDS and its LDS accesses are done, then for the others
+template <int NEWER>
 __device__ __forceinline__ void stage_barrier() {
-  if constexpr (DONE) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(NEWER) : "memory");
-  else asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(NEWER) : "memory");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(NEWER) : "memory");
 }
 
 template <class C, class T, bool A_ACROSS, bool B_ACROSS, bool DIRECT>
@@ -205,19 +209,23 @@ struct TileProduct {
     Fragments<C::BN, C::NI, C::DEPTH, B_ACROSS> fb;
     fa.start(wave_m());
     fb.start(wave_n());
-    auto fetch = [&](unsigned char* s, int i, int left) {
-      if (i < A::PIECES) oa.fetch(s, i, left);
-      else ob.fetch(s + A_BYTES, i - A::PIECES, left);
-    };
+    constexpr bool PAIRS = C::DEPTH == 32;
+    constexpr int STAGES_AHEAD = PAIRS ? C::STAGES - 1 : C::STAGES;      // a pair needs two free places
+    constexpr int A_TURN = PAIRS ? 2 * A::PIECES : A::PIECES, B_TURN = PAIRS ? 2 * B::PIECES : B::PIECES;
+    auto after = [](u32 p) { return p + C::STAGE_BYTES == C::LDS_BYTES ? 0 : p + C::STAGE_BYTES; };
+    int left_a = depth, left_b = depth;        // of the stages that are not on their way yet
 #pragma unroll
-    for (int s = 0; s < C::STAGES - 1; ++s) {
+    for (int s = 0; s < STAGES_AHEAD; ++s) {
 #pragma unroll
-      for (int i = 0; i < LOADS; ++i) fetch(lds + s * C::STAGE_BYTES, i, depth - s * C::DEPTH);
+      for (int i = 0; i < A::PIECES; ++i) oa.fetch(lds + s * C::STAGE_BYTES, i, left_a);
+#pragma unroll
+      for (int i = 0; i < B::PIECES; ++i) ob.fetch(lds + s * C::STAGE_BYTES + A_BYTES, i, left_b);
       oa.next_stage();
       ob.next_stage();
+      left_a -= C::DEPTH;
+      left_b -= C::DEPTH;
     }
-    int left = depth - (C::STAGES - 1) * C::DEPTH;      // of the stages that are not on their way yet
-    stage_barrier<DIRECT ? LOADS * (C::STAGES - 2) : 0, !DIRECT>();
+    stage_barrier<DIRECT ? LOADS * (STAGES_AHEAD - 1) : 0>();
     s16x8 va[PARTS][C::MI], even[PARTS][C::NI], odd[PARTS][C::NI];
 #pragma unroll
     for (int k = 0; k < PARTS; ++k) {
@@ -226,38 +234,100 @@ struct TileProduct {
 #pragma unroll
       for (int i = 0; i < C::MI; ++i) va[k][i] = fa.read(lds, i, k);
     }
-    // The stage that is multiplied is in registers, and another's place is free: everybody has multiplied the stage before, so has
-    // read it.  The fragments of A are replaced by the next stage's as soon as they have been used, those of B are used until the end.
+    // A step multiplies the stage that is in registers and reads the next one.  Its first turns need nothing from LDS; then the
+    // wavefronts wait for one another: the next stage has arrived everywhere, and the place of the stage in registers is free.
     // Stages beyond the last are zeros.
-    u32 free = (C::STAGES - 1) * C::STAGE_BYTES, next = C::STAGE_BYTES;
-    auto step = [&](const s16x8 (&vb)[PARTS][C::NI], s16x8 (&then)[PARTS][C::NI]) {
-      stage_barrier<DIRECT ? LOADS * (C::STAGES - 3) : 0, !DIRECT>();
+    u32 next = C::STAGE_BYTES, free = PAIRS ? (C::STAGES - 1) * C::STAGE_BYTES : 0;
+    constexpr int TURNS = PARTS * C::MI, HOLD = TURNS / 4 < 1 ? 1 : TURNS / 4;
+    auto step = [&](const s16x8 (&vb)[PARTS][C::NI], s16x8 (&then)[PARTS][C::NI], auto is_odd) {
+      constexpr bool ODD = decltype(is_odd)::value;
+      auto multiply = [&](int turn) {
+#pragma unroll
+        for (int j = 0; j < C::NI; ++j) acc[turn % C::MI][j] = mma(vb[turn / C::MI][j], va[turn / C::MI][turn % C::MI], acc[turn % C::MI][j], T());
+      };
+#pragma unroll
+      for (int turn = 0; turn < HOLD; ++turn) multiply(turn);
+      __builtin_amdgcn_sched_barrier(0);
+      stage_barrier<!DIRECT ? 0 : !PAIRS ? LOADS * (C::STAGES - 2) : ODD ? A_TURN : A_TURN + B_TURN>();
       const unsigned char* s = lds + next;
-      constexpr int TURNS = PARTS * C::MI;
-      int loaded = 0, read = 0;
+      // loads of this step: a stage, or both stages of a pair for one operand
+      constexpr int FIRST = !PAIRS || !ODD ? A_TURN : 0, ALL = FIRST + (!PAIRS || ODD ? B_TURN : 0);
+      const u32 second = after(free);
+      auto load = [&](int i) {
+        if (i < FIRST) {
+          if (i < A::PIECES) oa.fetch(lds + free, i, left_a);
+          else {
+            if (i == A::PIECES) oa.next_stage();
+            oa.fetch(lds + second, i - A::PIECES, left_a - C::DEPTH);
+          }
+        } else {
+          const int n = i - FIRST;
+          if (n < B::PIECES) ob.fetch(lds + free + A_BYTES, n, left_b);
+          else {
+            if (n == B::PIECES) ob.next_stage();
+            ob.fetch(lds + second + A_BYTES, n - B::PIECES, left_b - C::DEPTH);
+          }
+        }
+      };
+      int loaded = 0, read_b = 0;
 #pragma unroll
-      for (int turn = 0; turn < TURNS; ++turn) {
-        const int k = turn / C::MI, i = turn % C::MI;
+      for (int turn = HOLD; turn < TURNS; ++turn) {
+        const int share = turn + 1 - HOLD, of = TURNS - HOLD;
 #pragma unroll
-        for (; read < PARTS * C::NI * (turn + 1) / TURNS; ++read) then[read / C::NI][read % C::NI] = fb.read(s + A_BYTES, read % C::NI, read / C::NI);
+        for (; read_b < PARTS * C::NI * share / of; ++read_b) then[read_b / C::NI][read_b % C::NI] = fb.read(s + A_BYTES, read_b % C::NI, read_b / C::NI);
+        if (turn - HOLD < HOLD) va[(turn - HOLD) / C::MI][(turn - HOLD) % C::MI] = fa.read(s, (turn - HOLD) % C::MI, (turn - HOLD) / C::MI);
 #pragma unroll
-        for (; loaded < LOADS * (turn + 1) / TURNS; ++loaded) fetch(lds + free, loaded, left);
-#pragma unroll
-        for (int j = 0; j < C::NI; ++j) acc[i][j] = mma(vb[k][j], va[k][i], acc[i][j], T());
-        va[k][i] = fa.read(s, i, k);
+        for (; loaded < ALL * share / of; ++loaded) load(loaded);
+        multiply(turn);
+        va[turn / C::MI][turn % C::MI] = fa.read(s, turn % C::MI, turn / C::MI);
         __builtin_amdgcn_sched_barrier(0);
       }
-      oa.next_stage();
-      ob.next_stage();
-      left -= C::DEPTH;
-      free = free + C::STAGE_BYTES == C::LDS_BYTES ? 0 : free + C::STAGE_BYTES;
-      next = next + C::STAGE_BYTES == C::LDS_BYTES ? 0 : next + C::STAGE_BYTES;
+      constexpr int MOVED = PAIRS ? 2 * C::DEPTH : C::DEPTH;
+      if (!PAIRS || !ODD) { oa.next_stage(); left_a -= MOVED; }
+      if (!PAIRS || ODD) { ob.next_stage(); left_b -= MOVED; free = PAIRS ? after(second) : second; }
+      next = after(next);
     };
     for (int done = 0; done < depth; done += 2 * C::DEPTH) {
-      step(even, odd);
-      step(odd, even);
+      step(even, odd, std::false_type());
+      step(odd, even, std::true_type());
     }
-    stage_barrier<0, true>();
+    stage_barrier<0>();
+  }
+
+  // Writes the tile, scaled, to out: rows x cols of it exist.  Sums are rounded once, to nearest even.  A wavefront turns its share
+  // round in LDS, so that rows leave in whole cache lines (as the sums lie, a store would touch 16 rows, 32 bytes each); whole:
+  // rows are aligned to 16 bytes.  Follows run().
+  __device__ __forceinline__ void store(unsigned char* lds, T* out, i64 ldo, int rows, int cols, bool whole, float scale) const {
+    typedef __attribute__((ext_vector_type(4))) T t4;
+    constexpr int PIECES = C::TN / 8;
+    const u32 lane = threadIdx.x % CCLD_WAVE;
+    unsigned char* own = lds + threadIdx.x / CCLD_WAVE * (C::TM * C::TN * 2);
+#pragma unroll
+    for (int i = 0; i < C::MI; ++i)
+#pragma unroll
+      for (int j = 0; j < C::NI; ++j) {
+        const u32 m = 16 * i + lane % 16, n = 16 * j + 4 * (lane / 16);
+        const f32x4 v = acc[i][j] * scale;
+        *reinterpret_cast<t4*>(own + m * (C::TN * 2) + (((n / 8) ^ along_key<C::TN>(m)) * 16) + n % 8 * 2) = t4{(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
+      }
+    __builtin_amdgcn_wave_barrier();
+    const int m0 = (int)wave_m(), n0 = (int)wave_n();
+#pragma unroll
+    for (int i = 0; i < C::TM * PIECES / CCLD_WAVE; ++i) {
+      const int m = i * (CCLD_WAVE / PIECES) + (int)lane / PIECES, p = (int)lane % PIECES, n = n0 + 8 * p;
+      const s16x8 v = *reinterpret_cast<const s16x8*>(own + m * (C::TN * 2) + ((p ^ along_key<C::TN>(m)) * 16));
+      if (m0 + m < rows) {
+        T* q = out + (i64)(m0 + m) * ldo + n;
+        if (whole && n + 8 <= cols) *reinterpret_cast<s16x8*>(q) = v;
+        else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const short x = v[e];              // (a bit cast of a vector's element itself takes the vector's first one)
+            if (n + e < cols) q[e] = __builtin_bit_cast(T, x);
+          }
+        }
+      }
+    }
   }
 
   // f(m, n, four sums of n .. n + 3) for every block, m and n within the tile

@@ -219,26 +219,23 @@ __global__ __launch_bounds__(C::THREADS) void k_logit_grad(LogitJob j) {
   TileProduct<C, T, false, false, DIRECT> prod;
   prod.run(lds, static_cast<const T*>(j.rows.h) + (i64)m0 * j.dp, j.dp, rows, static_cast<const T*>(j.w) + (i64)n0 * j.ldw, j.ldw,
            cols, j.d);
-  T* dz = static_cast<T*>(j.dz) + (i64)m0 * j.lddz + n0;
   const u32 lane = lane_id(), n1 = prod.wave_n() + 4 * (lane / 16);
 #pragma unroll
   for (int i = 0; i < C::MI; ++i) {
     const int m = (int)prod.wave_m() + 16 * i + (int)(lane % 16);
-    if (m >= rows) continue;
-    const float lse = j.rows.lse[m0 + m], scale = j.rows.scale[m0 + m];
-    const int want = j.rows.label[m0 + m] - j.first - n0 - (int)n1;
+    const bool in = m < rows;
+    const float lse = in ? j.rows.lse[m0 + m] : 0, scale = in ? j.rows.scale[m0 + m] : 0;
+    const int want = in ? j.rows.label[m0 + m] - j.first - n0 - (int)n1 : -1;
 #pragma unroll
-    for (int b = 0; b < C::NI; ++b) {
-      f32x4 v;
+    for (int b = 0; b < C::NI; ++b)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         float p = __builtin_amdgcn_exp2f((prod.acc[i][b][r] - lse) * LOG2E);
         if (16 * b + r == want) p -= 1;
-        v[r] = (int)n1 + 16 * b + r < cols ? p * scale : 0;      // columns beyond the piece are zeros that products may read
+        prod.acc[i][b][r] = (int)n1 + 16 * b + r < cols ? p * scale : 0;      // columns beyond the piece are zeros that products may read
       }
-      store4(dz + (i64)m * j.lddz + n1 + 16 * b, v, 4, true);
-    }
   }
+  prod.store(lds, static_cast<T*>(j.dz) + (i64)m0 * j.lddz + n0, j.lddz, rows, C::BN, true, 1.0f);
 }
 
 struct InputJob {            // dh: dz [kept][width] times w [width][d]
@@ -300,7 +297,7 @@ struct WeightJob {           // dw of a piece: dz^T [width][kept] times h [kept]
   int d, dp, width;
   u32 n_tiles, k_tiles;
   float* part;               // [splits][width][d] or null
-  bool wide;
+  bool whole;                // rows of dw are aligned to 16 bytes
 };
 
 template <class C, class T>
@@ -323,8 +320,7 @@ __global__ __launch_bounds__(C::THREADS) void k_weight_grad(WeightJob j) {
     prod.each([&](u32 m, u32 n, f32x4 v) { if ((int)m < ns) store4(q + (i64)m * j.d + n, v, ks - (int)n, j.d % 4 == 0); });
   } else {
     const float back = ldexpf(1.0f, -reinterpret_cast<const i32*>(j.rows.count)[1]);
-    T* q = static_cast<T*>(j.dw) + (i64)n0 * j.lddw + k0;
-    prod.each([&](u32 m, u32 n, f32x4 v) { if ((int)m < ns) store4(q + (i64)m * j.lddw + n, v * back, ks - (int)n, j.wide); });
+    prod.store(lds, static_cast<T*>(j.dw) + (i64)n0 * j.lddw + k0, j.lddw, ns, ks, j.whole, back);
   }
 }
 
@@ -535,7 +531,7 @@ ccld_status gradient(const ccld_vocab_args* a, const Plan& p, hipStream_t stream
     if (a->dw) {
       T* dw = static_cast<T*>(a->dw) + first * a->lddw;
       const WeightJob j{p.rows, p.dz, p.width, dw, a->lddw, (int)a->d, p.dp, (int)cols, 0, 0, p.weight_part,
-                        a->lddw % 4 == 0 && aligned(dw, 8)};
+                        a->lddw % 8 == 0 && aligned(dw, 16)};
       if (p.weight == LARGE) launch_weight_grad<Large, T>(p, j, stream);
       else launch_weight_grad<Medium, T>(p, j, stream);
       if (p.weight_part)
@@ -565,7 +561,8 @@ hipError_t allow_tiling() {
 
 namespace ccld {
 hipError_t allow_lds_vocab() {
-  for (hipError_t e : {allow_tiling<Large, __bf16>(), allow_tiling<Large, _Float16>(), allow_tiling<Few, __bf16>(),
+  for (hipError_t e : {allow_tiling<Large, __bf16>(), allow_tiling<Large, _Float16>(), allow_tiling<Medium, __bf16>(),
+                       allow_tiling<Medium, _Float16>(), allow_tiling<Few, __bf16>(),
                        allow_tiling<Few, _Float16>()})
     if (e != hipSuccess) return e;
   return hipSuccess;
