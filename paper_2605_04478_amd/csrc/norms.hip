@@ -7,7 +7,7 @@
 //   dn = dx gate      db = r1 (dn w_post - b r1^2 mean(dn w_post b))      dw_post = sum dn b r1      dw_pre = sum du x r2
 //
 // Memory bounds both: a dozen operations per element, each row read once and kept in registers between its two reductions.  A
-// row belongs to one wavefront where it fits, else to a workgroup.  The gradient takes x from h and b again, which costs no more
+// row belongs to one wavefront where it is short, else to a workgroup.  The gradient takes x from h and b again, which costs no more
 // bytes than reading h' and is exact; its sums over rows are kept in registers by teams that take many rows each, and joined by a
 // second kernel in the teams' order.
 #include <algorithm>
@@ -20,66 +20,83 @@ using namespace ccld;
 
 namespace {
 
-// PIECES x 8 columns to each of a row's TEAM threads: neighbours of 8 where rows are aligned to that (WIDE), else one by one
-template <int TEAM, bool WIDE>
-__device__ __forceinline__ int first_column(int t, int p) { return WIDE ? (p * TEAM + t) * 8 : p * 8 * TEAM + t; }
-template <int TEAM, bool WIDE>
-constexpr int column_step() { return WIDE ? 1 : TEAM; }
+// A thread has PIECES x 8 of a row's columns, in vectors of VEC: 16 bytes where rows are aligned to that (VEC 8 or 4), else single
+// values.  The vectors of a team's TEAM threads lie side by side.
+template <class T>
+using Piece = T __attribute__((ext_vector_type(8)));
 
-template <class T, int TEAM, bool WIDE>
-__device__ __forceinline__ void load8(float* v, const T* p, int c, int d) {
-  if constexpr (WIDE) {
-    typedef __attribute__((ext_vector_type(16 / sizeof(T)))) T piece;
-    if (c < d) {
-#pragma unroll
-      for (int k = 0; k < 8; k += 16 / (int)sizeof(T)) {
-        const piece q = *reinterpret_cast<const piece*>(p + c + k);
-#pragma unroll
-        for (int i = 0; i < 16 / (int)sizeof(T); ++i) v[k + i] = (float)q[i];
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = 0;
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = c + i * TEAM < d ? (float)p[c + i * TEAM] : 0.0f;
-  }
+template <int TEAM, int VEC>
+__device__ __forceinline__ int column(int t, int p, int i) { return ((p * (8 / VEC) + i / VEC) * TEAM + t) * VEC + i % VEC; }
+
+// A row as a buffer of its d values: columns beyond them load zeros and are not stored, without a branch.  Every value of a row that is not
+// there (no pointer) is zero.
+template <class T>
+__device__ __forceinline__ auto row_buffer(const T* row, int d) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(row), 0, row ? d * (int)sizeof(T) : 0, 0x00027000);
 }
+typedef u32 u32x4 __attribute__((ext_vector_type(4)));
 
-template <class T, int TEAM, bool WIDE>
-__device__ __forceinline__ void store8(T* p, const float* v, int c, int d) {
-  if constexpr (WIDE) {
-    typedef __attribute__((ext_vector_type(16 / sizeof(T)))) T piece;
-    if (c < d) {
+template <int TEAM, int VEC, class T>
+__device__ __forceinline__ Piece<T> load_piece(const T* row, int t, int p, int d) {
+  Piece<T> v;
+  const auto buffer = row_buffer(row, d);
 #pragma unroll
-      for (int k = 0; k < 8; k += 16 / (int)sizeof(T)) {
-        piece q;
+  for (int i = 0; i < 8; i += VEC) {
+    const int at = column<TEAM, VEC>(t, p, i) * (int)sizeof(T);
+    typedef T vec __attribute__((ext_vector_type(VEC)));
+    vec q;
+    if constexpr (VEC > 1) q = __builtin_bit_cast(vec, __builtin_amdgcn_raw_buffer_load_b128(buffer, at, 0, 0));
+    else if constexpr (sizeof(T) == 4) q = __builtin_bit_cast(vec, __builtin_amdgcn_raw_buffer_load_b32(buffer, at, 0, 0));
+    else q = __builtin_bit_cast(vec, __builtin_amdgcn_raw_buffer_load_b16(buffer, at, 0, 0));
 #pragma unroll
-        for (int i = 0; i < 16 / (int)sizeof(T); ++i) q[i] = (T)v[k + i];
-        *reinterpret_cast<piece*>(p + c + k) = q;
-      }
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (c + i * TEAM < d) p[c + i * TEAM] = (T)v[i];
-  }
-}
-
-// the sum over a row's threads; every call of a kernel that has a workgroup to a row takes another of its two slots in LDS
-template <int TEAM>
-__device__ __forceinline__ float team_sum(float v, float (&slot)[16]) {
-#pragma unroll
-  for (int m = CCLD_WAVE / 2; m >= 1; m >>= 1) v += __shfl_xor(v, m, CCLD_WAVE);
-  if constexpr (TEAM > CCLD_WAVE) {
-    if (lane_id() == 0) slot[threadIdx.x / CCLD_WAVE] = v;
-    __syncthreads();
-    v = 0;
-#pragma unroll
-    for (int i = 0; i < TEAM / CCLD_WAVE; ++i) v += slot[i];
+    for (int e = 0; e < VEC; ++e) v[i + e] = q[e];
   }
   return v;
+}
+template <int TEAM, int VEC, class T>
+__device__ __forceinline__ void store_piece(T* row, const float (&v)[8], int t, int p, int d) {
+  const auto buffer = row_buffer(row, d);
+  if constexpr (VEC > 1) {
+    constexpr int N = 16 / sizeof(T);            // values of the stored type to 16 bytes: fewer than VEC where sums of 32 bits leave
+#pragma unroll
+    for (int i = 0; i < 8; i += N) {
+      typedef T vec __attribute__((ext_vector_type(N)));
+      vec q;
+#pragma unroll
+      for (int e = 0; e < N; ++e) q[e] = (T)v[i + e];
+      __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, q), buffer, column<TEAM, VEC>(t, p, i) * (int)sizeof(T), 0, 0);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int at = column<TEAM, 1>(t, p, i) * (int)sizeof(T);
+      const T x = (T)v[i];
+      if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(u32, x), buffer, at, 0, 0);
+      else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, x), buffer, at, 0, 0);
+    }
+  }
+}
+
+// The sums of N values over a row's threads.  Teams of several wavefronts are workgroups: a call's place in LDS is written
+// again by the call after the next, so one barrier is enough.
+template <int TEAM, int N>
+__device__ __forceinline__ void team_sums(float (&v)[N], float (&place)[16][4]) {
+#pragma unroll
+  for (int m = CCLD_WAVE / 2; m >= 1; m >>= 1)
+#pragma unroll
+    for (int n = 0; n < N; ++n) v[n] += __shfl_xor(v[n], m, CCLD_WAVE);
+  if constexpr (TEAM > CCLD_WAVE) {
+    if (lane_id() == 0)
+#pragma unroll
+      for (int n = 0; n < N; ++n) place[threadIdx.x / CCLD_WAVE][n] = v[n];
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < N; ++n) v[n] = 0;
+#pragma unroll
+    for (int i = 0; i < TEAM / CCLD_WAVE; ++i)
+#pragma unroll
+      for (int n = 0; n < N; ++n) v[n] += place[i][n];
+  }
 }
 
 struct NormJob {
@@ -97,51 +114,55 @@ struct NormJob {
   float* part_gate;              // [chunks][d], or null: a gate's rows are one chunk and its sum leaves at once
 };
 
-template <class T, int TEAM, int PIECES, bool WIDE>
-__global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_norm(NormJob j) {
-  constexpr int PER_GROUP = TEAM < 256 ? 256 / TEAM : 1;
-  __shared__ float slots[2][16];
+// a team of one wavefront shares a workgroup with three others
+template <int TEAM>
+constexpr int threads_of() { return TEAM == CCLD_WAVE ? 256 : TEAM; }
+
+template <class T, int TEAM, int PIECES, int VEC>
+__global__ __launch_bounds__(threads_of<TEAM>()) void k_norm(NormJob j) {
+  __shared__ float places[2][16][4];
   const int t = threadIdx.x % TEAM;
-  const i64 row = (i64)blockIdx.x * PER_GROUP + threadIdx.x / TEAM;
-  if (row >= j.rows) return;                       // whole teams: those of several wavefronts are whole workgroups
-  const T* b = static_cast<const T*>(j.b) + row * j.ldb;
-  const T* h = static_cast<const T*>(j.h) + row * j.ldh;
-  float vb[PIECES][8], vx[PIECES][8];
-  float sum = 0;
+  i64 row = blockIdx.x;
+  if (threads_of<TEAM>() > TEAM) row = row * (threads_of<TEAM>() / TEAM) + __builtin_amdgcn_readfirstlane(threadIdx.x / TEAM);
+  if (row >= j.rows) return;                       // whole teams
+  Piece<T> pb[PIECES], ph[PIECES];
 #pragma unroll
   for (int p = 0; p < PIECES; ++p) {
-    const int c = first_column<TEAM, WIDE>(t, p);
-    load8<T, TEAM, WIDE>(vb[p], b, c, j.d);
-    load8<T, TEAM, WIDE>(vx[p], h, c, j.d);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) sum += vb[p][i] * vb[p][i];
+    pb[p] = load_piece<TEAM, VEC>(static_cast<const T*>(j.b) + row * j.ldb, t, p, j.d);
+    ph[p] = load_piece<TEAM, VEC>(static_cast<const T*>(j.h) + row * j.ldh, t, p, j.d);
   }
-  const float r1 = 1.0f / sqrtf(team_sum<TEAM>(sum, slots[0]) / (float)j.d + j.eps);
+  float sum[1] = {0};
+#pragma unroll
+  for (int p = 0; p < PIECES; ++p)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum[0] += (float)pb[p][i] * (float)pb[p][i];
+  team_sums<TEAM>(sum, places[0]);
+  const float r1 = 1.0f / sqrtf(sum[0] / (float)j.d + j.eps);
   const T* gate = j.gate ? static_cast<const T*>(j.gate) + row / j.rows_per_gate * j.ldgate : nullptr;
-  sum = 0;
+  float x[PIECES][8];
+  sum[0] = 0;
 #pragma unroll
   for (int p = 0; p < PIECES; ++p) {
-    const int c = first_column<TEAM, WIDE>(t, p);
-    float w[8], g[8];
-    load8<T, TEAM, WIDE>(w, static_cast<const T*>(j.w_post), c, j.d);
-    if (gate) load8<T, TEAM, WIDE>(g, gate, c, j.d);
+    const Piece<T> w = load_piece<TEAM, VEC>(static_cast<const T*>(j.w_post), t, p, j.d);
+    Piece<T> g;
+    if (gate) g = load_piece<TEAM, VEC>(gate, t, p, j.d);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float n = vb[p][i] * r1 * w[i];
-      vx[p][i] = j.scale * vx[p][i] + (gate ? g[i] * n : n);
-      sum += vx[p][i] * vx[p][i];
+      const float n = (float)pb[p][i] * r1 * (float)w[i];
+      x[p][i] = j.scale * (float)ph[p][i] + (gate ? (float)g[i] * n : n);
+      sum[0] += x[p][i] * x[p][i];
     }
-    store8<T, TEAM, WIDE>(static_cast<T*>(j.h_out) + row * j.ldh_out, vx[p], c, j.d);
+    store_piece<TEAM, VEC>(static_cast<T*>(j.h_out) + row * j.ldh_out, x[p], t, p, j.d);
   }
-  const float r2 = 1.0f / sqrtf(team_sum<TEAM>(sum, slots[1]) / (float)j.d + j.eps);
+  team_sums<TEAM>(sum, places[1]);
+  const float r2 = 1.0f / sqrtf(sum[0] / (float)j.d + j.eps);
 #pragma unroll
   for (int p = 0; p < PIECES; ++p) {
-    const int c = first_column<TEAM, WIDE>(t, p);
-    float w[8];
-    load8<T, TEAM, WIDE>(w, static_cast<const T*>(j.w_pre), c, j.d);
+    const Piece<T> w = load_piece<TEAM, VEC>(static_cast<const T*>(j.w_pre), t, p, j.d);
+    float u[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] *= vx[p][i] * r2;
-    store8<T, TEAM, WIDE>(static_cast<T*>(j.u) + row * j.ldu, w, c, j.d);
+    for (int i = 0; i < 8; ++i) u[i] = x[p][i] * r2 * (float)w[i];
+    store_piece<TEAM, VEC>(static_cast<T*>(j.u) + row * j.ldu, u, t, p, j.d);
   }
   if (t == 0) {
     j.rstd_post[row] = r1;
@@ -149,83 +170,139 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_norm(NormJob j) {
   }
 }
 
-template <class T, int TEAM, int PIECES, bool WIDE>
-__global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_norm_grad(NormJob j) {
-  constexpr int PER_GROUP = TEAM < 256 ? 256 / TEAM : 1;
-  __shared__ float slots[2][16];
+// Values that stay packed in registers: the compiler cannot unpack them once for all rows, which would take twice the registers.
+template <class T>
+__device__ __forceinline__ void keep_packed(Piece<T>& v) {
+  typedef u32 words __attribute__((ext_vector_type(sizeof(Piece<T>) / 4)));
+  words w = __builtin_bit_cast(words, v);
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(Piece<T>) / 4; ++i) {
+    u32 x = w[i];
+    asm volatile("" : "+v"(x));
+    w[i] = x;
+  }
+  v = __builtin_bit_cast(Piece<T>, w);
+}
+
+// With e = du w_pre and q = gate w_post b both means follow from sums that need neither, so that a row has one reduction:
+//   mean(du w_pre x) = sum(e x) / d      sum(dn w_post b) = sum(q (dh' + r2 e)) - m2 sum(q x)      (m2 = r2^3 mean(e x))
+// 128 registers for 16-bit vectors, so that 16 wavefronts run on a compute unit (8 otherwise), each with its next row on the way while it
+// computes one.  Where that does not fit (REREAD: rows of more than 8,192 columns, or 4,096 of 32 bits) a row is read again, from the
+// caches, after its reduction.
+template <class T, int TEAM, int PIECES, int VEC, bool REREAD>
+__global__ __launch_bounds__(threads_of<TEAM>(), TEAM == 1024 || (sizeof(T) == 2 && VEC > 1) ? 4 : 2) void k_norm_grad(NormJob j) {
+  constexpr int PER_GROUP = threads_of<TEAM>() / TEAM;
+  __shared__ float places[2][16][4];
   const int t = threadIdx.x % TEAM;
-  const i64 team = (i64)blockIdx.x * PER_GROUP + threadIdx.x / TEAM, teams = (i64)gridDim.x * PER_GROUP;
+  // (rows are known to be the same for a wavefront: their addresses stay in scalar registers)
+  const i64 team = PER_GROUP == 1 ? (i64)blockIdx.x : (i64)blockIdx.x * PER_GROUP + __builtin_amdgcn_readfirstlane(threadIdx.x / TEAM);
+  const i64 teams = (i64)gridDim.x * PER_GROUP;
   float s_post[PIECES][8] = {}, s_pre[PIECES][8] = {}, s_gate[PIECES][8] = {};
   const float per_d = 1.0f / (float)j.d;
+  struct Columns { Piece<T> b, h, dh, du; };
+  struct Rstd { float post, pre; };
+  struct Weights { Piece<T> post, pre, gate; };
+  auto load = [&](i64 row, int p, bool there = true) {
+    Columns c;
+    c.b = load_piece<TEAM, VEC>(there ? static_cast<const T*>(j.b) + row * j.ldb : nullptr, t, p, j.d);
+    c.h = load_piece<TEAM, VEC>(there ? static_cast<const T*>(j.h) + row * j.ldh : nullptr, t, p, j.d);
+    c.dh = load_piece<TEAM, VEC>(there && j.dh_out ? static_cast<const T*>(j.dh_out) + row * j.lddh_out : nullptr, t, p, j.d);
+    c.du = load_piece<TEAM, VEC>(there && j.du ? static_cast<const T*>(j.du) + row * j.lddu : nullptr, t, p, j.d);
+    return c;
+  };
+  auto load_rstd = [&](i64 row) { return Rstd{j.rstd_post[row], j.rstd_pre[row]}; };
+  auto load_weights = [&](const T* gate, int p) {
+    Weights w;
+    w.post = load_piece<TEAM, VEC>(static_cast<const T*>(j.w_post), t, p, j.d);
+    w.pre = load_piece<TEAM, VEC>(static_cast<const T*>(j.w_pre), t, p, j.d);
+    if (gate) w.gate = load_piece<TEAM, VEC>(gate, t, p, j.d);
+    else
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w.gate[i] = (T)1.0f;
+    return w;
+  };
+  // x and y = dh' + r2 e of a thread's columns
+  auto values = [&](const Columns& c, const Weights& w, float r1, float r2, float (&x)[8], float (&y)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      x[i] = j.scale * (float)c.h[i] + (float)w.gate[i] * (float)w.post[i] * (float)c.b[i] * r1;
+      y[i] = (float)c.dh[i] + r2 * ((float)c.du[i] * (float)w.pre[i]);
+    }
+  };
+  int turn = 0;
   for (i64 chunk = team; chunk < j.chunks; chunk += teams) {
     const i64 g = chunk / j.chunks_per_gate, in = chunk - g * j.chunks_per_gate;
     const i64 row0 = g * j.rows_per_gate + in * j.chunk_rows;
     const i64 row1 = min(row0 + j.chunk_rows, (g + 1) * j.rows_per_gate);
     const T* gate = j.gate ? static_cast<const T*>(j.gate) + g * j.ldgate : nullptr;
+    if (row0 >= row1) continue;
+    Columns next[PIECES];
+    Weights w[PIECES];
+    Rstd next_rstd = load_rstd(row0);
+    if constexpr (!REREAD) {
+#pragma unroll
+      for (int p = 0; p < PIECES; ++p) {
+        w[p] = load_weights(gate, p);
+        next[p] = load(row0, p);
+      }
+    }
     for (i64 row = row0; row < row1; ++row) {
-      const float r1 = j.rstd_post[row], r2 = j.rstd_pre[row];
-      float vb[PIECES][8], vx[PIECES][8], vd[PIECES][8], vu[PIECES][8];
-      float sum = 0;
+      // (the row after the last is loaded as zeros: a branch would make the compiler wait for loads that it cannot count)
+      const float r1 = next_rstd.post, r2 = next_rstd.pre;
+      const bool more = row + 1 < row1;
+      next_rstd = load_rstd(more ? row + 1 : row);
+      Columns now[PIECES];
+      float x[PIECES][8], y[PIECES][8], sum[3] = {0, 0, 0};
+      if constexpr (!REREAD) {
 #pragma unroll
-      for (int p = 0; p < PIECES; ++p) {
-        const int c = first_column<TEAM, WIDE>(t, p);
-        load8<T, TEAM, WIDE>(vb[p], static_cast<const T*>(j.b) + row * j.ldb, c, j.d);
-        load8<T, TEAM, WIDE>(vx[p], static_cast<const T*>(j.h) + row * j.ldh, c, j.d);
-        if (j.du) load8<T, TEAM, WIDE>(vu[p], static_cast<const T*>(j.du) + row * j.lddu, c, j.d);
-        if (j.dh_out) load8<T, TEAM, WIDE>(vd[p], static_cast<const T*>(j.dh_out) + row * j.lddh_out, c, j.d);
-      }
-#pragma unroll
-      for (int p = 0; p < PIECES; ++p) {
-        const int c = first_column<TEAM, WIDE>(t, p);
-        float w1[8], w2[8], gt[8];
-        load8<T, TEAM, WIDE>(w1, static_cast<const T*>(j.w_post), c, j.d);
-        load8<T, TEAM, WIDE>(w2, static_cast<const T*>(j.w_pre), c, j.d);
-        if (gate) load8<T, TEAM, WIDE>(gt, gate, c, j.d);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float n = vb[p][i] * r1 * w1[i];
-          vx[p][i] = j.scale * vx[p][i] + (gate ? gt[i] * n : n);
-          const float du = j.du ? vu[p][i] : 0;
-          s_pre[p][i] += du * vx[p][i] * r2;
-          vu[p][i] = du * w2[i];
-          sum += vu[p][i] * vx[p][i];
+        for (int p = 0; p < PIECES; ++p) {
+          now[p] = next[p];
+          next[p] = load(row + 1, p, more);
+          keep_packed<T>(w[p].post);
+          keep_packed<T>(w[p].pre);
+          keep_packed<T>(w[p].gate);
         }
       }
-      const float m2 = team_sum<TEAM>(sum, slots[0]) * per_d * r2 * r2;
-      sum = 0;
 #pragma unroll
       for (int p = 0; p < PIECES; ++p) {
-        const int c = first_column<TEAM, WIDE>(t, p);
-        float w1[8], gt[8], out[8];
-        load8<T, TEAM, WIDE>(w1, static_cast<const T*>(j.w_post), c, j.d);
-        if (gate) load8<T, TEAM, WIDE>(gt, gate, c, j.d);
+        if constexpr (REREAD) { now[p] = load(row, p); w[p] = load_weights(gate, p); }
+        values(now[p], w[p], r1, r2, x[p], y[p]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const float dx = (j.dh_out ? vd[p][i] : 0) + r2 * (vu[p][i] - vx[p][i] * m2);
-          out[i] = j.scale * dx;
-          const float nb = vb[p][i] * r1, dn = gate ? dx * gt[i] : dx;
-          s_gate[p][i] += dx * nb * w1[i];
+          const float q = (float)w[p].gate[i] * (float)w[p].post[i] * (float)now[p].b[i], du = (float)now[p].du[i];
+          s_pre[p][i] += du * x[p][i] * r2;
+          sum[0] += du * (float)w[p].pre[i] * x[p][i];
+          sum[1] += q * y[p][i];
+          sum[2] += q * x[p][i];
+        }
+      }
+      team_sums<TEAM>(sum, places[turn]);
+      turn ^= 1;
+      const float m2 = sum[0] * per_d * r2 * r2 * r2, m1 = (sum[1] - m2 * sum[2]) * per_d * r1 * r1;
+      i64 again = row;
+      asm volatile("" : "+s"(again));           // not the values from before the reduction
+#pragma unroll
+      for (int p = 0; p < PIECES; ++p) {
+        if constexpr (REREAD) { now[p] = load(again, p); w[p] = load_weights(gate, p); values(now[p], w[p], r1, r2, x[p], y[p]); }
+        float dh[8], db[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float b = (float)now[p].b[i], w1 = (float)w[p].post[i], dx = y[p][i] - x[p][i] * m2, nb = b * r1;
+          const float dn = dx * (float)w[p].gate[i];
+          dh[i] = j.scale * dx;
+          s_gate[p][i] += dx * nb * w1;
           s_post[p][i] += dn * nb;
-          vd[p][i] = dn * w1[i];
-          sum += vd[p][i] * vb[p][i];
+          db[i] = r1 * (dn * w1 - b * m1);
         }
-        store8<T, TEAM, WIDE>(static_cast<T*>(j.dh) + row * j.lddh, out, c, j.d);
-      }
-      const float m1 = team_sum<TEAM>(sum, slots[1]) * per_d * r1 * r1;
-#pragma unroll
-      for (int p = 0; p < PIECES; ++p) {
-        const int c = first_column<TEAM, WIDE>(t, p);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) vd[p][i] = r1 * (vd[p][i] - vb[p][i] * m1);
-        store8<T, TEAM, WIDE>(static_cast<T*>(j.db) + row * j.lddb, vd[p], c, j.d);
+        store_piece<TEAM, VEC>(static_cast<T*>(j.dh) + row * j.lddh, dh, t, p, j.d);
+        store_piece<TEAM, VEC>(static_cast<T*>(j.db) + row * j.lddb, db, t, p, j.d);
       }
     }
     if (j.dgate) {
 #pragma unroll
       for (int p = 0; p < PIECES; ++p) {
-        const int c = first_column<TEAM, WIDE>(t, p);
-        if (j.part_gate) store8<float, TEAM, WIDE>(j.part_gate + chunk * j.d, s_gate[p], c, j.d);
-        else store8<T, TEAM, WIDE>(static_cast<T*>(j.dgate) + g * j.d, s_gate[p], c, j.d);
+        if (j.part_gate) store_piece<TEAM, VEC>(j.part_gate + chunk * j.d, s_gate[p], t, p, j.d);
+        else store_piece<TEAM, VEC>(static_cast<T*>(j.dgate) + g * j.d, s_gate[p], t, p, j.d);
 #pragma unroll
         for (int i = 0; i < 8; ++i) s_gate[p][i] = 0;
       }
@@ -233,9 +310,8 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_norm_grad(NormJob j
   }
 #pragma unroll
   for (int p = 0; p < PIECES; ++p) {
-    const int c = first_column<TEAM, WIDE>(t, p);
-    store8<float, TEAM, WIDE>(j.part_post + team * j.d, s_post[p], c, j.d);
-    store8<float, TEAM, WIDE>(j.part_pre + team * j.d, s_pre[p], c, j.d);
+    store_piece<TEAM, VEC>(j.part_post + team * j.d, s_post[p], t, p, j.d);
+    store_piece<TEAM, VEC>(j.part_pre + team * j.d, s_pre[p], t, p, j.d);
   }
 }
 
@@ -275,17 +351,17 @@ __global__ __launch_bounds__(SUM_THREADS) void k_norm_sums(SumJob j) {
 
 i64 div_up(i64 a, i64 b) { return (a + b - 1) / b; }
 
-// Threads to a row of the gradient, which keeps three sums per column in registers: 8 to 32 columns each.
-int grad_team(i64 d) { return d <= 512 ? 64 : d <= 4096 ? 256 : 512; }
+// Threads to a row of the gradient, which keeps three sums per column in registers: 8 columns each, 16 of the widest rows.
+int grad_team(i64 d) { return d <= 512 ? 64 : d <= 1024 ? 128 : d <= 2048 ? 256 : d <= 4096 ? 512 : 1024; }
 
 struct Plan { int team; i64 groups, teams, chunks, chunk_rows; u32 chunks_per_gate; float *part_post, *part_pre, *part_gate; u64 bytes; };
 
 Plan make_plan(const ccld_norm_args* a, uint8_t* base) {
   Plan p{};
   p.team = grad_team(a->d);
-  const i64 per_group = p.team < 256 ? 256 / p.team : 1, gates = a->gate ? a->groups : 1;
-  // two workgroups to a compute unit; as many chunks, so that each team has one, or one for each gate
-  const i64 want = std::max<i64>(1, std::min<i64>(a->rows, 2 * (i64)COMPUTE_UNITS * per_group));
+  const i64 per_group = p.team == CCLD_WAVE ? 4 : 1, gates = a->gate ? a->groups : 1;
+  // 16 wavefronts to a compute unit, 8 of teams of one; as many chunks, so that each team has one, or one for each gate
+  const i64 want = std::max<i64>(1, std::min<i64>(a->rows, (i64)COMPUTE_UNITS * (p.team == CCLD_WAVE ? 8 : 1024 / p.team)));
   const i64 per_gate = a->rows / gates;
   p.chunks_per_gate = (u32)std::max<i64>(1, std::min(per_gate, want / gates));
   p.chunk_rows = div_up(per_gate, p.chunks_per_gate);
@@ -319,18 +395,13 @@ template <class... P>
 bool all_aligned(uintptr_t bytes, P... p) { return (aligned(p, bytes) && ...); }
 template <class... L>
 bool all_at_least(i64 d, L... l) { return ((l >= d) && ...); }
-template <class... L>
-bool all_eights(L... l) { return ((l % 8 == 0) && ...); }
-
-// pieces of 8 columns start on 16 bytes in every row
+// vectors of 16 bytes do not reach over a row's end, and start on 16 bytes in every row
 bool wide(const ccld_norm_args* a, bool grad) {
-  bool w = a->d % 8 == 0 && all_eights(a->ldh, a->ldb) && all_aligned(16, a->h, a->b, a->w_post, a->w_pre, a->gate) &&
-           (!a->gate || a->ldgate % 8 == 0);
-  if (grad)
-    w = w && all_eights(a->lddh, a->lddb) && all_aligned(16, a->dh, a->db, a->dgate, a->dh_out, a->du) &&
-        (!a->dh_out || a->lddh_out % 8 == 0) && (!a->du || a->lddu % 8 == 0);
-  else w = w && all_eights(a->ldh_out, a->ldu) && all_aligned(16, a->h_out, a->u);
-  return w;
+  const i64 vec = 16 / element_bytes(a);
+  auto even = [&](i64 ld, const void* p) { return !p || (ld % vec == 0 && aligned(p, 16)); };
+  const bool w = a->d % vec == 0 && even(a->ldh, a->h) && even(a->ldb, a->b) && even(a->ldgate, a->gate) && even(0, a->w_post) && even(0, a->w_pre);
+  if (!grad) return w && even(a->ldh_out, a->h_out) && even(a->ldu, a->u);
+  return w && even(a->lddh, a->dh) && even(a->lddb, a->db) && even(0, a->dgate) && even(a->lddh_out, a->dh_out) && even(a->lddu, a->du);
 }
 
 NormJob make_job(const ccld_norm_args* a) {
@@ -349,12 +420,12 @@ NormJob make_job(const ccld_norm_args* a) {
 
 template <class T, int TEAM, int PIECES>
 void launch_forward(const NormJob& j, bool w, hipStream_t stream) {
-  constexpr int THREADS = TEAM < 256 ? 256 : TEAM;
+  constexpr int THREADS = threads_of<TEAM>(), VEC = 16 / sizeof(T);
   const u32 grid = (u32)div_up(j.rows, THREADS / TEAM);
-  const auto kernel = w ? &k_norm<T, TEAM, PIECES, true> : &k_norm<T, TEAM, PIECES, false>;
+  const auto kernel = w ? &k_norm<T, TEAM, PIECES, VEC> : &k_norm<T, TEAM, PIECES, 1>;
   kernel<<<grid, THREADS, 0, stream>>>(j);
 }
-// a wavefront to a row of up to 2,048 columns, a workgroup of four beyond
+// a wavefront to a row of up to 1,024 columns, a workgroup beyond
 template <class T>
 ccld_status forward(const ccld_norm_args* a, hipStream_t stream) {
   const NormJob j = make_job(a);
@@ -363,15 +434,16 @@ ccld_status forward(const ccld_norm_args* a, hipStream_t stream) {
   else if (a->d <= 1024) launch_forward<T, 64, 2>(j, w, stream);
   else if (a->d <= 2048) launch_forward<T, 256, 1>(j, w, stream);
   else if (a->d <= 4096) launch_forward<T, 256, 2>(j, w, stream);
-  else if (a->d <= 8192) launch_forward<T, 256, 4>(j, w, stream);
-  else launch_forward<T, 512, 4>(j, w, stream);
+  else if (a->d <= 8192) launch_forward<T, 512, 2>(j, w, stream);
+  else launch_forward<T, 1024, 2>(j, w, stream);
   return launched();
 }
 
 template <class T, int TEAM, int PIECES>
 void launch_gradient(const NormJob& j, const Plan& p, bool w, hipStream_t stream) {
-  const auto kernel = w ? &k_norm_grad<T, TEAM, PIECES, true> : &k_norm_grad<T, TEAM, PIECES, false>;
-  kernel<<<(u32)p.groups, TEAM < 256 ? 256 : TEAM, 0, stream>>>(j);
+  constexpr bool REREAD = PIECES > 1 || (TEAM == 1024 && sizeof(T) == 4);
+  const auto kernel = w ? &k_norm_grad<T, TEAM, PIECES, (int)(16 / sizeof(T)), REREAD> : &k_norm_grad<T, TEAM, PIECES, 1, REREAD>;
+  kernel<<<(u32)p.groups, threads_of<TEAM>(), 0, stream>>>(j);
 }
 template <class T>
 ccld_status gradient(const ccld_norm_args* a, hipStream_t stream) {
@@ -381,11 +453,12 @@ ccld_status gradient(const ccld_norm_args* a, hipStream_t stream) {
   j.part_post = p.part_post; j.part_pre = p.part_pre; j.part_gate = p.part_gate;
   const bool w = wide(a, true);
   if (p.groups) {
-    if (a->d <= 512) launch_gradient<T, 64, 1>(j, p, w, stream);
-    else if (a->d <= 2048) launch_gradient<T, 256, 1>(j, p, w, stream);
-    else if (a->d <= 4096) launch_gradient<T, 256, 2>(j, p, w, stream);
-    else if (a->d <= 8192) launch_gradient<T, 512, 2>(j, p, w, stream);
-    else launch_gradient<T, 512, 4>(j, p, w, stream);
+    if (p.team == 64) launch_gradient<T, 64, 1>(j, p, w, stream);
+    else if (p.team == 128) launch_gradient<T, 128, 1>(j, p, w, stream);
+    else if (p.team == 256) launch_gradient<T, 256, 1>(j, p, w, stream);
+    else if (p.team == 512) launch_gradient<T, 512, 1>(j, p, w, stream);
+    else if (a->d <= 8192) launch_gradient<T, 1024, 1>(j, p, w, stream);
+    else launch_gradient<T, 1024, 2>(j, p, w, stream);
   }
   SumJob s{p.part_post, p.part_pre, p.part_gate, a->dw_post, a->dw_pre, a->dgate, p.teams, a->rows ? p.chunks_per_gate : 0, 2, j.d};
   if (j.dgate && (p.part_gate || a->rows == 0)) s.sums += (u32)a->groups;

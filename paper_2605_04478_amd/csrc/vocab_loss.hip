@@ -411,8 +411,11 @@ Plan make_plan(const ccld_vocab_args* a, bool grad, Carver& c) {
   p.col_tiles = (u32)div_up(p.width, tile_n(p.logits));
   p.dz = c.take<uint16_t>(rows * p.width);
   if (a->dh) {
-    p.input = tile_size(a->rows, a->d);
-    const i64 steps = p.width / DEPTH, tiles = div_up(a->rows, tile_m(p.input)) * div_up(a->d, tile_n(p.input));
+    // the contraction is long: the largest tiles, in as many parts as fill the chip (1,200 rows of 50,021 x 1,536: 452 us in tiles of
+    // 128 and two parts)
+    const i64 steps = p.width / DEPTH;
+    p.input = a->rows < 48 ? FEW : a->rows <= 128 || a->d <= 128 || steps * div_up(a->rows, 256) * div_up(a->d, 256) < 16 * (i64)COMPUTE_UNITS ? MEDIUM : LARGE;
+    const i64 tiles = div_up(a->rows, tile_m(p.input)) * div_up(a->d, tile_n(p.input));
     const u32 s = splits_for(tiles, steps);
     p.input_split = (int)(div_up(steps, s) * DEPTH);
     p.input_splits = (u32)div_up(p.width, p.input_split);
