@@ -335,8 +335,18 @@ __global__ __launch_bounds__(SUM_THREADS) void k_norm_sums(SumJob j) {
     T* out = static_cast<T*>(what == 0 ? j.dw_post : what == 1 ? j.dw_pre : j.dgate) + (what < 2 ? 0 : (i64)(what - 2) * j.d);
     const i64 n = what < 2 ? j.teams : j.chunks_per_gate;
     float s = 0;
-    if (c < j.d)
-      for (i64 r = wave; r < n; r += SUM_THREADS / CCLD_WAVE) s += p[r * j.d + c];
+    if (c < j.d) {
+      i64 r = wave;
+      constexpr int AT_ONCE = 8;
+      for (; r + (AT_ONCE - 1) * (SUM_THREADS / CCLD_WAVE) < n; r += AT_ONCE * (SUM_THREADS / CCLD_WAVE)) {
+        float v[AT_ONCE];
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) v[i] = p[(r + i * (SUM_THREADS / CCLD_WAVE)) * j.d + c];
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) s += v[i];
+      }
+      for (; r < n; r += SUM_THREADS / CCLD_WAVE) s += p[r * j.d + c];
+    }
     __syncthreads();                   // the sums before are read
     sums[wave][lane] = s;
     __syncthreads();

@@ -53,28 +53,31 @@ def _require(ok: bool, what: str) -> None:
         raise ValueError(what)
 
 
-def _tensor(t, name: str, shape, dtype):
-    """A tensor of this shape (None: any size) and type."""
-    _require(torch.is_tensor(t), f"{name} is no tensor")
-    _require(t.dim() == len(shape) and all(s is None or s == n for s, n in zip(shape, t.shape)),
-             f"{name} has shape {tuple(t.shape)}, expected {tuple('any' if s is None else s for s in shape)}")
-    _require(t.dtype in dtype if isinstance(dtype, (tuple, dict)) else t.dtype == dtype, f"{name} has type {t.dtype}")
-    return t
+def _tensor(t, name: str, shape, dtypes):
+    """A tensor of this shape (None: any size) and one of these types."""
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name} is no tensor")
+    if len(shape) != t.dim() or any(s != n and s is not None for s, n in zip(shape, t.shape)):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple('any' if s is None else s for s in shape)}")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name} has type {t.dtype}")
 
 
-def _on_gpu(**tensors):
-    """All on one GPU."""
-    first = None
-    for name, t in tensors.items():
-        if t is not None:
-            _require(t.is_cuda, f"{name} is not on a GPU: there is no CPU path")
-            first = t if first is None else first
-            _require(t.device == first.device, f"{name} is on {t.device}, not on {first.device}")
+def _on_gpu(first, *others):
+    """The GPU that all of these (None apart) are on."""
+    device = first.device
+    for t in (first, *others):
+        if t is not None and t.device != device or device.type != "cuda":
+            raise ValueError("a tensor is not on a GPU: there is no CPU path" if "cpu" in (device.type, t.device.type)
+                             else f"tensors are on {device} and {t.device}")
+    return device
 
 
 def _rows(t):
     """The tensor itself where its last dimension has unit stride and its rows do not overlap, else a copy that does so
     (expanded and transposed tensors: gradients of broadcast outputs come as the former)."""
+    if t.is_contiguous():
+        return t
     if t.stride(-1) != 1 and t.shape[-1] > 1 or any(st < t.shape[-1] and n > 1 for st, n in zip(t.stride()[:-1], t.shape[:-1])):
         return t.contiguous()
     return t
@@ -94,32 +97,55 @@ def _check(status: int, where: str) -> None:
         raise CcldError(status, where)
 
 
+class _NoChange:
+    def __enter__(self): pass
+    def __exit__(self, *_): pass
+
+
+_NO_CHANGE = _NoChange()
+
+
+def _current(device):
+    """Makes a GPU the current one, where it is not (which takes some microseconds)."""
+    return _NO_CHANGE if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+
 def _workspace(query, args, device, *extra):
     """A buffer of the size that the query names, set in the arguments; torch's allocator starts buffers on 512 bytes."""
-    need = C.c_uint64(0)
+    need = C.c_uint64()
     _check(query(C.addressof(args), *extra, C.addressof(need)), query.__name__)
-    ws = torch.empty(need.value, dtype=torch.uint8, device=device) if need.value else None
-    args.workspace, args.workspace_bytes = _ptr(ws), need.value
+    if not need.value:
+        return None
+    ws = torch.empty(need.value, dtype=torch.uint8, device=device)
+    args.workspace, args.workspace_bytes = ws.data_ptr(), need.value
     return ws
 
 
 def _call(fn, args, device) -> None:
-    _check(fn(C.addressof(args), torch.cuda.current_stream(device).cuda_stream), fn.__name__)
+    _check(fn(C.addressof(args), torch._C._cuda_getCurrentRawStream(device.index)), fn.__name__)
 
 
 # ---- products grouped by expert ---------------------------------------------------------------------------------------
-def _expert_args(x, w, offsets):
+INTEGERS = (torch.int32, torch.int64)
+
+
+def _expert_inputs(x, w, offsets, *others):
     _tensor(w, "w", (None, None, None), DTYPES)
     e, n, k = w.shape
-    _tensor(x, "x", (None, k), w.dtype)
-    _tensor(offsets, "offsets", (e + 1,), (torch.int32, torch.int64))
+    _tensor(x, "x", (None, k), (w.dtype,))
+    _tensor(offsets, "offsets", (e + 1,), INTEGERS)
     _require(e > 0 and n > 0 and k > 0, f"w has shape {tuple(w.shape)}: no size may be zero")
-    _on_gpu(w=w, x=x, offsets=offsets)
-    x, w, offsets = _rows(x), _rows(w), offsets.contiguous()
-    a = _ExpertArgs(dtype=DTYPES[w.dtype], offsets_bits=8 * offsets.element_size(), rows=x.shape[0], k=k, n=n, n_experts=e,
-                    x=_ptr(x), w=_ptr(w), offsets=_ptr(offsets), ldx=_ld(x), ldw=_ld(w),
-                    expert_stride=w.stride(0) if e > 1 else 0)
-    return a, (x, w, offsets)
+    for t in others:
+        _tensor(t, "dy", (x.shape[0], n), (w.dtype,))
+    device = _on_gpu(w, x, offsets, *others)
+    return device, _rows(x), _rows(w), offsets.contiguous(), *map(_rows, others)
+
+
+def _expert_args(x, w, offsets, dy, y, dx, dw):
+    e, n, k = w.shape
+    return _ExpertArgs(DTYPES[w.dtype], 8 * offsets.element_size(), x.shape[0], k, n, e, x.data_ptr(), w.data_ptr(), offsets.data_ptr(),
+                       _ptr(dy), _ptr(y), _ptr(dx), _ptr(dw), _ld(x), _ld(w), w.stride(0) if e > 1 else 0,
+                       n if dy is None else _ld(dy), n, k, None, 0)
 
 
 def expert_product(x, w, offsets):
@@ -127,29 +153,28 @@ def expert_product(x, w, offsets):
 
     x [rows, k] and w [experts, n, k] in bfloat16 or float16, offsets [experts + 1] in int32 or int64 -> y [rows, n].
     Rows that belong to no expert are zero.  The offsets stay on the device; they must not decrease."""
-    a, keep = _expert_args(x, w, offsets)
-    with torch.cuda.device(w.device):
-        y = torch.empty(a.rows, a.n, dtype=w.dtype, device=w.device)
-        a.y, a.ldy = _ptr(y), a.n
-        ws = _workspace(lib().ccld_expert_workspace, a, w.device, 0)
-        _call(lib().ccld_expert_product, a, w.device)
-    del keep, ws
+    device, x, w, offsets = _expert_inputs(x, w, offsets)
+    L = lib()
+    with _current(device):
+        y = torch.empty(x.shape[0], w.shape[1], dtype=w.dtype, device=device)
+        a = _expert_args(x, w, offsets, None, y, None, None)
+        ws = _workspace(L.ccld_expert_workspace, a, device, 0)      # (kept until the call has been enqueued)
+        _call(L.ccld_expert_product, a, device)
+    del ws
     return y
 
 
 def expert_product_grad(dy, x, w, offsets, need_dx: bool = True, need_dw: bool = True):
     """Gradients of expert_product: (dx [rows, k], dw [experts, n, k]); None for one that is not needed."""
-    a, keep = _expert_args(x, w, offsets)
-    _tensor(dy, "dy", (a.rows, a.n), w.dtype)
-    _on_gpu(w=w, dy=dy)
-    dy = _rows(dy)
-    with torch.cuda.device(w.device):
-        dx = torch.empty(a.rows, a.k, dtype=w.dtype, device=w.device) if need_dx else None
-        dw = torch.empty(a.n_experts, a.n, a.k, dtype=w.dtype, device=w.device) if need_dw else None
-        a.dy, a.lddy, a.dx, a.lddx, a.dw = _ptr(dy), _ld(dy), _ptr(dx), a.k, _ptr(dw)
-        ws = _workspace(lib().ccld_expert_workspace, a, w.device, 1)
-        _call(lib().ccld_expert_product_grad, a, w.device)
-    del keep, ws
+    device, x, w, offsets, dy = _expert_inputs(x, w, offsets, dy)
+    L = lib()
+    with _current(device):
+        dx = torch.empty(x.shape, dtype=w.dtype, device=device) if need_dx else None
+        dw = torch.empty(w.shape, dtype=w.dtype, device=device) if need_dw else None
+        a = _expert_args(x, w, offsets, dy, None, dx, dw)
+        ws = _workspace(L.ccld_expert_workspace, a, device, 1)
+        _call(L.ccld_expert_product_grad, a, device)
+    del ws
     return dx, dw
 
 
@@ -169,17 +194,23 @@ class ExpertProduct(torch.autograd.Function):
 
 
 # ---- softmax cross entropy over a vocabulary ----------------------------------------------------------------------------
-def _vocab_args(h, w, labels):
+def _vocab_inputs(h, w, labels, *others):
     _tensor(w, "w", (None, None), DTYPES)
     v, d = w.shape
-    _tensor(h, "h", (None, d), w.dtype)
-    _tensor(labels, "labels", (h.shape[0],), (torch.int32, torch.int64))
+    _tensor(h, "h", (None, d), (w.dtype,))
+    _tensor(labels, "labels", (h.shape[0],), INTEGERS)
     _require(v > 0 and d > 0, f"w has shape {tuple(w.shape)}: no size may be zero")
-    _on_gpu(w=w, h=h, labels=labels)
-    h, w, labels = _rows(h), _rows(w), labels.contiguous()
-    a = _VocabArgs(dtype=DTYPES[w.dtype], label_bits=8 * labels.element_size(), rows=h.shape[0], d=d, vocab=v, h=_ptr(h),
-                   w=_ptr(w), labels=_ptr(labels), ldh=_ld(h), ldw=_ld(w))
-    return a, (h, w, labels)
+    for name, t in zip(("dloss", "lse"), others):
+        _tensor(t, name, (h.shape[0],), (torch.float32,))
+    device = _on_gpu(w, h, labels, *others)
+    return device, _rows(h), _rows(w), labels.contiguous()
+
+
+def _vocab_args(h, w, labels, dloss, loss, lse, dh, dw):
+    v, d = w.shape
+    return _VocabArgs(DTYPES[w.dtype], 8 * labels.element_size(), h.shape[0], d, v, h.data_ptr(), w.data_ptr(), labels.data_ptr(),
+                      _ptr(dloss), _ptr(loss), lse.data_ptr(), _ptr(dh), _ptr(dw), _ld(h), _ld(w),
+                      0 if dloss is None else dloss.stride(0), d, d, None, 0)
 
 
 def vocab_loss(h, w, labels):
@@ -187,13 +218,15 @@ def vocab_loss(h, w, labels):
 
     h and w in bfloat16 or float16, labels [rows] in int32 or int64 -> (loss [rows], lse [rows]) in float32, lse being the
     logarithm of the sum of the logits' exponentials.  A row whose label is outside [0, vocab) has no target: both are zero."""
-    a, keep = _vocab_args(h, w, labels)
-    with torch.cuda.device(w.device):
-        loss, lse = torch.empty(2, a.rows, dtype=torch.float32, device=w.device).unbind(0)
-        a.loss, a.lse = _ptr(loss), _ptr(lse)
-        ws = _workspace(lib().ccld_vocab_workspace, a, w.device, 0)
-        _call(lib().ccld_vocab_loss, a, w.device)
-    del keep, ws
+    device, h, w, labels = _vocab_inputs(h, w, labels)
+    L = lib()
+    with _current(device):
+        loss = torch.empty(h.shape[0], dtype=torch.float32, device=device)
+        lse = torch.empty(h.shape[0], dtype=torch.float32, device=device)
+        a = _vocab_args(h, w, labels, None, loss, lse, None, None)
+        ws = _workspace(L.ccld_vocab_workspace, a, device, 0)
+        _call(L.ccld_vocab_loss, a, device)
+    del ws
     return loss, lse
 
 
@@ -201,19 +234,16 @@ def vocab_loss_grad(dloss, h, w, labels, lse, need_dh: bool = True, need_dw: boo
     """Gradients of vocab_loss for dloss [rows], the gradient of each row's loss, and the lse that it returned:
     (dh [rows, d], dw [vocab, d]) in the type of h and w; None for one that is not needed.  The logits are taken again, in
     pieces of the vocabulary.  Rows without a target have no gradient, whatever they hold."""
-    a, keep = _vocab_args(h, w, labels)
-    _tensor(dloss, "dloss", (a.rows,), torch.float32)
-    _tensor(lse, "lse", (a.rows,), torch.float32)
-    _on_gpu(w=w, dloss=dloss, lse=lse)
+    device, h, w, labels = _vocab_inputs(h, w, labels, dloss, lse)
     lse = lse.contiguous()
-    with torch.cuda.device(w.device):
-        dh = torch.empty(a.rows, a.d, dtype=w.dtype, device=w.device) if need_dh else None
-        dw = torch.empty(a.vocab, a.d, dtype=w.dtype, device=w.device) if need_dw else None
-        a.dloss, a.dloss_stride, a.lse = _ptr(dloss), dloss.stride(0), _ptr(lse)
-        a.dh, a.lddh, a.dw, a.lddw = _ptr(dh), a.d, _ptr(dw), a.d
-        ws = _workspace(lib().ccld_vocab_workspace, a, w.device, 1)
-        _call(lib().ccld_vocab_loss_grad, a, w.device)
-    del keep, ws
+    L = lib()
+    with _current(device):
+        dh = torch.empty(h.shape, dtype=w.dtype, device=device) if need_dh else None
+        dw = torch.empty(w.shape, dtype=w.dtype, device=device) if need_dw else None
+        a = _vocab_args(h, w, labels, dloss, None, lse, dh, dw)
+        ws = _workspace(L.ccld_vocab_workspace, a, device, 1)
+        _call(L.ccld_vocab_loss_grad, a, device)
+    del ws
     return dh, dw
 
 
@@ -235,26 +265,27 @@ class VocabLoss(torch.autograd.Function):
 
 
 # ---- the norms around a block, its gate and the residual scale -----------------------------------------------------------
-def _norm_args(h, b, gate, w_post, w_pre, scale, eps):
+def _norm_inputs(h, b, gate, w_post, w_pre, eps, dh_out=None, du=None, *rstd):
     _tensor(h, "h", (None, None), NORM_DTYPES)
     rows, d = h.shape
-    _tensor(b, "b", (rows, d), h.dtype)
-    _tensor(w_post, "w_post", (d,), h.dtype)
-    _tensor(w_pre, "w_pre", (d,), h.dtype)
+    own = (h.dtype,)
+    _tensor(b, "b", (rows, d), own)
+    _tensor(w_post, "w_post", (d,), own)
+    _tensor(w_pre, "w_pre", (d,), own)
     _require(0 < d <= NORM_MAX, f"h has {d} columns: 1 to {NORM_MAX} are possible")
-    groups = 1
     if gate is not None:
-        _tensor(gate, "gate", (None, d), h.dtype)
+        _tensor(gate, "gate", (None, d), own)
         groups = gate.shape[0]
         _require(groups > 0 and rows % groups == 0, f"{rows} rows cannot share {groups} rows of gate evenly")
+        gate = _rows(gate)
     _require(eps >= 0, f"eps is {eps}")
-    _on_gpu(h=h, b=b, gate=gate, w_post=w_post, w_pre=w_pre)
-    h, b, w_post, w_pre = _rows(h), _rows(b), w_post.contiguous(), w_pre.contiguous()
-    gate = None if gate is None else _rows(gate)
-    a = _NormArgs(dtype=NORM_DTYPES[h.dtype], scale=scale, eps=eps, rows=rows, d=d, groups=groups, h=_ptr(h), b=_ptr(b),
-                  gate=_ptr(gate), w_post=_ptr(w_post), w_pre=_ptr(w_pre), ldh=_ld(h), ldb=_ld(b),
-                  ldgate=d if gate is None else _ld(gate))
-    return a, (h, b, gate, w_post, w_pre)
+    for name, t in (("dh_out", dh_out), ("du", du)):
+        if t is not None:
+            _tensor(t, name, (rows, d), own)
+    for name, t in zip(("rstd_post", "rstd_pre"), rstd):
+        _tensor(t, name, (rows,), (torch.float32,))
+    device = _on_gpu(h, b, gate, w_post, w_pre, dh_out, du, *rstd)
+    return device, _rows(h), _rows(b), gate, w_post.contiguous(), w_pre.contiguous()
 
 
 def norm_residual(h, b, gate, w_post, w_pre, scale: float = 1.0, eps: float = 1e-6):
@@ -265,40 +296,41 @@ def norm_residual(h, b, gate, w_post, w_pre, scale: float = 1.0, eps: float = 1e
 
     h, b [rows, d] in bfloat16, float16 or float32, w_post and w_pre [d]; gate [g, d], each of whose rows serves rows / g
     consecutive rows, or None.  -> (h', u, 1 / rms(b), 1 / rms(h')), the last two [rows] in float32."""
-    a, keep = _norm_args(h, b, gate, w_post, w_pre, scale, eps)
-    with torch.cuda.device(h.device):
-        h_out, u = (torch.empty(a.rows, a.d, dtype=h.dtype, device=h.device) for _ in range(2))
-        rstd_post, rstd_pre = torch.empty(2, a.rows, dtype=torch.float32, device=h.device).unbind(0)
-        a.h_out, a.u, a.ldh_out, a.ldu = _ptr(h_out), _ptr(u), a.d, a.d
-        a.rstd_post, a.rstd_pre = _ptr(rstd_post), _ptr(rstd_pre)
-        _call(lib().ccld_norm_residual, a, h.device)
-    del keep
+    device, h, b, gate, w_post, w_pre = _norm_inputs(h, b, gate, w_post, w_pre, eps)
+    rows, d = h.shape
+    with _current(device):
+        h_out = torch.empty(rows, d, dtype=h.dtype, device=device)
+        u = torch.empty(rows, d, dtype=h.dtype, device=device)
+        rstd_post = torch.empty(rows, dtype=torch.float32, device=device)
+        rstd_pre = torch.empty(rows, dtype=torch.float32, device=device)
+        a = _NormArgs(NORM_DTYPES[h.dtype], scale, eps, 0, rows, d, 1 if gate is None else gate.shape[0], h.data_ptr(), b.data_ptr(),
+                      _ptr(gate), w_post.data_ptr(), w_pre.data_ptr(), h_out.data_ptr(), u.data_ptr(), rstd_post.data_ptr(),
+                      rstd_pre.data_ptr(), None, None, None, None, None, None, None,
+                      _ld(h), _ld(b), d if gate is None else _ld(gate), d, d, d, d, d, d, None, 0)
+        _call(lib().ccld_norm_residual, a, device)
     return h_out, u, rstd_post, rstd_pre
 
 
 def norm_residual_grad(dh_out, du, h, b, gate, w_post, w_pre, rstd_post, rstd_pre, scale: float = 1.0):
     """Gradients of norm_residual for those of h' and u (either may be None: zero) and the two vectors that it returned:
     (dh, db, dgate, dw_post, dw_pre), all in the type of h; dgate is None without a gate."""
-    a, keep = _norm_args(h, b, gate, w_post, w_pre, scale, 0.0)
-    for name, t in (("dh_out", dh_out), ("du", du)):
-        if t is not None:
-            _tensor(t, name, (a.rows, a.d), h.dtype)
-    _tensor(rstd_post, "rstd_post", (a.rows,), torch.float32)
-    _tensor(rstd_pre, "rstd_pre", (a.rows,), torch.float32)
-    _on_gpu(h=h, dh_out=dh_out, du=du, rstd_post=rstd_post, rstd_pre=rstd_pre)
+    device, h, b, gate, w_post, w_pre = _norm_inputs(h, b, gate, w_post, w_pre, 0.0, dh_out, du, rstd_post, rstd_pre)
+    rows, d = h.shape
     dh_out, du = (None if t is None else _rows(t) for t in (dh_out, du))
     rstd_post, rstd_pre = rstd_post.contiguous(), rstd_pre.contiguous()
-    with torch.cuda.device(h.device):
-        dh, db = (torch.empty(a.rows, a.d, dtype=h.dtype, device=h.device) for _ in range(2))
-        dgate = None if gate is None else torch.empty(a.groups, a.d, dtype=h.dtype, device=h.device)
-        dw_post, dw_pre = (torch.empty(a.d, dtype=h.dtype, device=h.device) for _ in range(2))
-        a.dh_out, a.du, a.dh, a.db, a.dgate, a.dw_post, a.dw_pre = map(_ptr, (dh_out, du, dh, db, dgate, dw_post, dw_pre))
-        a.lddh_out, a.lddu = (a.d if t is None else _ld(t) for t in (dh_out, du))
-        a.lddh, a.lddb = a.d, a.d
-        a.rstd_post, a.rstd_pre = _ptr(rstd_post), _ptr(rstd_pre)
-        ws = _workspace(lib().ccld_norm_workspace, a, h.device)
-        _call(lib().ccld_norm_residual_grad, a, h.device)
-    del keep, ws
+    L = lib()
+    with _current(device):
+        new = lambda *shape: torch.empty(shape, dtype=h.dtype, device=device)
+        dh, db, dw_post, dw_pre = new(rows, d), new(rows, d), new(d), new(d)
+        dgate = None if gate is None else new(*gate.shape)
+        a = _NormArgs(NORM_DTYPES[h.dtype], scale, 0.0, 0, rows, d, 1 if gate is None else gate.shape[0], h.data_ptr(), b.data_ptr(),
+                      _ptr(gate), w_post.data_ptr(), w_pre.data_ptr(), None, None, rstd_post.data_ptr(), rstd_pre.data_ptr(),
+                      _ptr(dh_out), _ptr(du), dh.data_ptr(), db.data_ptr(), _ptr(dgate), dw_post.data_ptr(), dw_pre.data_ptr(),
+                      _ld(h), _ld(b), d if gate is None else _ld(gate), d, d, d if dh_out is None else _ld(dh_out),
+                      d if du is None else _ld(du), d, d, None, 0)
+        ws = _workspace(L.ccld_norm_workspace, a, device)
+        _call(L.ccld_norm_residual_grad, a, device)
+    del ws
     return dh, db, dgate, dw_post, dw_pre
 
 
