@@ -142,20 +142,27 @@ __global__ __launch_bounds__(C::THREADS) void k_expert_weights(WeightJob j) {
 
 u64 div_up(u64 a, u64 b) { return (a + b - 1) / b; }
 
-// How the rows' products are cut: tile size by the rows that an expert has on average, and the contraction in several parts
-// where the tiles alone leave compute units idle.
+// How the rows' products are cut.  Experts with less than 48 rows on average are bound by reading their weights: tiles of 32 rows.
 struct RowPlan { int bm, bn; u32 col_tiles; u64 groups; u32 splits; int split_depth; };
 RowPlan plan_rows(u64 rows, u64 experts, int cols, int depth) {
   RowPlan p;
-  const u64 busy = std::min(rows, experts), mean = rows / std::max<u64>(experts, 1);
-  p.bm = mean >= 512 ? 256 : mean >= 48 ? 128 : 32;
-  p.bn = p.bm == 256 ? 256 : 128;
+  const u64 busy = std::min(rows, experts), mean = rows / std::max<u64>(experts, 1), steps = div_up(depth, DEPTH);
+  u64 s = 1;
+  if (mean < 48) {
+    p.bm = 32;
+    p.bn = 128;
+    const u64 tiles = std::max<u64>(div_up(rows, 32), busy) * div_up(cols, 128);
+    while (tiles * s < COMPUTE_UNITS && steps / (2 * s) >= 8) s *= 2;
+  } else {
+    // a part's last tile is half full on average
+    const double m256 = std::max<double>(busy, rows / 256.0 + busy * 0.5), m128 = std::max<double>(busy, rows / 128.0 + busy * 0.5);
+    const Cut c = choose_cut(m256 * div_up(cols, 256), m128 * div_up(cols, 128), 2 * steps, (double)rows * cols, busy == 1);
+    p.bm = p.bn = c.large ? 256 : 128;
+    s = c.splits;
+  }
   p.col_tiles = (u32)div_up(cols, p.bn);
   // tiles of the worst division: every part may end in a tile of its own
   p.groups = (rows / p.bm + std::min(rows, experts + 2)) * p.col_tiles;
-  const u64 tiles = std::max<u64>(div_up(rows, p.bm), busy) * p.col_tiles, steps = div_up(depth, DEPTH);
-  u64 s = 1;
-  while (tiles * s < COMPUTE_UNITS && steps / (2 * s) >= 8) s *= 2;
   p.split_depth = (int)(div_up(steps, s) * DEPTH);
   p.splits = (u32)div_up(steps, div_up(steps, s));
   return p;
@@ -164,13 +171,12 @@ RowPlan plan_rows(u64 rows, u64 experts, int cols, int depth) {
 struct WeightPlan { int bm, bn; u32 n_tiles, k_tiles, splits; };
 WeightPlan plan_weights(u64 rows, u64 experts, int n, int k) {
   WeightPlan p;
-  p.bm = p.bn = experts * div_up(n, 256) * div_up(k, 256) >= COMPUTE_UNITS ? 256 : 128;
+  const Cut c = choose_cut((double)experts * div_up(n, 256) * div_up(k, 256), (double)experts * div_up(n, 128) * div_up(k, 128),
+                           div_up(rows, experts * 32), (double)experts * n * k, true);
+  p.bm = p.bn = c.large ? 256 : 128;
   p.n_tiles = (u32)div_up(n, p.bm);
   p.k_tiles = (u32)div_up(k, p.bn);
-  const u64 tiles = experts * p.n_tiles * p.k_tiles, steps = div_up(rows, experts * DEPTH);
-  u32 s = 1;
-  while (tiles * s < COMPUTE_UNITS && steps / (2 * s) >= 8) s *= 2;
-  p.splits = s;
+  p.splits = c.splits;
   return p;
 }
 

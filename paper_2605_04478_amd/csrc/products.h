@@ -14,6 +14,39 @@ constexpr int64_t MAX_ROWS = (int64_t)1 << 31, MAX_EXPERTS = (int64_t)1 << 20, M
 // a tile's last row starts below 2^31 bytes from its first: 256 rows (or DEPTH of them) of this many 16-bit elements, and a row
 constexpr int64_t MAX_LD = ((int64_t)1 << 22) - ((int64_t)1 << 14);
 
+// How a product is cut: tiles of 256 x 256, one to a compute unit, or of 128 x 128, two to one, and the contraction in `splits` parts whose
+// sums are joined.  A step of 32 of the contraction takes 0.77 us in the former (8192^3: 1,390 TFLOP/s) and 0.5 us in the latter (1,084), a tile's
+// start and end 10 and 6 us, and sums of parts move at 4.5 TB/s.  The smaller tiles win where the larger ones would leave
+// compute units idle: the weights of 12 experts, 1,000 x 1,336 each, are 288 tiles of 256 (48 us) or 1,056 of 128 (38 us); those of 64
+// experts, 1,024 x 2,048 each and 128 rows on average, 98 us and 123.  counted: the numbers of tiles are what they will be, not what ragged rows are expected to give.
+struct Cut { bool large; uint32_t splits; };
+inline Cut choose_cut(double tiles_256, double tiles_128, uint64_t steps, double results, bool counted, uint32_t most_splits = 16) {
+  Cut best{true, 1};
+  double least = 1e300;
+  for (int large = 1; large >= 0; --large)
+    for (uint32_t s = 1; s <= most_splits && (s == 1 || steps / s >= 16); s *= 2) {
+      double rounds = (large ? tiles_256 : tiles_128) * s / (double)(large ? COMPUTE_UNITS : 2 * COMPUTE_UNITS);
+      if (rounds < 0.7) rounds = 1;
+      else if (rounds < 4) rounds = counted ? (double)(int64_t)(rounds + 0.999) : rounds + 0.35;
+      const double us = rounds * ((large ? 10 : 6) + (double)((steps + s - 1) / s) * (large ? 0.77 : 0.5)) + (s > 1 ? 4 + results * (8.0 * s + 2) / 4.5e6 : 0);
+      if (us < least) { least = us; best = Cut{large != 0, s}; }
+    }
+  return best;
+}
+
+// In how many parts tiles of 256 x 256, `steps` of 32 deep, are computed where their number is known on the device only: what leaves the fewest
+// compute units idle, with no more than twice as many pieces as there are of them.
+constexpr uint32_t MOST_SPLITS = 16, MOST_PIECES = 2 * (uint32_t)COMPUTE_UNITS;
+__host__ __device__ inline uint32_t splits_of(uint32_t tiles, uint32_t steps) {
+  uint32_t best = 1, least = ~0u;
+  for (uint32_t s = 1; s <= MOST_SPLITS && (s == 1 || (tiles * s <= MOST_PIECES && steps / s >= 16)); ++s) {
+    // rounds / s in 64ths, and a little for the sums' way through memory
+    const uint32_t cost = (uint32_t)((tiles * s + COMPUTE_UNITS - 1) / COMPUTE_UNITS) * 1024 / s + 8 * s;
+    if (cost < least) { least = cost; best = s; }
+  }
+  return best;
+}
+
 inline bool aligned(const void* p, uintptr_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
 inline ccld_status launched() { return hipGetLastError() == hipSuccess ? CCLD_OK : CCLD_E_HIP; }
 

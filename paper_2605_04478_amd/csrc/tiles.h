@@ -73,7 +73,7 @@ struct Tiling {
 };
 
 using Large = Tiling<256, 256, 2, 4, 32, 5>;
-using Medium = Tiling<128, 128, 2, 2, 32, 5>;
+using Medium = Tiling<128, 128, 2, 4, 32, 5>;
 using Few = Tiling<32, 128, 1, 4, 64, 4>;
 
 // Which 32-byte piece of an operand that lies across c is kept at a position of row c in LDS: the wavefront's transposing
@@ -296,7 +296,7 @@ struct TileProduct {
 
   // Writes the tile, scaled, to out: rows x cols of it exist.  Sums are rounded once, to nearest even.  A wavefront turns its share
   // round in LDS, so that rows leave in whole cache lines (as the sums lie, a store would touch 16 rows, 32 bytes each); whole:
-  // rows are aligned to 16 bytes.  Follows run().
+  // rows are aligned to 16 bytes.  They are not kept in the L2, which the operands need (1 % of 8192^3).  Follows run().
   __device__ __forceinline__ void store(unsigned char* lds, T* out, i64 ldo, int rows, int cols, bool whole, float scale) const {
     typedef __attribute__((ext_vector_type(4))) T t4;
     constexpr int PIECES = C::TN / 8;
@@ -318,7 +318,7 @@ struct TileProduct {
       const s16x8 v = *reinterpret_cast<const s16x8*>(own + m * (C::TN * 2) + ((p ^ along_key<C::TN>(m)) * 16));
       if (m0 + m < rows) {
         T* q = out + (i64)(m0 + m) * ldo + n;
-        if (whole && n + 8 <= cols) *reinterpret_cast<s16x8*>(q) = v;
+        if (whole && n + 8 <= cols) __builtin_nontemporal_store(v, reinterpret_cast<s16x8*>(q));
         else {
 #pragma unroll
           for (int e = 0; e < 8; ++e) {

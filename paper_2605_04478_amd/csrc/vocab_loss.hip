@@ -45,13 +45,29 @@ __device__ __forceinline__ i64 label_at(const void* p, int bits, i64 i) {
   return bits == 64 ? static_cast<const i64*>(p)[i] : (i64)static_cast<const i32*>(p)[i];
 }
 
+// A kept row's values, padded with zeros to dp columns, V at a time; and, for the gradient, its lse and scaled dloss.
+template <class T, int V>
+__device__ __forceinline__ void gather_piece(const Rows& w, i64 i, i64 at, int c, i64 r, const T* h, i64 ldh, int d, const float* lse, const float* dloss,
+                                             i64 dloss_stride, float scale) {
+  if constexpr (V == 8) reinterpret_cast<s16x8*>(w.h)[i] = *reinterpret_cast<const s16x8*>(h + r * ldh + c);
+  else static_cast<T*>(w.h)[i] = c < d ? h[r * ldh + c] : (T)0.0f;
+  if (c == 0 && dloss) {
+    w.lse[at] = lse[r];
+    w.scale[at] = dloss[r * dloss_stride] * scale;
+  }
+}
+
 // Which rows have a target, in order; zeros for the loss of the others; the largest |dloss|.  One workgroup: the labels of 8,192
-// rows are 64 KB.
-__global__ __launch_bounds__(USED_THREADS) void k_used_rows(Rows w, const void* labels, int bits, i64 rows, i64 vocab, float* loss,
-                                                            float* lse, const float* dloss, i64 dloss_stride) {
+// rows are 64 KB.  GATHER: there are no more rows than threads, and every workgroup finds them by itself and copies its share of them too
+// (a launch less: 5 us of a handful of rows' 45).
+template <class T, int V, bool GATHER>
+__global__ __launch_bounds__(USED_THREADS) void k_used_rows(Rows w, const void* labels, int bits, i64 rows, i64 vocab, float* loss, float* lse_out,
+                                                            const T* h, i64 ldh, int d, int dp, const float* lse, const float* dloss, i64 dloss_stride) {
   __shared__ u32 sums[USED_THREADS / CCLD_WAVE];
   __shared__ float tops[USED_THREADS / CCLD_WAVE];
+  __shared__ i32 list[GATHER ? USED_THREADS : 1];
   const u32 lane = lane_id(), wave = threadIdx.x / CCLD_WAVE;
+  const bool writes = blockIdx.x == 0;
   u32 before = 0;
   float top = 0;
   for (i64 base = 0; base < rows; base += USED_THREADS) {
@@ -68,30 +84,41 @@ __global__ __launch_bounds__(USED_THREADS) void k_used_rows(Rows w, const void* 
     }
     __syncthreads();
     at += mbcnt64(mask);
-    if (used) {
-      w.row[at] = (i32)r;
-      w.label[at] = (i32)l;
-      if (dloss) top = fmaxf(top, fabsf(dloss[r * dloss_stride]));
-    } else if (r < rows && loss) {
-      loss[r] = 0;
-      lse[r] = 0;
+    if (used && dloss) top = fmaxf(top, fabsf(dloss[r * dloss_stride]));
+    if (GATHER && used) list[at] = (i32)r;
+    if (writes && r < rows) {
+      if (used) {
+        w.row[at] = (i32)r;
+        w.label[at] = (i32)l;
+      } else if (loss) {
+        loss[r] = 0;
+        lse_out[r] = 0;
+      }
+      w.place[r] = used ? (i32)at : -1;
     }
-    if (r < rows) w.place[r] = used ? (i32)at : -1;
   }
   for (int m = CCLD_WAVE / 2; m >= 1; m >>= 1) top = fmaxf(top, __shfl_xor(top, m, CCLD_WAVE));
   if (lane == 0) tops[wave] = top;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    for (u32 i = 0; i < USED_THREADS / CCLD_WAVE; ++i) top = fmaxf(top, tops[i]);
-    int e = 0;
-    if (top > 0 && top < __builtin_inff()) (void)frexpf(top, &e);
+  for (u32 i = 0; i < USED_THREADS / CCLD_WAVE; ++i) top = fmaxf(top, tops[i]);
+  int e = 0;
+  if (top > 0 && top < __builtin_inff()) (void)frexpf(top, &e);
+  // top 2^(15 - e) lies in [2^14, 2^15); the scale and its inverse stay within 32-bit floats
+  const int scaling = top > 0 && top < __builtin_inff() ? min(15 - e, 120) : 0;
+  if (writes && threadIdx.x == 0) {
     w.count[0] = before;
-    // top 2^(15 - e) lies in [2^14, 2^15); the scale and its inverse stay within 32-bit floats
-    reinterpret_cast<i32*>(w.count)[1] = top > 0 && top < __builtin_inff() ? min(15 - e, 120) : 0;
+    reinterpret_cast<i32*>(w.count)[1] = scaling;
+  }
+  if constexpr (GATHER) {
+    const int pieces = dp / V;
+    for (i64 i = (i64)blockIdx.x * USED_THREADS + threadIdx.x; i < (i64)before * pieces; i += (i64)gridDim.x * USED_THREADS) {
+      const i64 at = i / pieces;
+      gather_piece<T, V>(w, i, at, (int)(i - at * pieces) * V, list[at], h, ldh, d, lse, dloss, dloss_stride, ldexpf(1.0f, scaling));
+    }
   }
 }
 
-// The kept rows side by side, padded with zeros to dp columns, and what the gradient needs of each.
+// The kept rows side by side.
 template <class T, int V>
 __global__ __launch_bounds__(256) void k_gather_rows(Rows w, const T* __restrict__ h, i64 ldh, int d, int dp, const float* lse,
                                                      const float* dloss, i64 dloss_stride) {
@@ -100,17 +127,7 @@ __global__ __launch_bounds__(256) void k_gather_rows(Rows w, const T* __restrict
   const float scale = ldexpf(1.0f, reinterpret_cast<const i32*>(w.count)[1]);
   for (i64 i = (i64)blockIdx.x * 256 + threadIdx.x; i < n * pieces; i += (i64)gridDim.x * 256) {
     const i64 at = i / pieces;
-    const int c = (int)(i - at * pieces) * V;
-    const i64 r = w.row[at];
-    if constexpr (V == 8) {
-      reinterpret_cast<s16x8*>(w.h)[i] = *reinterpret_cast<const s16x8*>(h + r * ldh + c);
-    } else {
-      static_cast<T*>(w.h)[i] = c < d ? h[r * ldh + c] : (T)0.0f;
-    }
-    if (c == 0 && dloss) {
-      w.lse[at] = lse[r];
-      w.scale[at] = dloss[r * dloss_stride] * scale;
-    }
+    gather_piece<T, V>(w, i, at, (int)(i - at * pieces) * V, w.row[at], h, ldh, d, lse, dloss, dloss_stride, scale);
   }
 }
 
@@ -242,25 +259,33 @@ struct InputJob {            // dh: dz [kept][width] times w [width][d]
   Rows rows;
   const void *dz, *w;
   i64 lddz, ldw;
-  int d, width, split_width;
+  int d, width, full_width;  // this piece of the vocabulary's, and all but the last one's
   u32 col_tiles;
-  float* sum;                // [splits][rows][d]
-  i64 all_rows;
+  float* sum;                // [splits][kept rows][d]
   bool more;                 // add to what an earlier piece left
 };
 
+// the parts of dh's contraction, the same for all pieces
+template <class C>
+__device__ __forceinline__ u32 input_splits(u32 kept, u32 col_tiles, int full_width) {
+  return splits_of((kept + C::BM - 1) / C::BM * col_tiles, (u32)full_width / 32);
+}
+
 template <class C, class T, bool DIRECT>
 __global__ __launch_bounds__(C::THREADS) void k_input_grad(InputJob j) {
-  int m0, n0;
   const int kept = (int)j.rows.count[0];
-  if (!logit_tile<C>(kept, j.col_tiles, m0, n0)) return;
-  const int c0 = (int)blockIdx.y * j.split_width;
-  const int depth = max(0, min(j.split_width, j.width - c0));
+  const u32 tm = (u32)(kept + C::BM - 1) / C::BM, tiles = tm * j.col_tiles, splits = input_splits<C>((u32)kept, j.col_tiles, j.full_width);
+  if (blockIdx.x >= tiles * splits) return;
+  const u32 id = xcd_order(blockIdx.x, tiles * splits), split = id / tiles;
+  const uint2 place = grouped_order(id - split * tiles, tm, j.col_tiles, 8);
+  const int m0 = (int)place.x * C::BM, n0 = (int)place.y * C::BN;
+  const int split_width = (int)((j.full_width / 64 + splits - 1) / splits * 64), c0 = (int)split * split_width;
+  const int depth = max(0, min(split_width, j.width - c0));
   const int rows = min(C::BM, kept - m0), cols = min(C::BN, j.d - n0);
   TileProduct<C, T, false, true, DIRECT> prod;
-  prod.run(lds, static_cast<const T*>(j.dz) + (i64)m0 * j.lddz + c0, j.lddz, rows, static_cast<const T*>(j.w) + (i64)c0 * j.ldw + n0,
+  prod.run(lds, static_cast<const T*>(j.dz) + (i64)m0 * j.lddz + c0, j.lddz, rows, static_cast<const T*>(j.w) + (i64)(depth ? c0 : 0) * j.ldw + n0,
            j.ldw, cols, depth);
-  float* o = j.sum + ((i64)blockIdx.y * j.all_rows + m0) * j.d + n0;
+  float* o = j.sum + ((i64)split * kept + m0) * j.d + n0;
   prod.each([&](u32 m, u32 n, f32x4 v) {
     if ((int)m >= rows || (int)n >= cols) return;
     float* q = o + (i64)m * j.d + n;
@@ -275,16 +300,28 @@ __global__ __launch_bounds__(C::THREADS) void k_input_grad(InputJob j) {
   });
 }
 
-// dh leaves: the splits' sums in their order, rows back in their places, zeros for rows without a target
-template <class T>
-__global__ __launch_bounds__(256) void k_input_rows(Rows w, const float* __restrict__ sum, u32 splits, i64 rows, int d, T* dh, i64 lddh) {
+// dh leaves: the splits' sums in their order, rows back in their places, zeros for rows without a target.  V neighbouring columns to a
+// thread where rows allow it.
+template <class C, class T, int V>
+__global__ __launch_bounds__(256) void k_input_rows(Rows w, const float* __restrict__ sum, u32 col_tiles, int full_width, i64 rows, int d, T* dh, i64 lddh) {
+  const i64 kept = w.count[0];
+  const u32 splits = input_splits<C>((u32)kept, col_tiles, full_width);
   const float back = ldexpf(1.0f, -reinterpret_cast<const i32*>(w.count)[1]);
-  for (i64 i = (i64)blockIdx.x * 256 + threadIdx.x; i < rows * d; i += (i64)gridDim.x * 256) {
-    const i64 r = i / d, c = i - r * d, at = w.place[r];
-    float v = 0;
+  const int pieces = d / V;
+  for (i64 i = (i64)blockIdx.x * 256 + threadIdx.x; i < rows * pieces; i += (i64)gridDim.x * 256) {
+    const i64 r = i / pieces, c = (i - r * pieces) * V, at = w.place[r];
+    float v[V] = {};
     if (at >= 0)
-      for (u32 s = 0; s < splits; ++s) v += sum[((i64)s * rows + at) * d + c];
-    dh[r * lddh + c] = (T)(v * back);
+      for (u32 s = 0; s < splits; ++s) {
+        const float* q = sum + ((i64)s * kept + at) * d + c;
+        if constexpr (V == 4) {
+          const f32x4 x = *reinterpret_cast<const f32x4*>(q);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] += x[e];
+        } else v[0] += *q;
+      }
+    if constexpr (V == 4) store4(dh + r * lddh + c, f32x4{v[0], v[1], v[2], v[3]} * back, 4, true);
+    else dh[r * lddh + c] = (T)(v[0] * back);
   }
 }
 
@@ -340,18 +377,15 @@ i64 div_up(i64 a, i64 b) { return (a + b - 1) / b; }
 i64 round_up(i64 a, i64 b) { return div_up(a, b) * b; }
 
 enum Size { LARGE, MEDIUM, FEW };
-Size tile_size(i64 rows, i64 cols) {
+// for rows x cols of results; less than 48 rows are bound by reading the vocabulary's weights
+Size tile_size(i64 rows, i64 cols, i64 depth, u32 most_splits) {
   if (rows < 48) return FEW;
-  return div_up(rows, 256) * div_up(cols, 256) >= (i64)COMPUTE_UNITS * 3 / 4 ? LARGE : MEDIUM;
+  const Cut c = choose_cut((double)div_up(rows, 256) * div_up(cols, 256), (double)div_up(rows, 128) * div_up(cols, 128), div_up(depth, 32),
+                           (double)rows * cols, true, most_splits);
+  return c.large ? LARGE : MEDIUM;
 }
 int tile_m(Size s) { return s == LARGE ? Large::BM : s == MEDIUM ? Medium::BM : Few::BM; }
 int tile_n(Size s) { return s == LARGE ? Large::BN : s == MEDIUM ? Medium::BN : Few::BN; }
-
-u32 splits_for(i64 tiles, i64 steps) {
-  u32 s = 1;
-  while (tiles * s < (i64)COMPUTE_UNITS && steps / (2 * s) >= 8) s *= 2;
-  return s;
-}
 
 // dz of a piece is 2^28 values at most (512 MB), but a piece has 4,096 columns at least
 i64 piece_width(const ccld_vocab_args* a) {
@@ -381,7 +415,7 @@ struct Plan {
   i64 width;
   uint16_t* dz;
   Size input;
-  u32 input_splits; int input_split;
+  u32 pieces;              // workgroups for dh at most
   float* sum;
   Size weight;
   u32 weight_splits;
@@ -401,29 +435,27 @@ Plan make_plan(const ccld_vocab_args* a, bool grad, Carver& c) {
   p.rows.scale = c.take<float>(rows);
   p.rows.h = c.take<uint16_t>(rows * p.dp);
   if (!grad) {
-    p.logits = tile_size(a->rows, a->vocab);
+    p.logits = tile_size(a->rows, a->vocab, a->d, 1);
     p.col_tiles = (u32)div_up(a->vocab, tile_n(p.logits));
     p.part = c.take<float2>(rows * p.col_tiles);
     return p;
   }
   p.width = piece_width(a);
-  p.logits = tile_size(a->rows, p.width);
+  p.logits = tile_size(a->rows, p.width, a->d, 1);
   p.col_tiles = (u32)div_up(p.width, tile_n(p.logits));
   p.dz = c.take<uint16_t>(rows * p.width);
   if (a->dh) {
-    // the contraction is long: the largest tiles, in as many parts as fill the chip (1,200 rows of 50,021 x 1,536: 452 us in tiles of
-    // 128 and two parts)
-    const i64 steps = p.width / DEPTH;
-    p.input = a->rows < 48 ? FEW : a->rows <= 128 || a->d <= 128 || steps * div_up(a->rows, 256) * div_up(a->d, 256) < 16 * (i64)COMPUTE_UNITS ? MEDIUM : LARGE;
-    const i64 tiles = div_up(a->rows, tile_m(p.input)) * div_up(a->d, tile_n(p.input));
-    const u32 s = splits_for(tiles, steps);
-    p.input_split = (int)(div_up(steps, s) * DEPTH);
-    p.input_splits = (u32)div_up(p.width, p.input_split);
-    p.sum = c.take<float>((u64)p.input_splits * rows * a->d);
+    // the parts of the contraction are chosen on the device, by the rows that have a target: pieces are bounded, not parts
+    p.input = tile_size(a->rows, a->d, p.width, MOST_SPLITS);
+    const u64 tiles = (u64)div_up(a->rows, tile_m(p.input)) * div_up(a->d, tile_n(p.input));
+    p.pieces = (u32)std::max<u64>(tiles, MOST_PIECES);
+    p.sum = c.take<float>(std::max<u64>(rows * a->d, (u64)MOST_PIECES * tile_m(p.input) * tile_n(p.input)));
   }
   if (a->dw) {
-    p.weight = div_up(p.width, 256) * div_up(a->d, 256) >= (i64)COMPUTE_UNITS * 3 / 4 ? LARGE : MEDIUM;
-    p.weight_splits = splits_for(div_up(p.width, tile_m(p.weight)) * div_up(a->d, tile_n(p.weight)), div_up(a->rows, DEPTH));
+    const Cut w = choose_cut((double)div_up(p.width, 256) * div_up(a->d, 256), (double)div_up(p.width, 128) * div_up(a->d, 128),
+                             div_up(a->rows, 32), (double)p.width * a->d, true);
+    p.weight = w.large ? LARGE : MEDIUM;
+    p.weight_splits = w.splits;
     if (p.weight_splits > 1) p.weight_part = c.take<float>((u64)p.weight_splits * p.width * a->d);
   }
   return p;
@@ -460,16 +492,22 @@ ccld_status check_pointers(const ccld_vocab_args* a, bool grad) {
 
 u32 stream_groups(i64 threads) { return (u32)std::min<i64>(std::max<i64>(div_up(threads, 256), 1), 4096); }
 
-template <class T>
-void start(const ccld_vocab_args* a, const Plan& p, bool grad, hipStream_t stream) {
-  k_used_rows<<<1, USED_THREADS, 0, stream>>>(p.rows, a->labels, a->label_bits, a->rows, a->vocab, grad ? nullptr : a->loss,
-                                              grad ? nullptr : a->lse, grad ? a->dloss : nullptr, a->dloss_stride);
+template <class T, int V>
+void start_rows(const ccld_vocab_args* a, const Plan& p, bool grad, hipStream_t stream) {
   const T* h = static_cast<const T*>(a->h);
   const float *lse = grad ? a->lse : nullptr, *dloss = grad ? a->dloss : nullptr;
-  if (a->d % 8 == 0 && a->ldh % 8 == 0 && aligned(h, 16))
-    k_gather_rows<T, 8><<<stream_groups(a->rows * (p.dp / 8)), 256, 0, stream>>>(p.rows, h, a->ldh, (int)a->d, p.dp, lse, dloss, a->dloss_stride);
-  else
-    k_gather_rows<T, 1><<<stream_groups(a->rows * p.dp), 256, 0, stream>>>(p.rows, h, a->ldh, (int)a->d, p.dp, lse, dloss, a->dloss_stride);
+  float *loss = grad ? nullptr : a->loss, *lse_out = grad ? nullptr : a->lse;
+  const i64 pieces = a->rows * (p.dp / V);
+  const bool few = a->rows <= USED_THREADS;
+  const auto used = few ? &k_used_rows<T, V, true> : &k_used_rows<T, V, false>;
+  used<<<few ? (u32)std::min<i64>(std::max<i64>(div_up(pieces, USED_THREADS), 1), (i64)COMPUTE_UNITS) : 1, USED_THREADS, 0, stream>>>(
+      p.rows, a->labels, a->label_bits, a->rows, a->vocab, loss, lse_out, h, a->ldh, (int)a->d, p.dp, lse, dloss, a->dloss_stride);
+  if (!few) k_gather_rows<T, V><<<stream_groups(pieces), 256, 0, stream>>>(p.rows, h, a->ldh, (int)a->d, p.dp, lse, dloss, a->dloss_stride);
+}
+template <class T>
+void start(const ccld_vocab_args* a, const Plan& p, bool grad, hipStream_t stream) {
+  if (a->d % 8 == 0 && a->ldh % 8 == 0 && aligned(a->h, 16)) start_rows<T, 8>(a, p, grad, stream);
+  else start_rows<T, 1>(a, p, grad, stream);
 }
 
 bool direct(const ccld_vocab_args* a) { return a->d % 8 == 0 && a->ldw % 8 == 0 && aligned(a->w, 16); }
@@ -490,9 +528,16 @@ void launch_logit_grad(const ccld_vocab_args* a, LogitJob j, hipStream_t stream)
 template <class C, class T>
 void launch_input_grad(const ccld_vocab_args* a, const Plan& p, InputJob j, hipStream_t stream) {
   j.col_tiles = (u32)div_up(j.d, C::BN);
-  const dim3 grid((u32)(div_up(a->rows, C::BM) * j.col_tiles), p.input_splits);
   const auto kernel = direct(a) ? &k_input_grad<C, T, true> : &k_input_grad<C, T, false>;
-  kernel<<<grid, C::THREADS, C::LDS_BYTES, stream>>>(j);
+  kernel<<<p.pieces, C::THREADS, C::LDS_BYTES, stream>>>(j);
+}
+template <class C, class T>
+void launch_input_rows(const ccld_vocab_args* a, const Plan& p, hipStream_t stream) {
+  const int d = (int)a->d;
+  const bool wide = d % 4 == 0 && a->lddh % 4 == 0 && aligned(a->dh, 8);
+  const auto kernel = wide ? &k_input_rows<C, T, 4> : &k_input_rows<C, T, 1>;
+  kernel<<<stream_groups(a->rows * a->d / (wide ? 4 : 1)), 256, 0, stream>>>(p.rows, p.sum, (u32)div_up(d, C::BN), (int)p.width, a->rows, d,
+                                                                            static_cast<T*>(a->dh), a->lddh);
 }
 template <class C, class T>
 void launch_weight_grad(const Plan& p, WeightJob j, hipStream_t stream) {
@@ -526,7 +571,7 @@ ccld_status gradient(const ccld_vocab_args* a, const Plan& p, hipStream_t stream
       else launch_logit_grad<Few, T>(a, j, stream);
     }
     if (a->dh && a->rows) {
-      const InputJob j{p.rows, p.dz, w, p.width, a->ldw, (int)a->d, (int)cols, p.input_split, 0, p.sum, a->rows, first > 0};
+      const InputJob j{p.rows, p.dz, w, p.width, a->ldw, (int)a->d, (int)cols, (int)p.width, 0, p.sum, first > 0};
       if (p.input == LARGE) launch_input_grad<Large, T>(a, p, j, stream);
       else if (p.input == MEDIUM) launch_input_grad<Medium, T>(a, p, j, stream);
       else launch_input_grad<Few, T>(a, p, j, stream);
@@ -541,8 +586,11 @@ ccld_status gradient(const ccld_vocab_args* a, const Plan& p, hipStream_t stream
         k_weight_rows<T><<<stream_groups(cols * a->d), 256, 0, stream>>>(p.rows, p.weight_part, p.weight_splits, cols, (int)a->d, dw, a->lddw);
     }
   }
-  if (a->dh && a->rows)
-    k_input_rows<T><<<stream_groups(a->rows * a->d), 256, 0, stream>>>(p.rows, p.sum, p.input_splits, a->rows, (int)a->d, static_cast<T*>(a->dh), a->lddh);
+  if (a->dh && a->rows) {
+    if (p.input == LARGE) launch_input_rows<Large, T>(a, p, stream);
+    else if (p.input == MEDIUM) launch_input_rows<Medium, T>(a, p, stream);
+    else launch_input_rows<Few, T>(a, p, stream);
+  }
   return launched();
 }
 
