@@ -90,8 +90,8 @@ template <int DEPTH>
 __device__ __forceinline__ u32 along_key(u32 row) { return DEPTH == 64 ? row & 7 : (row >> 1) & 3; }
 
 // One operand's share of the stages: ROWS of its output index by DEPTH of c.
-// DIRECT loads need 16-byte pieces to be aligned and wholly inside or outside the operand; otherwise single values are loaded
-// with a check each and written to LDS from registers.
+// DIRECT loads need 16-byte pieces to be aligned and wholly inside or outside the operand; otherwise they pass through registers, and those
+// that reach over the operand's edge are loaded value by value.
 template <class T, int ROWS, int DEPTH, int THREADS, bool ACROSS, bool DIRECT>
 struct Operand {
   static constexpr int PIECES = ROWS * DEPTH / 8 / THREADS;      // 16-byte pieces per thread and stage
@@ -129,17 +129,24 @@ struct Operand {
       const u32 wave = __builtin_amdgcn_readfirstlane(threadIdx.x / CCLD_WAVE);
       const int c = ACROSS ? (int)(row + i * ROW_STEP) : (int)col;
       load_to_lds(base, tile + (i * THREADS + wave * CCLD_WAVE) * 16, c < depth ? offset[i] : OUTSIDE);
-    } else {
-      const u32 r = row + i * ROW_STEP;
-      s16x8 v;
+    } else put(tile, i, load(i, depth));
+  }
+  // The same through registers.
+  __device__ __forceinline__ s16x8 load(int i, int depth) const {
+    const u32 r = row + i * ROW_STEP;
+    const int x = (int)column(i), inside = ACROSS ? ((int)r < depth ? left - x : 0) : ((int)r < left ? depth - x : 0);
+    const T* p = base + (i64)r * ld + x;
+    s16x8 v = {};
+    if (inside >= 8) __builtin_memcpy(&v, p, 16);              // loads need no alignment
+    else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int x = (int)column(i) + e;
-        const bool in = ACROSS ? x < left && (int)r < depth : (int)r < left && x < depth;
-        v[e] = in ? __builtin_bit_cast(short, base[(i64)r * ld + x]) : (short)0;
-      }
-      *reinterpret_cast<s16x8*>(tile + (i * THREADS + threadIdx.x) * 16) = v;
+      for (int e = 0; e < 7; ++e)
+        if (e < inside) v[e] = __builtin_bit_cast(short, p[e]);
     }
+    return v;
+  }
+  __device__ __forceinline__ static void put(unsigned char* tile, int i, s16x8 v) {
+    *reinterpret_cast<s16x8*>(tile + (i * THREADS + threadIdx.x) * 16) = v;
   }
   __device__ __forceinline__ void next_stage() { base += ACROSS ? ld * DEPTH : (i64)DEPTH; }
 };
@@ -253,22 +260,26 @@ struct TileProduct {
       // loads of this step: a stage, or both stages of a pair for one operand
       constexpr int FIRST = !PAIRS || !ODD ? A_TURN : 0, ALL = FIRST + (!PAIRS || ODD ? B_TURN : 0);
       const u32 second = after(free);
+      // (through registers: all are loaded at once and written when the step ends)
+      s16x8 held[DIRECT ? 1 : ALL];
       auto load = [&](int i) {
         if (i < FIRST) {
-          if (i < A::PIECES) oa.fetch(lds + free, i, left_a);
-          else {
-            if (i == A::PIECES) oa.next_stage();
-            oa.fetch(lds + second, i - A::PIECES, left_a - C::DEPTH);
-          }
+          if (i == A::PIECES) oa.next_stage();
+          const int n = i % A::PIECES, left = i < A::PIECES ? left_a : left_a - C::DEPTH;
+          if constexpr (DIRECT) oa.fetch(lds + (i < A::PIECES ? free : second), n, left);
+          else held[i] = oa.load(n, left);
         } else {
-          const int n = i - FIRST;
-          if (n < B::PIECES) ob.fetch(lds + free + A_BYTES, n, left_b);
-          else {
-            if (n == B::PIECES) ob.next_stage();
-            ob.fetch(lds + second + A_BYTES, n - B::PIECES, left_b - C::DEPTH);
-          }
+          const int k = i - FIRST;
+          if (k == B::PIECES) ob.next_stage();
+          const int n = k % B::PIECES, left = k < B::PIECES ? left_b : left_b - C::DEPTH;
+          if constexpr (DIRECT) ob.fetch(lds + (k < B::PIECES ? free : second) + A_BYTES, n, left);
+          else held[i] = ob.load(n, left);
         }
       };
+      if constexpr (!DIRECT) {
+#pragma unroll
+        for (int i = 0; i < ALL; ++i) load(i);
+      }
       int loaded = 0, read_b = 0;
 #pragma unroll
       for (int turn = HOLD; turn < TURNS; ++turn) {
@@ -276,11 +287,22 @@ struct TileProduct {
 #pragma unroll
         for (; read_b < PARTS * C::NI * share / of; ++read_b) then[read_b / C::NI][read_b % C::NI] = fb.read(s + A_BYTES, read_b % C::NI, read_b / C::NI);
         if (turn - HOLD < HOLD) va[(turn - HOLD) / C::MI][(turn - HOLD) % C::MI] = fa.read(s, (turn - HOLD) % C::MI, (turn - HOLD) / C::MI);
+        if constexpr (DIRECT) {
 #pragma unroll
-        for (; loaded < ALL * share / of; ++loaded) load(loaded);
+          for (; loaded < ALL * share / of; ++loaded) load(loaded);
+        }
         multiply(turn);
         va[turn / C::MI][turn % C::MI] = fa.read(s, turn % C::MI, turn / C::MI);
         __builtin_amdgcn_sched_barrier(0);
+      }
+      if constexpr (!DIRECT) {
+#pragma unroll
+        for (int i = 0; i < ALL; ++i) {
+          const int k = i < FIRST ? i : i - FIRST, pieces = i < FIRST ? A::PIECES : B::PIECES;
+          unsigned char* stage = lds + (k < pieces ? free : second);
+          if (i < FIRST) A::put(stage, k % pieces, held[i]);
+          else B::put(stage + A_BYTES, k % pieces, held[i]);
+        }
       }
       constexpr int MOVED = PAIRS ? 2 * C::DEPTH : C::DEPTH;
       if (!PAIRS || !ODD) { oa.next_stage(); left_a -= MOVED; }
@@ -319,6 +341,7 @@ struct TileProduct {
       if (m0 + m < rows) {
         T* q = out + (i64)(m0 + m) * ldo + n;
         if (whole && n + 8 <= cols) __builtin_nontemporal_store(v, reinterpret_cast<s16x8*>(q));
+        else if (n + 8 <= cols) __builtin_memcpy(q, &v, 16);
         else {
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
