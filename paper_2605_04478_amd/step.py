@@ -4,7 +4,9 @@ A rank that the analysis calls computation-slow (Section 2.2, S1) has a slow car
 These operators are the work to run on such a card, and the kinds of work that are uneven by design: the products of
 a rank's experts, whose rows routing decides, and the loss over the vocabulary, which the last pipeline stage alone has; and the norms around a block, which only memory bounds.  The HIP library computes them; this module checks arguments and marshals them,
 PyTorch supplies memory and the stream.  Every call goes to the current stream of its tensors' device and returns before it is
-done; outputs and workspaces come from torch's allocator, so calls may be captured into a graph.
+done; outputs and workspaces come from torch's allocator, so calls may be captured into a graph.  (Who captures a backward pass of
+the classes below captures its forward pass with it, while no eager result of the same leaves is alive: torch would have the
+captured pass wait for a stream that is not captured.)
 
 Matrices have unit stride within a row and any row stride.  The functions named `*_grad` are the gradients by themselves;
 the classes at the end of each section give the same to automatic differentiation.
