@@ -20,7 +20,7 @@ using namespace ccld;
 
 namespace {
 
-// A thread has PIECES x 8 of a row's columns, in vectors of VEC: 16 bytes where rows are aligned to that (VEC 8 or 4), else single
+// A thread has PIECES x 8 of a row's columns, in vectors of VEC: 16 bytes (VEC 8 or 4) where rows are made of whole words, else single
 // values.  The vectors of a team's TEAM threads lie side by side.
 template <class T>
 using Piece = T __attribute__((ext_vector_type(8)));
@@ -28,7 +28,8 @@ using Piece = T __attribute__((ext_vector_type(8)));
 template <int TEAM, int VEC>
 __device__ __forceinline__ int column(int t, int p, int i) { return ((p * (8 / VEC) + i / VEC) * TEAM + t) * VEC + i % VEC; }
 
-// A row as a buffer of its d values: columns beyond them load zeros and are not stored, without a branch.  Every value of a row that is not
+// A row as a buffer of its d values: columns beyond them load zeros and are not stored, without a branch (words of 32 bits are checked one by
+// one, so that a vector may reach over the end).  Every value of a row that is not
 // there (no pointer) is zero.
 template <class T>
 __device__ __forceinline__ auto row_buffer(const T* row, int d) {
@@ -187,9 +188,10 @@ __device__ __forceinline__ void keep_packed(Piece<T>& v) {
 // With e = du w_pre and q = gate w_post b both means follow from sums that need neither, so that a row has one reduction:
 //   mean(du w_pre x) = sum(e x) / d      sum(dn w_post b) = sum(q (dh' + r2 e)) - m2 sum(q x)      (m2 = r2^3 mean(e x))
 // 128 registers for 16-bit vectors, so that 16 wavefronts run on a compute unit (8 otherwise), each with its next row on the way while it
-// computes one.  Where that does not fit (REREAD: rows of more than 8,192 columns, or 4,096 of 32 bits) a row is read again, from the
-// caches, after its reduction.
-template <class T, int TEAM, int PIECES, int VEC, bool REREAD>
+// computes one (ROWS_AHEAD).  Where that does not fit, a row is kept and the weights are loaded for each (ROWS_KEPT: 4,097 to 8,192 columns of
+// 32 bits), or the row is read again, from the caches, after its reduction (ROWS_AGAIN: more than 8,192 columns).
+enum { ROWS_AHEAD, ROWS_KEPT, ROWS_AGAIN };
+template <class T, int TEAM, int PIECES, int VEC, int ROWS>
 __global__ __launch_bounds__(threads_of<TEAM>(), TEAM == 1024 || (sizeof(T) == 2 && VEC > 1) ? 4 : 2) void k_norm_grad(NormJob j) {
   constexpr int PER_GROUP = threads_of<TEAM>() / TEAM;
   __shared__ float places[2][16][4];
@@ -239,7 +241,7 @@ __global__ __launch_bounds__(threads_of<TEAM>(), TEAM == 1024 || (sizeof(T) == 2
     Columns next[PIECES];
     Weights w[PIECES];
     Rstd next_rstd = load_rstd(row0);
-    if constexpr (!REREAD) {
+    if constexpr (ROWS == ROWS_AHEAD) {
 #pragma unroll
       for (int p = 0; p < PIECES; ++p) {
         w[p] = load_weights(gate, p);
@@ -253,7 +255,7 @@ __global__ __launch_bounds__(threads_of<TEAM>(), TEAM == 1024 || (sizeof(T) == 2
       next_rstd = load_rstd(more ? row + 1 : row);
       Columns now[PIECES];
       float x[PIECES][8], y[PIECES][8], sum[3] = {0, 0, 0};
-      if constexpr (!REREAD) {
+      if constexpr (ROWS == ROWS_AHEAD) {
 #pragma unroll
         for (int p = 0; p < PIECES; ++p) {
           now[p] = next[p];
@@ -265,7 +267,7 @@ __global__ __launch_bounds__(threads_of<TEAM>(), TEAM == 1024 || (sizeof(T) == 2
       }
 #pragma unroll
       for (int p = 0; p < PIECES; ++p) {
-        if constexpr (REREAD) { now[p] = load(row, p); w[p] = load_weights(gate, p); }
+        if constexpr (ROWS != ROWS_AHEAD) { now[p] = load(row, p); w[p] = load_weights(gate, p); }
         values(now[p], w[p], r1, r2, x[p], y[p]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -283,7 +285,8 @@ __global__ __launch_bounds__(threads_of<TEAM>(), TEAM == 1024 || (sizeof(T) == 2
       asm volatile("" : "+s"(again));           // not the values from before the reduction
 #pragma unroll
       for (int p = 0; p < PIECES; ++p) {
-        if constexpr (REREAD) { now[p] = load(again, p); w[p] = load_weights(gate, p); values(now[p], w[p], r1, r2, x[p], y[p]); }
+        if constexpr (ROWS == ROWS_KEPT) w[p] = load_weights(gate, p);
+        if constexpr (ROWS == ROWS_AGAIN) { now[p] = load(again, p); w[p] = load_weights(gate, p); values(now[p], w[p], r1, r2, x[p], y[p]); }
         float dh[8], db[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -405,13 +408,13 @@ template <class... P>
 bool all_aligned(uintptr_t bytes, P... p) { return (aligned(p, bytes) && ...); }
 template <class... L>
 bool all_at_least(i64 d, L... l) { return ((l >= d) && ...); }
-// vectors of 16 bytes do not reach over a row's end, and start on 16 bytes in every row
+// Vectors of 16 bytes need rows that are made of whole words of 32 bits: buffers are checked, and may be aligned, by the word.
 bool wide(const ccld_norm_args* a, bool grad) {
-  const i64 vec = 16 / element_bytes(a);
-  auto even = [&](i64 ld, const void* p) { return !p || (ld % vec == 0 && aligned(p, 16)); };
-  const bool w = a->d % vec == 0 && even(a->ldh, a->h) && even(a->ldb, a->b) && even(a->ldgate, a->gate) && even(0, a->w_post) && even(0, a->w_pre);
-  if (!grad) return w && even(a->ldh_out, a->h_out) && even(a->ldu, a->u);
-  return w && even(a->lddh, a->dh) && even(a->lddb, a->db) && even(0, a->dgate) && even(a->lddh_out, a->dh_out) && even(a->lddu, a->du);
+  const i64 word = 4 / element_bytes(a);
+  auto words = [&](i64 ld, const void* p) { return !p || (ld % word == 0 && aligned(p, 4)); };
+  const bool w = a->d % word == 0 && words(a->ldh, a->h) && words(a->ldb, a->b) && words(a->ldgate, a->gate) && words(0, a->w_post) && words(0, a->w_pre);
+  if (!grad) return w && words(a->ldh_out, a->h_out) && words(a->ldu, a->u);
+  return w && words(a->lddh, a->dh) && words(a->lddb, a->db) && words(0, a->dgate) && words(a->lddh_out, a->dh_out) && words(a->lddu, a->du);
 }
 
 NormJob make_job(const ccld_norm_args* a) {
@@ -451,8 +454,8 @@ ccld_status forward(const ccld_norm_args* a, hipStream_t stream) {
 
 template <class T, int TEAM, int PIECES>
 void launch_gradient(const NormJob& j, const Plan& p, bool w, hipStream_t stream) {
-  constexpr bool REREAD = PIECES > 1 || (TEAM == 1024 && sizeof(T) == 4);
-  const auto kernel = w ? &k_norm_grad<T, TEAM, PIECES, (int)(16 / sizeof(T)), REREAD> : &k_norm_grad<T, TEAM, PIECES, 1, REREAD>;
+  constexpr int ROWS = PIECES > 1 ? ROWS_AGAIN : TEAM == 1024 && sizeof(T) == 4 ? ROWS_KEPT : ROWS_AHEAD;
+  const auto kernel = w ? &k_norm_grad<T, TEAM, PIECES, (int)(16 / sizeof(T)), ROWS> : &k_norm_grad<T, TEAM, PIECES, 1, ROWS>;
   kernel<<<(u32)p.groups, threads_of<TEAM>(), 0, stream>>>(j);
 }
 template <class T>

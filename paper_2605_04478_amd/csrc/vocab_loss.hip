@@ -387,12 +387,14 @@ Size tile_size(i64 rows, i64 cols, i64 depth, u32 most_splits) {
 int tile_m(Size s) { return s == LARGE ? Large::BM : s == MEDIUM ? Medium::BM : Few::BM; }
 int tile_n(Size s) { return s == LARGE ? Large::BN : s == MEDIUM ? Medium::BN : Few::BN; }
 
-// dz of a piece is 2^28 values at most (512 MB), but a piece has 4,096 columns at least
+// dz of a piece is 2^28 values at most (512 MB), but a piece has 4,096 columns at least, and 2^21 at most: a tile of dz is reached by
+// 32-bit offsets.
 i64 piece_width(const ccld_vocab_args* a) {
-  const i64 w = std::max<i64>(round_up(((i64)1 << 28) / std::max<i64>(a->rows, 1), 256), 4096);
+  const i64 w = std::min<i64>(std::max<i64>(round_up(((i64)1 << 28) / std::max<i64>(a->rows, 1), 256), 4096), (i64)1 << 21);
   const i64 pieces = div_up(a->vocab, w);
   return round_up(div_up(a->vocab, pieces), 256);
 }
+static_assert(((i64)1 << 21) + 256 < MAX_LD, "dz's rows");
 
 struct Carver {
   uint8_t* base; u64 off;

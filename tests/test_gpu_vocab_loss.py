@@ -89,6 +89,11 @@ def test_several_pieces_of_the_vocabulary():
     _check(*_inputs(8192, 40, 40001, BF, 0.1))
 
 
+def test_few_rows_of_a_huge_vocabulary():
+    """5 million words: pieces are cut by their width, not by their rows."""
+    _check(*_inputs(40, 8, 5_000_003, BF, 0.1))
+
+
 @pytest.mark.parametrize("rows", [1, 5, 1024, 1025, 2500])
 def test_rows_without_a_target(rows):
     """None, all but one, and all rows masked; labels beyond the vocabulary; NaN and infinities in what is masked."""
