@@ -154,11 +154,14 @@ __device__ __forceinline__ bool logit_tile(u32 kept, u32 col_tiles, int& m0, int
   return true;
 }
 
-// (maximum, sum of exp(x - maximum)) of two sets; the maximum is -inf where all are, 0 where one is +inf
+// (maximum, sum of exp(x - maximum)) of two sets; the maximum is -inf where all are, 0 where one is +inf.  A factor is 2^-126 at least: an
+// infinite sum stays one beside a maximum of hundreds (a factor of zero would make it NaN), and finite sums, below 2^32, add nothing to
+// the other set's, which is one at least.
 __device__ __forceinline__ float2 join_sums(float2 a, float2 b) {
   const float top = fmaxf(a.x, b.x);
   const float ref = top == -__builtin_inff() ? 0 : top;
-  return make_float2(top, a.y * __builtin_amdgcn_exp2f((a.x - ref) * LOG2E) + b.y * __builtin_amdgcn_exp2f((b.x - ref) * LOG2E));
+  auto share = [&](float2 s) { return s.y * fmaxf(__builtin_amdgcn_exp2f((s.x - ref) * LOG2E), 0x1p-126f); };
+  return make_float2(top, share(a) + share(b));
 }
 
 template <class C, class T, bool DIRECT>

@@ -164,6 +164,20 @@ def test_infinite_logits():
     assert (lse == float("-inf")).all()
 
 
+@pytest.mark.parametrize("rows", [5, 50, 600])
+def test_infinite_logits_beside_large_ones(rows):
+    """A word's infinite logit decides the sum, whatever the largest finite one is and whichever tile it is in."""
+    from paper_2605_04478_amd import step
+    h, w, labels, _ = _inputs(rows, 64, 1400, BF)
+    h = h.abs() + 0.1
+    w[1300] = 20
+    for word in (7, 700, 1301):
+        wi = w.clone()
+        wi[word] = float("inf")
+        loss, lse = step.vocab_loss(h.to(DEV), wi.to(DEV), torch.where(labels == word, 9, labels).to(DEV))
+        assert (lse == float("inf")).all() and (loss == float("inf")).all(), word
+
+
 def test_strides_and_orders():
     h, w, labels, dloss = _inputs(150, 96, 700, BF, 0.3)
     plain = _check(h, w, labels, dloss)
