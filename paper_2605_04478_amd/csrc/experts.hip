@@ -82,7 +82,7 @@ __device__ __forceinline__ Place find_tile(const Offsets& off, u32 block, u32 co
       p.tiles = __builtin_amdgcn_readlane((int)t, src);
       p.at = id - (__builtin_amdgcn_readlane((int)incl, src) - p.tiles) * col_tiles;
       p.range = make_int2(__builtin_amdgcn_readlane(r.x, src), __builtin_amdgcn_readlane(r.y, src));
-      return p;
+      return p.at < p.tiles * col_tiles ? p : none;     // (offsets that decrease can make the counts pass 32 bits)
     }
     before = __builtin_amdgcn_readlane((int)incl, CCLD_WAVE - 1);
   }
