@@ -2,8 +2,8 @@
 
 A rank that the analysis calls computation-slow (Section 2.2, S1) has a slow card, or was given more work than its peers.
 These operators are the work to run on such a card, and the kinds of work that are uneven by design: the products of
-a rank's experts, whose rows routing decides, and the loss over the vocabulary, which the last pipeline stage alone has; and the norms around a block, which only memory bounds.  The HIP library computes them; this module checks arguments and marshals them,
-PyTorch supplies memory and the stream.  Every call goes to the current stream of its tensors' device and returns before it is
+a rank's experts, whose rows routing decides, and the loss over the vocabulary, which the last pipeline stage alone has; and the norms around a block, which only memory bounds.  The HIP library computes them; this module checks arguments and marshals them
+(for ordinary tensors in native code), PyTorch supplies memory and the stream.  Every call goes to the current stream of its tensors' device and returns before it is
 done; outputs and workspaces come from torch's allocator, so calls may be captured into a graph.  (Who captures a backward pass of
 the classes below captures its forward pass with it, while no eager result of the same leaves is alive: torch would have the
 captured pass wait for a stream that is not captured.)
@@ -47,6 +47,23 @@ class _NormArgs(C.Structure):
                                              "du", "dh", "db", "dgate", "dw_post", "dw_pre")]
                 + [(n, C.c_int64) for n in ("ldh", "ldb", "ldgate", "ldh_out", "ldu", "lddh_out", "lddu", "lddh", "lddb")]
                 + [("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)])
+
+
+# ---- the calls from native code ---
+_calls = None
+
+
+def _native():
+    """The module that makes a call of tensors that are as they should be, and returns None for all others."""
+    global _calls
+    if _calls is None:
+        lib()
+        try:
+            from . import _step
+        except ImportError as e:
+            raise RuntimeError("_step.so is missing or of another build: build it with `python -m paper_2605_04478_amd.build`") from e
+        _calls = _step
+    return _calls
 
 
 # ---- checks and marshalling -------------------------------------------------------------------------------------
@@ -155,6 +172,9 @@ def expert_product(x, w, offsets):
 
     x [rows, k] and w [experts, n, k] in bfloat16 or float16, offsets [experts + 1] in int32 or int64 -> y [rows, n].
     Rows that belong to no expert are zero.  The offsets stay on the device; they must not decrease."""
+    out = _native().expert_product(x, w, offsets)
+    if out is not None:
+        return out
     device, x, w, offsets = _expert_inputs(x, w, offsets)
     L = lib()
     with _current(device):
@@ -168,6 +188,9 @@ def expert_product(x, w, offsets):
 
 def expert_product_grad(dy, x, w, offsets, need_dx: bool = True, need_dw: bool = True):
     """Gradients of expert_product: (dx [rows, k], dw [experts, n, k]); None for one that is not needed."""
+    out = _native().expert_product_grad(dy, x, w, offsets, need_dx, need_dw)
+    if out is not None:
+        return out
     device, x, w, offsets, dy = _expert_inputs(x, w, offsets, dy)
     L = lib()
     with _current(device):
@@ -220,6 +243,9 @@ def vocab_loss(h, w, labels):
 
     h and w in bfloat16 or float16, labels [rows] in int32 or int64 -> (loss [rows], lse [rows]) in float32, lse being the
     logarithm of the sum of the logits' exponentials.  A row whose label is outside [0, vocab) has no target: both are zero."""
+    out = _native().vocab_loss(h, w, labels)
+    if out is not None:
+        return out
     device, h, w, labels = _vocab_inputs(h, w, labels)
     L = lib()
     with _current(device):
@@ -236,6 +262,9 @@ def vocab_loss_grad(dloss, h, w, labels, lse, need_dh: bool = True, need_dw: boo
     """Gradients of vocab_loss for dloss [rows], the gradient of each row's loss, and the lse that it returned:
     (dh [rows, d], dw [vocab, d]) in the type of h and w; None for one that is not needed.  The logits are taken again, in
     pieces of the vocabulary.  Rows without a target have no gradient, whatever they hold."""
+    out = _native().vocab_loss_grad(dloss, h, w, labels, lse, need_dh, need_dw)
+    if out is not None:
+        return out
     device, h, w, labels = _vocab_inputs(h, w, labels, dloss, lse)
     lse = lse.contiguous()
     L = lib()
@@ -298,6 +327,9 @@ def norm_residual(h, b, gate, w_post, w_pre, scale: float = 1.0, eps: float = 1e
 
     h, b [rows, d] in bfloat16, float16 or float32, w_post and w_pre [d]; gate [g, d], each of whose rows serves rows / g
     consecutive rows, or None.  -> (h', u, 1 / rms(b), 1 / rms(h')), the last two [rows] in float32."""
+    out = _native().norm_residual(h, b, gate, w_post, w_pre, scale, eps)
+    if out is not None:
+        return out
     device, h, b, gate, w_post, w_pre = _norm_inputs(h, b, gate, w_post, w_pre, eps)
     rows, d = h.shape
     with _current(device):
@@ -316,6 +348,9 @@ def norm_residual(h, b, gate, w_post, w_pre, scale: float = 1.0, eps: float = 1e
 def norm_residual_grad(dh_out, du, h, b, gate, w_post, w_pre, rstd_post, rstd_pre, scale: float = 1.0):
     """Gradients of norm_residual for those of h' and u (either may be None: zero) and the two vectors that it returned:
     (dh, db, dgate, dw_post, dw_pre), all in the type of h; dgate is None without a gate."""
+    out = _native().norm_residual_grad(dh_out, du, h, b, gate, w_post, w_pre, rstd_post, rstd_pre, scale)
+    if out is not None:
+        return out
     device, h, b, gate, w_post, w_pre = _norm_inputs(h, b, gate, w_post, w_pre, 0.0, dh_out, du, rstd_post, rstd_pre)
     rows, d = h.shape
     dh_out, du = (None if t is None else _rows(t) for t in (dh_out, du))
