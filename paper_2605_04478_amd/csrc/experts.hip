@@ -114,11 +114,10 @@ __global__ __launch_bounds__(C::THREADS) void k_expert_rows(RowJob j) {
 template <class C, class T, bool DIRECT>
 __global__ __launch_bounds__(C::THREADS) void k_expert_weights(WeightJob j) {
   // every expert's tiles are divided among the XCDs, since experts differ in their rows (an expert after another to an XCD: 1.5
-  // times the time at 32 experts whose rows spread like exp(0.7 N))
-  const u32 tiles = j.n_tiles * j.k_tiles, each = (tiles + 7) / 8 * 8, e = blockIdx.x / each, in = blockIdx.x - e * each;
-  const u32 place = in % 8 * (each / 8) + in / 8;
-  if (place >= tiles) return;
-  const uint2 t = grouped_order(place, j.n_tiles, j.k_tiles, 8);
+  // times the time at 32 experts whose rows spread like exp(0.7 N)).  Workgroups of the same number modulo 8 share an XCD within an
+  // expert too, whichever its first one has.
+  const u32 tiles = j.n_tiles * j.k_tiles, e = blockIdx.x / tiles;
+  const uint2 t = grouped_order(xcd_order(blockIdx.x - e * tiles, tiles), j.n_tiles, j.k_tiles, 8);
   const int n0 = (int)t.x * C::BM, k0 = (int)t.y * C::BN;
   const int2 r = j.off.range(e);
   // this split's rows: an equal share, in whole stages
@@ -202,7 +201,7 @@ ccld_status check(const ccld_expert_args* a, bool grad) {
   if (rows_product && plan_rows(a->rows, a->n_experts, (int)(grad ? a->k : a->n), (int)(grad ? a->n : a->k)).groups >= MAX_GROUPS) return CCLD_E_CAPACITY;
   if (grad && a->dw) {
     const WeightPlan p = plan_weights(a->rows, a->n_experts, (int)a->n, (int)a->k);
-    if ((u64)a->n_experts * ((u64)p.n_tiles * p.k_tiles + 7) >= MAX_GROUPS) return CCLD_E_CAPACITY;
+    if ((u64)a->n_experts * p.n_tiles * p.k_tiles >= MAX_GROUPS) return CCLD_E_CAPACITY;
   }
   return CCLD_OK;
 }
@@ -258,7 +257,7 @@ ccld_status product_of_rows(const ccld_expert_args* a, bool grad, hipStream_t st
 
 template <class C, class T>
 void launch_weights(const WeightJob& j, const WeightPlan& p, bool d, hipStream_t stream) {
-  const dim3 grid((u32)(j.off.n_experts * (((u64)p.n_tiles * p.k_tiles + 7) / 8 * 8)), p.splits);
+  const dim3 grid(j.off.n_experts * p.n_tiles * p.k_tiles, p.splits);
   if (d) k_expert_weights<C, T, true><<<grid, C::THREADS, C::LDS_BYTES, stream>>>(j);
   else k_expert_weights<C, T, false><<<grid, C::THREADS, C::LDS_BYTES, stream>>>(j);
 }

@@ -34,18 +34,8 @@ inline Cut choose_cut(double tiles_256, double tiles_128, uint64_t steps, double
   return best;
 }
 
-// In how many parts tiles of 256 x 256, `steps` of 32 deep, are computed where their number is known on the device only: what leaves the fewest
-// compute units idle, with no more than twice as many pieces as there are of them.
-constexpr uint32_t MOST_SPLITS = 16, MOST_PIECES = 2 * (uint32_t)COMPUTE_UNITS;
-__host__ __device__ inline uint32_t splits_of(uint32_t tiles, uint32_t steps) {
-  uint32_t best = 1, least = ~0u;
-  for (uint32_t s = 1; s <= MOST_SPLITS && (s == 1 || (tiles * s <= MOST_PIECES && steps / s >= 16)); ++s) {
-    // rounds / s in 64ths, and a little for the sums' way through memory
-    const uint32_t cost = (uint32_t)((tiles * s + COMPUTE_UNITS - 1) / COMPUTE_UNITS) * 1024 / s + 8 * s;
-    if (cost < least) { least = cost; best = s; }
-  }
-  return best;
-}
+// Where the number of tiles is known on the device only, the parts of their contraction are chosen there (tiles.h).
+constexpr uint32_t MOST_SPLITS = 64, MOST_PIECES = 2 * (uint32_t)COMPUTE_UNITS;
 
 inline bool aligned(const void* p, uintptr_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
 inline ccld_status launched() { return hipGetLastError() == hipSuccess ? CCLD_OK : CCLD_E_HIP; }

@@ -27,6 +27,7 @@
 #include <type_traits>
 
 #include "device_utils.h"
+#include "products.h"
 
 namespace ccld {
 
@@ -75,6 +76,7 @@ struct Tiling {
 using Large = Tiling<256, 256, 2, 4, 32, 5>;
 using Medium = Tiling<128, 128, 2, 4, 32, 5>;
 using Few = Tiling<32, 128, 1, 4, 64, 4>;
+using Narrow = Tiling<32, 32, 2, 1, 64, 8>;
 
 // Which 32-byte piece of an operand that lies across c is kept at a position of row c in LDS: the wavefront's transposing
 // reads touch rows c .. c + 3 and c + 8 .. c + 11 at once, 32 bytes of each.
@@ -377,6 +379,24 @@ __device__ __forceinline__ void store4(T* p, f32x4 v, int left, bool wide) {
     for (int r = 0; r < 4; ++r)
       if (r < left) p[r] = (T)v[r];
   }
+}
+
+// In how many parts the contraction of `tiles` tiles is computed: the least time by choose_cut's figures, in nanoseconds, with no more than
+// MOST_PIECES pieces.  steps: of 32 along the contraction.  A lane of the wavefront weighs each number.
+template <class C>
+__device__ __forceinline__ u32 splits_of(u32 tiles, u32 steps) {
+  static_assert(MOST_SPLITS == CCLD_WAVE, "one to a lane");
+  constexpr u32 AT_ONCE = (C::BM == 256 ? 1 : 2) * (u32)COMPUTE_UNITS, STEP_NS = C::BM == 256 ? 770 : C::BM == 128 ? 500 : 250;
+  const u32 s = lane_id() + 1;
+  const bool may = s == 1 || (tiles * s <= MOST_PIECES && steps >= 16 * s);
+  const u32 rounds = (tiles * s + AT_ONCE - 1) / AT_ONCE, depth = (steps + s - 1) / s;
+  u64 best = may ? ((u64)rounds * (10000 + (u64)depth * STEP_NS) + (u64)tiles * s * (C::BM * C::BN) / 560) * CCLD_WAVE + lane_id() : ~(u64)0;
+#pragma unroll
+  for (int x = 1; x < CCLD_WAVE; x *= 2) {
+    const u64 other = __shfl_xor(best, x, CCLD_WAVE);
+    best = other < best ? other : best;
+  }
+  return (u32)__builtin_amdgcn_readfirstlane((int)(best % CCLD_WAVE)) + 1;
 }
 
 // Workgroups are handed to the eight XCDs in turn, each with an L2 of its own: this gives each XCD a contiguous share of n

@@ -271,7 +271,7 @@ struct InputJob {            // dh: dz [kept][width] times w [width][d]
 // the parts of dh's contraction, the same for all pieces
 template <class C>
 __device__ __forceinline__ u32 input_splits(u32 kept, u32 col_tiles, int full_width) {
-  return splits_of((kept + C::BM - 1) / C::BM * col_tiles, (u32)full_width / 32);
+  return splits_of<C>((kept + C::BM - 1) / C::BM * col_tiles, (u32)full_width / 32);
 }
 
 template <class C, class T, bool DIRECT>
@@ -379,7 +379,7 @@ __global__ __launch_bounds__(256) void k_weight_rows(Rows w, const float* __rest
 i64 div_up(i64 a, i64 b) { return (a + b - 1) / b; }
 i64 round_up(i64 a, i64 b) { return div_up(a, b) * b; }
 
-enum Size { LARGE, MEDIUM, FEW };
+enum Size { LARGE, MEDIUM, FEW, NARROW };
 // for rows x cols of results; less than 48 rows are bound by reading the vocabulary's weights
 Size tile_size(i64 rows, i64 cols, i64 depth, u32 most_splits) {
   if (rows < 48) return FEW;
@@ -387,8 +387,14 @@ Size tile_size(i64 rows, i64 cols, i64 depth, u32 most_splits) {
                            (double)rows * cols, true, most_splits);
   return c.large ? LARGE : MEDIUM;
 }
+// Logits cannot be split along their contraction.  Few rows and a small vocabulary: narrow tiles, so that more compute units read it.
+Size logit_size(i64 rows, i64 cols, i64 depth) {
+  const Size s = tile_size(rows, cols, depth, 1);
+  return s == FEW && div_up(cols, Few::BN) < (i64)COMPUTE_UNITS / 2 ? NARROW : s;
+}
 int tile_m(Size s) { return s == LARGE ? Large::BM : s == MEDIUM ? Medium::BM : Few::BM; }
-int tile_n(Size s) { return s == LARGE ? Large::BN : s == MEDIUM ? Medium::BN : Few::BN; }
+int tile_n(Size s) { return s == LARGE ? Large::BN : s == NARROW ? Narrow::BN : Medium::BN; }
+static_assert(Medium::BN == Few::BN && Few::BM == Narrow::BM);
 
 // dz of a piece is 2^28 values at most (512 MB), but a piece has 4,096 columns at least, and 2^21 at most: a tile of dz is reached by
 // 32-bit offsets.
@@ -440,13 +446,13 @@ Plan make_plan(const ccld_vocab_args* a, bool grad, Carver& c) {
   p.rows.scale = c.take<float>(rows);
   p.rows.h = c.take<uint16_t>(rows * p.dp);
   if (!grad) {
-    p.logits = tile_size(a->rows, a->vocab, a->d, 1);
+    p.logits = logit_size(a->rows, a->vocab, a->d);
     p.col_tiles = (u32)div_up(a->vocab, tile_n(p.logits));
     p.part = c.take<float2>(rows * p.col_tiles);
     return p;
   }
   p.width = piece_width(a);
-  p.logits = tile_size(a->rows, p.width, a->d, 1);
+  p.logits = logit_size(a->rows, p.width, a->d);
   p.col_tiles = (u32)div_up(p.width, tile_n(p.logits));
   p.dz = c.take<uint16_t>(rows * p.width);
   if (a->dh) {
@@ -558,7 +564,8 @@ ccld_status loss(const ccld_vocab_args* a, const Plan& p, hipStream_t stream) {
   const LogitJob j{p.rows, a->w, a->ldw, (int)a->d, p.dp, 0, (int)a->vocab, p.col_tiles, p.part, nullptr, 0};
   if (p.logits == LARGE) launch_logit_sums<Large, T>(a, j, stream);
   else if (p.logits == MEDIUM) launch_logit_sums<Medium, T>(a, j, stream);
-  else launch_logit_sums<Few, T>(a, j, stream);
+  else if (p.logits == FEW) launch_logit_sums<Few, T>(a, j, stream);
+  else launch_logit_sums<Narrow, T>(a, j, stream);
   k_loss<<<(u32)div_up(a->rows, 4), 256, 0, stream>>>(p.rows, p.part, p.col_tiles, a->loss, a->lse);
   return launched();
 }
@@ -573,7 +580,8 @@ ccld_status gradient(const ccld_vocab_args* a, const Plan& p, hipStream_t stream
       const LogitJob j{p.rows, w, a->ldw, (int)a->d, p.dp, (int)first, (int)cols, 0, nullptr, p.dz, p.width};
       if (p.logits == LARGE) launch_logit_grad<Large, T>(a, j, stream);
       else if (p.logits == MEDIUM) launch_logit_grad<Medium, T>(a, j, stream);
-      else launch_logit_grad<Few, T>(a, j, stream);
+      else if (p.logits == FEW) launch_logit_grad<Few, T>(a, j, stream);
+      else launch_logit_grad<Narrow, T>(a, j, stream);
     }
     if (a->dh && a->rows) {
       const InputJob j{p.rows, p.dz, w, p.width, a->ldw, (int)a->d, (int)cols, (int)p.width, 0, p.sum, first > 0};
@@ -607,8 +615,10 @@ hipError_t allow_tiling() {
   allow(&k_logit_sums<C, T, false>);
   allow(&k_logit_grad<C, T, true>);
   allow(&k_logit_grad<C, T, false>);
-  allow(&k_input_grad<C, T, true>);
-  allow(&k_input_grad<C, T, false>);
+  if constexpr (C::BN > 32) {
+    allow(&k_input_grad<C, T, true>);
+    allow(&k_input_grad<C, T, false>);
+  }
   if constexpr (C::BM > 32) allow(&k_weight_grad<C, T>);
   return e;
 }
@@ -619,7 +629,7 @@ namespace ccld {
 hipError_t allow_lds_vocab() {
   for (hipError_t e : {allow_tiling<Large, __bf16>(), allow_tiling<Large, _Float16>(), allow_tiling<Medium, __bf16>(),
                        allow_tiling<Medium, _Float16>(), allow_tiling<Few, __bf16>(),
-                       allow_tiling<Few, _Float16>()})
+                       allow_tiling<Few, _Float16>(), allow_tiling<Narrow, __bf16>(), allow_tiling<Narrow, _Float16>()})
     if (e != hipSuccess) return e;
   return hipSuccess;
 }
