@@ -112,7 +112,7 @@ __global__ __launch_bounds__(C::THREADS) void k_expert_rows(RowJob j) {
 }
 
 template <class C, class T, bool DIRECT>
-__global__ __launch_bounds__(C::THREADS) void k_expert_weights(WeightJob j) {
+__global__ __launch_bounds__(C::THREADS, C::WAVES) void k_expert_weights(WeightJob j) {
   // every expert's tiles are divided among the XCDs, since experts differ in their rows (an expert after another to an XCD: 1.5
   // times the time at 32 experts whose rows spread like exp(0.7 N)).  Workgroups of the same number modulo 8 share an XCD within an
   // expert too, whichever its first one has.
@@ -142,47 +142,46 @@ __global__ __launch_bounds__(C::THREADS) void k_expert_weights(WeightJob j) {
 u64 div_up(u64 a, u64 b) { return (a + b - 1) / b; }
 
 // How the rows' products are cut.  Experts with less than 48 rows on average are bound by reading their weights: tiles of 32 rows.
-struct RowPlan { int bm, bn; u32 col_tiles; u64 groups; u32 splits; int split_depth; };
-RowPlan plan_rows(u64 rows, u64 experts, int cols, int depth) {
+struct RowPlan { Tile tile; u32 col_tiles; u64 groups; u32 splits; int split_depth; };
+RowPlan plan_rows(u64 rows, u64 experts, int cols, int depth, bool whole) {
   RowPlan p;
   const u64 busy = std::min(rows, experts), mean = rows / std::max<u64>(experts, 1), steps = div_up(depth, DEPTH);
   u64 s = 1;
   if (mean < 48) {
-    p.bm = 32;
-    p.bn = 128;
+    p.tile = FEW;
     const u64 tiles = std::max<u64>(div_up(rows, 32), busy) * div_up(cols, 128);
     while (tiles * s < COMPUTE_UNITS && steps / (2 * s) >= 8) s *= 2;
   } else {
     // a part's last tile is half full on average
     const double m256 = std::max<double>(busy, rows / 256.0 + busy * 0.5), m128 = std::max<double>(busy, rows / 128.0 + busy * 0.5);
-    const Cut c = choose_cut(m256 * div_up(cols, 256), m128 * div_up(cols, 128), 2 * steps, (double)rows * cols, busy == 1);
-    p.bm = p.bn = c.large ? 256 : 128;
+    const Cut c = choose_cut(m256 * div_up(cols, 256), m128 * div_up(cols, 128), 2 * steps, (double)rows * cols, busy == 1, whole);
+    p.tile = c.tile;
     s = c.splits;
   }
-  p.col_tiles = (u32)div_up(cols, p.bn);
+  p.col_tiles = (u32)div_up(cols, tile_n(p.tile));
   // tiles of the worst division: every part may end in a tile of its own
-  p.groups = (rows / p.bm + std::min(rows, experts + 2)) * p.col_tiles;
+  p.groups = (rows / tile_m(p.tile) + std::min(rows, experts + 2)) * p.col_tiles;
   p.split_depth = (int)(div_up(steps, s) * DEPTH);
   p.splits = (u32)div_up(steps, div_up(steps, s));
   return p;
 }
 
-struct WeightPlan { int bm, bn; u32 n_tiles, k_tiles, splits; };
-WeightPlan plan_weights(u64 rows, u64 experts, int n, int k) {
-  WeightPlan p;
-  const Cut c = choose_cut((double)experts * div_up(n, 256) * div_up(k, 256), (double)experts * div_up(n, 128) * div_up(k, 128),
-                           div_up(rows, experts * 32), (double)experts * n * k, true);
-  p.bm = p.bn = c.large ? 256 : 128;
-  p.n_tiles = (u32)div_up(n, p.bm);
-  p.k_tiles = (u32)div_up(k, p.bn);
-  p.splits = c.splits;
-  return p;
+struct WeightPlan { Tile tile; u32 n_tiles, k_tiles, splits; };
+WeightPlan plan_weights(u64 rows, u64 experts, int n, int k, bool whole) {
+  const Cut c = choose_weight_cut((u64)n, (u64)k, div_up(rows, experts), whole, experts);
+  return WeightPlan{c.tile, (u32)div_up(n, tile_m(c.tile)), (u32)div_up(k, tile_n(c.tile)), c.splits};
 }
 
-// 16-byte pieces lie wholly inside or outside the operands, and start on 16 bytes
-bool direct(const ccld_expert_args* a, const void* rows_at, i64 ld) {
-  return a->k % 8 == 0 && a->n % 8 == 0 && a->ldw % 8 == 0 && a->expert_stride % 8 == 0 && ld % 8 == 0 && aligned(a->w, 16) &&
-         aligned(rows_at, 16);
+// Pieces of 16 bytes lie wholly inside or outside the operands: x, dy, the weights (plans go by sizes and strides alone, so that the workspace does not
+// depend on addresses), and start on 16 bytes.
+bool whole_pieces(const ccld_expert_args* a, i64 ld) { return a->k % 8 == 0 && a->n % 8 == 0 && a->ldw % 8 == 0 && a->expert_stride % 8 == 0 && ld % 8 == 0; }
+bool direct(const ccld_expert_args* a, const void* rows_at, i64 ld) { return whole_pieces(a, ld) && aligned(a->w, 16) && aligned(rows_at, 16); }
+
+RowPlan row_plan(const ccld_expert_args* a, bool grad) {
+  return plan_rows((u64)a->rows, (u64)a->n_experts, (int)(grad ? a->k : a->n), (int)(grad ? a->n : a->k), whole_pieces(a, grad ? a->lddy : a->ldx));
+}
+WeightPlan weight_plan(const ccld_expert_args* a) {
+  return plan_weights((u64)a->rows, (u64)a->n_experts, (int)a->n, (int)a->k, a->n % 8 == 0 && a->k % 8 == 0 && a->lddy % 8 == 0 && a->ldx % 8 == 0);
 }
 
 ccld_status check(const ccld_expert_args* a, bool grad) {
@@ -198,9 +197,9 @@ ccld_status check(const ccld_expert_args* a, bool grad) {
   } else if (a->ldy < a->n) return CCLD_E_BAD_ARG;
   // a launch has less than 2^32 threads
   const bool rows_product = !grad || a->dx;
-  if (rows_product && plan_rows(a->rows, a->n_experts, (int)(grad ? a->k : a->n), (int)(grad ? a->n : a->k)).groups >= MAX_GROUPS) return CCLD_E_CAPACITY;
+  if (rows_product && row_plan(a, grad).groups >= MAX_GROUPS) return CCLD_E_CAPACITY;
   if (grad && a->dw) {
-    const WeightPlan p = plan_weights(a->rows, a->n_experts, (int)a->n, (int)a->k);
+    const WeightPlan p = weight_plan(a);
     if ((u64)a->n_experts * p.n_tiles * p.k_tiles >= MAX_GROUPS) return CCLD_E_CAPACITY;
   }
   return CCLD_OK;
@@ -228,15 +227,15 @@ void launch_rows(const RowJob& j, const RowPlan& p, hipStream_t stream) {
 }
 template <class T, bool W_ACROSS, bool DIRECT>
 void launch_rows(const RowJob& j, const RowPlan& p, hipStream_t stream) {
-  if (p.bm == 256) launch_rows<Large, T, W_ACROSS, DIRECT>(j, p, stream);
-  else if (p.bm == 128) launch_rows<Medium, T, W_ACROSS, DIRECT>(j, p, stream);
+  if (p.tile == LARGE) launch_rows<Large, T, W_ACROSS, DIRECT>(j, p, stream);
+  else if (p.tile == MEDIUM) launch_rows<Medium, T, W_ACROSS, DIRECT>(j, p, stream);
   else launch_rows<Few, T, W_ACROSS, DIRECT>(j, p, stream);
 }
 
 template <class T>
 ccld_status product_of_rows(const ccld_expert_args* a, bool grad, hipStream_t stream) {
   const int cols = (int)(grad ? a->k : a->n), depth = (int)(grad ? a->n : a->k);
-  const RowPlan p = plan_rows(a->rows, a->n_experts, cols, depth);
+  const RowPlan p = row_plan(a, grad);
   RowJob j{};
   j.a = grad ? a->dy : a->x;
   j.lda = grad ? a->lddy : a->ldx;
@@ -264,7 +263,7 @@ void launch_weights(const WeightJob& j, const WeightPlan& p, bool d, hipStream_t
 
 template <class T>
 ccld_status product_of_weights(const ccld_expert_args* a, hipStream_t stream) {
-  const WeightPlan p = plan_weights(a->rows, a->n_experts, (int)a->n, (int)a->k);
+  const WeightPlan p = weight_plan(a);
   WeightJob j{};
   j.dy = a->dy; j.x = a->x; j.out = a->dw;
   j.part = p.splits > 1 ? static_cast<float*>(a->workspace) : nullptr;
@@ -272,9 +271,10 @@ ccld_status product_of_weights(const ccld_expert_args* a, hipStream_t stream) {
   j.lddy = a->lddy; j.ldx = a->ldx; j.n = (int)a->n; j.k = (int)a->k;
   j.n_tiles = p.n_tiles; j.k_tiles = p.k_tiles;
   j.whole = a->k % 8 == 0 && aligned(a->dw, 16);
-  const bool d = direct(a, a->dy, a->lddy) && a->ldx % 8 == 0 && aligned(a->x, 16);
-  if (p.bm == 256) launch_weights<Large, T>(j, p, d, stream);
-  else launch_weights<Medium, T>(j, p, d, stream);
+  const bool d = a->n % 8 == 0 && a->k % 8 == 0 && a->lddy % 8 == 0 && a->ldx % 8 == 0 && aligned(a->dy, 16) && aligned(a->x, 16);
+  if (p.tile == LARGE) launch_weights<Large, T>(j, p, d, stream);
+  else if (p.tile == MEDIUM) launch_weights<Medium, T>(j, p, d, stream);
+  else launch_weights<Short, T>(j, p, d, stream);
   if (j.part) launch_join(j.part, p.splits, (u64)a->n_experts * a->n, (u64)a->k, j.out, a->k, a->dtype, stream);
   return launched();
 }
@@ -283,10 +283,12 @@ template <class C, class T>
 hipError_t allow_tiling() {
   hipError_t e = hipSuccess;
   auto allow = [&](auto k) { if (e == hipSuccess) e = allow_lds(reinterpret_cast<const void*>(k), C::LDS_BYTES); };
-  allow(&k_expert_rows<C, T, false, true>);
-  allow(&k_expert_rows<C, T, false, false>);
-  allow(&k_expert_rows<C, T, true, true>);
-  allow(&k_expert_rows<C, T, true, false>);
+  if constexpr (!std::is_same_v<C, Short>) {
+    allow(&k_expert_rows<C, T, false, true>);
+    allow(&k_expert_rows<C, T, false, false>);
+    allow(&k_expert_rows<C, T, true, true>);
+    allow(&k_expert_rows<C, T, true, false>);
+  }
   if constexpr (C::BM > 32) {
     allow(&k_expert_weights<C, T, true>);
     allow(&k_expert_weights<C, T, false>);
@@ -299,7 +301,8 @@ hipError_t allow_tiling() {
 namespace ccld {
 hipError_t allow_lds_experts() {
   for (hipError_t e : {allow_tiling<Large, __bf16>(), allow_tiling<Large, _Float16>(), allow_tiling<Medium, __bf16>(),
-                       allow_tiling<Medium, _Float16>(), allow_tiling<Few, __bf16>(), allow_tiling<Few, _Float16>()})
+                       allow_tiling<Medium, _Float16>(), allow_tiling<Short, __bf16>(), allow_tiling<Short, _Float16>(), allow_tiling<Few, __bf16>(),
+                       allow_tiling<Few, _Float16>()})
     if (e != hipSuccess) return e;
   return hipSuccess;
 }
@@ -311,9 +314,9 @@ extern "C" ccld_status ccld_expert_workspace(const ccld_expert_args* a, int32_t 
   if (s != CCLD_OK) return s;
   u64 need = 0;
   if (!grad || a->dx)
-    need = row_part_bytes(plan_rows(a->rows, a->n_experts, (int)(grad ? a->k : a->n), (int)(grad ? a->n : a->k)), a->rows, grad ? a->k : a->n);
+    need = row_part_bytes(row_plan(a, grad), a->rows, grad ? a->k : a->n);
   if (grad && a->dw)     // the two gradients follow one another: one workspace serves both
-    need = std::max(need, weight_part_bytes(plan_weights(a->rows, a->n_experts, (int)a->n, (int)a->k), a->n_experts, a->n, a->k));
+    need = std::max(need, weight_part_bytes(weight_plan(a), a->n_experts, a->n, a->k));
   *bytes = (need + 255) & ~(u64)255;
   return CCLD_OK;
 }

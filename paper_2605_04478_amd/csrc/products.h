@@ -14,24 +14,46 @@ constexpr int64_t MAX_ROWS = (int64_t)1 << 31, MAX_EXPERTS = (int64_t)1 << 20, M
 // a tile's last row starts below 2^31 bytes from its first: 256 rows (or DEPTH of them) of this many 16-bit elements, and a row
 constexpr int64_t MAX_LD = ((int64_t)1 << 22) - ((int64_t)1 << 14);
 
-// How a product is cut: tiles of 256 x 256, one to a compute unit, or of 128 x 128, two to one, and the contraction in `splits` parts whose
-// sums are joined.  A step of 32 of the contraction takes 0.77 us in the former (8192^3: 1,390 TFLOP/s) and 0.5 us in the latter (1,084), a tile's
-// start and end 10 and 6 us, and sums of parts move at 4.5 TB/s.  The smaller tiles win where the larger ones would leave
-// compute units idle: the weights of 12 experts, 1,000 x 1,336 each, are 288 tiles of 256 (48 us) or 1,056 of 128 (38 us); those of 64
-// experts, 1,024 x 2,048 each and 128 rows on average, 98 us and 123.  counted: the numbers of tiles are what they will be, not what ragged rows are expected to give.
-struct Cut { bool large; uint32_t splits; };
-inline Cut choose_cut(double tiles_256, double tiles_128, uint64_t steps, double results, bool counted, uint32_t most_splits = 16) {
-  Cut best{true, 1};
+// How a product is cut: the tiles (tiles.h) and the parts of the contraction, whose sums are joined.
+//
+// Tiles of 256 x 256, one to a compute unit, or of 128 x 128, two to one.  A step of 32 of the contraction takes 0.77 us in the former (8192^3: 1,390
+// TFLOP/s) and 0.5 us in the latter (1,084), a tile's start and end 10 and 6 us, and sums of parts move at 4.5 TB/s.  The smaller tiles win
+// where the larger ones would leave compute units idle: the weights of 12 experts, 1,000 x 1,336 each, are 288 tiles of 256 (48 us) or 1,056 of
+// 128 (38 us).  (Tiles of 256 x 128, two to a compute unit, were between the two in every case but one, by less than a tenth.)  Operands that pass through
+// registers need too many of them beside the sums of 256 x 256: 43 experts' dx, 598 x 3,722 each, 820 us in the larger tiles and 480 in the
+// smaller ones, dw 792 and 377.  counted: the numbers of tiles are what they will be, not what ragged rows are expected to give.
+enum Tile { LARGE, MEDIUM, SHORT, FEW, NARROW };
+inline uint32_t tile_m(Tile t) { return t == LARGE ? 256 : t == MEDIUM || t == SHORT ? 128 : 32; }
+inline uint32_t tile_n(Tile t) { return t == LARGE ? 256 : t == NARROW ? 32 : 128; }
+struct Cut { Tile tile; uint32_t splits; };
+inline Cut choose_cut(double tiles_256, double tiles_128, uint64_t steps, double results, bool counted, bool direct, uint32_t most_splits = 16) {
+  const struct { Tile tile; double tiles, at_once, start, step; } forms[] = {{MEDIUM, tiles_128, 2 * COMPUTE_UNITS, 6, 0.5},
+                                                                             {LARGE, tiles_256, COMPUTE_UNITS, 10, 0.77}};
+  Cut best{MEDIUM, 1};
   double least = 1e300;
-  for (int large = 1; large >= 0; --large)
+  for (const auto& f : forms) {
+    if (f.tile == LARGE && !direct) continue;
     for (uint32_t s = 1; s <= most_splits && (s == 1 || steps / s >= 16); s *= 2) {
-      double rounds = (large ? tiles_256 : tiles_128) * s / (double)(large ? COMPUTE_UNITS : 2 * COMPUTE_UNITS);
+      double rounds = f.tiles * s / f.at_once;
       if (rounds < 0.7) rounds = 1;
       else if (rounds < 4) rounds = counted ? (double)(int64_t)(rounds + 0.999) : rounds + 0.35;
-      const double us = rounds * ((large ? 10 : 6) + (double)((steps + s - 1) / s) * (large ? 0.77 : 0.5)) + (s > 1 ? 4 + results * (8.0 * s + 2) / 4.5e6 : 0);
-      if (us < least) { least = us; best = Cut{large != 0, s}; }
+      const double us = rounds * (f.start + (double)((steps + s - 1) / s) * f.step) + (s > 1 ? 4 + results * (8.0 * s + 2) / 4.5e6 : 0);
+      if (us < least) { least = us; best = Cut{f.tile, s}; }
     }
+  }
   return best;
+}
+inline uint64_t parts_of(uint64_t n, uint64_t by) { return (n + by - 1) / by; }
+// rows x cols of results, of as many products
+inline Cut choose_cut(uint64_t rows, uint64_t cols, uint64_t depth, bool direct, uint32_t most_splits = 16, uint64_t products = 1) {
+  return choose_cut((double)products * parts_of(rows, 256) * parts_of(cols, 256), (double)products * parts_of(rows, 128) * parts_of(cols, 128),
+                    parts_of(depth, 32), (double)products * rows * cols, true, direct, most_splits);
+}
+// Gradients of weights, n x k of them from so many rows.  Up to four steps are bound by writing the results: three small workgroups to a compute unit, so
+// that some write while others load (64 experts of 1,024 x 2,048: 2 rows each 47 us, 53 in the larger tiles and 58 in those of 128 x 128; 64 rows 57, 65
+// and 72; 128 rows 74, 81 and 89).
+inline Cut choose_weight_cut(uint64_t n, uint64_t k, uint64_t rows, bool direct, uint64_t products = 1) {
+  return direct && rows <= 4 * 32 ? Cut{SHORT, 1} : choose_cut(n, k, rows, direct, 16, products);
 }
 
 // Where the number of tiles is known on the device only, the parts of their contraction are chosen there (tiles.h).

@@ -70,11 +70,13 @@ struct Tiling {
   static constexpr int MI = TM / 16, NI = TN / 16;
   static constexpr int STAGE_BYTES = (BM + BN) * DEPTH * 2;
   static constexpr int LDS_BYTES = STAGES * STAGE_BYTES;
+  static constexpr int WAVES = THREADS / CCLD_WAVE * (163840 / LDS_BYTES) / 4;       // to a SIMD, as many workgroups as the LDS holds
   static_assert(TM % 16 == 0 && TN % 16 == 0, "blocks of 16 x 16");
 };
 
 using Large = Tiling<256, 256, 2, 4, 32, 5>;
 using Medium = Tiling<128, 128, 2, 4, 32, 5>;
+using Short = Tiling<128, 128, 2, 2, 32, 3>;
 using Few = Tiling<32, 128, 1, 4, 64, 4>;
 using Narrow = Tiling<32, 32, 2, 1, 64, 8>;
 
@@ -137,13 +139,18 @@ struct Operand {
   __device__ __forceinline__ s16x8 load(int i, int depth) const {
     const u32 r = row + i * ROW_STEP;
     const int x = (int)column(i), inside = ACROSS ? ((int)r < depth ? left - x : 0) : ((int)r < left ? depth - x : 0);
-    const T* p = base + (i64)r * ld + x;
+    const unsigned char* p = reinterpret_cast<const unsigned char*>(base) + offset[i];        // (inside the operand where anything is)
     s16x8 v = {};
     if (inside >= 8) __builtin_memcpy(&v, p, 16);              // loads need no alignment
-    else {
-#pragma unroll
-      for (int e = 0; e < 7; ++e)
-        if (e < inside) v[e] = __builtin_bit_cast(short, p[e]);
+    else if (inside > 0) {
+      u64 part[2] = {0, 0};
+#pragma unroll 1
+      for (int e = 0; e < inside; ++e) {                      // (not unrolled: it is rare, and its registers would be taken from the loop's)
+        const u64 one = (u64)reinterpret_cast<const unsigned short*>(p)[e] << (e % 4 * 16);
+        part[0] |= e < 4 ? one : 0;
+        part[1] |= e < 4 ? 0 : one;
+      }
+      __builtin_memcpy(&v, part, 16);
     }
     return v;
   }
@@ -218,7 +225,7 @@ struct TileProduct {
     Fragments<C::BN, C::NI, C::DEPTH, B_ACROSS> fb;
     fa.start(wave_m());
     fb.start(wave_n());
-    constexpr bool PAIRS = C::DEPTH == 32;
+    constexpr bool PAIRS = C::DEPTH == 32 && C::STAGES >= 5;
     constexpr int STAGES_AHEAD = PAIRS ? C::STAGES - 1 : C::STAGES;      // a pair needs two free places
     constexpr int A_TURN = PAIRS ? 2 * A::PIECES : A::PIECES, B_TURN = PAIRS ? 2 * B::PIECES : B::PIECES;
     auto after = [](u32 p) { return p + C::STAGE_BYTES == C::LDS_BYTES ? 0 : p + C::STAGE_BYTES; };

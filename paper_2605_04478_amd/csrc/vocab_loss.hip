@@ -313,17 +313,22 @@ __global__ __launch_bounds__(256) void k_input_rows(Rows w, const float* __restr
   const int pieces = d / V;
   for (i64 i = (i64)blockIdx.x * 256 + threadIdx.x; i < rows * pieces; i += (i64)gridDim.x * 256) {
     const i64 r = i / pieces, c = (i - r * pieces) * V, at = w.place[r];
-    float v[V] = {};
-    if (at >= 0)
-      for (u32 s = 0; s < splits; ++s) {
-        const float* q = sum + ((i64)s * kept + at) * d + c;
-        if constexpr (V == 4) {
-          const f32x4 x = *reinterpret_cast<const f32x4*>(q);
+    typedef float vec __attribute__((ext_vector_type(V)));
+    vec v = 0;
+    if (at >= 0) {
+      const float* q = sum + at * d + c;
+      const i64 step = kept * d;
+      u32 s = 0;
+      for (; s + 8 <= splits; s += 8) {              // eight on their way at once: a load after the other took 15 us of 64 parts
+        vec x[8];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] += x[e];
-        } else v[0] += *q;
+        for (int e = 0; e < 8; ++e) x[e] = *reinterpret_cast<const vec*>(q + (s + e) * step);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v += x[e];
       }
-    if constexpr (V == 4) store4(dh + r * lddh + c, f32x4{v[0], v[1], v[2], v[3]} * back, 4, true);
+      for (; s < splits; ++s) v += *reinterpret_cast<const vec*>(q + s * step);
+    }
+    if constexpr (V == 4) store4(dh + r * lddh + c, v * back, 4, true);
     else dh[r * lddh + c] = (T)(v[0] * back);
   }
 }
@@ -341,7 +346,7 @@ struct WeightJob {           // dw of a piece: dz^T [width][kept] times h [kept]
 };
 
 template <class C, class T>
-__global__ __launch_bounds__(C::THREADS) void k_weight_grad(WeightJob j) {
+__global__ __launch_bounds__(C::THREADS, C::WAVES) void k_weight_grad(WeightJob j) {
   const u32 id = xcd_order(blockIdx.x, gridDim.x);
   const uint2 t = grouped_order(id, j.n_tiles, j.k_tiles, 8);
   const int n0 = (int)t.x * C::BM, k0 = (int)t.y * C::BN;
@@ -379,22 +384,19 @@ __global__ __launch_bounds__(256) void k_weight_rows(Rows w, const float* __rest
 i64 div_up(i64 a, i64 b) { return (a + b - 1) / b; }
 i64 round_up(i64 a, i64 b) { return div_up(a, b) * b; }
 
-enum Size { LARGE, MEDIUM, FEW, NARROW };
+bool whole_pieces(const ccld_vocab_args* a) { return a->d % 8 == 0 && a->ldw % 8 == 0; }
+
 // for rows x cols of results; less than 48 rows are bound by reading the vocabulary's weights
-Size tile_size(i64 rows, i64 cols, i64 depth, u32 most_splits) {
-  if (rows < 48) return FEW;
-  const Cut c = choose_cut((double)div_up(rows, 256) * div_up(cols, 256), (double)div_up(rows, 128) * div_up(cols, 128), div_up(depth, 32),
-                           (double)rows * cols, true, most_splits);
-  return c.large ? LARGE : MEDIUM;
+Tile choose_tile(i64 rows, i64 cols, i64 depth, bool whole, u32 most_splits) {
+  return rows < 48 ? FEW : choose_cut((u64)rows, (u64)cols, (u64)depth, whole, most_splits).tile;
 }
-// Logits cannot be split along their contraction.  Few rows and a small vocabulary: narrow tiles, so that more compute units read it.
-Size logit_size(i64 rows, i64 cols, i64 depth) {
-  const Size s = tile_size(rows, cols, depth, 1);
-  return s == FEW && div_up(cols, Few::BN) < (i64)COMPUTE_UNITS / 2 ? NARROW : s;
+// Logits cannot be split along their contraction: where there are few tiles, smaller ones, so that more compute units read the weights.  60 rows, a vocabulary
+// of 3,047, 1,976 deep: 16.1 us in tiles of 32 x 32, 20.9 of 32 x 128, 25.5 of 128 x 128; 345 rows, 2,232, 944 deep: 20.1, 16.9 and 21.0; 100 rows,
+// 20,000, 1,000 deep: 41, 30 and 24.5.
+Tile logit_tiles(i64 rows, i64 cols, i64 depth, bool whole) {
+  const i64 few = div_up(rows, Few::BM) * div_up(cols, Few::BN);
+  return few < (i64)COMPUTE_UNITS / 2 ? NARROW : few <= (i64)COMPUTE_UNITS ? FEW : choose_tile(rows, cols, depth, whole, 1);
 }
-int tile_m(Size s) { return s == LARGE ? Large::BM : s == MEDIUM ? Medium::BM : Few::BM; }
-int tile_n(Size s) { return s == LARGE ? Large::BN : s == NARROW ? Narrow::BN : Medium::BN; }
-static_assert(Medium::BN == Few::BN && Few::BM == Narrow::BM);
 
 // dz of a piece is 2^28 values at most (512 MB), but a piece has 4,096 columns at least, and 2^21 at most: a tile of dz is reached by
 // 32-bit offsets.
@@ -419,16 +421,16 @@ struct Plan {
   Rows rows;
   int dp;
   // loss
-  Size logits;
+  Tile logits;
   u32 col_tiles;
   float2* part;
   // gradient
   i64 width;
   uint16_t* dz;
-  Size input;
+  Tile input;
   u32 pieces;              // workgroups for dh at most
   float* sum;
-  Size weight;
+  Tile weight;
   u32 weight_splits;
   float* weight_part;
 };
@@ -446,26 +448,25 @@ Plan make_plan(const ccld_vocab_args* a, bool grad, Carver& c) {
   p.rows.scale = c.take<float>(rows);
   p.rows.h = c.take<uint16_t>(rows * p.dp);
   if (!grad) {
-    p.logits = logit_size(a->rows, a->vocab, a->d);
+    p.logits = logit_tiles(a->rows, a->vocab, a->d, whole_pieces(a));
     p.col_tiles = (u32)div_up(a->vocab, tile_n(p.logits));
     p.part = c.take<float2>(rows * p.col_tiles);
     return p;
   }
   p.width = piece_width(a);
-  p.logits = logit_size(a->rows, p.width, a->d);
+  p.logits = logit_tiles(a->rows, p.width, a->d, whole_pieces(a));
   p.col_tiles = (u32)div_up(p.width, tile_n(p.logits));
   p.dz = c.take<uint16_t>(rows * p.width);
   if (a->dh) {
     // the parts of the contraction are chosen on the device, by the rows that have a target: pieces are bounded, not parts
-    p.input = tile_size(a->rows, a->d, p.width, MOST_SPLITS);
+    p.input = choose_tile(a->rows, a->d, p.width, whole_pieces(a), MOST_SPLITS);
     const u64 tiles = (u64)div_up(a->rows, tile_m(p.input)) * div_up(a->d, tile_n(p.input));
     p.pieces = (u32)std::max<u64>(tiles, MOST_PIECES);
     p.sum = c.take<float>(std::max<u64>(rows * a->d, (u64)MOST_PIECES * tile_m(p.input) * tile_n(p.input)));
   }
   if (a->dw) {
-    const Cut w = choose_cut((double)div_up(p.width, 256) * div_up(a->d, 256), (double)div_up(p.width, 128) * div_up(a->d, 128),
-                             div_up(a->rows, 32), (double)p.width * a->d, true);
-    p.weight = w.large ? LARGE : MEDIUM;
+    const Cut w = choose_weight_cut((u64)p.width, (u64)a->d, (u64)a->rows, true);
+    p.weight = w.tile;
     p.weight_splits = w.splits;
     if (p.weight_splits > 1) p.weight_part = c.take<float>((u64)p.weight_splits * p.width * a->d);
   }
@@ -521,7 +522,7 @@ void start(const ccld_vocab_args* a, const Plan& p, bool grad, hipStream_t strea
   else start_rows<T, 1>(a, p, grad, stream);
 }
 
-bool direct(const ccld_vocab_args* a) { return a->d % 8 == 0 && a->ldw % 8 == 0 && aligned(a->w, 16); }
+bool direct(const ccld_vocab_args* a) { return whole_pieces(a) && aligned(a->w, 16); }
 
 template <class C, class T>
 void launch_logit_sums(const ccld_vocab_args* a, const LogitJob& j, hipStream_t stream) {
@@ -594,7 +595,8 @@ ccld_status gradient(const ccld_vocab_args* a, const Plan& p, hipStream_t stream
       const WeightJob j{p.rows, p.dz, p.width, dw, a->lddw, (int)a->d, p.dp, (int)cols, 0, 0, p.weight_part,
                         a->lddw % 8 == 0 && aligned(dw, 16)};
       if (p.weight == LARGE) launch_weight_grad<Large, T>(p, j, stream);
-      else launch_weight_grad<Medium, T>(p, j, stream);
+      else if (p.weight == MEDIUM) launch_weight_grad<Medium, T>(p, j, stream);
+      else launch_weight_grad<Short, T>(p, j, stream);
       if (p.weight_part)
         k_weight_rows<T><<<stream_groups(cols * a->d), 256, 0, stream>>>(p.rows, p.weight_part, p.weight_splits, cols, (int)a->d, dw, a->lddw);
     }
@@ -611,11 +613,13 @@ template <class C, class T>
 hipError_t allow_tiling() {
   hipError_t e = hipSuccess;
   auto allow = [&](auto k) { if (e == hipSuccess) e = allow_lds(reinterpret_cast<const void*>(k), C::LDS_BYTES); };
-  allow(&k_logit_sums<C, T, true>);
-  allow(&k_logit_sums<C, T, false>);
-  allow(&k_logit_grad<C, T, true>);
-  allow(&k_logit_grad<C, T, false>);
-  if constexpr (C::BN > 32) {
+  if constexpr (!std::is_same_v<C, Short>) {
+    allow(&k_logit_sums<C, T, true>);
+    allow(&k_logit_sums<C, T, false>);
+    allow(&k_logit_grad<C, T, true>);
+    allow(&k_logit_grad<C, T, false>);
+  }
+  if constexpr (C::BN > 32 && !std::is_same_v<C, Short>) {
     allow(&k_input_grad<C, T, true>);
     allow(&k_input_grad<C, T, false>);
   }
@@ -628,7 +632,7 @@ hipError_t allow_tiling() {
 namespace ccld {
 hipError_t allow_lds_vocab() {
   for (hipError_t e : {allow_tiling<Large, __bf16>(), allow_tiling<Large, _Float16>(), allow_tiling<Medium, __bf16>(),
-                       allow_tiling<Medium, _Float16>(), allow_tiling<Few, __bf16>(),
+                       allow_tiling<Medium, _Float16>(), allow_tiling<Short, __bf16>(), allow_tiling<Short, _Float16>(), allow_tiling<Few, __bf16>(),
                        allow_tiling<Few, _Float16>(), allow_tiling<Narrow, __bf16>(), allow_tiling<Narrow, _Float16>()})
     if (e != hipSuccess) return e;
   return hipSuccess;
