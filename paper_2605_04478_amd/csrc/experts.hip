@@ -107,7 +107,7 @@ __global__ __launch_bounds__(C::THREADS) void k_expert_rows(RowJob j) {
     float* o = j.part + ((i64)blockIdx.y * j.off.rows + row0) * j.cols + col0;
     prod.each([&](u32 m, u32 n, f32x4 v) { if ((int)m < rows) store4(o + (i64)m * j.cols + n, v, cols - (int)n, j.cols % 4 == 0); });
   } else {
-    prod.store(lds, static_cast<T*>(j.out) + (i64)row0 * j.ldo + col0, j.ldo, rows, cols, j.whole, 1.0f);
+    prod.store(lds, static_cast<T*>(j.out) + (i64)row0 * j.ldo + col0, j.ldo, rows, cols, j.whole, streams(j.ldo, j.depth), 1.0f);
   }
 }
 
@@ -134,7 +134,7 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES) void k_expert_weights(WeightJ
     float* q = j.part + (i64)blockIdx.y * j.off.n_experts * j.n * j.k + o;
     prod.each([&](u32 m, u32 n, f32x4 v) { if ((int)m < ns) store4(q + (i64)m * j.k + n, v, ks - (int)n, j.k % 4 == 0); });
   } else {
-    prod.store(lds, static_cast<T*>(j.out) + o, j.k, ns, ks, j.whole, 1.0f);
+    prod.store(lds, static_cast<T*>(j.out) + o, j.k, ns, ks, j.whole, streams(j.k, depth), 1.0f);
   }
 }
 

@@ -197,6 +197,11 @@ __device__ __forceinline__ void stage_barrier() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(NEWER) : "memory");
 }
 
+// Whether results leave as a stream, which the L2 does not keep: rows that are made of whole lines (1 % of 8192^3, whose operands need the L2).  Where
+// workgroups share lines, these leave whole only from the L2 (64 experts' dw of 1,024 x 2,040 from 2 rows each: 156 us as a stream, 71 so), which
+// matters less than the operands in long contractions (8 experts of 4,000 x 4,000 and 2,000 rows each: 500 and 510 us).
+__device__ __forceinline__ bool streams(i64 ldo, int depth) { return ldo % 64 == 0 || depth > 1024; }
+
 template <class C, class T, bool A_ACROSS, bool B_ACROSS, bool DIRECT>
 struct TileProduct {
   f32x4 acc[C::MI][C::NI];
@@ -327,10 +332,9 @@ struct TileProduct {
 
   // Writes the tile, scaled, to out: rows x cols of it exist.  Sums are rounded once, to nearest even.  A wavefront turns its share
   // round in LDS, so that rows leave in whole cache lines (as the sums lie, a store would touch 16 rows, 32 bytes each); whole:
-  // rows are aligned to 16 bytes.  They are not kept in the L2, which the operands need (1 % of 8192^3).  Follows run().
-  __device__ __forceinline__ void store(unsigned char* lds, T* out, i64 ldo, int rows, int cols, bool whole, float scale) const {
+  // rows are aligned to 16 bytes; stream: they are not kept in the L2 (see streams()).  Follows run().
+  __device__ __forceinline__ void store(unsigned char* lds, T* out, i64 ldo, int rows, int cols, bool whole, bool stream, float scale) const {
     typedef __attribute__((ext_vector_type(4))) T t4;
-    constexpr int PIECES = C::TN / 8;
     const u32 lane = threadIdx.x % CCLD_WAVE;
     unsigned char* own = lds + threadIdx.x / CCLD_WAVE * (C::TM * C::TN * 2);
 #pragma unroll
@@ -342,15 +346,23 @@ struct TileProduct {
         *reinterpret_cast<t4*>(own + m * (C::TN * 2) + (((n / 8) ^ along_key<C::TN>(m)) * 16) + n % 8 * 2) = t4{(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
       }
     __builtin_amdgcn_wave_barrier();
-    const int m0 = (int)wave_m(), n0 = (int)wave_n();
+    if (whole && stream) store_rows<true>(own, out, ldo, rows, cols, true);
+    else store_rows<false>(own, out, ldo, rows, cols, whole);
+  }
+  template <bool STREAM>
+  __device__ __forceinline__ static void store_rows(const unsigned char* own, T* out, i64 ldo, int rows, int cols, bool whole) {
+    constexpr int PIECES = C::TN / 8;
+    const int lane = (int)(threadIdx.x % CCLD_WAVE), m0 = (int)wave_m(), n0 = (int)wave_n();
 #pragma unroll
     for (int i = 0; i < C::TM * PIECES / CCLD_WAVE; ++i) {
-      const int m = i * (CCLD_WAVE / PIECES) + (int)lane / PIECES, p = (int)lane % PIECES, n = n0 + 8 * p;
+      const int m = i * (CCLD_WAVE / PIECES) + lane / PIECES, p = lane % PIECES, n = n0 + 8 * p;
       const s16x8 v = *reinterpret_cast<const s16x8*>(own + m * (C::TN * 2) + ((p ^ along_key<C::TN>(m)) * 16));
       if (m0 + m < rows) {
         T* q = out + (i64)(m0 + m) * ldo + n;
-        if (whole && n + 8 <= cols) __builtin_nontemporal_store(v, reinterpret_cast<s16x8*>(q));
-        else if (n + 8 <= cols) __builtin_memcpy(q, &v, 16);
+        if (whole && n + 8 <= cols) {
+          if constexpr (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<s16x8*>(q));
+          else *reinterpret_cast<s16x8*>(q) = v;
+        } else if (n + 8 <= cols) __builtin_memcpy(q, &v, 16);
         else {
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
