@@ -74,6 +74,12 @@ struct Tiling {
   static_assert(TM % 16 == 0 && TN % 16 == 0, "blocks of 16 x 16");
 };
 
+// Large: the matrix cores' time for a step equals the LDS's (128 KB moved for 256 x 256 x 32), 4 stages ahead, one workgroup to a compute unit: 8192^3 in
+//   bfloat16 at 1,260 to 1,400 TFLOP/s (a library's 1,380).
+// Medium: two workgroups to a compute unit, one computes while the other starts or ends; the LDS bounds it: 1,084 TFLOP/s.
+// Short: three small workgroups, for contractions of up to four steps, which writing the results bounds (products.h).
+// Few: up to 32 rows against a stream of weights, 16 KB of them to a step, which reading the weights bounds (5.5 TB/s at 16 experts of 4,096 x 2,048).
+// Narrow: the same for so few columns that tiles of 128 would leave compute units without work; seven steps of 4 KB ahead.
 using Large = Tiling<256, 256, 2, 4, 32, 5>;
 using Medium = Tiling<128, 128, 2, 4, 32, 5>;
 using Short = Tiling<128, 128, 2, 2, 32, 3>;
@@ -92,6 +98,8 @@ __device__ __forceinline__ u32 across_key(u32 c) {
 // The same for operands that lie along c: reads touch eight rows at once, 16 bytes of each.
 template <int DEPTH>
 __device__ __forceinline__ u32 along_key(u32 row) { return DEPTH == 64 ? row & 7 : (row >> 1) & 3; }
+
+__device__ const unsigned char ZEROS[16] __attribute__((aligned(16))) = {};
 
 // One operand's share of the stages: ROWS of its output index by DEPTH of c.
 // DIRECT loads need 16-byte pieces to be aligned and wholly inside or outside the operand; otherwise they pass through registers, and those
@@ -135,22 +143,34 @@ struct Operand {
       load_to_lds(base, tile + (i * THREADS + wave * CCLD_WAVE) * 16, c < depth ? offset[i] : OUTSIDE);
     } else put(tile, i, load(i, depth));
   }
-  // The same through registers.
+  // The same through registers.  Every lane loads 16 bytes, from ZEROS where its piece is outside, so that the compiler can count the loads that are on
+  // their way.  A piece that reaches over the edge is loaded so that it ends there, and shifted; one at the start of a row's stage or tile,
+  // before which nothing may lie, value by value.
   __device__ __forceinline__ s16x8 load(int i, int depth) const {
     const u32 r = row + i * ROW_STEP;
     const int x = (int)column(i), inside = ACROSS ? ((int)r < depth ? left - x : 0) : ((int)r < left ? depth - x : 0);
-    const unsigned char* p = reinterpret_cast<const unsigned char*>(base) + offset[i];        // (inside the operand where anything is)
-    s16x8 v = {};
-    if (inside >= 8) __builtin_memcpy(&v, p, 16);              // loads need no alignment
-    else if (inside > 0) {
-      u64 part[2] = {0, 0};
-#pragma unroll 1
-      for (int e = 0; e < inside; ++e) {                      // (not unrolled: it is rare, and its registers would be taken from the loop's)
-        const u64 one = (u64)reinterpret_cast<const unsigned short*>(p)[e] << (e % 4 * 16);
-        part[0] |= e < 4 ? one : 0;
-        part[1] |= e < 4 ? 0 : one;
+    const bool over = inside > 0 && inside < 8;
+    const int back = over && x > 0 ? 8 - inside : 0;
+    const unsigned char* p = reinterpret_cast<const unsigned char*>(base) + offset[i];
+    s16x8 v;
+    __builtin_memcpy(&v, inside >= 8 || back ? p - 2 * back : ZEROS, 16);              // loads need no alignment
+    if (ballot64(over)) {
+      u64 part[2];
+      __builtin_memcpy(part, &v, 16);
+      const int bits = 16 * back;
+      if (bits >= 64) {
+        part[0] = part[1] >> (bits - 64);
+        part[1] = 0;
+      } else if (bits) {
+        part[0] = part[0] >> bits | part[1] << (64 - bits);
+        part[1] >>= bits;
       }
       __builtin_memcpy(&v, part, 16);
+      if (over && !back) {
+#pragma unroll
+        for (int e = 0; e < 7; ++e)
+          if (e < inside) v[e] = reinterpret_cast<const short*>(p)[e];
+      }
     }
     return v;
   }
@@ -259,6 +279,11 @@ struct TileProduct {
     // wavefronts wait for one another: the next stage has arrived everywhere, and the place of the stage in registers is free.
     // Stages beyond the last are zeros.
     u32 next = C::STAGE_BYTES, free = PAIRS ? (C::STAGES - 1) * C::STAGE_BYTES : 0;
+    // (through registers: what a step loads is written to LDS when the next one ends, so that it has the time of two)
+    constexpr int EVEN_LOADS = DIRECT ? 1 : PAIRS ? A_TURN : LOADS, ODD_LOADS = DIRECT ? 1 : PAIRS ? B_TURN : LOADS;
+    s16x8 held_even[EVEN_LOADS], held_odd[ODD_LOADS];
+    u32 held_free = 0, held_second = 0;
+    bool held = false;
     constexpr int TURNS = PARTS * C::MI, HOLD = TURNS / 4 < 1 ? 1 : TURNS / 4;
     auto step = [&](const s16x8 (&vb)[PARTS][C::NI], s16x8 (&then)[PARTS][C::NI], auto is_odd) {
       constexpr bool ODD = decltype(is_odd)::value;
@@ -269,25 +294,23 @@ struct TileProduct {
 #pragma unroll
       for (int turn = 0; turn < HOLD; ++turn) multiply(turn);
       __builtin_amdgcn_sched_barrier(0);
-      stage_barrier<!DIRECT ? 0 : !PAIRS ? LOADS * (C::STAGES - 2) : ODD ? A_TURN : A_TURN + B_TURN>();
+      stage_barrier<!DIRECT ? 63 : !PAIRS ? LOADS * (C::STAGES - 2) : ODD ? A_TURN : A_TURN + B_TURN>();
       const unsigned char* s = lds + next;
       // loads of this step: a stage, or both stages of a pair for one operand
       constexpr int FIRST = !PAIRS || !ODD ? A_TURN : 0, ALL = FIRST + (!PAIRS || ODD ? B_TURN : 0);
       const u32 second = after(free);
-      // (through registers: all are loaded at once and written when the step ends)
-      s16x8 held[DIRECT ? 1 : ALL];
       auto load = [&](int i) {
         if (i < FIRST) {
           if (i == A::PIECES) oa.next_stage();
           const int n = i % A::PIECES, left = i < A::PIECES ? left_a : left_a - C::DEPTH;
           if constexpr (DIRECT) oa.fetch(lds + (i < A::PIECES ? free : second), n, left);
-          else held[i] = oa.load(n, left);
+          else (ODD ? held_odd : held_even)[i] = oa.load(n, left);
         } else {
           const int k = i - FIRST;
           if (k == B::PIECES) ob.next_stage();
           const int n = k % B::PIECES, left = k < B::PIECES ? left_b : left_b - C::DEPTH;
           if constexpr (DIRECT) ob.fetch(lds + (k < B::PIECES ? free : second) + A_BYTES, n, left);
-          else held[i] = ob.load(n, left);
+          else (ODD ? held_odd : held_even)[i] = ob.load(n, left);
         }
       };
       if constexpr (!DIRECT) {
@@ -310,13 +333,20 @@ struct TileProduct {
         __builtin_amdgcn_sched_barrier(0);
       }
       if constexpr (!DIRECT) {
+        if (held) {
+          constexpr int A_HELD = !PAIRS || ODD ? A_TURN : 0, OTHERS = ODD ? EVEN_LOADS : ODD_LOADS;      // the other step's loads
 #pragma unroll
-        for (int i = 0; i < ALL; ++i) {
-          const int k = i < FIRST ? i : i - FIRST, pieces = i < FIRST ? A::PIECES : B::PIECES;
-          unsigned char* stage = lds + (k < pieces ? free : second);
-          if (i < FIRST) A::put(stage, k % pieces, held[i]);
-          else B::put(stage + A_BYTES, k % pieces, held[i]);
+          for (int i = 0; i < OTHERS; ++i) {
+            const int k = i < A_HELD ? i : i - A_HELD, pieces = i < A_HELD ? A::PIECES : B::PIECES;
+            unsigned char* stage = lds + (k < pieces ? held_free : held_second);
+            const s16x8 v = (ODD ? held_even : held_odd)[i];
+            if (i < A_HELD) A::put(stage, k % pieces, v);
+            else B::put(stage + A_BYTES, k % pieces, v);
+          }
         }
+        held = true;
+        held_free = free;
+        held_second = second;
       }
       constexpr int MOVED = PAIRS ? 2 * C::DEPTH : C::DEPTH;
       if (!PAIRS || !ODD) { oa.next_stage(); left_a -= MOVED; }
