@@ -423,7 +423,7 @@ enum { CCLD_BF16 = 0, CCLD_FP16 = 1, CCLD_FP32 = 2 };
 typedef struct {
   int32_t dtype;
   int32_t offsets_bits;              /* 32 or 64: signed integers                                       */
-  int64_t rows, k, n, n_experts;     /* rows may be 0; each below 2^31, and k, n < 2^22                 */
+  int64_t rows, k, n, n_experts;     /* rows may be 0, below 2^31; k, n < 2^22, n_experts < 2^20         */
   const void *x;                     /* [rows][k]                                                       */
   const void *w;                     /* [n_experts][n][k], expert_stride elements between experts       */
   const void *offsets;               /* [n_experts + 1]                                                 */
@@ -431,7 +431,7 @@ typedef struct {
   void *y;                           /* [rows][n] out (product call)                                    */
   void *dx;                          /* [rows][k] out, or NULL (grad call)                              */
   void *dw;                          /* [n_experts][n][k] contiguous, out, or NULL (grad call)          */
-  int64_t ldx, ldw, expert_stride, lddy, ldy, lddx;
+  int64_t ldx, ldw, expert_stride, lddy, ldy, lddx;    /* of inputs below 2^22 - 2^14                     */
   void *workspace;                   /* aligned to 256 bytes; may be NULL where the query gives 0       */
   uint64_t workspace_bytes;
 } ccld_expert_args;
@@ -448,7 +448,7 @@ ccld_status ccld_expert_product_grad(const ccld_expert_args *a, void *stream);
 typedef struct {
   int32_t dtype;
   int32_t label_bits;                /* 32 or 64: signed integers                                       */
-  int64_t rows, d, vocab;            /* rows may be 0; below 2^31, d < 2^22                             */
+  int64_t rows, d, vocab;            /* rows may be 0, below 2^31; d and ldw below 2^22 - 2^14         */
   const void *h, *w;
   const void *labels;                /* [rows]                                                          */
   const float *dloss;                /* [rows], dloss_stride elements apart (0: one for all) (grad)     */

@@ -49,11 +49,14 @@ inline Cut choose_cut(uint64_t rows, uint64_t cols, uint64_t depth, bool direct,
   return choose_cut((double)products * parts_of(rows, 256) * parts_of(cols, 256), (double)products * parts_of(rows, 128) * parts_of(cols, 128),
                     parts_of(depth, 32), (double)products * rows * cols, true, direct, most_splits);
 }
-// Gradients of weights, n x k of them from so many rows.  Up to four steps are bound by writing the results: three small workgroups to a compute unit, so
+// Gradients of weights, n x k of them from so many rows.  Few steps are bound by writing the results: three small workgroups to a compute unit, so
 // that some write while others load (64 experts of 1,024 x 2,048: 2 rows each 47 us, 53 in the larger tiles and 58 in those of 128 x 128; 64 rows 57, 65
-// and 72; 128 rows 74, 81 and 89).
+// and 72).  With three or four steps that holds where the results are few (4 experts of 3,000 x 1,000, 100 rows each, a whole step 43 us and 47; 64 of 1,024 x
+// 2,048, 128 rows each, 275 and 265).
 inline Cut choose_weight_cut(uint64_t n, uint64_t k, uint64_t rows, bool direct, uint64_t products = 1) {
-  return direct && rows <= 4 * 32 ? Cut{SHORT, 1} : choose_cut(n, k, rows, direct, 16, products);
+  const uint64_t tiles = products * parts_of(n, 128) * parts_of(k, 128), steps = parts_of(rows, 32);
+  if (direct && (steps <= 2 || (steps <= 4 && tiles <= 12 * COMPUTE_UNITS))) return Cut{SHORT, 1};
+  return choose_cut(n, k, rows, direct, 16, products);
 }
 
 // Where the number of tiles is known on the device only, the parts of their contraction are chosen there (tiles.h).
