@@ -200,12 +200,13 @@ ccld_status check(const ccld_expert_args* a, bool grad) {
     if (a->lddy < a->n || (a->dx && a->lddx < a->k)) return CCLD_E_BAD_ARG;
     if (a->lddy >= MAX_LD) return CCLD_E_CAPACITY;
   } else if (a->ldy < a->n) return CCLD_E_BAD_ARG;
-  // a launch has less than 2^32 threads
-  const bool rows_product = !grad || a->dx;
-  if (rows_product && row_plan(a, grad).groups >= MAX_GROUPS) return CCLD_E_CAPACITY;
+  if (!grad || a->dx) {
+    const RowPlan p = row_plan(a, grad);
+    if (!launches(p.tile, p.groups)) return CCLD_E_CAPACITY;
+  }
   if (grad && a->dw) {
     const WeightPlan p = weight_plan(a);
-    if ((u64)a->n_experts * p.n_tiles * p.k_tiles >= MAX_GROUPS) return CCLD_E_CAPACITY;
+    if (!launches(p.tile, (u64)a->n_experts * p.n_tiles * p.k_tiles)) return CCLD_E_CAPACITY;
   }
   return CCLD_OK;
 }

@@ -9,7 +9,6 @@ namespace ccld {
 
 constexpr int DEPTH = 64;              // contractions are divided in whole multiples of it
 constexpr uint64_t COMPUTE_UNITS = 256;
-constexpr uint64_t MAX_GROUPS = (uint64_t)1 << 22;      // workgroups of up to 1,024 threads in a launch
 constexpr int64_t MAX_ROWS = (int64_t)1 << 31, MAX_EXPERTS = (int64_t)1 << 20, MAX_WIDTH = (int64_t)1 << 22;
 // a tile's last row starts below 2^31 bytes from its first: 256 rows (or DEPTH of them) of this many 16-bit elements, and a row
 constexpr int64_t MAX_LD = ((int64_t)1 << 22) - ((int64_t)1 << 14);
@@ -25,6 +24,8 @@ constexpr int64_t MAX_LD = ((int64_t)1 << 22) - ((int64_t)1 << 14);
 enum Tile { LARGE, MEDIUM, SHORT, FEW, NARROW };
 inline uint32_t tile_m(Tile t) { return t == LARGE ? 256 : t == MEDIUM || t == SHORT ? 128 : 32; }
 inline uint32_t tile_n(Tile t) { return t == LARGE ? 256 : t == NARROW ? 32 : 128; }
+// a launch has less than 2^32 threads
+inline bool launches(Tile t, uint64_t groups) { return groups < ((uint64_t)1 << 32) / (t == LARGE || t == MEDIUM ? 512 : t == NARROW ? 128 : 256); }
 struct Cut { Tile tile; uint32_t splits; };
 inline Cut choose_cut(double tiles_256, double tiles_128, uint64_t steps, double results, bool counted, bool direct, uint32_t most_splits = 16) {
   const struct { Tile tile; double tiles, at_once, start, step; } forms[] = {{MEDIUM, tiles_128, 2 * COMPUTE_UNITS, 6, 0.5},

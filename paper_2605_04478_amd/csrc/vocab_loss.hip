@@ -490,9 +490,12 @@ ccld_status check(const ccld_vocab_args* a, bool grad) {
   if (a->ldh < a->d || a->ldw < a->d) return CCLD_E_BAD_ARG;
   if (a->ldw >= MAX_LD) return CCLD_E_CAPACITY;
   if (grad && (a->dloss_stride < 0 || (a->dh && a->lddh < a->d) || (a->dw && a->lddw < a->d))) return CCLD_E_BAD_ARG;
-  if ((u64)div_up(a->rows, 32) * div_up(a->vocab, 128) >= MAX_GROUPS && (u64)div_up(a->rows, 256) * div_up(a->vocab, 256) >= MAX_GROUPS)
-    return CCLD_E_CAPACITY;
-  if (grad && (u64)div_up(std::max<i64>(a->rows, piece_width(a)), 256) * div_up(a->d, 256) >= MAX_GROUPS) return CCLD_E_CAPACITY;
+  const i64 cols = grad ? piece_width(a) : a->vocab;
+  const bool whole = whole_pieces(a);
+  auto fits = [](Tile t, i64 m, i64 n) { return launches(t, (u64)div_up(m, tile_m(t)) * div_up(n, tile_n(t))); };
+  if (!fits(logit_tiles(a->rows, cols, a->d, whole), a->rows, cols)) return CCLD_E_CAPACITY;
+  if (grad && !fits(choose_tile(a->rows, a->d, cols, whole, MOST_SPLITS), a->rows, a->d)) return CCLD_E_CAPACITY;
+  if (grad && !fits(choose_weight_cut((u64)cols, (u64)a->d, (u64)a->rows, true).tile, cols, a->d)) return CCLD_E_CAPACITY;
   return CCLD_OK;
 }
 
