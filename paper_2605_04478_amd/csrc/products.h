@@ -52,11 +52,13 @@ inline Cut choose_cut(uint64_t rows, uint64_t cols, uint64_t depth, bool direct,
 }
 // Gradients of weights, n x k of them from so many rows.  Few steps are bound by writing the results: three small workgroups to a compute unit, so
 // that some write while others load (64 experts of 1,024 x 2,048: 2 rows each 47 us, 53 in the larger tiles and 58 in those of 128 x 128; 64 rows 57, 65
-// and 72).  With three or four steps that holds where the results are few (4 experts of 3,000 x 1,000, 100 rows each, a whole step 43 us and 47; 64 of 1,024 x
-// 2,048, 128 rows each, 275 and 265).
+// and 72).  With more steps that holds where there are neither many results nor so few that the contraction is better taken in parts, whole steps of experts: 16 of
+// 1,024 x 1,024, 625 rows each (20 steps), 104 us instead of 111; 43 of 224 x 888, 216 rows each, 49 and 53; but 64 of 1,024 x 2,048, 128 rows each, 275 and 265,
+// and 2 of 768 x 512, 400 rows each, 8.7 and 8.1 for dw alone.
 inline Cut choose_weight_cut(uint64_t n, uint64_t k, uint64_t rows, bool direct, uint64_t products = 1) {
   const uint64_t tiles = products * parts_of(n, 128) * parts_of(k, 128), steps = parts_of(rows, 32);
-  if (direct && (steps <= 2 || (steps <= 4 && tiles <= 12 * COMPUTE_UNITS))) return Cut{SHORT, 1};
+  const bool few = steps <= 4 || (steps <= 20 && tiles >= 2 * COMPUTE_UNITS);
+  if (direct && (steps <= 2 || (few && tiles <= 12 * COMPUTE_UNITS))) return Cut{SHORT, 1};
   return choose_cut(n, k, rows, direct, 16, products);
 }
 
