@@ -13,8 +13,8 @@
 //
 // Exponentials are 2^(x log2 e) in 32 bits: for x down to -30 off by 30 roundings of 2^-24 at most, a thousandth of a step of the
 // 16-bit types that gradients leave in.  dz is rounded to the operands' type for the matrix cores, after a scaling by the power of two that
-// brings the largest |g| just under 2^15: half-precision gradients of 10^-9 keep their bits.  (That rounding is what dh and dw have beside their own: a
-// relative error of 0.0024 in bfloat16 where one rounding alone gives 0.0017.)
+// brings the largest |g| just under 2^15: half-precision gradients of 10^-9 keep their bits.  (That rounding is what dh and dw of more than 128 rows have beside
+// their own: a relative error of 0.0024 in bfloat16 where one rounding alone gives 0.0017.)
 //
 // What bounds it: the matrix cores, with the logits taken twice (4 products for the 3 of an implementation that keeps them); for a handful of rows
 // reading the vocabulary's weights, and then its launches.  Measured: 8,192 rows x 4,096 x 128,000 in bfloat16, loss and gradients, 26.5 ms = 1,300
@@ -38,6 +38,7 @@ constexpr int USED_THREADS = 1024;
 // what the kernels share in the workspace
 struct Rows {
   u32* count;          // rows with a target; then the exponent of the scaling of dz
+  u32 parts;           // 16-bit values that make a value of dz: the kept rows of dz and h are there as many times
   i32* row;            // [rows] which they are
   i32* place;          // [rows] a row's place among them, or -1
   i32* label;          // [rows] of the kept rows, as are the following
@@ -53,10 +54,12 @@ __device__ __forceinline__ i64 label_at(const void* p, int bits, i64 i) {
 
 // A kept row's values, padded with zeros to dp columns, V at a time; and, for the gradient, its lse and scaled dloss.
 template <class T, int V>
-__device__ __forceinline__ void gather_piece(const Rows& w, i64 i, i64 at, int c, i64 r, const T* h, i64 ldh, int d, const float* lse, const float* dloss,
+__device__ __forceinline__ void gather_piece(const Rows& w, i64 i, i64 step, i64 at, int c, i64 r, const T* h, i64 ldh, int d, const float* lse, const float* dloss,
                                              i64 dloss_stride, float scale) {
-  if constexpr (V == 8) reinterpret_cast<s16x8*>(w.h)[i] = *reinterpret_cast<const s16x8*>(h + r * ldh + c);
-  else static_cast<T*>(w.h)[i] = c < d ? h[r * ldh + c] : (T)0.0f;
+  for (u32 part = 0; part < w.parts; ++part, i += step) {
+    if constexpr (V == 8) reinterpret_cast<s16x8*>(w.h)[i] = *reinterpret_cast<const s16x8*>(h + r * ldh + c);
+    else static_cast<T*>(w.h)[i] = c < d ? h[r * ldh + c] : (T)0.0f;
+  }
   if (c == 0 && dloss) {
     w.lse[at] = lse[r];
     w.scale[at] = dloss[r * dloss_stride] * scale;
@@ -119,7 +122,7 @@ __global__ __launch_bounds__(USED_THREADS) void k_used_rows(Rows w, const void* 
     const int pieces = dp / V;
     for (i64 i = (i64)blockIdx.x * USED_THREADS + threadIdx.x; i < (i64)before * pieces; i += (i64)gridDim.x * USED_THREADS) {
       const i64 at = i / pieces;
-      gather_piece<T, V>(w, i, at, (int)(i - at * pieces) * V, list[at], h, ldh, d, lse, dloss, dloss_stride, ldexpf(1.0f, scaling));
+      gather_piece<T, V>(w, i, (i64)before * pieces, at, (int)(i - at * pieces) * V, list[at], h, ldh, d, lse, dloss, dloss_stride, ldexpf(1.0f, scaling));
     }
   }
 }
@@ -133,7 +136,7 @@ __global__ __launch_bounds__(256) void k_gather_rows(Rows w, const T* __restrict
   const float scale = ldexpf(1.0f, reinterpret_cast<const i32*>(w.count)[1]);
   for (i64 i = (i64)blockIdx.x * 256 + threadIdx.x; i < n * pieces; i += (i64)gridDim.x * 256) {
     const i64 at = i / pieces;
-    gather_piece<T, V>(w, i, at, (int)(i - at * pieces) * V, w.row[at], h, ldh, d, lse, dloss, dloss_stride, scale);
+    gather_piece<T, V>(w, i, n * pieces, at, (int)(i - at * pieces) * V, w.row[at], h, ldh, d, lse, dloss, dloss_stride, scale);
   }
 }
 
@@ -230,9 +233,10 @@ __global__ __launch_bounds__(256) void k_loss(Rows w, const float2* __restrict__
   for (int x = 1; x < CCLD_WAVE; x *= 2)
     s = join_sums(s, make_float2(__shfl_xor(s.x, x, CCLD_WAVE), __shfl_xor(s.y, x, CCLD_WAVE)));
   if (lane_id() == 0) {
-    const float l = (s.x == -__builtin_inff() ? 0 : s.x) + logf(s.y);
-    lse[w.row[at]] = l;
-    loss[w.row[at]] = l - w.target[at];
+    // (the largest logit and the target's first: where they are one, the loss keeps bits that lse has not)
+    const float top = s.x == -__builtin_inff() ? 0 : s.x, more = logf(s.y);
+    lse[w.row[at]] = top + more;
+    loss[w.row[at]] = (top - w.target[at]) + more;
   }
 }
 
@@ -261,7 +265,18 @@ __global__ __launch_bounds__(C::THREADS) void k_logit_grad(LogitJob j) {
         prod.acc[i][b][r] = (int)n1 + 16 * b + r < cols ? p * scale : 0;      // columns beyond the piece are zeros that products may read
       }
   }
-  prod.store(lds, static_cast<T*>(j.dz) + (i64)m0 * j.lddz + n0, j.lddz, rows, C::BN, true, true, 1.0f);
+  T* dz = static_cast<T*>(j.dz) + (i64)m0 * j.lddz + n0;
+  prod.store(lds, dz, j.lddz, rows, C::BN, true, true, 1.0f);
+  if (j.rows.parts > 1) {              // what that rounding left, exactly
+#pragma unroll
+    for (int i = 0; i < C::MI; ++i)
+#pragma unroll
+      for (int b = 0; b < C::NI; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) prod.acc[i][b][r] -= (float)(T)prod.acc[i][b][r];
+    __builtin_amdgcn_wave_barrier();
+    prod.store(lds, dz + (i64)kept * j.lddz, j.lddz, rows, C::BN, true, true, 1.0f);
+  }
 }
 
 struct InputJob {            // dh: dz [kept][width] times w [width][d]
@@ -282,7 +297,7 @@ __device__ __forceinline__ u32 input_splits(u32 kept, u32 col_tiles, int full_wi
 
 template <class C, class T, bool DIRECT>
 __global__ __launch_bounds__(C::THREADS) void k_input_grad(InputJob j) {
-  const int kept = (int)j.rows.count[0];
+  const int kept = (int)(j.rows.count[0] * j.rows.parts);
   const u32 tm = (u32)(kept + C::BM - 1) / C::BM, tiles = tm * j.col_tiles, splits = input_splits<C>((u32)kept, j.col_tiles, j.full_width);
   if (blockIdx.x >= tiles * splits) return;
   const u32 id = xcd_order(blockIdx.x, tiles * splits), split = id / tiles;
@@ -313,17 +328,17 @@ __global__ __launch_bounds__(C::THREADS) void k_input_grad(InputJob j) {
 // thread where rows allow it.
 template <class C, class T, int V>
 __global__ __launch_bounds__(256) void k_input_rows(Rows w, const float* __restrict__ sum, u32 col_tiles, int full_width, i64 rows, int d, T* dh, i64 lddh) {
-  const i64 kept = w.count[0];
-  const u32 splits = input_splits<C>((u32)kept, col_tiles, full_width);
+  const i64 kept = w.count[0], all = kept * w.parts;
+  const u32 splits = input_splits<C>((u32)all, col_tiles, full_width);
   const float back = ldexpf(1.0f, -reinterpret_cast<const i32*>(w.count)[1]);
   const int pieces = d / V;
   for (i64 i = (i64)blockIdx.x * 256 + threadIdx.x; i < rows * pieces; i += (i64)gridDim.x * 256) {
     const i64 r = i / pieces, c = (i - r * pieces) * V, at = w.place[r];
     typedef float vec __attribute__((ext_vector_type(V)));
     vec v = 0;
-    if (at >= 0) {
-      const float* q = sum + at * d + c;
-      const i64 step = kept * d;
+    for (i64 of = at; of >= 0 && of < all; of += kept) {
+      const float* q = sum + of * d + c;
+      const i64 step = all * d;
       u32 s = 0;
       for (; s + 8 <= splits; s += 8) {              // eight on their way at once: a load after the other took 15 us of 64 parts
         vec x[8];
@@ -356,7 +371,7 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES) void k_weight_grad(WeightJob 
   const u32 id = xcd_order(blockIdx.x, gridDim.x);
   const uint2 t = grouped_order(id, j.n_tiles, j.k_tiles, 8);
   const int n0 = (int)t.x * C::BM, k0 = (int)t.y * C::BN;
-  const int kept = (int)j.rows.count[0];
+  const int kept = (int)(j.rows.count[0] * j.rows.parts);
   const int share = ((kept + (int)gridDim.y - 1) / (int)gridDim.y + C::DEPTH - 1) / C::DEPTH * C::DEPTH;
   const i64 first = (i64)blockIdx.y * share;
   const int depth = (int)max((i64)0, min((i64)share, kept - first));
@@ -392,6 +407,12 @@ __global__ __launch_bounds__(256) void k_weight_rows(Rows w, const float* __rest
 
 i64 div_up(i64 a, i64 b) { return (a + b - 1) / b; }
 i64 round_up(i64 a, i64 b) { return div_up(a, b) * b; }
+
+// Up to 128 rows dz is kept in two 16-bit parts, its rounding and what that left, so that it costs no bits: with few rows one value's rounding
+// can be all that a row of dw is off by (one row in bfloat16: 0.0031 beside 0.0017).  The products of so few rows are bound by the vocabulary's weights: 9 rows
+// x 2,504 x 10,082 take 73 us instead of 70, 57 x 1,432 x 55,406 202 instead of 174.  With many rows the roundings are independent and add what one
+// more of them does, and the products would take half as long again.
+i64 parts_of_dz(const ccld_vocab_args* a) { return a->rows <= 128 ? 2 : 1; }
 
 bool whole_pieces(const ccld_vocab_args* a) { return a->d % 8 == 0 && a->ldw % 8 == 0; }
 
@@ -448,6 +469,8 @@ Plan make_plan(const ccld_vocab_args* a, bool grad, Carver& c) {
   Plan p{};
   const u64 rows = (u64)a->rows;
   p.dp = (int)round_up(a->d, 8);
+  p.rows.parts = grad ? parts_of_dz(a) : 1;
+  const u64 all = rows * p.rows.parts;
   p.rows.count = c.take<u32>(2);
   p.rows.row = c.take<i32>(rows);
   p.rows.place = c.take<i32>(rows);
@@ -455,7 +478,7 @@ Plan make_plan(const ccld_vocab_args* a, bool grad, Carver& c) {
   p.rows.target = c.take<float>(rows);
   p.rows.lse = c.take<float>(rows);
   p.rows.scale = c.take<float>(rows);
-  p.rows.h = c.take<uint16_t>(rows * p.dp);
+  p.rows.h = c.take<uint16_t>(all * p.dp);
   if (!grad) {
     p.logits = logit_tiles(a->rows, a->vocab, a->d, whole_pieces(a));
     p.col_tiles = (u32)div_up(a->vocab, tile_n(p.logits));
@@ -465,16 +488,16 @@ Plan make_plan(const ccld_vocab_args* a, bool grad, Carver& c) {
   p.width = piece_width(a);
   p.logits = logit_tiles(a->rows, p.width, a->d, whole_pieces(a));
   p.col_tiles = (u32)div_up(p.width, tile_n(p.logits));
-  p.dz = c.take<uint16_t>(rows * p.width);
+  p.dz = c.take<uint16_t>(all * p.width);
   if (a->dh) {
     // the parts of the contraction are chosen on the device, by the rows that have a target: pieces are bounded, not parts
-    p.input = choose_tile(a->rows, a->d, p.width, whole_pieces(a), MOST_SPLITS);
-    const u64 tiles = (u64)div_up(a->rows, tile_m(p.input)) * div_up(a->d, tile_n(p.input));
+    p.input = choose_tile((i64)all, a->d, p.width, whole_pieces(a), MOST_SPLITS);
+    const u64 tiles = (u64)div_up((i64)all, tile_m(p.input)) * div_up(a->d, tile_n(p.input));
     p.pieces = (u32)std::max<u64>(tiles, MOST_PIECES);
-    p.sum = c.take<float>(std::max<u64>(rows * a->d, (u64)MOST_PIECES * tile_m(p.input) * tile_n(p.input)));
+    p.sum = c.take<float>(std::max<u64>(all * a->d, (u64)MOST_PIECES * tile_m(p.input) * tile_n(p.input)));
   }
   if (a->dw) {
-    const Cut w = choose_weight_cut((u64)p.width, (u64)a->d, (u64)a->rows, true);
+    const Cut w = choose_weight_cut((u64)p.width, (u64)a->d, all, true);
     p.weight = w.tile;
     p.weight_splits = w.splits;
     if (p.weight_splits > 1) p.weight_part = c.take<float>((u64)p.weight_splits * p.width * a->d);
@@ -494,8 +517,9 @@ ccld_status check(const ccld_vocab_args* a, bool grad) {
   const bool whole = whole_pieces(a);
   auto fits = [](Tile t, i64 m, i64 n) { return launches(t, (u64)div_up(m, tile_m(t)) * div_up(n, tile_n(t))); };
   if (!fits(logit_tiles(a->rows, cols, a->d, whole), a->rows, cols)) return CCLD_E_CAPACITY;
-  if (grad && !fits(choose_tile(a->rows, a->d, cols, whole, MOST_SPLITS), a->rows, a->d)) return CCLD_E_CAPACITY;
-  if (grad && !fits(choose_weight_cut((u64)cols, (u64)a->d, (u64)a->rows, true).tile, cols, a->d)) return CCLD_E_CAPACITY;
+  const i64 all = a->rows * parts_of_dz(a);
+  if (grad && !fits(choose_tile(all, a->d, cols, whole, MOST_SPLITS), all, a->d)) return CCLD_E_CAPACITY;
+  if (grad && !fits(choose_weight_cut((u64)cols, (u64)a->d, (u64)all, true).tile, cols, a->d)) return CCLD_E_CAPACITY;
   return CCLD_OK;
 }
 

@@ -117,6 +117,28 @@ def test_rows_without_a_target(rows):
         assert all(torch.equal(got[k], again[k]) for k in got)
 
 
+@pytest.mark.parametrize("dtype", [BF, FP], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("rows,masked", [(1, 0.0), (5, 0.0), (64, 0.5), (128, 0.2)])
+def test_few_rows_round_once(rows, masked, dtype):
+    """dz of few rows is kept in two parts: the gradients are off by their own rounding, the square of a half step of dz, and sums in 32 bits."""
+    h, w, labels, dloss = _inputs(rows, 72, 700, dtype, masked, seed=rows)
+    got = _run(h.to(DEV), w.to(DEV), labels.to(DEV), dloss.to(DEV))
+    hd, wd, g = h.to(DEV).double(), w.to(DEV).double(), dloss.to(DEV).double()
+    used = (labels >= 0).to(DEV)
+    z = _mm(hd, wd.t())
+    p = torch.exp(z - torch.logsumexp(z, 1)[:, None])
+    dz = p.clone()
+    dz[torch.arange(rows, device=DEV), labels.to(DEV).clamp(min=0)] -= 1
+    scale = (g * used)[:, None]
+    dz *= scale
+    # the logits' sums (80 additions of |h| |w|) and lse move p by their error; the half step of a half step, twice; subnormal parts
+    size = 2 * F32 * 80 * _mm(hd.abs(), wd.abs().t())
+    d_dz = scale * (p * (size + size.amax(1, keepdim=True) + 400 * F32) + 4 * F32) + 2 * HALF_STEP[dtype] ** 2 * dz.abs() + 2.0 ** -38 * float(g.max())
+    for k, want, parts in (("dh", _mm(dz, wd), (d_dz, wd.abs(), dz.abs(), 2 * 716)), ("dw", _mm(dz.t(), hd), (d_dz.t(), hd.abs(), dz.t().abs(), 2 * (rows + 16)))):
+        off, other, there, terms = parts
+        close(got[k], want, rounding(want, dtype) + _mm(off, other) + 2 * F32 * terms * _mm(there, other), k)
+
+
 def test_no_rows():
     from paper_2605_04478_amd import step
     h, w = torch.empty(0, 64, dtype=BF, device=DEV), torch.randn(100, 64, device=DEV).to(BF)
