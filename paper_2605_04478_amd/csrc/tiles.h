@@ -102,8 +102,7 @@ __device__ __forceinline__ u32 along_key(u32 row) { return DEPTH == 64 ? row & 7
 __device__ const unsigned char ZEROS[16] __attribute__((aligned(16))) = {};
 
 // One operand's share of the stages: ROWS of its output index by DEPTH of c.
-// DIRECT loads need 16-byte pieces to be aligned and wholly inside or outside the operand; otherwise they pass through registers, and those
-// that reach over the operand's edge are loaded value by value.
+// DIRECT loads need 16-byte pieces to be aligned and wholly inside or outside the operand; otherwise they pass through registers (load()).
 template <class T, int ROWS, int DEPTH, int THREADS, bool ACROSS, bool DIRECT>
 struct Operand {
   static constexpr int PIECES = ROWS * DEPTH / 8 / THREADS;      // 16-byte pieces per thread and stage
@@ -250,7 +249,7 @@ struct TileProduct {
     Fragments<C::BN, C::NI, C::DEPTH, B_ACROSS> fb;
     fa.start(wave_m());
     fb.start(wave_n());
-    constexpr bool PAIRS = C::DEPTH == 32 && C::STAGES >= 5;
+    constexpr bool PAIRS = C::DEPTH == 32 && C::STAGES >= 5;            // (fewer stages have no two free places)
     constexpr int STAGES_AHEAD = PAIRS ? C::STAGES - 1 : C::STAGES;      // a pair needs two free places
     constexpr int A_TURN = PAIRS ? 2 * A::PIECES : A::PIECES, B_TURN = PAIRS ? 2 * B::PIECES : B::PIECES;
     auto after = [](u32 p) { return p + C::STAGE_BYTES == C::LDS_BYTES ? 0 : p + C::STAGE_BYTES; };
