@@ -284,11 +284,17 @@ struct TileProduct {
     u32 held_free = 0, held_second = 0;
     bool held = false;
     constexpr int TURNS = PARTS * C::MI, HOLD = TURNS / 4 < 1 ? 1 : TURNS / 4;
+    // Tiles of few rows have registers to spare: their sums are held in four, a part of a step each, which are off by a quarter as much.
+    constexpr int CHAINS = C::BM == 32 ? 2 * PARTS : 1;
+    f32x4 chain[CHAINS][C::MI][C::NI] = {};
     auto step = [&](const s16x8 (&vb)[PARTS][C::NI], s16x8 (&then)[PARTS][C::NI], auto is_odd) {
       constexpr bool ODD = decltype(is_odd)::value;
       auto multiply = [&](int turn) {
 #pragma unroll
-        for (int j = 0; j < C::NI; ++j) acc[turn % C::MI][j] = mma(vb[turn / C::MI][j], va[turn / C::MI][turn % C::MI], acc[turn % C::MI][j], T());
+        for (int j = 0; j < C::NI; ++j) {
+          f32x4& sum = CHAINS == 1 ? acc[turn % C::MI][j] : chain[ODD * PARTS + turn / C::MI][turn % C::MI][j];
+          sum = mma(vb[turn / C::MI][j], va[turn / C::MI][turn % C::MI], sum, T());
+        }
       };
 #pragma unroll
       for (int turn = 0; turn < HOLD; ++turn) multiply(turn);
@@ -355,6 +361,13 @@ struct TileProduct {
     for (int done = 0; done < depth; done += 2 * C::DEPTH) {
       step(even, odd, std::false_type());
       step(odd, even, std::true_type());
+    }
+    if constexpr (CHAINS > 1) {
+      static_assert(CHAINS == 4, "pairs of pairs");
+#pragma unroll
+      for (int i = 0; i < C::MI; ++i)
+#pragma unroll
+        for (int j = 0; j < C::NI; ++j) acc[i][j] = (chain[0][i][j] + chain[1][i][j]) + (chain[2][i][j] + chain[3][i][j]);
     }
     stage_barrier<0>();
   }
