@@ -13,8 +13,9 @@
 //
 // Exponentials are 2^(x log2 e) in 32 bits: for x down to -30 off by 30 roundings of 2^-24 at most, a thousandth of a step of the
 // 16-bit types that gradients leave in.  dz is rounded to the operands' type for the matrix cores, after a scaling by the power of two that
-// brings the largest |g| just under 2^15: half-precision gradients of 10^-9 keep their bits.  (That rounding is what dh and dw of more than 128 rows have beside
-// their own: a relative error of 0.0024 in bfloat16 where one rounding alone gives 0.0017.)
+// brings the largest |g| just under 2^15: half-precision gradients of 10^-9 keep their bits.  What the rounding leaves of a row's target, which is most of
+// dz where a model is unsure, is kept for itself and added to both gradients (add_targets, k_input_rows); up to 128 kept rows the whole of dz
+// is kept in two 16-bit parts (dz_parts).
 //
 // What bounds it: the matrix cores, with the logits taken twice (4 products for the 3 of an implementation that keeps them); for a handful of rows
 // reading the vocabulary's weights, and then its launches.  Measured: 8,192 rows x 4,096 x 128,000 in bfloat16, loss and gradients, 26.5 ms = 1,300
@@ -38,15 +39,23 @@ constexpr int USED_THREADS = 1024;
 // what the kernels share in the workspace
 struct Rows {
   u32* count;          // rows with a target; then the exponent of the scaling of dz
-  u32 parts;           // 16-bit values that make a value of dz: the kept rows of dz and h are there as many times
   i32* row;            // [rows] which they are
   i32* place;          // [rows] a row's place among them, or -1
   i32* label;          // [rows] of the kept rows, as are the following
   float* target;       // [rows] z_label
   float* lse;          // [rows] (gradient)
   float* scale;        // [rows] dloss (gradient), scaled
-  void* h;             // [rows][dp]
+  float* rest;         // [rows] what rounding leaves of the target's dz (gradient, where dz has one part)
+  void* h;             // [kept rows][dp], for each part of dz
 };
+
+// Up to 128 kept rows dz is two 16-bit parts, its rounding and what that left, so that it costs no bits: with few rows any one value's rounding
+// can be all that a row of dw is off by (one row in bfloat16: 0.0031 beside 0.0017).  The products of so few rows are bound by the vocabulary's weights: 9 rows
+// x 2,504 x 10,082 take 73 us instead of 70, 57 x 1,432 x 55,406 202 instead of 174.  With more rows the products would take half as long again; there
+// the rest of each row's target alone is kept, one value to a row.  A word's row of dw that is no row's target may still be off by
+// dz's rounding and its own (a half step each), and so may dh of a row that is sure of a wrong word.
+constexpr u32 TWO_PARTS = 128;
+__host__ __device__ __forceinline__ u32 dz_parts(u32 kept) { return kept <= TWO_PARTS ? 2 : 1; }
 
 __device__ __forceinline__ i64 label_at(const void* p, int bits, i64 i) {
   return bits == 64 ? static_cast<const i64*>(p)[i] : (i64)static_cast<const i32*>(p)[i];
@@ -54,9 +63,10 @@ __device__ __forceinline__ i64 label_at(const void* p, int bits, i64 i) {
 
 // A kept row's values, padded with zeros to dp columns, V at a time; and, for the gradient, its lse and scaled dloss.
 template <class T, int V>
-__device__ __forceinline__ void gather_piece(const Rows& w, i64 i, i64 step, i64 at, int c, i64 r, const T* h, i64 ldh, int d, const float* lse, const float* dloss,
-                                             i64 dloss_stride, float scale) {
-  for (u32 part = 0; part < w.parts; ++part, i += step) {
+__device__ __forceinline__ void gather_piece(const Rows& w, i64 i, i64 kept, i64 step, i64 at, int c, i64 r, const T* h, i64 ldh, int d, const float* lse,
+                                             const float* dloss, i64 dloss_stride, float scale) {
+  const u32 parts = dloss ? dz_parts((u32)kept) : 1;
+  for (u32 part = 0; part < parts; ++part, i += step) {
     if constexpr (V == 8) reinterpret_cast<s16x8*>(w.h)[i] = *reinterpret_cast<const s16x8*>(h + r * ldh + c);
     else static_cast<T*>(w.h)[i] = c < d ? h[r * ldh + c] : (T)0.0f;
   }
@@ -122,7 +132,7 @@ __global__ __launch_bounds__(USED_THREADS) void k_used_rows(Rows w, const void* 
     const int pieces = dp / V;
     for (i64 i = (i64)blockIdx.x * USED_THREADS + threadIdx.x; i < (i64)before * pieces; i += (i64)gridDim.x * USED_THREADS) {
       const i64 at = i / pieces;
-      gather_piece<T, V>(w, i, (i64)before * pieces, at, (int)(i - at * pieces) * V, list[at], h, ldh, d, lse, dloss, dloss_stride, ldexpf(1.0f, scaling));
+      gather_piece<T, V>(w, i, before, (i64)before * pieces, at, (int)(i - at * pieces) * V, list[at], h, ldh, d, lse, dloss, dloss_stride, ldexpf(1.0f, scaling));
     }
   }
 }
@@ -136,7 +146,7 @@ __global__ __launch_bounds__(256) void k_gather_rows(Rows w, const T* __restrict
   const float scale = ldexpf(1.0f, reinterpret_cast<const i32*>(w.count)[1]);
   for (i64 i = (i64)blockIdx.x * 256 + threadIdx.x; i < n * pieces; i += (i64)gridDim.x * 256) {
     const i64 at = i / pieces;
-    gather_piece<T, V>(w, i, n * pieces, at, (int)(i - at * pieces) * V, w.row[at], h, ldh, d, lse, dloss, dloss_stride, scale);
+    gather_piece<T, V>(w, i, n, n * pieces, at, (int)(i - at * pieces) * V, w.row[at], h, ldh, d, lse, dloss, dloss_stride, scale);
   }
 }
 
@@ -240,6 +250,13 @@ __global__ __launch_bounds__(256) void k_loss(Rows w, const float2* __restrict__
   }
 }
 
+// what rounding to T leaves of a finite value, exactly
+template <class T>
+__device__ __forceinline__ float rest_of(float v) {
+  const float rest = v - (float)(T)v;
+  return fabsf(rest) < __builtin_inff() ? rest : 0;
+}
+
 template <class C, class T, bool DIRECT>
 __global__ __launch_bounds__(C::THREADS) void k_logit_grad(LogitJob j) {
   int m0, n0;
@@ -249,25 +266,31 @@ __global__ __launch_bounds__(C::THREADS) void k_logit_grad(LogitJob j) {
   TileProduct<C, T, false, false, DIRECT> prod;
   prod.run(lds, static_cast<const T*>(j.rows.h) + (i64)m0 * j.dp, j.dp, rows, static_cast<const T*>(j.w) + (i64)n0 * j.ldw, j.ldw,
            cols, j.d);
-  const u32 lane = lane_id(), n1 = prod.wave_n() + 4 * (lane / 16);
+  const u32 lane = lane_id(), n1 = prod.wave_n() + 4 * (lane / 16), parts = dz_parts((u32)kept);
 #pragma unroll
   for (int i = 0; i < C::MI; ++i) {
     const int m = (int)prod.wave_m() + 16 * i + (int)(lane % 16);
     const bool in = m < rows;
     const float lse = in ? j.rows.lse[m0 + m] : 0, scale = in ? j.rows.scale[m0 + m] : 0;
     const int want = in ? j.rows.label[m0 + m] - j.first - n0 - (int)n1 : -1;
+    float target = 0;
 #pragma unroll
     for (int b = 0; b < C::NI; ++b)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         float p = __builtin_amdgcn_exp2f((prod.acc[i][b][r] - lse) * LOG2E);
-        if (16 * b + r == want) p -= 1;
+        if (16 * b + r == want) {
+          p -= 1;
+          target = p * scale;
+        }
         prod.acc[i][b][r] = (int)n1 + 16 * b + r < cols ? p * scale : 0;      // columns beyond the piece are zeros that products may read
       }
+    const bool mine = want >= 0 && want < 16 * C::NI && want % 16 < 4 && (int)n1 + want < cols;
+    if (mine && parts == 1) j.rows.rest[m0 + m] = rest_of<T>(target);
   }
   T* dz = static_cast<T*>(j.dz) + (i64)m0 * j.lddz + n0;
   prod.store(lds, dz, j.lddz, rows, C::BN, true, true, 1.0f);
-  if (j.rows.parts > 1) {              // what that rounding left, exactly
+  if (parts > 1) {                     // what that rounding left, exactly
 #pragma unroll
     for (int i = 0; i < C::MI; ++i)
 #pragma unroll
@@ -297,7 +320,7 @@ __device__ __forceinline__ u32 input_splits(u32 kept, u32 col_tiles, int full_wi
 
 template <class C, class T, bool DIRECT>
 __global__ __launch_bounds__(C::THREADS) void k_input_grad(InputJob j) {
-  const int kept = (int)(j.rows.count[0] * j.rows.parts);
+  const int kept = (int)(j.rows.count[0] * dz_parts(j.rows.count[0]));
   const u32 tm = (u32)(kept + C::BM - 1) / C::BM, tiles = tm * j.col_tiles, splits = input_splits<C>((u32)kept, j.col_tiles, j.full_width);
   if (blockIdx.x >= tiles * splits) return;
   const u32 id = xcd_order(blockIdx.x, tiles * splits), split = id / tiles;
@@ -324,11 +347,13 @@ __global__ __launch_bounds__(C::THREADS) void k_input_grad(InputJob j) {
   });
 }
 
-// dh leaves: the splits' sums in their order, rows back in their places, zeros for rows without a target.  V neighbouring columns to a
-// thread where rows allow it.
+// dh leaves: the splits' sums in their order, what rounding left of the target's dz, rows back in their places, zeros for rows without a target.  V
+// neighbouring columns to a thread where rows allow it.
 template <class C, class T, int V>
-__global__ __launch_bounds__(256) void k_input_rows(Rows w, const float* __restrict__ sum, u32 col_tiles, int full_width, i64 rows, int d, T* dh, i64 lddh) {
-  const i64 kept = w.count[0], all = kept * w.parts;
+__global__ __launch_bounds__(256) void k_input_rows(Rows w, const float* __restrict__ sum, u32 col_tiles, int full_width, i64 rows, int d,
+                                                    const T* __restrict__ words, i64 ldw, T* dh, i64 lddh) {
+  const u32 parts = dz_parts(w.count[0]);
+  const i64 kept = w.count[0], all = kept * parts;
   const u32 splits = input_splits<C>((u32)all, col_tiles, full_width);
   const float back = ldexpf(1.0f, -reinterpret_cast<const i32*>(w.count)[1]);
   const int pieces = d / V;
@@ -336,6 +361,10 @@ __global__ __launch_bounds__(256) void k_input_rows(Rows w, const float* __restr
     const i64 r = i / pieces, c = (i - r * pieces) * V, at = w.place[r];
     typedef float vec __attribute__((ext_vector_type(V)));
     vec v = 0;
+    const bool has_rest = parts == 1 && at >= 0;
+    const float rest = has_rest ? w.rest[at] : 0;
+    T word[V];                                           // on its way with the sums
+    __builtin_memcpy(word, words + (has_rest ? w.label[at] * ldw : 0) + c, sizeof(word));
     for (i64 of = at; of >= 0 && of < all; of += kept) {
       const float* q = sum + of * d + c;
       const i64 step = all * d;
@@ -349,6 +378,11 @@ __global__ __launch_bounds__(256) void k_input_rows(Rows w, const float* __restr
       }
       for (; s < splits; ++s) v += *reinterpret_cast<const vec*>(q + s * step);
     }
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const float more = rest * (float)word[e];
+      if (fabsf(more) < __builtin_inff()) v[e] += more;      // (beside an infinite product a rest says nothing)
+    }
     if constexpr (V == 4) store4(dh + r * lddh + c, v * back, 4, true);
     else dh[r * lddh + c] = (T)(v[0] * back);
   }
@@ -360,10 +394,135 @@ struct WeightJob {           // dw of a piece: dz^T [width][kept] times h [kept]
   i64 lddz;
   void* dw;                  // first row of the piece
   i64 lddw;
+  int first;                 // word of the piece's first row
   int d, dp, width;
   u32 n_tiles, k_tiles;
   float* part;               // [splits][width][d] or null
   bool whole;                // rows of dw are aligned to 16 bytes
+};
+
+// Adds to a tile's sums what rounding left of the targets' dz: rest times h for every kept row whose word is one of the tile's.  Each wavefront looks
+// through its share of the labels; what all found is the contraction of further steps, whose matrix of dz has one value to a row.
+// Rows are added in an order that their places decide.  The first labels are loaded before the tile's product, and rows while those before them are
+// multiplied: nothing else runs beside the largest tiles, and each load that is waited for costs them a microsecond.  Measured, dw alone: 8,192 rows x
+// 4,096 x 32,000 1,700 us without and 1,720 with; 1,200 rows x 1,536 x 50,021 182 and 195, 207 where half of the rows have one tile's words, 230 where all have.
+template <class C, class T>
+struct Targets {
+  static constexpr int WAVES = C::THREADS / CCLD_WAVE, SHARE = 512, AT_ONCE = WAVES * SHARE;
+  static constexpr int STEPS = C::BM == 256 ? 4 : std::is_same_v<C, Medium> ? 2 : 1, ROWS = 32 * STEPS;      // of a contraction, by the room in LDS
+  static constexpr int TURN = 4 * CCLD_WAVE;           // labels that a wavefront loads at once
+  typedef __attribute__((ext_vector_type(4))) int i32x4;
+  typedef Operand<T, C::BN, ROWS, C::THREADS, true, false> H;
+  struct Place { u32 list[WAVES][SHARE], count[WAVES]; int word[2][ROWS]; short rest[2][ROWS]; };
+  static constexpr int STAGE = C::BN * ROWS * 2;
+  static_assert(AT_ONCE <= 1 << 16 && C::BM <= 1 << 16 && ROWS <= C::THREADS, "a row and a word to an entry");
+  static_assert(2 * STAGE + sizeof(Place) <= C::LDS_BYTES, "room");
+
+  i32x4 first;                                         // of the product's time
+
+  // a lane's labels of a turn, or none (beyond the last are no rows': the workspace goes on behind them)
+  __device__ __forceinline__ static int at_of(int turn) {
+    return (turn * WAVES + (int)__builtin_amdgcn_readfirstlane(threadIdx.x / CCLD_WAVE)) * TURN + 4 * (int)lane_id();
+  }
+  __device__ __forceinline__ static i32x4 labels(const WeightJob& j, i64 base, int turn, int kept) {
+    const i64 at = base + at_of(turn);
+    return at < kept ? *reinterpret_cast<const i32x4*>(j.rows.label + at) : i32x4{-1, -1, -1, -1};
+  }
+  __device__ __forceinline__ void start(const WeightJob& j, int kept) { first = labels(j, 0, 0, kept); }
+
+  template <class P>
+  __device__ __forceinline__ void add(P& prod, const WeightJob& j, int kept, int n0, int ns, int k0) {
+    Place& place = *reinterpret_cast<Place*>(lds + 2 * STAGE);
+    const u32 lane = lane_id(), wave = threadIdx.x / CCLD_WAVE;
+    const T* h = static_cast<const T*>(j.rows.h) + k0;
+    H oh;
+    oh.start(h, j.dp, min(C::BN, j.dp - k0));
+    Fragments<C::BN, C::NI, ROWS, true> fh;
+    fh.start(prod.wave_n());
+    const int from = j.first + n0;
+    for (i64 base = 0; base < kept; base += AT_ONCE) {
+      i32x4 label = base ? labels(j, base, 0, kept) : first;
+      u32 n = 0;
+      for (int turn = 0; turn < SHARE / TURN && base + turn * (WAVES * TURN) < kept; ++turn) {
+        const i32x4 then = labels(j, turn + 1 < SHARE / TURN ? base : kept, turn + 1, kept);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int at = at_of(turn) + e, word = label[e] - from;
+          const bool mine = base + at < kept && word >= 0 && word < ns;
+          const u64 mask = ballot64(mine);
+          if (mine) place.list[wave][n + mbcnt64(mask)] = (u32)at << 16 | (u32)word;
+          n += (u32)__popcll(mask);
+        }
+        label = then;
+      }
+      if (lane == 0) place.count[wave] = n;
+      __syncthreads();
+      u32 found = 0, before[WAVES];
+#pragma unroll
+      for (int i = 0; i < WAVES; ++i) {
+        before[i] = found;
+        found += (u32)__builtin_amdgcn_readfirstlane((int)place.count[i]);
+      }
+      // entry k of all that were found, or none
+      auto entry = [&](u32 k) {
+        u32 at = k;
+#pragma unroll
+        for (int i = 1; i < WAVES; ++i) at = k >= before[i] ? i * SHARE + k - before[i] : at;
+        return k < found ? (&place.list[0][0])[at] : 0xFFFFFFFFu;
+      };
+      s16x8 next[H::PIECES];
+      int next_word = -1;
+      float next_rest = 0;
+      auto fetch = [&](u32 at) {
+#pragma unroll
+        for (int i = 0; i < H::PIECES; ++i) {
+          const u32 e = entry(at + oh.row + i * H::ROW_STEP);
+          const int x = (int)oh.column(i);
+          next[i] = s16x8{0, 0, 0, 0, 0, 0, 0, 0};
+          if (e != 0xFFFFFFFFu && x < oh.left) next[i] = *reinterpret_cast<const s16x8*>(h + (base + (e >> 16)) * j.dp + x);
+        }
+        if (threadIdx.x < ROWS) {
+          const u32 e = entry(at + threadIdx.x);
+          next_word = e != 0xFFFFFFFFu ? (int)(e & 0xFFFF) : -1;
+          next_rest = e != 0xFFFFFFFFu ? j.rows.rest[base + (e >> 16)] : 0;
+        }
+      };
+      if (found) fetch(0);
+      // a place is written again two rounds on, when all have passed the barrier of the round between
+      for (u32 at = 0, turn = 0; at < found; at += ROWS, turn ^= 1) {
+        unsigned char* stage = lds + turn * STAGE;
+#pragma unroll
+        for (int i = 0; i < H::PIECES; ++i) H::put(stage, i, next[i]);
+        if (threadIdx.x < ROWS) {
+          place.word[turn][threadIdx.x] = next_word;
+          place.rest[turn][threadIdx.x] = __builtin_bit_cast(short, (T)next_rest);
+        }
+        __syncthreads();
+        if (at + ROWS < found) fetch(at + ROWS);
+        for (int step = 0; step < STEPS && at + 32 * step < found; ++step) {
+          s16x8 vh[C::NI], rest;
+          int word[8];
+#pragma unroll
+          for (int b = 0; b < C::NI; ++b) vh[b] = fh.read(stage, b, step);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int c = 32 * step + 8 * (int)(lane / 16) + e;
+            word[e] = place.word[turn][c] - (int)(prod.wave_m() + lane % 16);
+            rest[e] = place.rest[turn][c];
+          }
+#pragma unroll
+          for (int i = 0; i < C::MI; ++i) {
+            s16x8 v;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = word[e] == 16 * i ? rest[e] : (short)0;
+#pragma unroll
+            for (int b = 0; b < C::NI; ++b) prod.acc[i][b] = mma(vh[b], v, prod.acc[i][b], T());
+          }
+        }
+      }
+      __syncthreads();               // the lists and places are read
+    }
+  }
 };
 
 template <class C, class T>
@@ -371,16 +530,21 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES) void k_weight_grad(WeightJob 
   const u32 id = xcd_order(blockIdx.x, gridDim.x);
   const uint2 t = grouped_order(id, j.n_tiles, j.k_tiles, 8);
   const int n0 = (int)t.x * C::BM, k0 = (int)t.y * C::BN;
-  const int kept = (int)(j.rows.count[0] * j.rows.parts);
+  const u32 parts = dz_parts(j.rows.count[0]);
+  const int kept = (int)(j.rows.count[0] * parts);
   const int share = ((kept + (int)gridDim.y - 1) / (int)gridDim.y + C::DEPTH - 1) / C::DEPTH * C::DEPTH;
   const i64 first = (i64)blockIdx.y * share;
   const int depth = (int)max((i64)0, min((i64)share, kept - first));
   const i64 at = depth ? first : 0;
   // dz has whole tiles of columns, h rows padded to 16 bytes
   const int ns = min(C::BM, j.width - n0), ks = min(C::BN, j.d - k0);
+  const bool has_targets = parts == 1 && blockIdx.y == 0;
+  Targets<C, T> targets;
+  if (has_targets) targets.start(j, kept);
   TileProduct<C, T, true, true, true> prod;
   prod.run(lds, static_cast<const T*>(j.dz) + at * j.lddz + n0, j.lddz, C::BM, static_cast<const T*>(j.rows.h) + at * j.dp + k0, j.dp,
            min(C::BN, j.dp - k0), depth);
+  if (has_targets) targets.add(prod, j, kept, n0, ns, k0);
   if (j.part) {
     float* q = j.part + ((i64)blockIdx.y * j.width + n0) * j.d + k0;
     prod.each([&](u32 m, u32 n, f32x4 v) { if ((int)m < ns) store4(q + (i64)m * j.d + n, v, ks - (int)n, j.d % 4 == 0); });
@@ -408,11 +572,8 @@ __global__ __launch_bounds__(256) void k_weight_rows(Rows w, const float* __rest
 i64 div_up(i64 a, i64 b) { return (a + b - 1) / b; }
 i64 round_up(i64 a, i64 b) { return div_up(a, b) * b; }
 
-// Up to 128 rows dz is kept in two 16-bit parts, its rounding and what that left, so that it costs no bits: with few rows one value's rounding
-// can be all that a row of dw is off by (one row in bfloat16: 0.0031 beside 0.0017).  The products of so few rows are bound by the vocabulary's weights: 9 rows
-// x 2,504 x 10,082 take 73 us instead of 70, 57 x 1,432 x 55,406 202 instead of 174.  With many rows the roundings are independent and add what one
-// more of them does, and the products would take half as long again.
-i64 parts_of_dz(const ccld_vocab_args* a) { return a->rows <= 128 ? 2 : 1; }
+// rows of dz, all parts, at most: how many rows are kept is known on the device
+i64 dz_rows(const ccld_vocab_args* a) { return std::max(a->rows, std::min<i64>(a->rows, TWO_PARTS) * 2); }
 
 bool whole_pieces(const ccld_vocab_args* a) { return a->d % 8 == 0 && a->ldw % 8 == 0; }
 
@@ -469,8 +630,7 @@ Plan make_plan(const ccld_vocab_args* a, bool grad, Carver& c) {
   Plan p{};
   const u64 rows = (u64)a->rows;
   p.dp = (int)round_up(a->d, 8);
-  p.rows.parts = grad ? parts_of_dz(a) : 1;
-  const u64 all = rows * p.rows.parts;
+  const u64 all = grad ? (u64)dz_rows(a) : rows;
   p.rows.count = c.take<u32>(2);
   p.rows.row = c.take<i32>(rows);
   p.rows.place = c.take<i32>(rows);
@@ -478,6 +638,7 @@ Plan make_plan(const ccld_vocab_args* a, bool grad, Carver& c) {
   p.rows.target = c.take<float>(rows);
   p.rows.lse = c.take<float>(rows);
   p.rows.scale = c.take<float>(rows);
+  p.rows.rest = c.take<float>(rows);
   p.rows.h = c.take<uint16_t>(all * p.dp);
   if (!grad) {
     p.logits = logit_tiles(a->rows, a->vocab, a->d, whole_pieces(a));
@@ -517,7 +678,7 @@ ccld_status check(const ccld_vocab_args* a, bool grad) {
   const bool whole = whole_pieces(a);
   auto fits = [](Tile t, i64 m, i64 n) { return launches(t, (u64)div_up(m, tile_m(t)) * div_up(n, tile_n(t))); };
   if (!fits(logit_tiles(a->rows, cols, a->d, whole), a->rows, cols)) return CCLD_E_CAPACITY;
-  const i64 all = a->rows * parts_of_dz(a);
+  const i64 all = dz_rows(a);
   if (grad && !fits(choose_tile(all, a->d, cols, whole, MOST_SPLITS), all, a->d)) return CCLD_E_CAPACITY;
   if (grad && !fits(choose_weight_cut((u64)cols, (u64)a->d, (u64)all, true).tile, cols, a->d)) return CCLD_E_CAPACITY;
   return CCLD_OK;
@@ -585,7 +746,7 @@ void launch_input_rows(const ccld_vocab_args* a, const Plan& p, hipStream_t stre
   const bool wide = d % 4 == 0 && a->lddh % 4 == 0 && aligned(a->dh, 8);
   const auto kernel = wide ? &k_input_rows<C, T, 4> : &k_input_rows<C, T, 1>;
   kernel<<<stream_groups(a->rows * a->d / (wide ? 4 : 1)), 256, 0, stream>>>(p.rows, p.sum, (u32)div_up(d, C::BN), (int)p.width, a->rows, d,
-                                                                            static_cast<T*>(a->dh), a->lddh);
+                                                                            static_cast<const T*>(a->w), a->ldw, static_cast<T*>(a->dh), a->lddh);
 }
 template <class C, class T>
 void launch_weight_grad(const Plan& p, WeightJob j, hipStream_t stream) {
@@ -628,7 +789,7 @@ ccld_status gradient(const ccld_vocab_args* a, const Plan& p, hipStream_t stream
     }
     if (a->dw) {
       T* dw = static_cast<T*>(a->dw) + first * a->lddw;
-      const WeightJob j{p.rows, p.dz, p.width, dw, a->lddw, (int)a->d, p.dp, (int)cols, 0, 0, p.weight_part,
+      const WeightJob j{p.rows, p.dz, p.width, dw, a->lddw, (int)first, (int)a->d, p.dp, (int)cols, 0, 0, p.weight_part,
                         a->lddw % 8 == 0 && aligned(dw, 16)};
       if (p.weight == LARGE) launch_weight_grad<Large, T>(p, j, stream);
       else if (p.weight == MEDIUM) launch_weight_grad<Medium, T>(p, j, stream);
