@@ -1,4 +1,4 @@
-"""What rounding dz to 16 bits may leave of the vocabulary loss's gradients."""
+"""What rounding dz to 16 bits may leave of the vocabulary loss's gradients, and what reaches dh from every piece of a huge vocabulary."""
 import pytest
 import torch
 
@@ -91,3 +91,23 @@ def test_targets_of_many_rows(d, vocab):
     labels[torch.rand(17000, generator=g) < 0.05] = -1
     dloss = 0.25 + torch.rand(17000, generator=g)
     _check_gradients(h, w, labels, dloss, _run(h, w, labels, dloss), vocab + 16)
+
+
+@pytest.mark.parametrize("rows", [24, 40])
+def test_every_piece_of_a_huge_vocabulary_reaches_dh(rows):
+    """5 million words in three pieces, each with words of its own mean: dh without any one piece would be far off.  A product passes the
+    additions of its part's steps of 32 (all of a piece's at most), 32 within a step, 64 parts and 3 pieces."""
+    vocab, d = 5_000_003, 8
+    piece = -(-vocab // 3 // 256) * 256
+    g = torch.Generator().manual_seed(rows)
+    mean = torch.randint(0, 2, (3, d), generator=g).float() * 2 - 1
+    mean = (0.5 + torch.rand(3, d, generator=g)) * mean
+    word = torch.arange(vocab) // piece
+    w = (mean[word.clamp(max=2)] + 0.1 * torch.randn(vocab, d, generator=g)).to(BF)
+    h = (0.05 * torch.randn(rows, d, generator=g)).to(BF)
+    labels = torch.randint(0, vocab, (rows,), generator=g)
+    dloss = 0.25 + torch.rand(rows, generator=g)
+    dz, wd, bounds = _check_gradients(h, w, labels, dloss, _run(h, w, labels, dloss), (1 << 21) // 32 + 32 + 64 + 3)
+    for i in range(3):
+        share = _mm(dz[:, i * piece:(i + 1) * piece], wd[i * piece:(i + 1) * piece])
+        assert (share.abs() > 2 * bounds["dh"]).all(), i
