@@ -42,7 +42,8 @@ double number(PyObject* p) {
 struct Device {
   c10::Device device;
   explicit Device(const Tensor& first) : device(first.device()) { require(device.is_cuda() && device.index() == c10::hip::current_device()); }
-  void has(const Tensor& t) const { require(t.device() == device && !t.is_neg()); }
+  // (a tensor whose memory holds its values: neither lazily negated nor zeros without memory)
+  void has(const Tensor& t) const { require(t.device() == device && !t.is_neg() && !t._is_zerotensor()); }
   // rows of unit stride that do not overlap
   void matrix(const Tensor& t, int64_t rows, int64_t cols, at::ScalarType type) const {
     has(t);

@@ -92,9 +92,20 @@ def _on_gpu(first, *others):
     return device
 
 
+def _plain(t):
+    """The tensor itself where its memory holds its values, else a copy: torch negates lazily (the gradient of an imaginary part
+    is a view with the negative bit), and keeps zeros that have no memory."""
+    return t.clone() if t.is_neg() or t._is_zerotensor() else t
+
+
+def _vector(t):
+    return _plain(t).contiguous()
+
+
 def _rows(t):
     """The tensor itself where its last dimension has unit stride and its rows do not overlap, else a copy that does so
     (expanded and transposed tensors: gradients of broadcast outputs come as the former)."""
+    t = _plain(t)
     if t.is_contiguous():
         return t
     if t.stride(-1) != 1 and t.shape[-1] > 1 or any(st < t.shape[-1] and n > 1 for st, n in zip(t.stride()[:-1], t.shape[:-1])):
@@ -157,7 +168,7 @@ def _expert_inputs(x, w, offsets, *others):
     for t in others:
         _tensor(t, "dy", (x.shape[0], n), (w.dtype,))
     device = _on_gpu(w, x, offsets, *others)
-    return device, _rows(x), _rows(w), offsets.contiguous(), *map(_rows, others)
+    return device, _rows(x), _rows(w), _vector(offsets), *map(_rows, others)
 
 
 def _expert_args(x, w, offsets, dy, y, dx, dw):
@@ -228,7 +239,7 @@ def _vocab_inputs(h, w, labels, *others):
     for name, t in zip(("dloss", "lse"), others):
         _tensor(t, name, (h.shape[0],), (torch.float32,))
     device = _on_gpu(w, h, labels, *others)
-    return device, _rows(h), _rows(w), labels.contiguous()
+    return device, _rows(h), _rows(w), _vector(labels)
 
 
 def _vocab_args(h, w, labels, dloss, loss, lse, dh, dw):
@@ -266,7 +277,7 @@ def vocab_loss_grad(dloss, h, w, labels, lse, need_dh: bool = True, need_dw: boo
     if out is not None:
         return out
     device, h, w, labels = _vocab_inputs(h, w, labels, dloss, lse)
-    lse = lse.contiguous()
+    dloss, lse = _plain(dloss), _vector(lse)
     L = lib()
     with _current(device):
         dh = torch.empty(h.shape, dtype=w.dtype, device=device) if need_dh else None
@@ -316,7 +327,7 @@ def _norm_inputs(h, b, gate, w_post, w_pre, eps, dh_out=None, du=None, *rstd):
     for name, t in zip(("rstd_post", "rstd_pre"), rstd):
         _tensor(t, name, (rows,), (torch.float32,))
     device = _on_gpu(h, b, gate, w_post, w_pre, dh_out, du, *rstd)
-    return device, _rows(h), _rows(b), gate, w_post.contiguous(), w_pre.contiguous()
+    return device, _rows(h), _rows(b), gate, _vector(w_post), _vector(w_pre)
 
 
 def norm_residual(h, b, gate, w_post, w_pre, scale: float = 1.0, eps: float = 1e-6):
@@ -354,7 +365,7 @@ def norm_residual_grad(dh_out, du, h, b, gate, w_post, w_pre, rstd_post, rstd_pr
     device, h, b, gate, w_post, w_pre = _norm_inputs(h, b, gate, w_post, w_pre, 0.0, dh_out, du, rstd_post, rstd_pre)
     rows, d = h.shape
     dh_out, du = (None if t is None else _rows(t) for t in (dh_out, du))
-    rstd_post, rstd_pre = rstd_post.contiguous(), rstd_pre.contiguous()
+    rstd_post, rstd_pre = _vector(rstd_post), _vector(rstd_pre)
     L = lib()
     with _current(device):
         new = lambda *shape: torch.empty(shape, dtype=h.dtype, device=device)
