@@ -13,7 +13,7 @@
 //
 // Exponentials are 2^(x log2 e) in 32 bits: for x down to -30 off by 30 roundings of 2^-24 at most, a thousandth of a step of the
 // 16-bit types that gradients leave in.  dz is rounded to the operands' type for the matrix cores, after a scaling by the power of two that
-// brings the largest |g| just under 2^15: half-precision gradients of 10^-9 keep their bits.  What the rounding leaves of a row's target, which is most of
+// brings the largest finite |g| just under 2^15: half-precision gradients of 10^-9 keep their bits.  What the rounding leaves of a row's target, which is most of
 // dz where a model is unsure, is kept for itself and added to both gradients (add_targets, k_input_rows); up to 128 kept rows the whole of dz
 // is kept in two 16-bit parts (dz_parts).
 //
@@ -76,7 +76,7 @@ __device__ __forceinline__ void gather_piece(const Rows& w, i64 i, i64 kept, i64
   }
 }
 
-// Which rows have a target, in order; zeros for the loss of the others; the largest |dloss|.  One workgroup: the labels of 8,192
+// Which rows have a target, in order; zeros for the loss of the others; the largest finite |dloss|.  One workgroup: the labels of 8,192
 // rows are 64 KB.  GATHER: there are no more rows than threads, and every workgroup finds them by itself and copies its share of them too
 // (a launch less: 5 us of a handful of rows' 45).
 template <class T, int V, bool GATHER>
@@ -103,7 +103,10 @@ __global__ __launch_bounds__(USED_THREADS) void k_used_rows(Rows w, const void* 
     }
     __syncthreads();
     at += mbcnt64(mask);
-    if (used && dloss) top = fmaxf(top, fabsf(dloss[r * dloss_stride]));
+    if (used && dloss) {
+      const float size = fabsf(dloss[r * dloss_stride]);
+      if (size < __builtin_inff()) top = fmaxf(top, size);      // (an infinite row's dz is infinite at any scale)
+    }
     if (GATHER && used) list[at] = (i32)r;
     if (writes && r < rows) {
       if (used) {
@@ -121,9 +124,9 @@ __global__ __launch_bounds__(USED_THREADS) void k_used_rows(Rows w, const void* 
   __syncthreads();
   for (u32 i = 0; i < USED_THREADS / CCLD_WAVE; ++i) top = fmaxf(top, tops[i]);
   int e = 0;
-  if (top > 0 && top < __builtin_inff()) (void)frexpf(top, &e);
+  if (top > 0) (void)frexpf(top, &e);
   // top 2^(15 - e) lies in [2^14, 2^15); the scale and its inverse stay within 32-bit floats
-  const int scaling = top > 0 && top < __builtin_inff() ? min(15 - e, 120) : 0;
+  const int scaling = top > 0 ? min(15 - e, 120) : 0;
   if (writes && threadIdx.x == 0) {
     w.count[0] = before;
     reinterpret_cast<i32*>(w.count)[1] = scaling;
@@ -250,7 +253,7 @@ __global__ __launch_bounds__(256) void k_loss(Rows w, const float2* __restrict__
   }
 }
 
-// what rounding to T leaves of a finite value, exactly
+// what rounding to T leaves of a value, exactly; nothing of an infinite one (infinity less itself would make the products NaN)
 template <class T>
 __device__ __forceinline__ float rest_of(float v) {
   const float rest = v - (float)(T)v;
@@ -296,7 +299,7 @@ __global__ __launch_bounds__(C::THREADS) void k_logit_grad(LogitJob j) {
 #pragma unroll
       for (int b = 0; b < C::NI; ++b)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) prod.acc[i][b][r] -= (float)(T)prod.acc[i][b][r];
+        for (int r = 0; r < 4; ++r) prod.acc[i][b][r] = rest_of<T>(prod.acc[i][b][r]);
     __builtin_amdgcn_wave_barrier();
     prod.store(lds, dz + (i64)kept * j.lddz, j.lddz, rows, C::BN, true, true, 1.0f);
   }

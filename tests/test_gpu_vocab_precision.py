@@ -1,4 +1,5 @@
-"""What rounding dz to 16 bits may leave of the vocabulary loss's gradients, and what reaches dh from every piece of a huge vocabulary."""
+"""What rounding dz to 16 bits may leave of the vocabulary loss's gradients, what reaches dh from every piece of a huge vocabulary, and rows
+whose gradient is infinite."""
 import pytest
 import torch
 
@@ -111,3 +112,24 @@ def test_every_piece_of_a_huge_vocabulary_reaches_dh(rows):
     for i in range(3):
         share = _mm(dz[:, i * piece:(i + 1) * piece], wd[i * piece:(i + 1) * piece])
         assert (share.abs() > 2 * bounds["dh"]).all(), i
+
+
+@pytest.mark.parametrize("dtype", [BF, FP], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("rows", [20, 300])
+def test_an_infinite_gradient_stays_with_its_row(rows, dtype):
+    """A row whose dloss is infinite (a loss scale that overflowed) leaves the other rows' dh as they are without it, and is infinite, not
+    NaN, in dw."""
+    h, w, labels, dloss = _inputs(rows, 64, 400, dtype, _any, seed=rows)
+    h = torch.where(h == 0, torch.ones_like(h), h)
+    for scale in (1.0, 1e-6):
+        g = dloss * scale
+        g[3] = 0
+        clean = _run(h, w, labels, g)
+        for value in (float("inf"), -float("inf")):
+            g[3] = value
+            dh, dw = _run(h, w, labels, g)
+            rest = torch.arange(rows) != 3
+            assert torch.equal(dh[rest.to(DEV)], clean[0][rest.to(DEV)])
+            sign = torch.ones(400, 1)
+            sign[labels[3]] = -1
+            assert torch.equal(dw.cpu(), sign.to(dtype) * h[3:4] * value)
