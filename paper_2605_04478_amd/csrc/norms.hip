@@ -110,6 +110,7 @@ struct NormJob {
   float *rstd_post, *rstd_pre;
   i64 ldh, ldb, ldgate, ldh_out, ldu, lddh_out, lddu, lddh, lddb;
   i64 rows, rows_per_gate;
+  i64 row0;                      // first row of the launch (forward)
   int d;
   float scale, eps;
   // gradient: the rows in chunks that lie within a gate's, and where sums go
@@ -129,6 +130,7 @@ __global__ __launch_bounds__(threads_of<TEAM>()) void k_norm(NormJob j) {
   const int t = threadIdx.x % TEAM;
   i64 row = blockIdx.x;
   if (threads_of<TEAM>() > TEAM) row = row * (threads_of<TEAM>() / TEAM) + __builtin_amdgcn_readfirstlane(threadIdx.x / TEAM);
+  row += j.row0;
   if (row >= j.rows) return;                       // whole teams
   Piece<T> pb[PIECES], ph[PIECES];
 #pragma unroll
@@ -436,11 +438,11 @@ NormJob make_job(const ccld_norm_args* a) {
 }
 
 template <class T, int TEAM, int PIECES>
-void launch_forward(const NormJob& j, bool w, hipStream_t stream) {
-  constexpr int THREADS = threads_of<TEAM>(), VEC = 16 / sizeof(T);
-  const u32 grid = (u32)div_up(j.rows, THREADS / TEAM);
+void launch_forward(NormJob j, bool w, hipStream_t stream) {
+  constexpr int THREADS = threads_of<TEAM>(), VEC = 16 / sizeof(T), PER_GROUP = THREADS / TEAM;
   const auto kernel = w ? &k_norm<T, TEAM, PIECES, VEC> : &k_norm<T, TEAM, PIECES, 1>;
-  kernel<<<grid, THREADS, 0, stream>>>(j);
+  for (; j.row0 < j.rows; j.row0 += most_groups(THREADS) * PER_GROUP)
+    kernel<<<(u32)std::min(div_up(j.rows - j.row0, PER_GROUP), most_groups(THREADS)), THREADS, 0, stream>>>(j);
 }
 // a wavefront to a row of up to 1,024 columns, a workgroup beyond
 template <class T>

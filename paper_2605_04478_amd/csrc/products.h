@@ -25,7 +25,8 @@ enum Tile { LARGE, MEDIUM, SHORT, FEW, NARROW };
 inline uint32_t tile_m(Tile t) { return t == LARGE ? 256 : t == MEDIUM || t == SHORT ? 128 : 32; }
 inline uint32_t tile_n(Tile t) { return t == LARGE ? 256 : t == NARROW ? 32 : 128; }
 // a launch has less than 2^32 threads
-inline bool launches(Tile t, uint64_t groups) { return groups < ((uint64_t)1 << 32) / (t == LARGE || t == MEDIUM ? 512 : t == NARROW ? 128 : 256); }
+inline int64_t most_groups(int threads) { return ((int64_t)1 << 32) / threads - 1; }
+inline bool launches(Tile t, uint64_t groups) { return groups <= (uint64_t)most_groups(t == LARGE || t == MEDIUM ? 512 : t == NARROW ? 128 : 256); }
 struct Cut { Tile tile; uint32_t splits; };
 inline Cut choose_cut(double tiles_256, double tiles_128, uint64_t steps, double results, bool counted, bool direct, uint32_t most_splits = 16) {
   const struct { Tile tile; double tiles, at_once, start, step; } forms[] = {{MEDIUM, tiles_128, 2 * COMPUTE_UNITS, 6, 0.5},

@@ -235,10 +235,10 @@ __global__ __launch_bounds__(C::THREADS) void k_logit_sums(LogitJob j) {
   }
 }
 
-// a wavefront to a row: its tiles' sums
-__global__ __launch_bounds__(256) void k_loss(Rows w, const float2* __restrict__ part, u32 col_tiles, float* loss, float* lse) {
+// a wavefront to a row, from the kept row `first` on: its tiles' sums
+__global__ __launch_bounds__(256) void k_loss(Rows w, i64 first, const float2* __restrict__ part, u32 col_tiles, float* loss, float* lse) {
   const i64 n = w.count[0];
-  const i64 at = (i64)blockIdx.x * 4 + threadIdx.x / CCLD_WAVE;
+  const i64 at = first + (i64)blockIdx.x * 4 + threadIdx.x / CCLD_WAVE;
   if (at >= n) return;
   float2 s = make_float2(-__builtin_inff(), 0);
   for (u32 i = lane_id(); i < col_tiles; i += CCLD_WAVE) s = join_sums(s, part[at * col_tiles + i]);
@@ -767,7 +767,8 @@ ccld_status loss(const ccld_vocab_args* a, const Plan& p, hipStream_t stream) {
   else if (p.logits == MEDIUM) launch_logit_sums<Medium, T>(a, j, stream);
   else if (p.logits == FEW) launch_logit_sums<Few, T>(a, j, stream);
   else launch_logit_sums<Narrow, T>(a, j, stream);
-  k_loss<<<(u32)div_up(a->rows, 4), 256, 0, stream>>>(p.rows, p.part, p.col_tiles, a->loss, a->lse);
+  for (i64 first = 0; first < a->rows; first += 4 * most_groups(256))
+    k_loss<<<(u32)std::min(div_up(a->rows - first, 4), most_groups(256)), 256, 0, stream>>>(p.rows, first, p.part, p.col_tiles, a->loss, a->lse);
   return launched();
 }
 
