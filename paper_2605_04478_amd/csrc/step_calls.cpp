@@ -3,7 +3,8 @@
 // A small operator is bound by the host: checks, outputs and arguments of a norm take 15 us in Python and 3 here, its kernel 3.  These
 // functions have the arguments of their namesakes in step.py, which describes them.  They return what those return, or None where anything is out
 // of the ordinary (a tensor of another shape, type, device or layout, a refusal of the library's): nothing has been enqueued then,
-// and step.py, which knows how to lay tensors out and what to say of wrong ones, makes the call.
+// and step.py, which knows how to lay tensors out and what to say of wrong ones, makes the call.  A failure of the device's raises what step.py
+// raises: work may have been enqueued.
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <ATen/ops/empty.h>
@@ -18,6 +19,13 @@ using at::Tensor;
 
 struct Declined {};
 void require(bool ok) { if (!ok) throw Declined(); }
+
+struct Failed { ccld_status status; const char* call; };
+// the library refuses before it enqueues anything, in every way but this one
+void made(ccld_status s, const char* call) {
+  if (s == CCLD_E_HIP) throw Failed{s, call};
+  require(s == CCLD_OK);
+}
 
 // the arguments of a call; tensors are borrowed
 const Tensor& tensor(PyObject* p) {
@@ -83,7 +91,7 @@ struct WithoutInterpreter {
 
 // Makes the call with a workspace of the size that the query names; torch's allocator keeps its memory for the stream's later work.
 template <class A, class Query, class Call>
-void run(A& a, const Device& d, Query query, Call call) {
+void run(A& a, const Device& d, Query query, Call call, const char* name) {
   uint64_t need = 0;
   require(query(&a, &need) == CCLD_OK);
   Tensor ws;
@@ -92,7 +100,7 @@ void run(A& a, const Device& d, Query query, Call call) {
     a.workspace = ws.data_ptr();
     a.workspace_bytes = need;
   }
-  require(call(&a, d.stream()) == CCLD_OK);
+  made(call(&a, d.stream()), name);
 }
 
 PyObject* wrap(const Tensor& t) {
@@ -137,7 +145,7 @@ PyObject* expert_product(PyObject* const* args) {
     WithoutInterpreter free;
     y = d.empty({a.rows, a.n}, w.scalar_type());
     a.y = out(y);
-    run(a, d, [](auto* p, uint64_t* need) { return ccld_expert_workspace(p, 0, need); }, ccld_expert_product);
+    run(a, d, [](auto* p, uint64_t* need) { return ccld_expert_workspace(p, 0, need); }, ccld_expert_product, "ccld_expert_product");
   }
   return wrap(y);
 }
@@ -156,7 +164,7 @@ PyObject* expert_product_grad(PyObject* const* args) {
     if (need_dx) dx = d.empty({a.rows, a.k}, w.scalar_type());
     if (need_dw) dw = d.empty(w.sizes(), w.scalar_type());
     a.dx = out(dx); a.dw = out(dw);
-    run(a, d, [](auto* p, uint64_t* need) { return ccld_expert_workspace(p, 1, need); }, ccld_expert_product_grad);
+    run(a, d, [](auto* p, uint64_t* need) { return ccld_expert_workspace(p, 1, need); }, ccld_expert_product_grad, "ccld_expert_product_grad");
   }
   return tuple(dx, dw);
 }
@@ -190,7 +198,7 @@ PyObject* vocab_loss(PyObject* const* args) {
     lse = d.empty({a.rows}, at::kFloat);
     a.loss = static_cast<float*>(out(loss));
     a.lse = static_cast<float*>(out(lse));
-    run(a, d, [](auto* p, uint64_t* need) { return ccld_vocab_workspace(p, 0, need); }, ccld_vocab_loss);
+    run(a, d, [](auto* p, uint64_t* need) { return ccld_vocab_workspace(p, 0, need); }, ccld_vocab_loss, "ccld_vocab_loss");
   }
   return tuple(loss, lse);
 }
@@ -212,7 +220,7 @@ PyObject* vocab_loss_grad(PyObject* const* args) {
     if (need_dh) dh = d.empty({a.rows, a.d}, w.scalar_type());
     if (need_dw) dw = d.empty({a.vocab, a.d}, w.scalar_type());
     a.dh = out(dh); a.dw = out(dw);
-    run(a, d, [](auto* p, uint64_t* need) { return ccld_vocab_workspace(p, 1, need); }, ccld_vocab_loss_grad);
+    run(a, d, [](auto* p, uint64_t* need) { return ccld_vocab_workspace(p, 1, need); }, ccld_vocab_loss_grad, "ccld_vocab_loss_grad");
   }
   return tuple(dh, dw);
 }
@@ -262,7 +270,7 @@ PyObject* norm_residual(PyObject* const* args) {
     a.h_out = out(h_out); a.u = out(u);
     a.rstd_post = static_cast<float*>(out(rstd_post));
     a.rstd_pre = static_cast<float*>(out(rstd_pre));
-    require(ccld_norm_residual(&a, d.stream()) == CCLD_OK);
+    made(ccld_norm_residual(&a, d.stream()), "ccld_norm_residual");
   }
   return tuple(h_out, u, rstd_post, rstd_pre);
 }
@@ -296,9 +304,21 @@ PyObject* norm_residual_grad(PyObject* const* args) {
     dw_post = d.empty({a.d}, type);
     dw_pre = d.empty({a.d}, type);
     a.dh = out(dh); a.db = out(db); a.dgate = out(dgate); a.dw_post = out(dw_post); a.dw_pre = out(dw_pre);
-    run(a, d, ccld_norm_workspace, ccld_norm_residual_grad);
+    run(a, d, ccld_norm_workspace, ccld_norm_residual_grad, "ccld_norm_residual_grad");
   }
   return tuple(dh, db, dgate, dw_post, dw_pre);
+}
+
+// raises CcldError
+PyObject* raise(const Failed& f) {
+  PyObject* module = PyImport_ImportModule("paper_2605_04478_amd.ccld");
+  PyObject* type = module ? PyObject_GetAttrString(module, "CcldError") : nullptr;
+  PyObject* error = type ? PyObject_CallFunction(type, "is", (int)f.status, f.call) : nullptr;
+  if (error) PyErr_SetObject(type, error);
+  Py_XDECREF(error);
+  Py_XDECREF(type);
+  Py_XDECREF(module);
+  return nullptr;
 }
 
 // ---- the module ------------------------------------------------------------------------------------------------------
@@ -310,6 +330,8 @@ PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t n) {
     return F(args);
   } catch (const Declined&) {
     Py_RETURN_NONE;
+  } catch (const Failed& f) {
+    return raise(f);
   }
   END_HANDLE_TH_ERRORS
 }
