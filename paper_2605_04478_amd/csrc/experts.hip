@@ -177,17 +177,19 @@ WeightPlan plan_weights(u64 rows, u64 experts, int n, int k, bool whole) {
   return WeightPlan{c.tile, (u32)div_up(n, tile_m(c.tile)), (u32)div_up(k, tile_n(c.tile)), c.splits};
 }
 
-// Pieces of 16 bytes lie wholly inside or outside the operands: x, dy, the weights (plans go by sizes and strides alone, so that the workspace does not
-// depend on addresses), and start on 16 bytes.
+// Pieces of 16 bytes lie wholly inside or outside the operands: x, dy, the weights.  Where they also start on 16 bytes they are loaded to LDS directly, else
+// through registers, which the largest and the short tiles have none to spare for: tiles go by addresses too.  The workspace does not: it
+// serves both.
 bool whole_pieces(const ccld_expert_args* a, i64 ld) { return a->k % 8 == 0 && a->n % 8 == 0 && a->ldw % 8 == 0 && a->expert_stride % 8 == 0 && ld % 8 == 0; }
-bool direct(const ccld_expert_args* a, const void* rows_at, i64 ld) { return whole_pieces(a, ld) && aligned(a->w, 16) && aligned(rows_at, 16); }
+bool rows_whole(const ccld_expert_args* a, bool grad) { return whole_pieces(a, grad ? a->lddy : a->ldx); }
+bool rows_direct(const ccld_expert_args* a, bool grad) { return rows_whole(a, grad) && aligned(a->w, 16) && aligned(grad ? a->dy : a->x, 16); }
+bool weights_whole(const ccld_expert_args* a) { return a->n % 8 == 0 && a->k % 8 == 0 && a->lddy % 8 == 0 && a->ldx % 8 == 0; }
+bool weights_direct(const ccld_expert_args* a) { return weights_whole(a) && aligned(a->dy, 16) && aligned(a->x, 16); }
 
-RowPlan row_plan(const ccld_expert_args* a, bool grad) {
-  return plan_rows((u64)a->rows, (u64)a->n_experts, (int)(grad ? a->k : a->n), (int)(grad ? a->n : a->k), whole_pieces(a, grad ? a->lddy : a->ldx));
+RowPlan row_plan(const ccld_expert_args* a, bool grad, bool direct) {
+  return plan_rows((u64)a->rows, (u64)a->n_experts, (int)(grad ? a->k : a->n), (int)(grad ? a->n : a->k), direct);
 }
-WeightPlan weight_plan(const ccld_expert_args* a) {
-  return plan_weights((u64)a->rows, (u64)a->n_experts, (int)a->n, (int)a->k, a->n % 8 == 0 && a->k % 8 == 0 && a->lddy % 8 == 0 && a->ldx % 8 == 0);
-}
+WeightPlan weight_plan(const ccld_expert_args* a, bool direct) { return plan_weights((u64)a->rows, (u64)a->n_experts, (int)a->n, (int)a->k, direct); }
 
 ccld_status check(const ccld_expert_args* a, bool grad) {
   if (!a) return CCLD_E_NULL;
@@ -200,13 +202,11 @@ ccld_status check(const ccld_expert_args* a, bool grad) {
     if (a->lddy < a->n || (a->dx && a->lddx < a->k)) return CCLD_E_BAD_ARG;
     if (a->lddy >= MAX_LD) return CCLD_E_CAPACITY;
   } else if (a->ldy < a->n) return CCLD_E_BAD_ARG;
-  if (!grad || a->dx) {
-    const RowPlan p = row_plan(a, grad);
-    if (!launches(p.tile, p.groups)) return CCLD_E_CAPACITY;
-  }
-  if (grad && a->dw) {
-    const WeightPlan p = weight_plan(a);
-    if (!launches(p.tile, (u64)a->n_experts * p.n_tiles * p.k_tiles)) return CCLD_E_CAPACITY;
+  for (bool direct : {false, true}) {
+    const RowPlan p = row_plan(a, grad, direct);
+    if ((!grad || a->dx) && !launches(p.tile, p.groups)) return CCLD_E_CAPACITY;
+    const WeightPlan w = weight_plan(a, direct);
+    if (grad && a->dw && !launches(w.tile, (u64)a->n_experts * w.n_tiles * w.k_tiles)) return CCLD_E_CAPACITY;
   }
   return CCLD_OK;
 }
@@ -233,15 +233,17 @@ void launch_rows(const RowJob& j, const RowPlan& p, hipStream_t stream) {
 }
 template <class T, bool W_ACROSS, bool DIRECT>
 void launch_rows(const RowJob& j, const RowPlan& p, hipStream_t stream) {
-  if (p.tile == LARGE) launch_rows<Large, T, W_ACROSS, DIRECT>(j, p, stream);
-  else if (p.tile == MEDIUM) launch_rows<Medium, T, W_ACROSS, DIRECT>(j, p, stream);
+  if constexpr (DIRECT)
+    if (p.tile == LARGE) return launch_rows<Large, T, W_ACROSS, true>(j, p, stream);
+  if (p.tile == MEDIUM) launch_rows<Medium, T, W_ACROSS, DIRECT>(j, p, stream);
   else launch_rows<Few, T, W_ACROSS, DIRECT>(j, p, stream);
 }
 
 template <class T>
 ccld_status product_of_rows(const ccld_expert_args* a, bool grad, hipStream_t stream) {
   const int cols = (int)(grad ? a->k : a->n), depth = (int)(grad ? a->n : a->k);
-  const RowPlan p = row_plan(a, grad);
+  const bool d = rows_direct(a, grad);
+  const RowPlan p = row_plan(a, grad, d);
   RowJob j{};
   j.a = grad ? a->dy : a->x;
   j.lda = grad ? a->lddy : a->ldx;
@@ -253,23 +255,21 @@ ccld_status product_of_rows(const ccld_expert_args* a, bool grad, hipStream_t st
   j.ldw = a->ldw; j.estride = a->expert_stride;
   j.cols = cols; j.depth = depth; j.split_depth = p.split_depth; j.col_tiles = p.col_tiles;
   j.whole = j.ldo % 8 == 0 && aligned(j.out, 16);
-  const bool d = direct(a, j.a, j.lda);
   if (grad) d ? launch_rows<T, true, true>(j, p, stream) : launch_rows<T, true, false>(j, p, stream);
   else d ? launch_rows<T, false, true>(j, p, stream) : launch_rows<T, false, false>(j, p, stream);
   if (j.part) launch_join(j.part, p.splits, (u64)a->rows, (u64)cols, j.out, j.ldo, a->dtype, stream);
   return launched();
 }
 
-template <class C, class T>
-void launch_weights(const WeightJob& j, const WeightPlan& p, bool d, hipStream_t stream) {
-  const dim3 grid(j.off.n_experts * p.n_tiles * p.k_tiles, p.splits);
-  if (d) k_expert_weights<C, T, true><<<grid, C::THREADS, C::LDS_BYTES, stream>>>(j);
-  else k_expert_weights<C, T, false><<<grid, C::THREADS, C::LDS_BYTES, stream>>>(j);
+template <class C, class T, bool DIRECT>
+void launch_weights(const WeightJob& j, const WeightPlan& p, hipStream_t stream) {
+  k_expert_weights<C, T, DIRECT><<<dim3(j.off.n_experts * p.n_tiles * p.k_tiles, p.splits), C::THREADS, C::LDS_BYTES, stream>>>(j);
 }
 
 template <class T>
 ccld_status product_of_weights(const ccld_expert_args* a, hipStream_t stream) {
-  const WeightPlan p = weight_plan(a);
+  const bool d = weights_direct(a);
+  const WeightPlan p = weight_plan(a, d);
   WeightJob j{};
   j.dy = a->dy; j.x = a->x; j.out = a->dw;
   j.part = p.splits > 1 ? static_cast<float*>(a->workspace) : nullptr;
@@ -277,10 +277,10 @@ ccld_status product_of_weights(const ccld_expert_args* a, hipStream_t stream) {
   j.lddy = a->lddy; j.ldx = a->ldx; j.n = (int)a->n; j.k = (int)a->k;
   j.n_tiles = p.n_tiles; j.k_tiles = p.k_tiles;
   j.whole = a->k % 8 == 0 && aligned(a->dw, 16);
-  const bool d = a->n % 8 == 0 && a->k % 8 == 0 && a->lddy % 8 == 0 && a->ldx % 8 == 0 && aligned(a->dy, 16) && aligned(a->x, 16);
-  if (p.tile == LARGE) launch_weights<Large, T>(j, p, d, stream);
-  else if (p.tile == MEDIUM) launch_weights<Medium, T>(j, p, d, stream);
-  else launch_weights<Short, T>(j, p, d, stream);
+  if (!d) launch_weights<Medium, T, false>(j, p, stream);
+  else if (p.tile == LARGE) launch_weights<Large, T, true>(j, p, stream);
+  else if (p.tile == MEDIUM) launch_weights<Medium, T, true>(j, p, stream);
+  else launch_weights<Short, T, true>(j, p, stream);
   if (j.part) launch_join(j.part, p.splits, (u64)a->n_experts * a->n, (u64)a->k, j.out, a->k, a->dtype, stream);
   return launched();
 }
@@ -291,14 +291,14 @@ hipError_t allow_tiling() {
   auto allow = [&](auto k) { if (e == hipSuccess) e = allow_lds(reinterpret_cast<const void*>(k), C::LDS_BYTES); };
   if constexpr (!std::is_same_v<C, Short>) {
     allow(&k_expert_rows<C, T, false, true>);
-    allow(&k_expert_rows<C, T, false, false>);
     allow(&k_expert_rows<C, T, true, true>);
+  }
+  if constexpr (std::is_same_v<C, Medium> || std::is_same_v<C, Few>) {
+    allow(&k_expert_rows<C, T, false, false>);
     allow(&k_expert_rows<C, T, true, false>);
   }
-  if constexpr (C::BM > 32) {
-    allow(&k_expert_weights<C, T, true>);
-    allow(&k_expert_weights<C, T, false>);
-  }
+  if constexpr (C::BM > 32) allow(&k_expert_weights<C, T, true>);
+  if constexpr (std::is_same_v<C, Medium>) allow(&k_expert_weights<C, T, false>);
   return e;
 }
 
@@ -319,10 +319,12 @@ extern "C" ccld_status ccld_expert_workspace(const ccld_expert_args* a, int32_t 
   const ccld_status s = check(a, grad != 0);
   if (s != CCLD_OK) return s;
   u64 need = 0;
-  if (!grad || a->dx)
-    need = row_part_bytes(row_plan(a, grad), a->rows, grad ? a->k : a->n);
-  if (grad && a->dw)     // the two gradients follow one another: one workspace serves both
-    need = std::max(need, weight_part_bytes(weight_plan(a), a->n_experts, a->n, a->k));
+  auto rows = [&](bool direct) { need = std::max(need, row_part_bytes(row_plan(a, grad, direct), a->rows, grad ? a->k : a->n)); };
+  auto weights = [&](bool direct) { need = std::max(need, weight_part_bytes(weight_plan(a, direct), a->n_experts, a->n, a->k)); };
+  if (!grad || a->dx) rows(false);
+  if ((!grad || a->dx) && rows_whole(a, grad)) rows(true);
+  if (grad && a->dw) weights(false);                       // the two gradients follow one another: one workspace serves both
+  if (grad && a->dw && weights_whole(a)) weights(true);
   *bytes = (need + 255) & ~(u64)255;
   return CCLD_OK;
 }

@@ -19,8 +19,8 @@ constexpr int64_t MAX_LD = ((int64_t)1 << 22) - ((int64_t)1 << 14);
 // TFLOP/s) and 0.5 us in the latter (1,084), a tile's start and end 10 and 6 us, and sums of parts move at 4.5 TB/s.  The smaller tiles win
 // where the larger ones would leave compute units idle: the weights of 12 experts, 1,000 x 1,336 each, are 288 tiles of 256 (48 us) or 1,056 of
 // 128 (38 us).  (Tiles of 256 x 128, two to a compute unit, were between the two in every case but one, by less than a tenth.)  Operands that pass through
-// registers need too many of them beside the sums of 256 x 256: 43 experts' dx, 598 x 3,722 each, 820 us in the larger tiles and 480 in the
-// smaller ones, dw 792 and 377.  counted: the numbers of tiles are what they will be, not what ragged rows are expected to give.
+// registers need too many of them beside the sums of 256 x 256 (dx and dw of 43 experts of 600 x 3,728, 504 rows each, not aligned, 398 and 413 us in the larger
+// tiles and 311 and 296 in the smaller ones; 4 of 4,096 x 4,096, 4,096 rows each, y, dx and dw 1,090, 1,379 and 1,278, and 1,079, 1,012 and 988).  counted: the numbers of tiles are what they will be, not what ragged rows are expected to give.
 enum Tile { LARGE, MEDIUM, SHORT, FEW, NARROW };
 inline uint32_t tile_m(Tile t) { return t == LARGE ? 256 : t == MEDIUM || t == SHORT ? 128 : 32; }
 inline uint32_t tile_n(Tile t) { return t == LARGE ? 256 : t == NARROW ? 32 : 128; }

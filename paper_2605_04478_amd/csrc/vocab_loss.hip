@@ -578,18 +578,21 @@ i64 round_up(i64 a, i64 b) { return div_up(a, b) * b; }
 // rows of dz, all parts, at most: how many rows are kept is known on the device
 i64 dz_rows(const ccld_vocab_args* a) { return std::max(a->rows, std::min<i64>(a->rows, TWO_PARTS) * 2); }
 
+// The vocabulary's weights are loaded to LDS directly where pieces of 16 bytes lie wholly inside or outside them and start on 16 bytes, else through
+// registers, which the largest tiles have none to spare for: tiles go by addresses too.  The workspace does not: it serves both.
 bool whole_pieces(const ccld_vocab_args* a) { return a->d % 8 == 0 && a->ldw % 8 == 0; }
+bool is_direct(const ccld_vocab_args* a) { return whole_pieces(a) && aligned(a->w, 16); }
 
 // for rows x cols of results; less than 48 rows are bound by reading the vocabulary's weights
-Tile choose_tile(i64 rows, i64 cols, i64 depth, bool whole, u32 most_splits) {
-  return rows < 48 ? FEW : choose_cut((u64)rows, (u64)cols, (u64)depth, whole, most_splits).tile;
+Tile choose_tile(i64 rows, i64 cols, i64 depth, bool direct, u32 most_splits) {
+  return rows < 48 ? FEW : choose_cut((u64)rows, (u64)cols, (u64)depth, direct, most_splits).tile;
 }
 // Logits cannot be split along their contraction: where there are few tiles, smaller ones, so that more compute units read the weights.  60 rows, a vocabulary
 // of 3,047, 1,976 deep: 16.1 us in tiles of 32 x 32, 20.9 of 32 x 128, 25.5 of 128 x 128; 345 rows, 2,232, 944 deep: 20.1, 16.9 and 21.0; 100 rows,
 // 20,000, 1,000 deep: 41, 30 and 24.5.
-Tile logit_tiles(i64 rows, i64 cols, i64 depth, bool whole) {
+Tile logit_tiles(i64 rows, i64 cols, i64 depth, bool direct) {
   const i64 few = div_up(rows, Few::BM) * div_up(cols, Few::BN);
-  return few < (i64)COMPUTE_UNITS / 2 ? NARROW : few <= (i64)COMPUTE_UNITS ? FEW : choose_tile(rows, cols, depth, whole, 1);
+  return few < (i64)COMPUTE_UNITS / 2 ? NARROW : few <= (i64)COMPUTE_UNITS ? FEW : choose_tile(rows, cols, depth, direct, 1);
 }
 
 // dz of a piece is 2^28 values at most (512 MB), but a piece has 4,096 columns at least, and 2^21 at most: a tile of dz is reached by
@@ -612,6 +615,7 @@ struct Carver {
 };
 
 struct Plan {
+  bool direct;
   Rows rows;
   int dp;
   // loss
@@ -629,8 +633,9 @@ struct Plan {
   float* weight_part;
 };
 
-Plan make_plan(const ccld_vocab_args* a, bool grad, Carver& c) {
+Plan make_plan(const ccld_vocab_args* a, bool grad, bool direct, Carver& c) {
   Plan p{};
+  p.direct = direct;
   const u64 rows = (u64)a->rows;
   p.dp = (int)round_up(a->d, 8);
   const u64 all = grad ? (u64)dz_rows(a) : rows;
@@ -644,18 +649,18 @@ Plan make_plan(const ccld_vocab_args* a, bool grad, Carver& c) {
   p.rows.rest = c.take<float>(rows);
   p.rows.h = c.take<uint16_t>(all * p.dp);
   if (!grad) {
-    p.logits = logit_tiles(a->rows, a->vocab, a->d, whole_pieces(a));
+    p.logits = logit_tiles(a->rows, a->vocab, a->d, direct);
     p.col_tiles = (u32)div_up(a->vocab, tile_n(p.logits));
     p.part = c.take<float2>(rows * p.col_tiles);
     return p;
   }
   p.width = piece_width(a);
-  p.logits = logit_tiles(a->rows, p.width, a->d, whole_pieces(a));
+  p.logits = logit_tiles(a->rows, p.width, a->d, direct);
   p.col_tiles = (u32)div_up(p.width, tile_n(p.logits));
   p.dz = c.take<uint16_t>(all * p.width);
   if (a->dh) {
     // the parts of the contraction are chosen on the device, by the rows that have a target: pieces are bounded, not parts
-    p.input = choose_tile((i64)all, a->d, p.width, whole_pieces(a), MOST_SPLITS);
+    p.input = choose_tile((i64)all, a->d, p.width, direct, MOST_SPLITS);
     const u64 tiles = (u64)div_up((i64)all, tile_m(p.input)) * div_up(a->d, tile_n(p.input));
     p.pieces = (u32)std::max<u64>(tiles, MOST_PIECES);
     p.sum = c.take<float>(std::max<u64>(all * a->d, (u64)MOST_PIECES * tile_m(p.input) * tile_n(p.input)));
@@ -678,11 +683,12 @@ ccld_status check(const ccld_vocab_args* a, bool grad) {
   if (a->ldw >= MAX_LD) return CCLD_E_CAPACITY;
   if (grad && (a->dloss_stride < 0 || (a->dh && a->lddh < a->d) || (a->dw && a->lddw < a->d))) return CCLD_E_BAD_ARG;
   const i64 cols = grad ? piece_width(a) : a->vocab;
-  const bool whole = whole_pieces(a);
   auto fits = [](Tile t, i64 m, i64 n) { return launches(t, (u64)div_up(m, tile_m(t)) * div_up(n, tile_n(t))); };
-  if (!fits(logit_tiles(a->rows, cols, a->d, whole), a->rows, cols)) return CCLD_E_CAPACITY;
   const i64 all = dz_rows(a);
-  if (grad && !fits(choose_tile(all, a->d, cols, whole, MOST_SPLITS), all, a->d)) return CCLD_E_CAPACITY;
+  for (bool direct : {false, true}) {
+    if (!fits(logit_tiles(a->rows, cols, a->d, direct), a->rows, cols)) return CCLD_E_CAPACITY;
+    if (grad && !fits(choose_tile(all, a->d, cols, direct, MOST_SPLITS), all, a->d)) return CCLD_E_CAPACITY;
+  }
   if (grad && !fits(choose_weight_cut((u64)cols, (u64)a->d, (u64)all, true).tile, cols, a->d)) return CCLD_E_CAPACITY;
   return CCLD_OK;
 }
@@ -722,25 +728,27 @@ void start(const ccld_vocab_args* a, const Plan& p, bool grad, hipStream_t strea
   else start_rows<T, 1>(a, p, grad, stream);
 }
 
-bool direct(const ccld_vocab_args* a) { return whole_pieces(a) && aligned(a->w, 16); }
+// whether a tiling's kernels that are not direct are: the largest tiles, which no plan through registers takes, have the direct ones alone
+template <class C>
+constexpr bool ELSE_DIRECT = std::is_same_v<C, Large>;
 
 template <class C, class T>
-void launch_logit_sums(const ccld_vocab_args* a, const LogitJob& j, hipStream_t stream) {
+void launch_logit_sums(const ccld_vocab_args* a, const Plan& p, const LogitJob& j, hipStream_t stream) {
   const u32 grid = (u32)(div_up(a->rows, C::BM) * j.col_tiles);
-  const auto kernel = direct(a) ? &k_logit_sums<C, T, true> : &k_logit_sums<C, T, false>;
+  const auto kernel = p.direct ? &k_logit_sums<C, T, true> : &k_logit_sums<C, T, ELSE_DIRECT<C>>;
   kernel<<<grid, C::THREADS, C::LDS_BYTES, stream>>>(j);
 }
 template <class C, class T>
-void launch_logit_grad(const ccld_vocab_args* a, LogitJob j, hipStream_t stream) {
+void launch_logit_grad(const ccld_vocab_args* a, const Plan& p, LogitJob j, hipStream_t stream) {
   j.col_tiles = (u32)div_up(j.cols, C::BN);
   const u32 grid = (u32)(div_up(a->rows, C::BM) * j.col_tiles);
-  const auto kernel = direct(a) ? &k_logit_grad<C, T, true> : &k_logit_grad<C, T, false>;
+  const auto kernel = p.direct ? &k_logit_grad<C, T, true> : &k_logit_grad<C, T, ELSE_DIRECT<C>>;
   kernel<<<grid, C::THREADS, C::LDS_BYTES, stream>>>(j);
 }
 template <class C, class T>
-void launch_input_grad(const ccld_vocab_args* a, const Plan& p, InputJob j, hipStream_t stream) {
+void launch_input_grad(const Plan& p, InputJob j, hipStream_t stream) {
   j.col_tiles = (u32)div_up(j.d, C::BN);
-  const auto kernel = direct(a) ? &k_input_grad<C, T, true> : &k_input_grad<C, T, false>;
+  const auto kernel = p.direct ? &k_input_grad<C, T, true> : &k_input_grad<C, T, ELSE_DIRECT<C>>;
   kernel<<<p.pieces, C::THREADS, C::LDS_BYTES, stream>>>(j);
 }
 template <class C, class T>
@@ -763,10 +771,10 @@ template <class T>
 ccld_status loss(const ccld_vocab_args* a, const Plan& p, hipStream_t stream) {
   start<T>(a, p, false, stream);
   const LogitJob j{p.rows, a->w, a->ldw, (int)a->d, p.dp, 0, (int)a->vocab, p.col_tiles, p.part, nullptr, 0};
-  if (p.logits == LARGE) launch_logit_sums<Large, T>(a, j, stream);
-  else if (p.logits == MEDIUM) launch_logit_sums<Medium, T>(a, j, stream);
-  else if (p.logits == FEW) launch_logit_sums<Few, T>(a, j, stream);
-  else launch_logit_sums<Narrow, T>(a, j, stream);
+  if (p.logits == LARGE) launch_logit_sums<Large, T>(a, p, j, stream);
+  else if (p.logits == MEDIUM) launch_logit_sums<Medium, T>(a, p, j, stream);
+  else if (p.logits == FEW) launch_logit_sums<Few, T>(a, p, j, stream);
+  else launch_logit_sums<Narrow, T>(a, p, j, stream);
   for (i64 first = 0; first < a->rows; first += 4 * most_groups(256))
     k_loss<<<(u32)std::min(div_up(a->rows - first, 4), most_groups(256)), 256, 0, stream>>>(p.rows, first, p.part, p.col_tiles, a->loss, a->lse);
   return launched();
@@ -780,16 +788,16 @@ ccld_status gradient(const ccld_vocab_args* a, const Plan& p, hipStream_t stream
     const T* w = static_cast<const T*>(a->w) + first * a->ldw;
     if (a->rows) {
       const LogitJob j{p.rows, w, a->ldw, (int)a->d, p.dp, (int)first, (int)cols, 0, nullptr, p.dz, p.width};
-      if (p.logits == LARGE) launch_logit_grad<Large, T>(a, j, stream);
-      else if (p.logits == MEDIUM) launch_logit_grad<Medium, T>(a, j, stream);
-      else if (p.logits == FEW) launch_logit_grad<Few, T>(a, j, stream);
-      else launch_logit_grad<Narrow, T>(a, j, stream);
+      if (p.logits == LARGE) launch_logit_grad<Large, T>(a, p, j, stream);
+      else if (p.logits == MEDIUM) launch_logit_grad<Medium, T>(a, p, j, stream);
+      else if (p.logits == FEW) launch_logit_grad<Few, T>(a, p, j, stream);
+      else launch_logit_grad<Narrow, T>(a, p, j, stream);
     }
     if (a->dh && a->rows) {
       const InputJob j{p.rows, p.dz, w, p.width, a->ldw, (int)a->d, (int)cols, (int)p.width, 0, p.sum, first > 0};
-      if (p.input == LARGE) launch_input_grad<Large, T>(a, p, j, stream);
-      else if (p.input == MEDIUM) launch_input_grad<Medium, T>(a, p, j, stream);
-      else launch_input_grad<Few, T>(a, p, j, stream);
+      if (p.input == LARGE) launch_input_grad<Large, T>(p, j, stream);
+      else if (p.input == MEDIUM) launch_input_grad<Medium, T>(p, j, stream);
+      else launch_input_grad<Few, T>(p, j, stream);
     }
     if (a->dw) {
       T* dw = static_cast<T*>(a->dw) + first * a->lddw;
@@ -816,13 +824,13 @@ hipError_t allow_tiling() {
   auto allow = [&](auto k) { if (e == hipSuccess) e = allow_lds(reinterpret_cast<const void*>(k), C::LDS_BYTES); };
   if constexpr (!std::is_same_v<C, Short>) {
     allow(&k_logit_sums<C, T, true>);
-    allow(&k_logit_sums<C, T, false>);
+    allow(&k_logit_sums<C, T, ELSE_DIRECT<C>>);
     allow(&k_logit_grad<C, T, true>);
-    allow(&k_logit_grad<C, T, false>);
+    allow(&k_logit_grad<C, T, ELSE_DIRECT<C>>);
   }
   if constexpr (C::BN > 32 && !std::is_same_v<C, Short>) {
     allow(&k_input_grad<C, T, true>);
-    allow(&k_input_grad<C, T, false>);
+    allow(&k_input_grad<C, T, ELSE_DIRECT<C>>);
   }
   if constexpr (C::BM > 32) allow(&k_weight_grad<C, T>);
   return e;
@@ -844,9 +852,14 @@ extern "C" ccld_status ccld_vocab_workspace(const ccld_vocab_args* a, int32_t gr
   if (!bytes) return CCLD_E_NULL;
   const ccld_status s = check(a, grad != 0);
   if (s != CCLD_OK) return s;
-  Carver c{nullptr, 0};
-  (void)make_plan(a, grad != 0, c);
-  *bytes = (c.off + 255) & ~(u64)255;
+  u64 need = 0;
+  for (bool direct : {false, true}) {
+    if (direct && !whole_pieces(a)) continue;
+    Carver c{nullptr, 0};
+    (void)make_plan(a, grad != 0, direct, c);
+    need = std::max(need, c.off);
+  }
+  *bytes = (need + 255) & ~(u64)255;
   return CCLD_OK;
 }
 
@@ -856,7 +869,7 @@ extern "C" ccld_status ccld_vocab_loss(const ccld_vocab_args* a, void* stream) {
   if (s == CCLD_OK) s = ccld_device_init();
   if (s != CCLD_OK || a->rows == 0) return s;
   Carver c{static_cast<uint8_t*>(a->workspace), 0};
-  const Plan p = make_plan(a, false, c);
+  const Plan p = make_plan(a, false, is_direct(a), c);
   const hipStream_t st = static_cast<hipStream_t>(stream);
   return a->dtype == CCLD_BF16 ? loss<__bf16>(a, p, st) : loss<_Float16>(a, p, st);
 }
@@ -867,7 +880,7 @@ extern "C" ccld_status ccld_vocab_loss_grad(const ccld_vocab_args* a, void* stre
   if (s == CCLD_OK) s = ccld_device_init();
   if (s != CCLD_OK) return s;
   Carver c{static_cast<uint8_t*>(a->workspace), 0};
-  const Plan p = make_plan(a, true, c);
+  const Plan p = make_plan(a, true, is_direct(a), c);
   const hipStream_t st = static_cast<hipStream_t>(stream);
   return a->dtype == CCLD_BF16 ? gradient<__bf16>(a, p, st) : gradient<_Float16>(a, p, st);
 }
