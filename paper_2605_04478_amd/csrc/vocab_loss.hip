@@ -595,10 +595,10 @@ Tile logit_tiles(i64 rows, i64 cols, i64 depth, bool direct) {
   return few < (i64)COMPUTE_UNITS / 2 ? NARROW : few <= (i64)COMPUTE_UNITS ? FEW : choose_tile(rows, cols, depth, direct, 1);
 }
 
-// dz of a piece is 2^28 values at most (512 MB), but a piece has 4,096 columns at least, and 2^21 at most: a tile of dz is reached by
-// 32-bit offsets.
+// dz of a piece, both of its parts, is 2^28 values (512 MB) and a line of 256 to a row at most, up to 65,536 rows; more rows have pieces of 4,096 columns all the same,
+// 8 KB to a row.  A piece has 2^21 columns at most: a tile of dz is reached by 32-bit offsets.
 i64 piece_width(const ccld_vocab_args* a) {
-  const i64 w = std::min<i64>(std::max<i64>(round_up(((i64)1 << 28) / std::max<i64>(a->rows, 1), 256), 4096), (i64)1 << 21);
+  const i64 w = std::min<i64>(std::max<i64>(round_up(((i64)1 << 28) / std::max<i64>(dz_rows(a), 1), 256), 4096), (i64)1 << 21);
   const i64 pieces = div_up(a->vocab, w);
   return round_up(div_up(a->vocab, pieces), 256);
 }
