@@ -1,11 +1,11 @@
 """A rank's training step, computed on this card, and the trace of a job whose ranks take it.
 
-The analysis names a rank whose computation is slow (Section 2.2, S1).  Whether its card is slow or it was given more work shows when the
-same work is run: `RankStep` is a step's computation (experts, norms with gate and residual scale, the vocabulary's loss; forward
-and backward) with the operators of `step`, `measure` times it for given loads, and `trace` lets the ranks of a job compute
-for so long between their collectives, so that the analyzer sees what these times would do to a job.
+The analysis names a rank whose computation is slow (Section 2.2, S1).  Its card may be slow, or it was given more work: what its work takes on a
+card that is known to be sound tells, beside what it took in the job.  `RankStep` is a step's computation (experts, norms with gate and
+residual scale, the vocabulary's loss; forward and backward) with the operators of `step`, `measure` times it on this card for given loads, and
+`trace` lets the ranks of a job compute for so long between their collectives, so that the analyzer sees what these times would do to a job.
 
-    python -m paper_2605_04478_amd.rankstep --ranks 16 --busy-rank 5
+    python -m paper_2605_04478_amd.rankstep --ranks 16 --busy-rank 5 --took-us 9000
 """
 from __future__ import annotations
 
@@ -112,15 +112,19 @@ def trace(compute_ns: np.ndarray, n_slots: int = 200, seed: int = 0) -> tg.Trace
 
 
 def main(argv=None) -> int:
-    p = argparse.ArgumentParser(description="Times a training step's computation for the ranks of a job and has the analyzer name the late one.")
+    p = argparse.ArgumentParser(description="Times a training step's computation on this card for an ordinary and for a larger load, has the analyzer name "
+                                            "the late rank in the trace of a job made of these times, and compares a rank's time with its load's.")
     p.add_argument("--ranks", type=int, default=16)
     p.add_argument("--rows", type=int, default=4096, help="rows of a rank")
     p.add_argument("--busy-rank", type=int, default=5, help="the rank that routing sends more rows")
     p.add_argument("--times", type=float, default=2.0, help="how many times the rows of the others")
     p.add_argument("--slots", type=int, default=200, help="collectives of the trace")
+    p.add_argument("--took-us", type=float, help="what the busy rank's step took in its job, on its own card")
     a = p.parse_args(argv)
     if a.ranks < 3 or not 0 <= a.busy_rank < a.ranks or a.rows < 1:
         p.error("at least 3 ranks, one of them busy, and a row")
+    if a.took_us is not None and not a.took_us > 0:
+        p.error("a step takes more than no time")
     from . import ccld
     work = RankStep()
     usual, busy = even_load(a.rows, work.spec.experts), even_load(int(a.rows * a.times), work.spec.experts)
@@ -138,9 +142,8 @@ def main(argv=None) -> int:
           f"({usual_ns / sum(usual):.0f} and {busy_ns / sum(busy):.0f} ns a row)")
     named = int(order[0])
     print(f"{result.n_records} records, {result.n_flag} flags; most late entries: rank {named} ({int(blame['n_late_enter'][named])} of {a.slots})")
-    per_row = (busy_ns / sum(busy)) / (usual_ns / sum(usual))
-    print("its card is as fast as the others' by the row: it was given more work" if per_row < 1.2 else
-          f"its rows take {per_row:.2f} times as long as the others'")
+    print(f"its rows take {busy_ns / usual_ns:.2f} times as long as the others' on this card" +
+          (f"; it took {a.took_us * 1e3 / busy_ns:.2f} times as long as its rows take here" if a.took_us else ""))
     return 0 if named == a.busy_rank else 1
 
 
