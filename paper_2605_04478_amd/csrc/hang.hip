@@ -1624,7 +1624,7 @@ struct StaticCarver {
 };
 }  // namespace
 
-// called by ccld_create with the context's device current: no other call comes first on a device
+// called by ccld_create with the context's device current, before any other call on it, and by the operators that need no context
 ccld_status ccld_device_init() {
   unsigned char* p = nullptr;
   return device_scratch(&p);

@@ -53,9 +53,11 @@ inline Cut choose_cut(uint64_t rows, uint64_t cols, uint64_t depth, bool direct,
 }
 // Gradients of weights, n x k of them from so many rows.  Few steps are bound by writing the results: three small workgroups to a compute unit, so
 // that some write while others load (64 experts of 1,024 x 2,048: 2 rows each 47 us, 53 in the larger tiles and 58 in those of 128 x 128; 64 rows 57, 65
-// and 72).  With more steps that holds where there are neither many results nor so few that the contraction is better taken in parts, whole steps of experts: 16 of
-// 1,024 x 1,024, 625 rows each (20 steps), 104 us instead of 111; 43 of 224 x 888, 216 rows each, 49 and 53; but 64 of 1,024 x 2,048, 128 rows each, 275 and 265,
-// and 2 of 768 x 512, 400 rows each, 8.7 and 8.1 for dw alone.
+// and 72).  With more steps that holds for ragged rows, as routing leaves them, where there are neither many results nor so few that the contraction
+// is better taken in parts.  dw alone in small workgroups and else, rows spread like exp(0.7 N): 16 experts of 1,024 x 1,024 at 8 steps on average 22 and 25 us, at 20
+// 46 and 50, at 32 64 and 72; 16 of 1,024 x 2,048 at 13 48 and 57; 43 of 224 x 888 at 8 20 and 29, at 20 47 and 60; 12 of 1,336 x 1,000 at 13 34 and 34.  Beyond 20 steps
+// more results lose: 32 of 1,024 x 1,024 at 20 74 and 71, at 32 112 and 99; so do equal rows at any number: 16 of 1,024 x 1,024 at 8 20 and 18, at 20 35 and 28.  (The
+// host does not know the rows.)
 inline Cut choose_weight_cut(uint64_t n, uint64_t k, uint64_t rows, bool direct, uint64_t products = 1) {
   const uint64_t tiles = products * parts_of(n, 128) * parts_of(k, 128), steps = parts_of(rows, 32);
   const bool few = steps <= 4 || (steps <= 20 && tiles >= 2 * COMPUTE_UNITS);

@@ -77,7 +77,7 @@ struct Tiling {
 // Large: the matrix cores' time for a step equals the LDS's (128 KB moved for 256 x 256 x 32), 4 stages ahead, one workgroup to a compute unit: 8192^3 in
 //   bfloat16 at 1,260 to 1,400 TFLOP/s (a library's 1,380).
 // Medium: two workgroups to a compute unit, one computes while the other starts or ends; the LDS bounds it: 1,084 TFLOP/s.
-// Short: three small workgroups, for contractions of up to four steps, which writing the results bounds (products.h).
+// Short: three small workgroups, for gradients of weights from few rows, which writing the results bounds (products.h).
 // Few: up to 32 rows against a stream of weights, 16 KB of them to a step, which reading the weights bounds (5.5 TB/s at 16 experts of 4,096 x 2,048).
 // Narrow: the same for so few columns that tiles of 128 would leave compute units without work; seven steps of 4 KB ahead.
 using Large = Tiling<256, 256, 2, 4, 32, 5>;
@@ -442,8 +442,9 @@ __device__ __forceinline__ void store4(T* p, f32x4 v, int left, bool wide) {
   }
 }
 
-// In how many parts the contraction of `tiles` tiles is computed: the least time by choose_cut's figures, in nanoseconds, with no more than
-// MOST_PIECES pieces.  steps: of 32 along the contraction.  A lane of the wavefront weighs each number.
+// In how many parts the contraction of `tiles` tiles is computed: the least time in nanoseconds, by choose_cut's figures for a step (0.25 us in tiles of 32
+// rows) and 10 us for every tile's start and end, with no more than MOST_PIECES pieces.  steps: of 32 along the contraction.  A lane of the
+// wavefront weighs each number.
 template <class C>
 __device__ __forceinline__ u32 splits_of(u32 tiles, u32 steps) {
   static_assert(MOST_SPLITS == CCLD_WAVE, "one to a lane");
