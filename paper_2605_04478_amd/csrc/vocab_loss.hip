@@ -407,17 +407,18 @@ struct WeightJob {           // dw of a piece: dz^T [width][kept] times h [kept]
 // Adds to a tile's sums what rounding left of the targets' dz: rest times h for every kept row whose word is one of the tile's.  Each wavefront looks
 // through its share of the labels; what all found is the contraction of further steps, whose matrix of dz has one value to a row.
 // Rows are added in an order that their places decide.  The first labels are loaded before the tile's product, and rows while those before them are
-// multiplied: nothing else runs beside the largest tiles, and each load that is waited for costs them a microsecond.  Measured, dw alone: 8,192 rows x
-// 4,096 x 32,000 1,700 us without and 1,720 with; 1,200 rows x 1,536 x 50,021 182 and 195, 207 where half of the rows have one tile's words, 230 where all have.
+// multiplied: nothing else runs beside the largest tiles, and each load that is waited for costs them a microsecond.  Measured, dw alone, without and with: 8,192 rows x
+// 4,096 x 32,000 1,660 and 1,680 us; 1,200 rows x 1,536 x 50,021 180 and 191, 196 where half of the rows have one tile's words, 221 where all have; 700 rows x
+// 800 x 5,000, half of them of one tile's words, 15 and 23.
 template <class C, class T>
 struct Targets {
-  static constexpr int WAVES = C::THREADS / CCLD_WAVE, SHARE = 512, AT_ONCE = WAVES * SHARE;
-  static constexpr int STEPS = C::BM == 256 ? 4 : std::is_same_v<C, Medium> ? 2 : 1, ROWS = 32 * STEPS;      // of a contraction, by the room in LDS
+  static constexpr int WAVES = C::THREADS / CCLD_WAVE, SHARE = C::BM == 256 ? 512 : 256, AT_ONCE = WAVES * SHARE;
+  static constexpr int STEPS = std::is_same_v<C, Short> ? 1 : 2, ROWS = 32 * STEPS;      // of a contraction, by the room in LDS
   static constexpr int TURN = 4 * CCLD_WAVE;           // labels that a wavefront loads at once
   typedef __attribute__((ext_vector_type(4))) int i32x4;
   typedef Operand<T, C::BN, ROWS, C::THREADS, true, false> H;
-  struct Place { u32 list[WAVES][SHARE], count[WAVES]; int word[2][ROWS]; short rest[2][ROWS]; };
-  static constexpr int STAGE = C::BN * ROWS * 2;
+  struct Place { u32 list[WAVES][SHARE], count[WAVES]; };
+  static constexpr int DZ = C::BM * ROWS * 2, STAGE = DZ + C::BN * ROWS * 2;        // a round's dz and h
   static_assert(AT_ONCE <= 1 << 16 && C::BM <= 1 << 16 && ROWS <= C::THREADS, "a row and a word to an entry");
   static_assert(2 * STAGE + sizeof(Place) <= C::LDS_BYTES, "room");
 
@@ -440,8 +441,18 @@ struct Targets {
     const T* h = static_cast<const T*>(j.rows.h) + k0;
     H oh;
     oh.start(h, j.dp, min(C::BN, j.dp - k0));
+    Fragments<C::BM, C::MI, ROWS, true> fz;
     Fragments<C::BN, C::NI, ROWS, true> fh;
+    fz.start(prod.wave_m());
     fh.start(prod.wave_n());
+    // dz's places are zeros but for one value to a row, which the row's thread takes back
+    const s16x8 zeros = {0, 0, 0, 0, 0, 0, 0, 0};
+    for (int i = (int)threadIdx.x * 16; i < DZ; i += C::THREADS * 16) {
+      *reinterpret_cast<s16x8*>(lds + i) = zeros;
+      *reinterpret_cast<s16x8*>(lds + STAGE + i) = zeros;
+    }
+    short* mine[2] = {nullptr, nullptr};
+    u32 turn = 0;
     const int from = j.first + n0;
     for (i64 base = 0; base < kept; base += AT_ONCE) {
       i32x4 label = base ? labels(j, base, 0, kept) : first;
@@ -451,9 +462,9 @@ struct Targets {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int at = at_of(turn) + e, word = label[e] - from;
-          const bool mine = base + at < kept && word >= 0 && word < ns;
-          const u64 mask = ballot64(mine);
-          if (mine) place.list[wave][n + mbcnt64(mask)] = (u32)at << 16 | (u32)word;
+          const bool in = base + at < kept && word >= 0 && word < ns;
+          const u64 mask = ballot64(in);
+          if (in) place.list[wave][n + mbcnt64(mask)] = (u32)at << 16 | (u32)word;
           n += (u32)__popcll(mask);
         }
         label = then;
@@ -492,32 +503,29 @@ struct Targets {
       };
       if (found) fetch(0);
       // a place is written again two rounds on, when all have passed the barrier of the round between
-      for (u32 at = 0, turn = 0; at < found; at += ROWS, turn ^= 1) {
-        unsigned char* stage = lds + turn * STAGE;
+      for (u32 at = 0; at < found; at += ROWS, turn ^= 1) {
+        unsigned char *dz = lds + turn * STAGE, *rows = dz + DZ;
 #pragma unroll
-        for (int i = 0; i < H::PIECES; ++i) H::put(stage, i, next[i]);
+        for (int i = 0; i < H::PIECES; ++i) H::put(rows, i, next[i]);
         if (threadIdx.x < ROWS) {
-          place.word[turn][threadIdx.x] = next_word;
-          place.rest[turn][threadIdx.x] = __builtin_bit_cast(short, (T)next_rest);
+          short*& place_of = turn ? mine[1] : mine[0];
+          if (place_of) *place_of = 0;
+          place_of = nullptr;
+          if (next_word >= 0) {
+            const u32 c = threadIdx.x, x = (u32)next_word;
+            place_of = reinterpret_cast<short*>(dz + c * (C::BM * 2) + ((x / 16) ^ across_key<C::BM>(c)) * 32 + x % 16 * 2);
+            *place_of = __builtin_bit_cast(short, (T)next_rest);
+          }
         }
         __syncthreads();
         if (at + ROWS < found) fetch(at + ROWS);
         for (int step = 0; step < STEPS && at + 32 * step < found; ++step) {
-          s16x8 vh[C::NI], rest;
-          int word[8];
+          s16x8 vh[C::NI];
 #pragma unroll
-          for (int b = 0; b < C::NI; ++b) vh[b] = fh.read(stage, b, step);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int c = 32 * step + 8 * (int)(lane / 16) + e;
-            word[e] = place.word[turn][c] - (int)(prod.wave_m() + lane % 16);
-            rest[e] = place.rest[turn][c];
-          }
+          for (int b = 0; b < C::NI; ++b) vh[b] = fh.read(rows, b, step);
 #pragma unroll
           for (int i = 0; i < C::MI; ++i) {
-            s16x8 v;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = word[e] == 16 * i ? rest[e] : (short)0;
+            const s16x8 v = fz.read(dz, i, step);
 #pragma unroll
             for (int b = 0; b < C::NI; ++b) prod.acc[i][b] = mma(vh[b], v, prod.acc[i][b], T());
           }
