@@ -22,6 +22,7 @@ from .ccld import CcldError, lib
 DTYPES = {torch.bfloat16: 0, torch.float16: 1}
 NORM_DTYPES = {**DTYPES, torch.float32: 2}
 NORM_MAX = 16384
+MAX_LD = (1 << 22) - (1 << 14)      # a product's operands have their rows closer than this many elements
 
 
 class _ExpertArgs(C.Structure):
@@ -113,6 +114,12 @@ def _rows(t):
     return t
 
 
+def _operand(t):
+    """The same for an operand of a product, whose rows are not too far apart either."""
+    t = _rows(t)
+    return t.contiguous() if t.shape[-2] > 1 and t.stride(-2) >= MAX_LD else t
+
+
 def _ld(t) -> int:
     """Elements between rows; that of a single row may be anything."""
     return max(t.stride(-2), t.shape[-1]) if t.shape[-2] > 1 else t.shape[-1]
@@ -168,7 +175,7 @@ def _expert_inputs(x, w, offsets, *others):
     for t in others:
         _tensor(t, "dy", (x.shape[0], n), (w.dtype,))
     device = _on_gpu(w, x, offsets, *others)
-    return device, _rows(x), _rows(w), _vector(offsets), *map(_rows, others)
+    return device, _operand(x), _operand(w), _vector(offsets), *map(_operand, others)
 
 
 def _expert_args(x, w, offsets, dy, y, dx, dw):
@@ -239,7 +246,7 @@ def _vocab_inputs(h, w, labels, *others):
     for name, t in zip(("dloss", "lse"), others):
         _tensor(t, name, (h.shape[0],), (torch.float32,))
     device = _on_gpu(w, h, labels, *others)
-    return device, _rows(h), _rows(w), _vector(labels)
+    return device, _rows(h), _operand(w), _vector(labels)
 
 
 def _vocab_args(h, w, labels, dloss, loss, lse, dh, dw):

@@ -1,4 +1,5 @@
-"""Tensors whose values are not what their memory holds: torch's lazily negated views, and zeros without memory."""
+"""Tensors whose values are not what their memory holds (torch's lazily negated views, and zeros without memory), and rows millions of values
+apart."""
 import pytest
 import torch
 
@@ -91,3 +92,18 @@ def test_a_loss_that_became_complex():
         loss.sum().backward()
         grads.append([t.grad for t in leaves])
     assert all(torch.equal(a, b) and a.any() for a, b in zip(*grads))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", list(_arguments("cpu")))
+def test_rows_that_are_far_apart(name):
+    args = _with_values(DEV, name)
+    want = _results(name, args)
+    for i, t in enumerate(args):
+        if not isinstance(t, torch.Tensor) or t.dim() < 2:
+            continue
+        for apart in (step.MAX_LD - 8, step.MAX_LD, 5_000_008):
+            wide = torch.empty(*t.shape[:-1], apart, dtype=t.dtype, device=DEV)[..., :t.shape[-1]]
+            wide.copy_(t)
+            got = _results(name, [*args[:i], wide, *args[i + 1:]])
+            assert all(torch.equal(a, b) for a, b in zip(got, want)), (name, i, apart)
