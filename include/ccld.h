@@ -444,7 +444,8 @@ ccld_status ccld_expert_product_grad(const ccld_expert_args *a, void *stream);
  *   lse[t] = log sum over v of exp z[t, v]      loss[t] = lse[t] - z[t, labels[t]]
  *   dz = dloss[t] (exp(z - lse[t]) - [v = labels[t]])      dh = dz w      dw = dz^T h
  * A row whose label is outside [0, vocab) has no target: its loss, lse and dh are zero and it has no part
- * in dw, whatever its h and dloss hold. */
+ * in dw, whatever its h and dloss hold.  dz is rounded to the elements' type for the products: in two parts up to
+ * 128 rows with a target (no bits are lost then), else once, but for the target's value, whose rest is added. */
 typedef struct {
   int32_t dtype;
   int32_t label_bits;                /* 32 or 64: signed integers                                       */

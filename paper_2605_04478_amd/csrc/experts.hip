@@ -7,10 +7,10 @@
 // wavefront); those beyond the last tile end at once.  What bounds the kernels: the matrix cores from about 500 rows for an expert on, moving
 // the experts' weights below 128, both and the start and end of a tile's work between.
 //
-// Measured (bfloat16 unless said; a copy of 2 GB moves 4.9 TB/s here, reads alone more): 37 rows of 16 experts, 4,096 x 2,048 each, 37 us = 7.3 TB/s where
+// Measured (bfloat16 unless said, on one of several cards, whose matrix cores differ by 7 %; a copy of 2 GB moves 4.9 TB/s here, reads alone more): 37 rows of 16 experts, 4,096 x 2,048 each, 37 us = 7.3 TB/s where
 // the weights lie in the memory's cache, 48 us = 5.6 TB/s where not; 32,768 rows of 32 experts, 4,096 x 4,096, 3.0 ms for the three products = 1,090
 // TFLOP/s, 1,230 with the ragged ends of the tiles, which are 13 % of the work; 8,192 rows of 64 experts, 1,024 x 2,048, half precision, 265 us = 390
-// TFLOP/s and 2.4 TB/s; 5,003 rows of 12 experts, 1,336 x 1,000, 29, 30 and 39 us.
+// TFLOP/s and 2.4 TB/s; 5,003 rows of 12 experts, 1,336 x 1,000, 28, 29 and 41 us.
 #include <algorithm>
 
 #include "ccld_internal.h"

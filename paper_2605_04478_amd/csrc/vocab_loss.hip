@@ -14,13 +14,13 @@
 // Exponentials are 2^(x log2 e) in 32 bits: for x down to -30 off by 30 roundings of 2^-24 at most, a thousandth of a step of the
 // 16-bit types that gradients leave in.  dz is rounded to the operands' type for the matrix cores, after a scaling by the power of two that
 // brings the largest finite |g| just under 2^15: half-precision gradients of 10^-9 keep their bits.  What the rounding leaves of a row's target, which is most of
-// dz where a model is unsure, is kept for itself and added to both gradients (add_targets, k_input_rows); up to 128 kept rows the whole of dz
+// dz where a model is unsure, is kept for itself and added to both gradients (Targets, k_input_rows); up to 128 kept rows the whole of dz
 // is kept in two 16-bit parts (dz_parts).
 //
 // What bounds it: the matrix cores, with the logits taken twice (4 products for the 3 of an implementation that keeps them); for a handful of rows
-// reading the vocabulary's weights, and then its launches.  Measured: 8,192 rows x 4,096 x 128,000 in bfloat16, loss and gradients, 26.5 ms = 1,300
-// TFLOP/s of the four products; 4,096 x 2,048 x 65,536, the loss alone, 0.92 to 0.94 ms = 1,180 TFLOP/s, where the exponentials take what the product does
-// not hide; 5 rows x 2,048 x 32,000 41 us, of which 22 read the weights at 6 TB/s, three launches and their gaps are the rest.
+// reading the vocabulary's weights, and then its launches.  Measured, on different cards: 8,192 rows x 4,096 x 128,000 in bfloat16, loss and gradients, 26.8 to 28.5 ms =
+// 1,200 to 1,280 TFLOP/s of the four products; 4,096 x 2,048 x 65,536, the loss alone, 0.92 to 1.03 ms = 1,070 to 1,180 TFLOP/s, where the exponentials take what the
+// product does not hide; 5 rows x 2,048 x 32,000 34 to 41 us, of which 22 read the weights at 6 TB/s, three launches and their gaps are the rest.
 #include <algorithm>
 
 #include "ccld_internal.h"
