@@ -35,12 +35,16 @@ def test_the_current_stream_is_waited_for(native, monkeypatch):
     old, new = n(100, 72), n(100, 72)
     work = torch.zeros(1 << 28, device=DEV)          # 1 GB: an addition takes 0.3 ms
     side = torch.cuda.Stream()
+    with torch.cuda.stream(side):                    # (first uses load their kernels, which takes its time)
+        work.add_(1.0)
+        old.clone().copy_(new)
+        side.record_event().query()
     for name, call in calls.items():
         want, x = call(new), old.clone()
         assert not all(torch.equal(a, b) for a, b in zip(want, call(x))), name
         torch.cuda.synchronize()
         with torch.cuda.stream(side):
-            for _ in range(30):                      # 10 ms before x has its new values
+            for _ in range(60):                      # 20 ms before x has its new values
                 work.add_(1.0)
             x.copy_(new)
             got = call(x)
