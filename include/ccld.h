@@ -493,6 +493,70 @@ ccld_status ccld_norm_workspace(const ccld_norm_args *a, uint64_t *bytes);      
 ccld_status ccld_norm_residual(const ccld_norm_args *a, void *stream);
 ccld_status ccld_norm_residual_grad(const ccld_norm_args *a, void *stream);
 
+/* Choice of every token's experts: its k largest scores, in descending order, equal ones by the lower expert.
+ * A score that is -infinity or NaN belongs to an expert that is switched off: it is never chosen.  Where fewer than k are left the
+ * rest of the row is expert -1 with weight 0.
+ *   weights[t, j] = exp(scores[t, experts[t, j]] - m) / sum exp(scores - m)      over the chosen, or (over_all) all experts
+ *   dscores[t, experts[t, j]] = w_j dw_j, less p sum over j of w_j dw_j; p is the same softmax, zero for others than the chosen unless over_all
+ * Where the largest score is +infinity, those that are share the weight.  What dweights holds for expert -1 does not matter. */
+typedef struct {
+  int32_t dtype;                     /* of scores and dscores; CCLD_FP32 too                            */
+  int32_t over_all;
+  int64_t tokens, n_experts, k;      /* n_experts <= CCLD_ROUTE_EXPERTS, k <= n_experts, CCLD_ROUTE_MOST */
+  const void *scores;                /* [tokens][n_experts]                                             */
+  int32_t *experts;                  /* [tokens][k] out, in of the grad call                            */
+  float *weights;                    /* [tokens][k] out, in of the grad call                            */
+  const float *dweights;             /* [tokens][k] (grad call)                                         */
+  void *dscores;                     /* [tokens][n_experts] out (grad call)                             */
+  int64_t ldscores, lddscores;
+} ccld_route_args;
+#define CCLD_ROUTE_EXPERTS 1024
+#define CCLD_ROUTE_MOST 64
+ccld_status ccld_route(const ccld_route_args *a, void *stream);
+ccld_status ccld_route_grad(const ccld_route_args *a, void *stream);
+
+/* Entries (token, choice) sorted by expert, in the order of the tokens within an expert:
+ *   offsets[e] = entries of the experts before e      places[t, j] = offsets[e] + entries of e = experts[t, j] before (t, j)
+ * An entry whose expert is outside [0, n_experts) has place -1; offsets[n_experts] entries have one. */
+typedef struct {
+  int32_t expert_bits;               /* 32 or 64: signed integers                                       */
+  int32_t reserved;
+  int64_t tokens, k, n_experts;      /* tokens x k below 2^31, n_experts <= CCLD_ROUTE_EXPERTS          */
+  const void *experts;               /* [tokens][k]                                                     */
+  int32_t *places;                   /* [tokens][k] out                                                 */
+  int32_t *offsets;                  /* [n_experts + 1] out                                             */
+  void *workspace;
+  uint64_t workspace_bytes;
+} ccld_order_args;
+ccld_status ccld_order_workspace(const ccld_order_args *a, uint64_t *bytes);
+ccld_status ccld_expert_order(const ccld_order_args *a, void *stream);
+
+/* Rows sorted by expert and back.  There are tokens x k rows; places says which one is an entry's.
+ *   dispatch:       rows[places[t, j]] = x[t]                               dispatch_grad:  dx[t] = sum over j of drows[places[t, j]]
+ *   combine:        out[t] = sum over j of weights[t, j] y[places[t, j]]
+ *   combine_grad:   dy[places[t, j]] = weights[t, j] dout[t]                dweights[t, j] = sum over d of dout[t] y[places[t, j]]
+ * Sums are taken in the order of j.  An entry whose place is outside [0, tokens x k) has no part in anything and its dweights is
+ * zero; rows from *used on (used: offsets + n_experts of ccld_expert_order) belong to no entry: rows and dy are zero there.  The others have to be some entry's:
+ * places as ccld_expert_order leaves them. */
+typedef struct {
+  int32_t dtype;                     /* CCLD_FP32 too                                                   */
+  int32_t reserved;
+  int64_t tokens, k, d;              /* tokens x k below 2^31, k <= CCLD_ROUTE_MOST, d below 2^28       */
+  const int32_t *places;             /* [tokens][k]                                                     */
+  const int32_t *used;               /* one number (dispatch, combine_grad)                             */
+  const float *weights;              /* [tokens][k] (combine, combine_grad)                             */
+  const void *x;                     /* [tokens][d]: x, or dout                                         */
+  const void *y;                     /* [tokens x k][d]: y, or drows                                    */
+  void *x_out;                       /* [tokens][d] out: out, or dx                                     */
+  void *y_out;                       /* [tokens x k][d] out: rows, or dy                                */
+  float *dweights;                   /* [tokens][k] out, or NULL (combine_grad)                         */
+  int64_t ldx, ldy, ldx_out, ldy_out;
+} ccld_exchange_args;
+ccld_status ccld_dispatch(const ccld_exchange_args *a, void *stream);
+ccld_status ccld_dispatch_grad(const ccld_exchange_args *a, void *stream);
+ccld_status ccld_combine(const ccld_exchange_args *a, void *stream);
+ccld_status ccld_combine_grad(const ccld_exchange_args *a, void *stream);
+
 const char *ccld_status_str(ccld_status s);
 
 #ifdef __cplusplus

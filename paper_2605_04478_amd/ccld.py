@@ -117,7 +117,9 @@ EXPORTS = ("ccld_profile_enable", "ccld_profile_read", "ccld_default_params", "c
            "ccld_decode_frames", "ccld_reset_frames", "ccld_status_str",
            "ccld_expert_workspace", "ccld_expert_product", "ccld_expert_product_grad",
            "ccld_vocab_workspace", "ccld_vocab_loss", "ccld_vocab_loss_grad",
-           "ccld_norm_workspace", "ccld_norm_residual", "ccld_norm_residual_grad")
+           "ccld_norm_workspace", "ccld_norm_residual", "ccld_norm_residual_grad",
+           "ccld_route", "ccld_route_grad", "ccld_order_workspace", "ccld_expert_order",
+           "ccld_dispatch", "ccld_dispatch_grad", "ccld_combine", "ccld_combine_grad")
 
 
 def lib() -> C.CDLL:
@@ -154,6 +156,14 @@ def lib() -> C.CDLL:
         L.ccld_norm_workspace.argtypes = [vp, vp]
         L.ccld_norm_residual.argtypes = [vp, vp]
         L.ccld_norm_residual_grad.argtypes = [vp, vp]
+        L.ccld_route.argtypes = [vp, vp]
+        L.ccld_route_grad.argtypes = [vp, vp]
+        L.ccld_order_workspace.argtypes = [vp, vp]
+        L.ccld_expert_order.argtypes = [vp, vp]
+        L.ccld_dispatch.argtypes = [vp, vp]
+        L.ccld_dispatch_grad.argtypes = [vp, vp]
+        L.ccld_combine.argtypes = [vp, vp]
+        L.ccld_combine_grad.argtypes = [vp, vp]
         L.ccld_status_str.argtypes = [C.c_int32]
         L.ccld_status_str.restype = C.c_char_p
         for name in EXPORTS:

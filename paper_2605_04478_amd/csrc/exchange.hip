@@ -1,0 +1,241 @@
+// Rows of tokens sorted by expert and back, with their weights, and the gradients of both ways (ccld_dispatch*, ccld_combine*).
+//
+//   rows[place[t, j]] = x[t]                               dx[t] = sum_j drows[place[t, j]]
+//   out[t] = sum_j w[t, j] y[place[t, j]]                  dy[place[t, j]] = w[t, j] dout[t]      dw[t, j] = dout[t] . y[place[t, j]]
+//
+// Memory bounds all four.  A token belongs to a team of threads, so that its own row is moved once however many experts it has: spreading writes
+// one loaded vector to k rows, gathering adds k rows up in registers in the order of j, rounded once.  A place outside the rows is
+// never followed.
+#include <algorithm>
+
+#include "ccld_internal.h"
+#include "operators.h"
+
+using namespace ccld;
+
+namespace {
+
+struct ExchangeJob {
+  const int32_t *places, *used;
+  const float* weights;
+  const void *x, *y;
+  void *x_out, *y_out;
+  float* dweights;
+  i64 ldx, ldy, ldx_out, ldy_out, tokens;
+  u32 rows;                      // tokens x k
+  int k, d;
+};
+
+constexpr int EXCHANGE_THREADS = 256;
+
+// A token's places and weights.  A team's token is the same for all of its lanes, so these are scalar loads, which no lane has to be active for.
+struct Places {
+  const __attribute__((address_space(4))) int32_t* place;
+  const __attribute__((address_space(4))) float* weight;
+  u32 rows;
+  __device__ __forceinline__ Places(const ExchangeJob& j, i64 t)
+      : place((const __attribute__((address_space(4))) int32_t*)(uintptr_t)(j.places + t * j.k)),
+        weight((const __attribute__((address_space(4))) float*)(uintptr_t)(j.weights + t * j.k)), rows(j.rows) {}
+  __device__ __forceinline__ int at(int i) const { return (u32)place[i] < rows ? place[i] : -1; }
+  __device__ __forceinline__ float weight_at(int i) const { return weight[i]; }
+};
+
+// the rows that no entry has, zeroed by the tokens of the same numbers
+template <int TEAM, class T>
+__device__ __forceinline__ void clear_unused(const ExchangeJob& j, i64 t, int me, u32 used) {
+  constexpr int N = 16 / sizeof(T);
+  for (u32 r = max((u32)(t * j.k), used); r < (u32)(t * j.k) + (u32)j.k; ++r) {
+    T* const row = static_cast<T*>(j.y_out) + (i64)r * j.ldy_out;
+    int c = me * N;
+    for (; c + N <= j.d; c += TEAM * N) store_vec<N>(row + c, Vec<T, N>{});
+    for (; c < j.d; ++c) row[c] = (T)0.0f;
+  }
+}
+
+// (a thread that the end of the row falls on takes what is left of it value by value)
+template <class T, int TEAM>
+__global__ __launch_bounds__(EXCHANGE_THREADS) void k_dispatch(ExchangeJob j) {
+  constexpr int N = 16 / sizeof(T), TEAMS = EXCHANGE_THREADS / TEAM;
+  const int me = threadIdx.x % TEAM;
+  const u32 used = (u32)max(*j.used, 0);
+  i64 t = (i64)blockIdx.x * TEAMS + (TEAMS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / TEAM) : 0);
+  for (; t < j.tokens; t += (i64)gridDim.x * TEAMS) {
+    const Places p(j, t);
+    const T* const x = static_cast<const T*>(j.x) + t * j.ldx;
+    T* const y = static_cast<T*>(j.y_out);
+    int c = me * N;
+    for (; c + N <= j.d; c += TEAM * N) {
+      const Vec<T, N> v = load_vec<N>(x + c);
+      for (int i = 0; i < j.k; ++i) {
+        const int at = p.at(i);
+        if (at >= 0) store_vec<N>(y + at * j.ldy_out + c, v);
+      }
+    }
+    for (; c < j.d; ++c) {
+      for (int i = 0; i < j.k; ++i) {
+        const int at = p.at(i);
+        if (at >= 0) y[at * j.ldy_out + c] = x[c];
+      }
+    }
+    clear_unused<TEAM, T>(j, t, me, used);
+  }
+}
+
+// WEIGHTED: combine, else the gradient of dispatch
+template <class T, int TEAM, bool WEIGHTED>
+__global__ __launch_bounds__(EXCHANGE_THREADS) void k_gather(ExchangeJob j) {
+  constexpr int N = 16 / sizeof(T), TEAMS = EXCHANGE_THREADS / TEAM, AT_ONCE = 4;
+  const int me = threadIdx.x % TEAM;
+  i64 t = (i64)blockIdx.x * TEAMS + (TEAMS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / TEAM) : 0);
+  for (; t < j.tokens; t += (i64)gridDim.x * TEAMS) {
+    const Places p(j, t);
+    const T* const y = static_cast<const T*>(j.y);
+    T* const out = static_cast<T*>(j.x_out) + t * j.ldx_out;
+    int c = me * N;
+    for (; c + N <= j.d; c += TEAM * N) {
+      float sum[N] = {};
+      for (int i0 = 0; i0 < j.k; i0 += AT_ONCE) {
+        // (the first row stands for those that are not there: loads without a branch are all on their way at once)
+        Vec<T, N> v[AT_ONCE];
+        bool there[AT_ONCE];
+        float w[AT_ONCE];
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+          const int at = i0 + i < j.k ? p.at(i0 + i) : -1;
+          there[i] = at >= 0;
+          w[i] = !there[i] ? 0.0f : WEIGHTED ? p.weight_at(i0 + i) : 1.0f;
+          v[i] = load_vec<N>(y + max(at, 0) * j.ldy + c);
+        }
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i)
+#pragma unroll
+          for (int n = 0; n < N; ++n) sum[n] += there[i] ? w[i] * (float)v[i][n] : 0.0f;
+      }
+      Vec<T, N> o;
+#pragma unroll
+      for (int n = 0; n < N; ++n) o[n] = (T)sum[n];
+      store_vec<N>(out + c, o);
+    }
+    for (; c < j.d; ++c) {
+      float sum = 0;
+      for (int i = 0; i < j.k; ++i) {
+        const int at = p.at(i);
+        if (at >= 0) sum += (WEIGHTED ? p.weight_at(i) : 1.0f) * (float)y[at * j.ldy + c];
+      }
+      out[c] = (T)sum;
+    }
+  }
+}
+
+// The gradient of combine: AT_ONCE entries in a pass over the row, their products with y summed over the team.
+template <class T, int TEAM>
+__global__ __launch_bounds__(EXCHANGE_THREADS) void k_combine_grad(ExchangeJob j) {
+  constexpr int N = 16 / sizeof(T), TEAMS = EXCHANGE_THREADS / TEAM, AT_ONCE = 8, WAVES = TEAM / CCLD_WAVE;
+  __shared__ float sums[2][EXCHANGE_THREADS / CCLD_WAVE][AT_ONCE];
+  const int me = threadIdx.x % TEAM;
+  const u32 used = (u32)max(*j.used, 0);
+  int turn = 0;
+  i64 t = (i64)blockIdx.x * TEAMS + (TEAMS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / TEAM) : 0);
+  for (; t < j.tokens; t += (i64)gridDim.x * TEAMS) {
+    const Places p(j, t);
+    const T* const x = static_cast<const T*>(j.x) + t * j.ldx;
+    const T* const y = static_cast<const T*>(j.y);
+    T* const dy = static_cast<T*>(j.y_out);
+    for (int i0 = 0; i0 < j.k; i0 += AT_ONCE) {
+      float dot[AT_ONCE] = {};
+      int c = me * N;
+      for (; c + N <= j.d; c += TEAM * N) {
+        const Vec<T, N> v = load_vec<N>(x + c);
+        Vec<T, N> q[AT_ONCE];
+        if (j.dweights)
+#pragma unroll
+          for (int i = 0; i < AT_ONCE; ++i) q[i] = load_vec<N>(y + (i0 + i < j.k ? max(p.at(i0 + i), 0) : 0) * j.ldy + c);
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+          if (i0 + i >= j.k || p.at(i0 + i) < 0) continue;
+          const float w = p.weight_at(i0 + i);
+          Vec<T, N> o;
+#pragma unroll
+          for (int n = 0; n < N; ++n) o[n] = (T)(w * (float)v[n]);
+          store_vec<N>(dy + p.at(i0 + i) * j.ldy_out + c, o);
+          if (j.dweights)
+#pragma unroll
+            for (int n = 0; n < N; ++n) dot[i] += (float)v[n] * (float)q[i][n];
+        }
+      }
+      for (; c < j.d; ++c) {
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+          if (i0 + i >= j.k || p.at(i0 + i) < 0) continue;
+          dy[p.at(i0 + i) * j.ldy_out + c] = (T)(p.weight_at(i0 + i) * (float)x[c]);
+          if (j.dweights) dot[i] += (float)x[c] * (float)y[p.at(i0 + i) * j.ldy + c];
+        }
+      }
+      if (j.dweights) {
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) dot[i] = wave_total(dot[i]);
+        if constexpr (WAVES > 1) {
+          // (the place is written again by the pass after the next: one barrier is enough)
+          const int wave = threadIdx.x / CCLD_WAVE;
+          if (lane_id() == 0)
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; ++i) sums[turn][wave][i] = dot[i];
+          __syncthreads();
+#pragma unroll
+          for (int i = 0; i < AT_ONCE; ++i) {
+            dot[i] = 0;
+            for (int w = 0; w < WAVES; ++w) dot[i] += sums[turn][w][i];
+          }
+          turn ^= 1;
+        }
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i)
+          if (me == 0 && i0 + i < j.k) j.dweights[t * j.k + i0 + i] = p.at(i0 + i) < 0 ? 0.0f : dot[i];
+      }
+    }
+    clear_unused<TEAM, T>(j, t, me, used);
+  }
+}
+
+enum Way { DISPATCH, DISPATCH_GRAD, COMBINE, COMBINE_GRAD };
+
+template <class T, int TEAM>
+void launch(const ExchangeJob& j, Way way, hipStream_t stream) {
+  const u32 grid = (u32)std::min<i64>(blocks_for(j.tokens, EXCHANGE_THREADS / TEAM), 64 * COMPUTE_UNITS);
+  if (way == DISPATCH) k_dispatch<T, TEAM><<<grid, EXCHANGE_THREADS, 0, stream>>>(j);
+  else if (way == DISPATCH_GRAD) k_gather<T, TEAM, false><<<grid, EXCHANGE_THREADS, 0, stream>>>(j);
+  else if (way == COMBINE) k_gather<T, TEAM, true><<<grid, EXCHANGE_THREADS, 0, stream>>>(j);
+  else k_combine_grad<T, TEAM><<<grid, EXCHANGE_THREADS, 0, stream>>>(j);
+}
+
+ccld_status exchange(const ccld_exchange_args* a, Way way, void* stream) {
+  if (!a) return CCLD_E_NULL;
+  const bool reads_x = way == DISPATCH || way == COMBINE_GRAD, weighted = way == COMBINE || way == COMBINE_GRAD;
+  const bool reads_y = !reads_x || (way == COMBINE_GRAD && a->dweights);
+  if (!known_type(a->dtype) || a->tokens < 0 || a->k < 1 || a->d < 1) return CCLD_E_BAD_ARG;
+  if (a->tokens >= MAX_ROWS || a->k > CCLD_ROUTE_MOST || a->tokens * a->k >= MAX_ROWS || a->d >= (i64)1 << 28) return CCLD_E_CAPACITY;
+  if (a->tokens && (!a->places || (weighted && !a->weights) || (reads_x && (!a->x || !a->y_out || !a->used)) || (!reads_x && !a->x_out) || (reads_y && !a->y)))
+    return CCLD_E_NULL;
+  auto matrix = [&](const void* p, i64 ld) { return ld >= a->d && aligned(p, size_of(a->dtype)); };
+  if (reads_x ? !matrix(a->x, a->ldx) || !matrix(a->y_out, a->ldy_out) : !matrix(a->x_out, a->ldx_out)) return CCLD_E_BAD_ARG;
+  if ((reads_y && !matrix(a->y, a->ldy)) || !aligned(a->places, 4) || (weighted && !aligned(a->weights, 4)) || (reads_x && !aligned(a->used, 4)) ||
+      (way == COMBINE_GRAD && !aligned(a->dweights, 4))) return CCLD_E_BAD_ARG;
+  if (a->tokens == 0) return CCLD_OK;
+  const ExchangeJob j{a->places, a->used, weighted ? a->weights : nullptr, a->x, a->y, a->x_out, a->y_out, way == COMBINE_GRAD ? a->dweights : nullptr,
+                      a->ldx, a->ldy, a->ldx_out, a->ldy_out, a->tokens, (u32)(a->tokens * a->k), (int)a->k, (int)a->d};
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  with_type(a->dtype, [&](auto zero) {
+    using T = decltype(zero);
+    // a wavefront to a row of two vectors a lane and less
+    if (a->d <= 2 * CCLD_WAVE * 16 / (i64)sizeof(T)) launch<T, CCLD_WAVE>(j, way, st);
+    else launch<T, EXCHANGE_THREADS>(j, way, st);
+  });
+  return launched();
+}
+
+}  // namespace
+
+extern "C" ccld_status ccld_dispatch(const ccld_exchange_args* a, void* stream) { return exchange(a, DISPATCH, stream); }
+extern "C" ccld_status ccld_dispatch_grad(const ccld_exchange_args* a, void* stream) { return exchange(a, DISPATCH_GRAD, stream); }
+extern "C" ccld_status ccld_combine(const ccld_exchange_args* a, void* stream) { return exchange(a, COMBINE, stream); }
+extern "C" ccld_status ccld_combine_grad(const ccld_exchange_args* a, void* stream) { return exchange(a, COMBINE_GRAD, stream); }

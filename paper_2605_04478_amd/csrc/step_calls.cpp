@@ -36,6 +36,13 @@ bool truth(PyObject* p) {
   require(PyBool_Check(p));
   return p == Py_True;
 }
+int64_t whole(PyObject* p) {
+  require(PyLong_CheckExact(p));
+  int over = 0;
+  const int64_t v = PyLong_AsLongLongAndOverflow(p, &over);
+  require(!over);
+  return v;
+}
 double number(PyObject* p) {
   require(PyFloat_CheckExact(p) || PyLong_CheckExact(p));
   const double v = PyFloat_AsDouble(p);
@@ -309,6 +316,177 @@ PyObject* norm_residual_grad(PyObject* const* args) {
   return tuple(dh, db, dgate, dw_post, dw_pre);
 }
 
+// ---- the choice of experts, and tokens sorted by expert and back -----------------------------------------------------
+ccld_route_args route_args(const Device& d, const Tensor& scores, int64_t k, bool over_all) {
+  require(scores.dim() == 2);
+  ccld_route_args a{};
+  a.dtype = type_of(scores, true);
+  a.over_all = over_all;
+  a.tokens = scores.size(0); a.n_experts = scores.size(1); a.k = k;
+  require(k >= 1 && k <= a.n_experts && k <= CCLD_ROUTE_MOST && a.n_experts <= CCLD_ROUTE_EXPERTS);
+  d.matrix(scores, a.tokens, a.n_experts, scores.scalar_type());
+  a.scores = in(scores);
+  a.ldscores = ld(scores);
+  a.lddscores = a.n_experts;
+  return a;
+}
+void contiguous(const Device& d, const Tensor& t, int64_t rows, int64_t cols, at::ScalarType type) {
+  d.matrix(t, rows, cols, type);
+  require(t.is_contiguous());
+}
+
+PyObject* route(PyObject* const* args) {
+  const Tensor& scores = tensor(args[0]);
+  const Device d(scores);
+  ccld_route_args a = route_args(d, scores, whole(args[1]), truth(args[2]));
+  Tensor experts, weights;
+  {
+    WithoutInterpreter free;
+    experts = d.empty({a.tokens, a.k}, at::kInt);
+    weights = d.empty({a.tokens, a.k}, at::kFloat);
+    a.experts = static_cast<int32_t*>(out(experts));
+    a.weights = static_cast<float*>(out(weights));
+    made(ccld_route(&a, d.stream()), "ccld_route");
+  }
+  return tuple(experts, weights);
+}
+
+PyObject* route_grad(PyObject* const* args) {
+  const Tensor &dweights = tensor(args[0]), &scores = tensor(args[1]), &experts = tensor(args[2]), &weights = tensor(args[3]);
+  const Device d(scores);
+  require(experts.dim() == 2);
+  ccld_route_args a = route_args(d, scores, experts.size(1), truth(args[4]));
+  contiguous(d, experts, a.tokens, a.k, at::kInt);
+  contiguous(d, weights, a.tokens, a.k, at::kFloat);
+  contiguous(d, dweights, a.tokens, a.k, at::kFloat);
+  a.experts = static_cast<int32_t*>(const_cast<void*>(in(experts)));          // read only in this call
+  a.weights = static_cast<float*>(const_cast<void*>(in(weights)));
+  a.dweights = static_cast<const float*>(in(dweights));
+  Tensor dscores;
+  {
+    WithoutInterpreter free;
+    dscores = d.empty({a.tokens, a.n_experts}, scores.scalar_type());
+    a.dscores = out(dscores);
+    made(ccld_route_grad(&a, d.stream()), "ccld_route_grad");
+  }
+  return wrap(dscores);
+}
+
+PyObject* expert_order(PyObject* const* args) {
+  const Tensor& experts = tensor(args[0]);
+  const Device d(experts);
+  require(experts.dim() == 2 && experts.is_contiguous());
+  d.has(experts);
+  ccld_order_args a{};
+  a.expert_bits = bits_of(experts);
+  a.tokens = experts.size(0); a.k = experts.size(1); a.n_experts = whole(args[1]);
+  require(a.k > 0 && a.n_experts >= 1 && a.n_experts <= CCLD_ROUTE_EXPERTS);
+  a.experts = in(experts);
+  Tensor places, offsets;
+  {
+    WithoutInterpreter free;
+    places = d.empty({a.tokens, a.k}, at::kInt);
+    offsets = d.empty({a.n_experts + 1}, at::kInt);
+    a.places = static_cast<int32_t*>(out(places));
+    a.offsets = static_cast<int32_t*>(out(offsets));
+    run(a, d, ccld_order_workspace, ccld_expert_order, "ccld_expert_order");
+  }
+  return tuple(places, offsets);
+}
+
+// x [tokens][d] and y [tokens k][d], one of which may be missing
+ccld_exchange_args exchange_args(const Device& d, const Tensor& places, const Tensor* x, const Tensor* y, const Tensor* weights, const Tensor* offsets) {
+  require(places.dim() == 2);
+  const Tensor& m = x ? *x : *y;
+  require(m.dim() == 2);
+  ccld_exchange_args a{};
+  a.dtype = type_of(m, true);
+  a.tokens = places.size(0); a.k = places.size(1); a.d = m.size(1);
+  require(a.k > 0 && a.k <= CCLD_ROUTE_MOST && a.d > 0);
+  contiguous(d, places, a.tokens, a.k, at::kInt);
+  a.places = static_cast<const int32_t*>(in(places));
+  a.ldx = a.ldy = a.ldx_out = a.ldy_out = a.d;
+  if (x) {
+    d.matrix(*x, a.tokens, a.d, m.scalar_type());
+    a.x = in(*x);
+    a.ldx = ld(*x);
+  }
+  if (y) {
+    d.matrix(*y, a.tokens * a.k, a.d, m.scalar_type());
+    a.y = in(*y);
+    a.ldy = ld(*y);
+  }
+  if (weights) {
+    contiguous(d, *weights, a.tokens, a.k, at::kFloat);
+    a.weights = static_cast<const float*>(in(*weights));
+  }
+  if (offsets) {
+    require(offsets->dim() == 1 && offsets->size(0) > 0);
+    d.vector(*offsets, offsets->size(0), at::kInt);
+    a.used = static_cast<const int32_t*>(in(*offsets)) + offsets->size(0) - 1;
+  }
+  return a;
+}
+
+PyObject* dispatch(PyObject* const* args) {
+  const Tensor &x = tensor(args[0]), &places = tensor(args[1]), &offsets = tensor(args[2]);
+  const Device d(x);
+  ccld_exchange_args a = exchange_args(d, places, &x, nullptr, nullptr, &offsets);
+  Tensor rows;
+  {
+    WithoutInterpreter free;
+    rows = d.empty({a.tokens * a.k, a.d}, x.scalar_type());
+    a.y_out = out(rows);
+    made(ccld_dispatch(&a, d.stream()), "ccld_dispatch");
+  }
+  return wrap(rows);
+}
+
+PyObject* dispatch_grad(PyObject* const* args) {
+  const Tensor &drows = tensor(args[0]), &places = tensor(args[1]);
+  const Device d(drows);
+  ccld_exchange_args a = exchange_args(d, places, nullptr, &drows, nullptr, nullptr);
+  Tensor dx;
+  {
+    WithoutInterpreter free;
+    dx = d.empty({a.tokens, a.d}, drows.scalar_type());
+    a.x_out = out(dx);
+    made(ccld_dispatch_grad(&a, d.stream()), "ccld_dispatch_grad");
+  }
+  return wrap(dx);
+}
+
+PyObject* combine(PyObject* const* args) {
+  const Tensor &y = tensor(args[0]), &places = tensor(args[1]), &weights = tensor(args[2]);
+  const Device d(y);
+  ccld_exchange_args a = exchange_args(d, places, nullptr, &y, &weights, nullptr);
+  Tensor res;
+  {
+    WithoutInterpreter free;
+    res = d.empty({a.tokens, a.d}, y.scalar_type());
+    a.x_out = out(res);
+    made(ccld_combine(&a, d.stream()), "ccld_combine");
+  }
+  return wrap(res);
+}
+
+PyObject* combine_grad(PyObject* const* args) {
+  const Tensor &dout = tensor(args[0]), &y = tensor(args[1]), &places = tensor(args[2]), &weights = tensor(args[3]), &offsets = tensor(args[4]);
+  const bool need_dweights = truth(args[5]);
+  const Device d(y);
+  ccld_exchange_args a = exchange_args(d, places, &dout, &y, &weights, &offsets);
+  Tensor dy, dweights;
+  {
+    WithoutInterpreter free;
+    dy = d.empty({a.tokens * a.k, a.d}, y.scalar_type());
+    if (need_dweights) dweights = d.empty({a.tokens, a.k}, at::kFloat);
+    a.y_out = out(dy);
+    a.dweights = static_cast<float*>(out(dweights));
+    made(ccld_combine_grad(&a, d.stream()), "ccld_combine_grad");
+  }
+  return tuple(dy, dweights);
+}
+
 // raises CcldError
 PyObject* raise(const Failed& f) {
   PyObject* module = PyImport_ImportModule("paper_2605_04478_amd.ccld");
@@ -343,7 +521,10 @@ PyMethodDef method(const char* name) {
 PyMethodDef methods[] = {method<expert_product, 3>("expert_product"), method<expert_product_grad, 6>("expert_product_grad"),
                          method<vocab_loss, 3>("vocab_loss"),         method<vocab_loss_grad, 7>("vocab_loss_grad"),
                          method<norm_residual, 7>("norm_residual"),   method<norm_residual_grad, 10>("norm_residual_grad"),
-                         {nullptr, nullptr, 0, nullptr}};
+                         method<route, 3>("route"),                   method<route_grad, 5>("route_grad"),
+                         method<expert_order, 2>("expert_order"),     method<dispatch, 3>("dispatch"),
+                         method<dispatch_grad, 2>("dispatch_grad"),   method<combine, 3>("combine"),
+                         method<combine_grad, 6>("combine_grad"),     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef definition = {PyModuleDef_HEAD_INIT, "_step", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

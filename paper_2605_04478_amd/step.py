@@ -22,6 +22,7 @@ from .ccld import CcldError, lib
 DTYPES = {torch.bfloat16: 0, torch.float16: 1}
 NORM_DTYPES = {**DTYPES, torch.float32: 2}
 NORM_MAX = 16384
+ROUTE_EXPERTS, ROUTE_MOST = 1024, 64                # most experts, and most of them for a token
 MAX_LD = (1 << 22) - (1 << 14)      # a product's operands have their rows closer than this many elements
 
 
@@ -48,6 +49,24 @@ class _NormArgs(C.Structure):
                                              "du", "dh", "db", "dgate", "dw_post", "dw_pre")]
                 + [(n, C.c_int64) for n in ("ldh", "ldb", "ldgate", "ldh_out", "ldu", "lddh_out", "lddu", "lddh", "lddb")]
                 + [("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)])
+
+
+class _RouteArgs(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("over_all", C.c_int32), ("tokens", C.c_int64), ("n_experts", C.c_int64), ("k", C.c_int64),
+                ("scores", C.c_void_p), ("experts", C.c_void_p), ("weights", C.c_void_p), ("dweights", C.c_void_p), ("dscores", C.c_void_p),
+                ("ldscores", C.c_int64), ("lddscores", C.c_int64)]
+
+
+class _OrderArgs(C.Structure):
+    _fields_ = [("expert_bits", C.c_int32), ("reserved", C.c_int32), ("tokens", C.c_int64), ("k", C.c_int64), ("n_experts", C.c_int64),
+                ("experts", C.c_void_p), ("places", C.c_void_p), ("offsets", C.c_void_p), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_uint64)]
+
+
+class _ExchangeArgs(C.Structure):
+    _fields_ = ([("dtype", C.c_int32), ("reserved", C.c_int32), ("tokens", C.c_int64), ("k", C.c_int64), ("d", C.c_int64)]
+                + [(n, C.c_void_p) for n in ("places", "used", "weights", "x", "y", "x_out", "y_out", "dweights")]
+                + [(n, C.c_int64) for n in ("ldx", "ldy", "ldx_out", "ldy_out")])
 
 
 # ---- the calls from native code ---
@@ -234,6 +253,219 @@ class ExpertProduct(torch.autograd.Function):
     def backward(ctx, dy):
         dx, dw = expert_product_grad(dy, *ctx.saved_tensors, need_dx=ctx.needs_input_grad[0], need_dw=ctx.needs_input_grad[1])
         return dx, dw, None
+
+
+# ---- the choice of experts, and tokens sorted by expert and back -----------------------------------------------------------
+def _integer(v, name: str, low: int, high: int) -> int:
+    _require(isinstance(v, int) and not isinstance(v, bool) and low <= v <= high, f"{name} is {v!r}: {low} to {high} are possible")
+    return v
+
+
+def _route_inputs(scores, k, *others):
+    _tensor(scores, "scores", (None, None), NORM_DTYPES)
+    t, e = scores.shape
+    _require(0 < e <= ROUTE_EXPERTS, f"scores has {e} columns: 1 to {ROUTE_EXPERTS} are possible")
+    _integer(k, "k", 1, min(e, ROUTE_MOST))
+    for (name, dtype), x in zip((("experts", torch.int32), ("weights", torch.float32), ("dweights", torch.float32)), others):
+        _tensor(x, name, (t, k), (dtype,))
+    return _on_gpu(scores, *others)
+
+
+def _route_args(scores, k, over_all, experts, weights, dweights, dscores):
+    t, e = scores.shape
+    return _RouteArgs(NORM_DTYPES[scores.dtype], bool(over_all), t, e, k, scores.data_ptr(), experts.data_ptr(), weights.data_ptr(), _ptr(dweights),
+                      _ptr(dscores), _ld(scores), e)
+
+
+def route(scores, k: int, over_all: bool = False):
+    """The k experts with the largest scores of every token, in descending order, equal ones by the lower expert, and their weights: a softmax
+    over the chosen scores, or (over_all) their part of the softmax over all.
+
+    scores [tokens, experts] in bfloat16, float16 or float32 -> (experts [tokens, k] int32, weights [tokens, k] float32).  A score of
+    -infinity (or NaN) is never chosen; where fewer than k others are left, the rest of the row is expert -1 with weight 0."""
+    out = _native().route(scores, k, over_all)
+    if out is not None:
+        return out
+    device = _route_inputs(scores, k)
+    scores = _rows(scores)
+    with _current(device):
+        experts = torch.empty(scores.shape[0], k, dtype=torch.int32, device=device)
+        weights = torch.empty(scores.shape[0], k, dtype=torch.float32, device=device)
+        _call(lib().ccld_route, _route_args(scores, k, over_all, experts, weights, None, None), device)
+    return experts, weights
+
+
+def route_grad(dweights, scores, experts, weights, over_all: bool = False):
+    """Gradient of route for dweights [tokens, k] and what it returned: dscores [tokens, experts] in the type of scores.  What
+    dweights holds for expert -1 does not matter."""
+    out = _native().route_grad(dweights, scores, experts, weights, over_all)
+    if out is not None:
+        return out
+    _tensor(experts, "experts", (None, None), (torch.int32,))
+    device = _route_inputs(scores, experts.shape[1], experts, weights, dweights)
+    scores, experts, weights, dweights = _rows(scores), _vector(experts), _vector(weights), _vector(dweights)
+    with _current(device):
+        dscores = torch.empty(scores.shape, dtype=scores.dtype, device=device)
+        _call(lib().ccld_route_grad, _route_args(scores, experts.shape[1], over_all, experts, weights, dweights, dscores), device)
+    return dscores
+
+
+class Route(torch.autograd.Function):
+    """route with its gradient: Route.apply(scores, k, over_all) -> (experts, weights)."""
+
+    @staticmethod
+    def forward(ctx, scores, k, over_all):
+        experts, weights = route(scores, k, over_all)
+        ctx.over_all = over_all
+        ctx.save_for_backward(scores, experts, weights)
+        ctx.mark_non_differentiable(experts)
+        return experts, weights
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, _, dweights):
+        return route_grad(dweights, *ctx.saved_tensors, over_all=ctx.over_all), None, None
+
+
+def expert_order(experts, n_experts: int):
+    """The places of entries sorted by expert, in the order of the tokens within an expert.
+
+    experts [tokens, k] in int32 or int64 -> (places [tokens, k], offsets [n_experts + 1]), both int32: entry (t, j) is row places[t, j] of
+    the sorted rows, and the rows of expert e are offsets[e] .. offsets[e + 1) - 1, as expert_product takes them.  An
+    entry whose expert is outside [0, n_experts) has place -1."""
+    out = _native().expert_order(experts, n_experts)
+    if out is not None:
+        return out
+    _tensor(experts, "experts", (None, None), INTEGERS)
+    t, k = experts.shape
+    _require(k > 0, "experts has no columns")
+    _integer(n_experts, "n_experts", 1, ROUTE_EXPERTS)
+    device = _on_gpu(experts)
+    experts = _vector(experts)
+    L = lib()
+    with _current(device):
+        places = torch.empty(t, k, dtype=torch.int32, device=device)
+        offsets = torch.empty(n_experts + 1, dtype=torch.int32, device=device)
+        a = _OrderArgs(8 * experts.element_size(), 0, t, k, n_experts, experts.data_ptr(), places.data_ptr(), offsets.data_ptr(), None, 0)
+        ws = _workspace(L.ccld_order_workspace, a, device)
+        _call(L.ccld_expert_order, a, device)
+    del ws
+    return places, offsets
+
+
+def _exchange_inputs(places, x=None, y=None, weights=None, offsets=None, names=("x", "y")):
+    """Checks a side's rows against places; x [tokens, d] and y [tokens x k, d]."""
+    _tensor(places, "places", (None, None), (torch.int32,))
+    t, k = places.shape
+    _require(0 < k <= ROUTE_MOST, f"places has {k} columns: 1 to {ROUTE_MOST} are possible")
+    first = x if x is not None else y
+    d = dtype = None
+    for name, m, rows in ((names[0], x, t), (names[1], y, t * k)):
+        if m is not None:
+            _tensor(m, name, (rows, d), NORM_DTYPES if dtype is None else (dtype,))
+            d, dtype = m.shape[1], m.dtype
+            _require(d > 0, f"{name} has no columns")
+    if weights is not None:
+        _tensor(weights, "weights", (t, k), (torch.float32,))
+    if offsets is not None:
+        _tensor(offsets, "offsets", (None,), (torch.int32,))
+        _require(offsets.shape[0] > 0, "offsets is empty")
+    device = _on_gpu(first, places, x, y, weights, offsets)
+    keep = lambda f, m: None if m is None else f(m)
+    return device, _vector(places), keep(_rows, x), keep(_rows, y), keep(_vector, weights), keep(_vector, offsets)
+
+
+def _exchange(fn, device, places, x, y, weights, offsets, x_out, y_out, dweights=None) -> None:
+    t, k = places.shape
+    m = next(v for v in (x, y) if v is not None)
+    d = m.shape[1]
+    used = None if offsets is None else offsets.data_ptr() + 4 * (offsets.shape[0] - 1)
+    a = _ExchangeArgs(NORM_DTYPES[m.dtype], 0, t, k, d, places.data_ptr(), used, _ptr(weights), _ptr(x), _ptr(y), _ptr(x_out), _ptr(y_out),
+                      _ptr(dweights), d if x is None else _ld(x), d if y is None else _ld(y), d, d)
+    _call(fn, a, device)
+
+
+def dispatch(x, places, offsets):
+    """Rows of tokens sorted by expert: rows[places[t, j]] = x[t], for places and offsets of expert_order.
+
+    x [tokens, d] in bfloat16, float16 or float32 -> rows [tokens k, d]; those from offsets[-1] on, which no entry has, are zero."""
+    out = _native().dispatch(x, places, offsets)
+    if out is not None:
+        return out
+    device, places, x, _, _, offsets = _exchange_inputs(places, x=x, offsets=offsets)
+    with _current(device):
+        rows = torch.empty(places.numel(), x.shape[1], dtype=x.dtype, device=device)
+        _exchange(lib().ccld_dispatch, device, places, x, None, None, offsets, None, rows)
+    return rows
+
+
+def dispatch_grad(drows, places):
+    """Gradient of dispatch for drows [tokens k, d]: dx [tokens, d], the sum of each token's rows."""
+    out = _native().dispatch_grad(drows, places)
+    if out is not None:
+        return out
+    device, places, _, drows, _, _ = _exchange_inputs(places, y=drows, names=("x", "drows"))
+    with _current(device):
+        dx = torch.empty(places.shape[0], drows.shape[1], dtype=drows.dtype, device=device)
+        _exchange(lib().ccld_dispatch_grad, device, places, None, drows, None, None, dx, None)
+    return dx
+
+
+class Dispatch(torch.autograd.Function):
+    """dispatch with its gradient: Dispatch.apply(x, places, offsets) -> rows."""
+
+    @staticmethod
+    def forward(ctx, x, places, offsets):
+        ctx.save_for_backward(places)
+        return dispatch(x, places, offsets)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, drows):
+        return dispatch_grad(drows, *ctx.saved_tensors), None, None
+
+
+def combine(y, places, weights):
+    """The sorted rows back at their tokens, with weights: out[t] = sum over j of weights[t, j] y[places[t, j]].
+
+    y [tokens k, d] in bfloat16, float16 or float32, weights [tokens, k] in float32 -> out [tokens, d].  Entries without a place have no part."""
+    out = _native().combine(y, places, weights)
+    if out is not None:
+        return out
+    device, places, _, y, weights, _ = _exchange_inputs(places, y=y, weights=weights)
+    with _current(device):
+        res = torch.empty(places.shape[0], y.shape[1], dtype=y.dtype, device=device)
+        _exchange(lib().ccld_combine, device, places, None, y, weights, None, res, None)
+    return res
+
+
+def combine_grad(dout, y, places, weights, offsets, need_dweights: bool = True):
+    """Gradients of combine for dout [tokens, d]: (dy [tokens k, d], dweights [tokens, k] float32, or None where it is not needed).
+    Rows of dy from offsets[-1] on are zero, and so is dweights of an entry without a place."""
+    out = _native().combine_grad(dout, y, places, weights, offsets, need_dweights)
+    if out is not None:
+        return out
+    device, places, dout, y, weights, offsets = _exchange_inputs(places, x=dout, y=y, weights=weights, offsets=offsets, names=("dout", "y"))
+    with _current(device):
+        dy = torch.empty(y.shape, dtype=y.dtype, device=device)
+        dweights = torch.empty(places.shape, dtype=torch.float32, device=device) if need_dweights else None
+        _exchange(lib().ccld_combine_grad, device, places, dout, y, weights, offsets, None, dy, dweights)
+    return dy, dweights
+
+
+class Combine(torch.autograd.Function):
+    """combine with its gradients: Combine.apply(y, places, weights, offsets) -> out."""
+
+    @staticmethod
+    def forward(ctx, y, places, weights, offsets):
+        ctx.save_for_backward(y, places, weights, offsets)
+        return combine(y, places, weights)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout):
+        dy, dweights = combine_grad(dout, *ctx.saved_tensors, need_dweights=ctx.needs_input_grad[2])
+        return dy, None, dweights, None
 
 
 # ---- softmax cross entropy over a vocabulary ----------------------------------------------------------------------------
