@@ -557,6 +557,40 @@ ccld_status ccld_dispatch_grad(const ccld_exchange_args *a, void *stream);
 ccld_status ccld_combine(const ccld_exchange_args *a, void *stream);
 ccld_status ccld_combine_grad(const ccld_exchange_args *a, void *stream);
 
+/* A step of AdamW over many tensors at once, in place:
+ *   t = ++*count      g' = scale g      m = beta1 m + (1 - beta1) g'      v = beta2 v + (1 - beta2) g'^2
+ *   p = p - lr weight_decay p - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * The states of all tensors lie in one buffer each, `total` elements; a tensor's start at a multiple of CCLD_ADAMW_BLOCK and
+ * are followed by zeros up to the next.  With masters, p is only written: the rounded value of its 32-bit master.
+ * bits = 32: m and v are 32-bit values.  bits = 8: m is an OCP e4m3 and v an OCP e5m2 number, times the scale of its block of
+ * CCLD_ADAMW_BLOCK elements: the block's largest |m| (at least 2^-80) / 448, or v / 57344.  The step is taken with the new m and v as they
+ * are before they are rounded, up or down at random with the odds that keep the mean, from 16 bits each (m the lower ones) of a hash
+ * of seed, count and the element's place in the buffer (adamw.hip).  v does not become zero unless it is.  A value that is not finite makes its block's scale NaN. */
+typedef struct {
+  void *p;                           /* [n] contiguous, in and out                                      */
+  const void *g;                     /* [n] contiguous                                                  */
+  int64_t n;
+  int64_t start;                     /* of its states, a multiple of CCLD_ADAMW_BLOCK                   */
+} ccld_adamw_tensor;
+typedef struct {
+  int32_t dtype, grad_dtype;         /* of p and of g (that of p, or CCLD_FP32)                         */
+  int32_t bits, reserved;
+  double lr, beta1, beta2, eps, weight_decay, scale;
+  const float *scale_by;             /* one number on the device that scale is multiplied by, or NULL   */
+  uint64_t seed;
+  const ccld_adamw_tensor *tensors;  /* host memory, read before the call returns                       */
+  int64_t n_tensors, total;
+  int64_t *count;                    /* on the device: steps taken, in and out                          */
+  void *m, *v;                       /* [total]                                                         */
+  float *m_scale, *v_scale;          /* [total / CCLD_ADAMW_BLOCK] (8 bits)                             */
+  float *master;                     /* [total] or NULL                                                 */
+  void *workspace;                   /* CCLD_ADAMW_WORKSPACE bytes                                      */
+  uint64_t workspace_bytes;
+} ccld_adamw_args;
+#define CCLD_ADAMW_BLOCK 256
+#define CCLD_ADAMW_WORKSPACE 256
+ccld_status ccld_adamw(const ccld_adamw_args *a, void *stream);
+
 const char *ccld_status_str(ccld_status s);
 
 #ifdef __cplusplus

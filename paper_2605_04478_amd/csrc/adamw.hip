@@ -1,0 +1,282 @@
+// A step of AdamW over many tensors at once, with states in 32 or in 8 bits (ccld_adamw).
+//
+//   t = ++count      g' = scale g      m = b1 m + (1 - b1) g'      v = b2 v + (1 - b2) g'^2
+//   p = p - lr wd p - lr / (1 - b1^t) m / (sqrt(v) / sqrt(1 - b2^t) + eps)
+//
+// Memory bounds it: some thirty operations to the 10 to 30 bytes of an element.  The tensors of a launch are listed in its arguments, so that nothing has to
+// be copied to the device and a captured launch keeps its list; a workgroup finds its tensor by a ballot over the list.  What depends on
+// the count is computed once, on the device, by a launch of one thread: a replayed graph counts on.
+//
+// States in 8 bits: blocks of 256 elements (32 lanes with 8 each) share a scale.  m is an e4m3, v an e5m2 number: a block in which one gradient is
+// thousands of times the others' must not lift the others' v, for which its 32 powers of two matter more than a bit of precision.  Rounding to nearest would not
+// follow b2 = 0.999, whose steps are a hundredth of what two or three bits tell apart; values are rounded up or down at random, with the odds that keep
+// the mean.  Both formats' values are those of 32-bit floats whose exponents and mantissas are cut, once they are scaled so that the formats' smallest exponent
+// is that of a float: numbers below it are subnormal in both, and an addition of random bits below the cut rounds.
+#include <algorithm>
+
+#include <math.h>
+
+#include "ccld_internal.h"
+#include "operators.h"
+
+using namespace ccld;
+
+namespace {
+
+constexpr int BLOCK = CCLD_ADAMW_BLOCK, ADAMW_THREADS = 256;
+constexpr int EACH = 8;                                  // neighbouring elements of a thread
+constexpr int PASSES = 2, CHUNK = ADAMW_THREADS * EACH * PASSES;
+constexpr int LISTED = 112;                              // tensors of a launch: its arguments have 4 KB
+
+// What a step's elements share.
+struct Step { float step_size, root, decay, scale; u32 key; };
+
+struct Tensor { void* p; const void* g; i64 n; u32 start, chunk0; };      // start: in blocks; chunk0: its first workgroup
+struct AdamwJob {
+  Tensor tensors[LISTED];
+  const Step* step;
+  void *m, *v;
+  float *m_scale, *v_scale, *master;
+  float b1, b2, c1, c2, eps;
+  int n_tensors;
+};
+static_assert(sizeof(AdamwJob) <= 4096, "arguments of a launch");
+
+// 32 bits of a number from 32 bits of another, each of which depends on all of them
+__device__ __forceinline__ u32 mix(u32 x) {
+  x = (x ^ x >> 16) * 0x9E3779B1u;
+  x = (x ^ x >> 15) * 0xBB67AE85u;
+  return x ^ x >> 16;
+}
+
+struct BeginJob {
+  i64* count;
+  const float* scale_by;
+  Step* step;
+  double lr, b1, b2, weight_decay, scale;
+  u64 seed;
+};
+__global__ void k_adamw_begin(BeginJob j) {
+  const i64 t = ++*j.count;
+  Step s;
+  s.step_size = (float)(j.lr / (1.0 - pow(j.b1, (double)t)));
+  s.root = (float)(1.0 / sqrt(1.0 - pow(j.b2, (double)t)));
+  // (1 - lr wd would lose most of lr wd's bits in 32 of them)
+  s.decay = (float)(j.lr * j.weight_decay);
+  s.scale = (float)(j.scale_by ? j.scale * (double)*j.scale_by : j.scale);
+  s.key = mix(mix(mix(mix((u32)j.seed) ^ (u32)(j.seed >> 32)) ^ (u32)t) ^ (u32)(t >> 32));
+  *j.step = s;
+}
+
+// One of the two formats: BITS of mantissa, the smallest normal value 2^LEAST, the largest MOST with code TOP.
+template <int BITS, int LEAST, int TOP>
+struct Format {
+  static constexpr int CUT = 23 - BITS;
+  // the code of |x| by `random`, 16 bits; inverse: 1 / scale
+  static __device__ __forceinline__ u32 code(float x, float inverse, u32 random) {
+    const float q = fabsf(x) * inverse * __builtin_ldexpf(1.0f, -126 - LEAST);
+    return min((__builtin_bit_cast(u32, q) + (random << (CUT - 16)) + (1u << (CUT - 17))) >> CUT, (u32)TOP);
+  }
+  static __device__ __forceinline__ float value(u32 code, float scale) {
+    return __builtin_bit_cast(float, code << CUT) * __builtin_ldexpf(1.0f, 126 + LEAST) * scale;
+  }
+};
+typedef Format<3, -6, 0x7E> FirstFormat;            // e4m3: up to 448
+typedef Format<2, -14, 0x7B> SecondFormat;          // e5m2: up to 57344
+constexpr float FIRST_MOST = 448.0f, SECOND_MOST = 57344.0f;
+
+// The largest of 32 lanes' values, which are not negative: as whole numbers these have the same order, with NaN above all others.
+__device__ __forceinline__ u32 half_max(u32 v) {
+#pragma unroll
+  for (int m = 16; m >= 1; m >>= 1) v = max(v, (u32)__shfl_xor((int)v, m, 32));
+  return v;
+}
+// a block's scale: NaN where a value of it is not finite
+__device__ __forceinline__ float scale_of(u32 largest, float most) {
+  if (largest >= 0x7F800000u) return __builtin_nanf("");
+  return fmaxf(__builtin_bit_cast(float, largest), __builtin_ldexpf(1.0f, -80)) * (1.0f / most);
+}
+
+template <class T, class G, int BITS, bool MASTERS>
+__global__ __launch_bounds__(ADAMW_THREADS) void k_adamw(AdamwJob j) {
+  // the last tensor that starts at or before this workgroup
+  int mine = -1;
+  for (int i = 0; i < j.n_tensors; i += CCLD_WAVE) {
+    const int at = i + (int)lane_id();
+    mine += __builtin_popcountll(ballot64(at < j.n_tensors && j.tensors[at < j.n_tensors ? at : 0].chunk0 <= blockIdx.x));
+  }
+  const Tensor x = j.tensors[__builtin_amdgcn_readfirstlane(mine)];
+  const Step s = *j.step;
+  const i64 chunk = (i64)(blockIdx.x - x.chunk0) * CHUNK, padded = (x.n + BLOCK - 1) / BLOCK * BLOCK, start = (i64)x.start * BLOCK;
+#pragma unroll
+  for (int pass = 0; pass < PASSES; ++pass) {
+    // (whole blocks: 32 lanes are in or out together)
+    const i64 at = chunk + (i64)pass * (ADAMW_THREADS * EACH) + threadIdx.x * EACH;
+    if (at >= padded) break;
+    const i64 state = start + at;
+    float g[EACH], p[EACH], m[EACH], v[EACH];
+    T* const to = static_cast<T*>(x.p) + at;
+    const G* const from = static_cast<const G*>(x.g) + at;
+    const bool whole = at + EACH <= x.n;
+    if (whole) {
+      const Vec<G, EACH> q = load_vec<EACH>(from);
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) g[i] = s.scale * (float)q[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) g[i] = at + i < x.n ? s.scale * (float)from[i] : 0.0f;
+    }
+    if constexpr (MASTERS) {
+      const Vec<float, EACH> q = load_vec<EACH>(j.master + state);
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) p[i] = q[i];
+    } else if (whole) {
+      const Vec<T, EACH> q = load_vec<EACH>(to);
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) p[i] = (float)q[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) p[i] = at + i < x.n ? (float)to[i] : 0.0f;
+    }
+    const i64 block = state / BLOCK;
+    if constexpr (BITS == 32) {
+      const Vec<float, EACH> qm = load_vec<EACH>(static_cast<const float*>(j.m) + state), qv = load_vec<EACH>(static_cast<const float*>(j.v) + state);
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) { m[i] = qm[i]; v[i] = qv[i]; }
+    } else {
+      const Vec<uint8_t, EACH> qm = load_vec<EACH>(static_cast<const uint8_t*>(j.m) + state), qv = load_vec<EACH>(static_cast<const uint8_t*>(j.v) + state);
+      const float sm = j.m_scale[block], sv = j.v_scale[block];
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) {
+        const float a = FirstFormat::value(qm[i] & 0x7F, sm);
+        m[i] = qm[i] & 0x80 ? -a : a;
+        v[i] = SecondFormat::value(qv[i] & 0x7F, sv);
+      }
+    }
+    u32 most_m = 0, most_v = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      m[i] = j.b1 * m[i] + j.c1 * g[i];
+      v[i] = j.b2 * v[i] + j.c2 * (g[i] * g[i]);
+      most_m = max(most_m, __builtin_bit_cast(u32, m[i]) & 0x7FFFFFFFu);
+      most_v = max(most_v, __builtin_bit_cast(u32, v[i]) & 0x7FFFFFFFu);
+      const float ratio = m[i] / (sqrtf(v[i]) * s.root + j.eps);
+      p[i] = p[i] - s.decay * p[i] - s.step_size * ratio;
+    }
+    if constexpr (MASTERS) {
+      // (behind the last element: zeros stay)
+      Vec<float, EACH> q;
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) q[i] = at + i < x.n ? p[i] : 0.0f;
+      store_vec<EACH>(j.master + state, q);
+    }
+    if (whole) {
+      Vec<T, EACH> q;
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) q[i] = (T)p[i];
+      store_vec<EACH>(to, q);
+    } else {
+#pragma unroll
+      for (int i = 0; i < EACH; ++i)
+        if (at + i < x.n) to[i] = (T)p[i];
+    }
+    if constexpr (BITS == 32) {
+      Vec<float, EACH> qm, qv;
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) { qm[i] = m[i]; qv[i] = v[i]; }
+      store_vec<EACH>(static_cast<float*>(j.m) + state, qm);
+      store_vec<EACH>(static_cast<float*>(j.v) + state, qv);
+    } else {
+      const float sm = scale_of(half_max(most_m), FIRST_MOST), sv = scale_of(half_max(most_v), SECOND_MOST);
+      const float im = 1.0f / sm, iv = 1.0f / sv;
+      const u32 key = mix(s.key ^ (u32)((u64)state >> 32));
+      Vec<uint8_t, EACH> qm, qv;
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) {
+        const u32 r = mix(key + (u32)state + i);
+        const u32 a = FirstFormat::code(m[i], im, r & 0xFFFF), b = SecondFormat::code(v[i], iv, r >> 16);
+        qm[i] = (uint8_t)(a | (__builtin_bit_cast(u32, m[i]) >> 24 & 0x80));
+        qv[i] = (uint8_t)(v[i] > 0 ? max(b, 1u) : 0u);
+      }
+      store_vec<EACH>(static_cast<uint8_t*>(j.m) + state, qm);
+      store_vec<EACH>(static_cast<uint8_t*>(j.v) + state, qv);
+      if (threadIdx.x % (BLOCK / EACH) == 0) {
+        j.m_scale[block] = sm;
+        j.v_scale[block] = sv;
+      }
+    }
+  }
+}
+
+template <class T, class G>
+void launch(const AdamwJob& j, u32 groups, int bits, hipStream_t stream) {
+  const bool masters = j.master != nullptr;
+  if constexpr (sizeof(T) == 2) {
+    if (masters) {
+      if (bits == 32) k_adamw<T, G, 32, true><<<groups, ADAMW_THREADS, 0, stream>>>(j);
+      else k_adamw<T, G, 8, true><<<groups, ADAMW_THREADS, 0, stream>>>(j);
+      return;
+    }
+  }
+  if (bits == 32) k_adamw<T, G, 32, false><<<groups, ADAMW_THREADS, 0, stream>>>(j);
+  else k_adamw<T, G, 8, false><<<groups, ADAMW_THREADS, 0, stream>>>(j);
+}
+
+ccld_status check(const ccld_adamw_args* a) {
+  if (!a) return CCLD_E_NULL;
+  if (!known_type(a->dtype) || (a->grad_dtype != a->dtype && a->grad_dtype != CCLD_FP32) || (a->bits != 8 && a->bits != 32)) return CCLD_E_BAD_ARG;
+  if (!isfinite(a->lr) || !isfinite(a->weight_decay) || !isfinite(a->scale) || !(a->eps >= 0) || !isfinite(a->eps)) return CCLD_E_BAD_ARG;
+  if (!(a->beta1 >= 0 && a->beta1 < 1 && a->beta2 >= 0 && a->beta2 < 1)) return CCLD_E_BAD_ARG;
+  if (a->n_tensors < 0 || a->total < 0 || a->total % BLOCK || (a->master && a->dtype == CCLD_FP32)) return CCLD_E_BAD_ARG;
+  if (a->total / BLOCK >= (i64)1 << 32) return CCLD_E_CAPACITY;
+  if (!a->count || (a->n_tensors && !a->tensors) || (a->total && (!a->m || !a->v || (a->bits == 8 && (!a->m_scale || !a->v_scale))))) return CCLD_E_NULL;
+  const uintptr_t state = a->bits == 32 ? 4 : 1;
+  if (!aligned(a->count, 8) || !aligned(a->m, state) || !aligned(a->v, state) || !aligned(a->m_scale, 4) || !aligned(a->v_scale, 4) || !aligned(a->master, 4) ||
+      !aligned(a->scale_by, 4)) return CCLD_E_BAD_ARG;
+  if (a->workspace_bytes < CCLD_ADAMW_WORKSPACE || !a->workspace || !aligned(a->workspace, 256)) return CCLD_E_WORKSPACE;
+  for (i64 i = 0; i < a->n_tensors; ++i) {
+    const ccld_adamw_tensor& t = a->tensors[i];
+    if (t.n < 0 || t.start < 0 || t.start % BLOCK || t.start > a->total || t.n > a->total - t.start) return CCLD_E_BAD_ARG;
+    if (t.n && (!t.p || !t.g)) return CCLD_E_NULL;
+    if (!aligned(t.p, size_of(a->dtype)) || !aligned(t.g, size_of(a->grad_dtype))) return CCLD_E_BAD_ARG;
+  }
+  return CCLD_OK;
+}
+
+}  // namespace
+
+extern "C" ccld_status ccld_adamw(const ccld_adamw_args* a, void* stream) {
+  const ccld_status st = check(a);
+  if (st != CCLD_OK) return st;
+  const hipStream_t hs = static_cast<hipStream_t>(stream);
+  Step* const step = static_cast<Step*>(a->workspace);
+  k_adamw_begin<<<1, 1, 0, hs>>>(BeginJob{a->count, a->scale_by, step, a->lr, a->beta1, a->beta2, a->weight_decay, a->scale, a->seed});
+  AdamwJob j{};
+  j.step = step;
+  j.m = a->m; j.v = a->v; j.m_scale = a->m_scale; j.v_scale = a->v_scale; j.master = a->master;
+  j.b1 = (float)a->beta1; j.b2 = (float)a->beta2; j.c1 = (float)(1.0 - a->beta1); j.c2 = (float)(1.0 - a->beta2); j.eps = (float)a->eps;
+  u32 groups = 0;
+  auto flush = [&] {
+    if (!groups) return;
+    if (a->dtype == CCLD_FP32) launch<float, float>(j, groups, a->bits, hs);
+    else if (a->dtype == CCLD_BF16) a->grad_dtype == CCLD_FP32 ? launch<__bf16, float>(j, groups, a->bits, hs) : launch<__bf16, __bf16>(j, groups, a->bits, hs);
+    else a->grad_dtype == CCLD_FP32 ? launch<_Float16, float>(j, groups, a->bits, hs) : launch<_Float16, _Float16>(j, groups, a->bits, hs);
+    groups = 0;
+    j.n_tensors = 0;
+  };
+  const i64 most = most_groups(ADAMW_THREADS);
+  for (i64 i = 0; i < a->n_tensors; ++i) {
+    const ccld_adamw_tensor& t = a->tensors[i];
+    // (a tensor that is too long for a launch is taken in pieces)
+    for (i64 done = 0; done < t.n;) {
+      if (j.n_tensors == LISTED || groups == (u32)most) flush();
+      const i64 n = std::min(t.n - done, (most - groups) * CHUNK);
+      j.tensors[j.n_tensors++] = Tensor{static_cast<uint8_t*>(t.p) + done * size_of(a->dtype), static_cast<const uint8_t*>(t.g) + done * size_of(a->grad_dtype), n,
+                                        (u32)((t.start + done) / BLOCK), groups};
+      groups += (u32)blocks_for(n, CHUNK);
+      done += n;
+    }
+  }
+  flush();
+  return launched();
+}

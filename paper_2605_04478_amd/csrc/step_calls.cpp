@@ -5,6 +5,10 @@
 // of the ordinary (a tensor of another shape, type, device or layout, a refusal of the library's): nothing has been enqueued then,
 // and step.py, which knows how to lay tensors out and what to say of wrong ones, makes the call.  A failure of the device's raises what step.py
 // raises: work may have been enqueued.
+#include <algorithm>
+#include <utility>
+#include <vector>
+
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <ATen/ops/empty.h>
@@ -487,6 +491,106 @@ PyObject* combine_grad(PyObject* const* args) {
   return tuple(dy, dweights);
 }
 
+// ---- the optimizer -----------------------------------------------------------------------------------------------------
+// a list or tuple
+struct Sequence {
+  PyObject* p;
+  Py_ssize_t n;
+  explicit Sequence(PyObject* o) : p(o), n(0) {
+    require(PyList_CheckExact(o) || PyTuple_CheckExact(o));
+    n = Py_SIZE(o);
+  }
+  PyObject* operator[](Py_ssize_t i) const { return PyList_CheckExact(p) ? PyList_GET_ITEM(p, i) : PyTuple_GET_ITEM(p, i); }
+};
+
+// (parameters may be of a subclass of tensors)
+const Tensor& parameter(PyObject* p) {
+  require(THPVariable_Check(p));
+  return THPVariable_Unpack(p);
+}
+
+PyObject* adamw(PyObject* const* args) {
+  const Sequence params(args[0]), grads(args[1]), betas(args[4]);
+  PyObject* const state = args[2];
+  require(PyDict_CheckExact(state) && params.n > 0 && grads.n == params.n && betas.n == 2);
+  const Tensor& first = parameter(params[0]);
+  const Device d(first);
+  ccld_adamw_args a{};
+  a.dtype = a.grad_dtype = type_of(first, true);
+  std::vector<ccld_adamw_tensor> tensors;
+  std::vector<Tensor> stepped;
+  std::vector<std::pair<uintptr_t, uintptr_t>> ranges;
+  tensors.reserve(params.n);
+  stepped.reserve(params.n);
+  ranges.reserve(params.n);
+  at::ScalarType grad_type = at::ScalarType::Undefined;
+  for (Py_ssize_t i = 0; i < params.n; ++i) {
+    const Tensor& p = parameter(params[i]);
+    d.has(p);
+    require(p.scalar_type() == first.scalar_type() && p.is_contiguous());
+    const int64_t n = p.numel();
+    if (n) ranges.emplace_back((uintptr_t)p.data_ptr(), (uintptr_t)p.data_ptr() + n * p.element_size());
+    if (grads[i] != Py_None) {
+      const Tensor& g = tensor(grads[i]);
+      d.has(g);
+      require(g.is_contiguous() && g.sizes() == p.sizes() && (g.scalar_type() == p.scalar_type() || g.scalar_type() == at::kFloat));
+      require(grad_type == at::ScalarType::Undefined || grad_type == g.scalar_type());
+      grad_type = g.scalar_type();
+      tensors.push_back({p.data_ptr(), in(g), n, a.total});
+      stepped.push_back(p);
+    }
+    a.total += (n + CCLD_ADAMW_BLOCK - 1) / CCLD_ADAMW_BLOCK * CCLD_ADAMW_BLOCK;
+  }
+  std::sort(ranges.begin(), ranges.end());
+  for (size_t i = 1; i < ranges.size(); ++i) require(ranges[i].first >= ranges[i - 1].second);
+  if (grad_type == at::kFloat) a.grad_dtype = CCLD_FP32;
+  auto kept = [&](const char* name, int64_t n, at::ScalarType type) -> void* {
+    PyObject* const o = PyDict_GetItemString(state, name);
+    require(o);
+    const Tensor& t = tensor(o);
+    d.vector(t, n, type);
+    return t.data_ptr();
+  };
+  PyObject* const m = PyDict_GetItemString(state, "m");
+  require(m);
+  a.bits = tensor(m).scalar_type() == at::kFloat ? 32 : 8;
+  a.count = static_cast<int64_t*>(kept("count", 1, at::kLong));
+  a.m = kept("m", a.total, a.bits == 32 ? at::kFloat : at::kFloat8_e4m3fn);
+  a.v = kept("v", a.total, a.bits == 32 ? at::kFloat : at::kFloat8_e5m2);
+  if (a.bits == 8) {
+    a.m_scale = static_cast<float*>(kept("m_scale", a.total / CCLD_ADAMW_BLOCK, at::kFloat));
+    a.v_scale = static_cast<float*>(kept("v_scale", a.total / CCLD_ADAMW_BLOCK, at::kFloat));
+  }
+  if (PyObject* const o = PyDict_GetItemString(state, "master"); o && o != Py_None) {
+    require(first.scalar_type() != at::kFloat);
+    a.master = static_cast<float*>(kept("master", a.total, at::kFloat));
+  }
+  a.lr = number(args[3]); a.beta1 = number(betas[0]); a.beta2 = number(betas[1]); a.eps = number(args[5]); a.weight_decay = number(args[6]);
+  if (THPVariable_CheckExact(args[7])) {
+    const Tensor& by = tensor(args[7]);
+    d.has(by);
+    require(by.numel() == 1 && by.scalar_type() == at::kFloat);
+    a.scale = 1;
+    a.scale_by = static_cast<const float*>(in(by));
+  } else {
+    a.scale = number(args[7]);
+  }
+  a.seed = (uint64_t)whole(args[8]);
+  a.tensors = tensors.data();
+  a.n_tensors = (int64_t)tensors.size();
+  {
+    WithoutInterpreter free;
+    const Tensor ws = d.empty({CCLD_ADAMW_WORKSPACE}, at::kByte);
+    a.workspace = ws.data_ptr();
+    a.workspace_bytes = CCLD_ADAMW_WORKSPACE;
+    made(ccld_adamw(&a, d.stream()), "ccld_adamw");
+    // (who saved a parameter for a backward pass is told that it has changed)
+    for (const Tensor& p : stepped)
+      if (!p.is_inference()) p.unsafeGetTensorImpl()->bump_version();
+  }
+  Py_RETURN_TRUE;
+}
+
 // raises CcldError
 PyObject* raise(const Failed& f) {
   PyObject* module = PyImport_ImportModule("paper_2605_04478_amd.ccld");
@@ -524,7 +628,8 @@ PyMethodDef methods[] = {method<expert_product, 3>("expert_product"), method<exp
                          method<route, 3>("route"),                   method<route_grad, 5>("route_grad"),
                          method<expert_order, 2>("expert_order"),     method<dispatch, 3>("dispatch"),
                          method<dispatch_grad, 2>("dispatch_grad"),   method<combine, 3>("combine"),
-                         method<combine_grad, 6>("combine_grad"),     {nullptr, nullptr, 0, nullptr}};
+                         method<combine_grad, 6>("combine_grad"),     method<adamw, 9>("adamw"),
+                         {nullptr, nullptr, 0, nullptr}};
 PyModuleDef definition = {PyModuleDef_HEAD_INIT, "_step", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -14,6 +14,7 @@ the classes at the end of each section give the same to automatic differentiatio
 from __future__ import annotations
 
 import ctypes as C
+import math
 
 import torch
 
@@ -23,6 +24,8 @@ DTYPES = {torch.bfloat16: 0, torch.float16: 1}
 NORM_DTYPES = {**DTYPES, torch.float32: 2}
 NORM_MAX = 16384
 ROUTE_EXPERTS, ROUTE_MOST = 1024, 64                # most experts, and most of them for a token
+ADAMW_BLOCK = 256                   # elements of 8-bit states that share a scale, and what a tensor's states start on a multiple of
+ADAMW_WORKSPACE = 256
 MAX_LD = (1 << 22) - (1 << 14)      # a product's operands have their rows closer than this many elements
 
 
@@ -67,6 +70,18 @@ class _ExchangeArgs(C.Structure):
     _fields_ = ([("dtype", C.c_int32), ("reserved", C.c_int32), ("tokens", C.c_int64), ("k", C.c_int64), ("d", C.c_int64)]
                 + [(n, C.c_void_p) for n in ("places", "used", "weights", "x", "y", "x_out", "y_out", "dweights")]
                 + [(n, C.c_int64) for n in ("ldx", "ldy", "ldx_out", "ldy_out")])
+
+
+class _AdamwTensor(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("g", C.c_void_p), ("n", C.c_int64), ("start", C.c_int64)]
+
+
+class _AdamwArgs(C.Structure):
+    _fields_ = ([("dtype", C.c_int32), ("grad_dtype", C.c_int32), ("bits", C.c_int32), ("reserved", C.c_int32)]
+                + [(n, C.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay", "scale")]
+                + [("scale_by", C.c_void_p), ("seed", C.c_uint64), ("tensors", C.c_void_p), ("n_tensors", C.c_int64), ("total", C.c_int64)]
+                + [(n, C.c_void_p) for n in ("count", "m", "v", "m_scale", "v_scale", "master", "workspace")]
+                + [("workspace_bytes", C.c_uint64)])
 
 
 # ---- the calls from native code ---
@@ -636,3 +651,147 @@ class NormResidual(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, dh_out, du):
         return (*norm_residual_grad(dh_out, du, *ctx.saved_tensors, scale=ctx.scale), None, None)
+
+
+# ---- the optimizer --------------------------------------------------------------------------------------------------------
+def _padded(n: int) -> int:
+    return -(-n // ADAMW_BLOCK) * ADAMW_BLOCK
+
+
+def _adamw_params(params):
+    _require(isinstance(params, (list, tuple)), "params is no list")
+    for i, p in enumerate(params):
+        if not isinstance(p, torch.Tensor):
+            raise ValueError(f"params[{i}] is no tensor")
+        if p.dtype not in NORM_DTYPES or p.dtype != params[0].dtype:
+            raise ValueError(f"params[{i}] has type {p.dtype}" + (f", params[0] {params[0].dtype}: one call takes one type" if i else ""))
+        _require(p.is_contiguous(), f"params[{i}] is not contiguous")
+        _require(not p.is_neg() and not p._is_zerotensor(), f"params[{i}] is a view that cannot be written to")
+    ranges = sorted((p.data_ptr(), p.data_ptr() + p.numel() * p.element_size(), i) for i, p in enumerate(params) if p.numel())
+    for (_, end, i), (start, _, k) in zip(ranges, ranges[1:]):
+        _require(start >= end, f"params[{min(i, k)}] and params[{max(i, k)}] share memory")
+
+
+def adamw_state(params, bits: int = 32, masters: bool = False) -> dict:
+    """The state of adamw for these parameters before the first step: `count` (steps taken, int64 on the GPU) and the moments `m` and `v` of all
+    tensors in one buffer each, in float32, or (bits=8) as float8_e4m3fn and float8_e5m2 relative to `m_scale` and `v_scale`, one for each
+    ADAMW_BLOCK elements.  A tensor's values start at a multiple of ADAMW_BLOCK and zeros follow them up to the next.  masters adds `master`,
+    the parameters in float32, of which 16-bit ones are then a rounding."""
+    _adamw_params(params)
+    _require(len(params) > 0, "params is empty")
+    _require(bits in (8, 32), f"bits is {bits!r}: 8 and 32 are possible")
+    _require(not masters or params[0].dtype != torch.float32, "masters are for 16-bit parameters")
+    device, total = _on_gpu(*params), sum(_padded(p.numel()) for p in params)
+    zeros = lambda n, dtype: torch.zeros(n, dtype=dtype, device=device)
+    state = {"count": zeros(1, torch.int64), "m": zeros(total, torch.float32 if bits == 32 else torch.float8_e4m3fn),
+             "v": zeros(total, torch.float32 if bits == 32 else torch.float8_e5m2)}
+    if bits == 8:
+        state.update(m_scale=zeros(total // ADAMW_BLOCK, torch.float32), v_scale=zeros(total // ADAMW_BLOCK, torch.float32))
+    if masters:
+        state["master"], at = zeros(total, torch.float32), 0
+        for p in params:
+            state["master"][at:at + p.numel()] = p.detach().reshape(-1)
+            at += _padded(p.numel())
+    return state
+
+
+def _adamw_inputs(params, grads, state, lr, betas, eps, weight_decay, scale, seed):
+    """(device, gradients as they can be read, their type, bits, total)"""
+    _adamw_params(params)
+    _require(isinstance(grads, (list, tuple)) and len(grads) == len(params), f"grads is no list of {len(params)}")
+    _require(isinstance(betas, (list, tuple)) and len(betas) == 2 and all(isinstance(b, (int, float)) and 0 <= b < 1 for b in betas),
+             f"betas is {betas!r}: two numbers from 0 to less than 1 are possible")
+    for name, v in (("lr", lr), ("eps", eps), ("weight_decay", weight_decay)) + (() if isinstance(scale, torch.Tensor) else (("scale", scale),)):
+        _require(isinstance(v, (int, float)) and math.isfinite(v), f"{name} is {v!r}: finite numbers are possible")
+    _require(eps >= 0, f"eps is {eps}")
+    _require(isinstance(seed, int), f"seed is {seed!r}")
+    _require(isinstance(state, dict), "state is no dict")
+    total = sum(_padded(p.numel()) for p in params)
+    _tensor(state.get("count"), "count", (1,), (torch.int64,))
+    m = state.get("m")
+    _tensor(m, "m", (total,), (torch.float32, torch.float8_e4m3fn))
+    bits = 32 if m.dtype == torch.float32 else 8
+    _tensor(state.get("v"), "v", (total,), (torch.float32 if bits == 32 else torch.float8_e5m2,))
+    names = ["count", "m", "v"]
+    if bits == 8:
+        names += ["m_scale", "v_scale"]
+    for name in names[3:]:
+        _tensor(state.get(name), name, (total // ADAMW_BLOCK,), (torch.float32,))
+    if state.get("master") is not None:
+        names.append("master")
+        _tensor(state["master"], "master", (total,), (torch.float32,))
+        _require(not params or params[0].dtype != torch.float32, "masters are for 16-bit parameters")
+    for name in names:
+        _require(state[name].is_contiguous(), f"{name} is not contiguous")
+    of = [g for g in grads if g is not None]
+    dtype = of[0].dtype if of and isinstance(of[0], torch.Tensor) else torch.float32
+    for i, (p, g) in enumerate(zip(params, grads)):
+        if g is not None:
+            _tensor(g, f"grads[{i}]", p.shape, (p.dtype, torch.float32))
+            _require(g.dtype == dtype, f"grads[{i}] has type {g.dtype}, others {dtype}: one call takes one type")
+    if isinstance(scale, torch.Tensor):
+        _require(scale.numel() == 1, f"scale has shape {tuple(scale.shape)}")
+        _require(scale.dtype == torch.float32, f"scale has type {scale.dtype}")
+    device = _on_gpu(state["m"], *params, *of, *(state[n] for n in names), scale if isinstance(scale, torch.Tensor) else None)
+    return device, [None if g is None else _vector(g) for g in grads], dtype, bits, total
+
+
+def adamw(params, grads, state, lr: float, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.0, scale=1.0, seed: int = 0) -> None:
+    """A step of AdamW over all tensors of params, in place, with their gradients and the state that adamw_state made for them:
+
+        m = b1 m + (1 - b1) scale g      v = b2 v + (1 - b2) (scale g)^2
+        p = p - lr weight_decay p - lr / (1 - b1^count) m / (sqrt(v) / sqrt(1 - b2^count) + eps)
+
+    params are contiguous and of one type, bfloat16, float16 or float32; grads of that type or float32, all of one.  A tensor whose
+    gradient is None is left as it is, with its state.  scale is a number, or a tensor of one float32 on the GPU (a clipping that was
+    computed there).  The count is kept on the GPU: a captured step counts on when it is replayed.  8-bit states are rounded up or down
+    at random, by `seed`, the count and the element.  A gradient that is not finite leaves NaN: in 8-bit states, in its whole block."""
+    if _native().adamw(params, grads, state, lr, betas, eps, weight_decay, scale, seed) is not None:
+        return
+    device, grads, grad_dtype, bits, total = _adamw_inputs(params, grads, state, lr, betas, eps, weight_decay, scale, seed)
+    if not params:
+        return
+    at, listed = 0, []
+    for p, g in zip(params, grads):
+        if g is not None:
+            listed.append(_AdamwTensor(p.data_ptr(), g.data_ptr(), p.numel(), at))
+        at += _padded(p.numel())
+    table = (_AdamwTensor * len(listed))(*listed)
+    with _current(device):
+        by = scale if isinstance(scale, torch.Tensor) else None
+        by = None if by is None else _plain(by)
+        ws = torch.empty(ADAMW_WORKSPACE, dtype=torch.uint8, device=device)
+        a = _AdamwArgs(NORM_DTYPES[params[0].dtype], NORM_DTYPES[grad_dtype if listed else params[0].dtype], bits, 0, lr, betas[0], betas[1], eps, weight_decay,
+                       1.0 if by is not None else scale, _ptr(by), seed & (1 << 64) - 1, C.addressof(table) if listed else None, len(listed), total,
+                       state["count"].data_ptr(), state["m"].data_ptr(), state["v"].data_ptr(), _ptr(state.get("m_scale")), _ptr(state.get("v_scale")),
+                       _ptr(state.get("master")), ws.data_ptr(), ADAMW_WORKSPACE)
+        _call(lib().ccld_adamw, a, device)
+    del ws
+    torch.autograd.graph.increment_version([p for p, g in zip(params, grads) if g is not None])
+
+
+class AdamW:
+    """adamw with the state that it keeps: AdamW(params, lr), then step() after every backward pass."""
+
+    def __init__(self, params, lr: float, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.0, bits: int = 32, masters: bool = False,
+                 seed: int = 0):
+        self.params = list(params)
+        self.lr, self.betas, self.eps, self.weight_decay, self.seed = lr, betas, eps, weight_decay, seed
+        self.state = adamw_state(self.params, bits, masters)
+
+    def step(self, grads=None, scale=1.0) -> None:
+        """One step with the parameters' gradients, or with those that are given."""
+        grads = [p.grad for p in self.params] if grads is None else grads
+        adamw(self.params, grads, self.state, self.lr, self.betas, self.eps, self.weight_decay, scale, self.seed)
+
+    def state_dict(self) -> dict:
+        """Copies of the state's tensors."""
+        return {name: t.clone() for name, t in self.state.items()}
+
+    def load_state_dict(self, state: dict) -> None:
+        """Takes over a state of the same parameters and kind."""
+        _require(set(state) == set(self.state), f"the state has {sorted(state)}, expected {sorted(self.state)}")
+        for name, t in self.state.items():
+            _tensor(state[name], name, t.shape, (t.dtype,))
+        for name, t in self.state.items():
+            t.copy_(state[name])
