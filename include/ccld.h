@@ -591,6 +591,35 @@ typedef struct {
 #define CCLD_ADAMW_WORKSPACE 256
 ccld_status ccld_adamw(const ccld_adamw_args *a, void *stream);
 
+/* Log probabilities of given tokens under logits [rows][vocab], z = logits / temperature:
+ *   lse = log sum exp z      logp = z[token] - lse      entropy = -sum p log p, p = exp(z - lse)
+ * and the `top` largest logits of a row in descending order, equal ones by the lower word, with their log probabilities.
+ *   dlogits = (dlogp ([v = token] - p) - dentropy p (log p + entropy)) / temperature
+ * A token outside [0, vocab) is no target: its logp is zero and its dlogp does not matter.  A logit of -infinity has no part in anything but its own logp; a
+ * row of nothing else has lse = -infinity, entropy 0 and no gradient (another's lse is finite).  Top entries that are not there are word -1, log probability -infinity.  A NaN or +infinity makes its row's
+ * values and gradient NaN (NaN is not listed). */
+typedef struct {
+  int32_t dtype;                     /* of logits and dlogits; CCLD_FP32 too                            */
+  int32_t token_bits;                /* 32 or 64: signed integers                                       */
+  float temperature;                 /* 2^-64 to 2^64                                                   */
+  int32_t top;                       /* 0 to CCLD_TOP_MOST                                              */
+  int64_t rows, vocab;               /* below 2^31; vocab at least 1                                    */
+  const void *logits;                /* [rows][vocab]                                                   */
+  const void *tokens;                /* [rows]                                                          */
+  float *logp, *entropy, *lse;       /* [rows] out; entropy and lse in of the grad call                 */
+  int32_t *top_ids;                  /* [rows][top] out                                                 */
+  float *top_logp;                   /* [rows][top] out                                                 */
+  const float *dlogp, *dentropy;     /* [rows], strides apart, or NULL: zero (grad call)                */
+  void *dlogits;                     /* [rows][vocab] out (grad call)                                   */
+  int64_t ldlogits, lddlogits, dlogp_stride, dentropy_stride;
+  void *workspace;
+  uint64_t workspace_bytes;
+} ccld_logprob_args;
+#define CCLD_TOP_MOST 64
+ccld_status ccld_logprob_workspace(const ccld_logprob_args *a, uint64_t *bytes);      /* of the first call */
+ccld_status ccld_token_logprobs(const ccld_logprob_args *a, void *stream);
+ccld_status ccld_token_logprobs_grad(const ccld_logprob_args *a, void *stream);
+
 const char *ccld_status_str(ccld_status s);
 
 #ifdef __cplusplus

@@ -12,7 +12,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libccld.so")
 SOURCES = ("radix_sort.hip", "window.hip", "segments.hip", "groups.hip", "grid.hip", "merge.hip", "chains.hip", "hang.hip", "api.hip",
-           "experts.hip", "join.hip", "vocab_loss.hip", "norms.hip", "routing.hip", "exchange.hip", "adamw.hip")
+           "experts.hip", "join.hip", "vocab_loss.hip", "norms.hip", "routing.hip", "exchange.hip", "adamw.hip", "logprobs.hip")
 STEP_SOURCE, STEP = os.path.join(CSRC, "step_calls.cpp"), os.path.join(HERE, "_step.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ROCM_INCLUDE = os.path.join(os.path.dirname(os.path.dirname(HIPCC)), "include")

@@ -119,7 +119,8 @@ EXPORTS = ("ccld_profile_enable", "ccld_profile_read", "ccld_default_params", "c
            "ccld_vocab_workspace", "ccld_vocab_loss", "ccld_vocab_loss_grad",
            "ccld_norm_workspace", "ccld_norm_residual", "ccld_norm_residual_grad",
            "ccld_route", "ccld_route_grad", "ccld_order_workspace", "ccld_expert_order",
-           "ccld_dispatch", "ccld_dispatch_grad", "ccld_combine", "ccld_combine_grad", "ccld_adamw")
+           "ccld_dispatch", "ccld_dispatch_grad", "ccld_combine", "ccld_combine_grad", "ccld_adamw",
+           "ccld_logprob_workspace", "ccld_token_logprobs", "ccld_token_logprobs_grad")
 
 
 def lib() -> C.CDLL:
@@ -165,6 +166,9 @@ def lib() -> C.CDLL:
         L.ccld_combine.argtypes = [vp, vp]
         L.ccld_combine_grad.argtypes = [vp, vp]
         L.ccld_adamw.argtypes = [vp, vp]
+        L.ccld_logprob_workspace.argtypes = [vp, vp]
+        L.ccld_token_logprobs.argtypes = [vp, vp]
+        L.ccld_token_logprobs_grad.argtypes = [vp, vp]
         L.ccld_status_str.argtypes = [C.c_int32]
         L.ccld_status_str.restype = C.c_char_p
         for name in EXPORTS:

@@ -236,6 +236,76 @@ PyObject* vocab_loss_grad(PyObject* const* args) {
   return tuple(dh, dw);
 }
 
+// ---- log probabilities of given tokens -------------------------------------------------------------------------------
+ccld_logprob_args logprob_args(const Device& d, const Tensor& logits, const Tensor& tokens, double temperature) {
+  require(logits.dim() == 2);
+  ccld_logprob_args a{};
+  a.dtype = type_of(logits, true);
+  a.rows = logits.size(0); a.vocab = logits.size(1);
+  require(a.vocab > 0);
+  d.matrix(logits, a.rows, a.vocab, logits.scalar_type());
+  a.token_bits = bits_of(tokens);
+  d.vector(tokens, a.rows, tokens.scalar_type());
+  a.temperature = (float)temperature;
+  a.logits = in(logits); a.tokens = in(tokens);
+  a.ldlogits = ld(logits);
+  a.lddlogits = a.vocab;
+  return a;
+}
+
+PyObject* token_logprobs(PyObject* const* args) {
+  const Tensor &logits = tensor(args[0]), &tokens = tensor(args[1]);
+  const Device d(logits);
+  ccld_logprob_args a = logprob_args(d, logits, tokens, number(args[2]));
+  const int64_t top = whole(args[3]);
+  require(top >= 0 && top <= CCLD_TOP_MOST);
+  a.top = (int32_t)top;
+  Tensor logp, entropy, lse, top_ids, top_logp;
+  {
+    WithoutInterpreter free;
+    logp = d.empty({a.rows}, at::kFloat);
+    entropy = d.empty({a.rows}, at::kFloat);
+    lse = d.empty({a.rows}, at::kFloat);
+    top_ids = d.empty({a.rows, top}, at::kInt);
+    top_logp = d.empty({a.rows, top}, at::kFloat);
+    a.logp = static_cast<float*>(out(logp));
+    a.entropy = static_cast<float*>(out(entropy));
+    a.lse = static_cast<float*>(out(lse));
+    a.top_ids = static_cast<int32_t*>(out(top_ids));
+    a.top_logp = static_cast<float*>(out(top_logp));
+    run(a, d, ccld_logprob_workspace, ccld_token_logprobs, "ccld_token_logprobs");
+  }
+  return tuple(logp, entropy, lse, top_ids, top_logp);
+}
+
+PyObject* token_logprobs_grad(PyObject* const* args) {
+  const Tensor &logits = tensor(args[2]), &tokens = tensor(args[3]), &lse = tensor(args[4]), &entropy = tensor(args[5]);
+  const Device d(logits);
+  ccld_logprob_args a = logprob_args(d, logits, tokens, number(args[6]));
+  auto gradient = [&](PyObject* p, const float*& at, int64_t& stride) {
+    if (p == Py_None) return;
+    const Tensor& t = tensor(p);
+    d.has(t);
+    require(t.dim() == 1 && t.size(0) == a.rows && t.scalar_type() == at::kFloat);
+    at = static_cast<const float*>(in(t));
+    stride = t.stride(0);
+  };
+  gradient(args[0], a.dlogp, a.dlogp_stride);
+  gradient(args[1], a.dentropy, a.dentropy_stride);
+  d.vector(lse, a.rows, at::kFloat);
+  d.vector(entropy, a.rows, at::kFloat);
+  a.lse = static_cast<float*>(const_cast<void*>(in(lse)));          // read only in this call
+  a.entropy = static_cast<float*>(const_cast<void*>(in(entropy)));
+  Tensor dlogits;
+  {
+    WithoutInterpreter free;
+    dlogits = d.empty({a.rows, a.vocab}, logits.scalar_type());
+    a.dlogits = out(dlogits);
+    made(ccld_token_logprobs_grad(&a, d.stream()), "ccld_token_logprobs_grad");
+  }
+  return wrap(dlogits);
+}
+
 // ---- the norms around a block, its gate and the residual scale ---------------------------------------------------------
 ccld_norm_args norm_args(const Device& d, const Tensor& h, const Tensor& b, PyObject* gate, const Tensor& w_post, const Tensor& w_pre) {
   require(h.dim() == 2);
@@ -629,6 +699,7 @@ PyMethodDef methods[] = {method<expert_product, 3>("expert_product"), method<exp
                          method<expert_order, 2>("expert_order"),     method<dispatch, 3>("dispatch"),
                          method<dispatch_grad, 2>("dispatch_grad"),   method<combine, 3>("combine"),
                          method<combine_grad, 6>("combine_grad"),     method<adamw, 9>("adamw"),
+                         method<token_logprobs, 4>("token_logprobs"), method<token_logprobs_grad, 7>("token_logprobs_grad"),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef definition = {PyModuleDef_HEAD_INIT, "_step", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -26,6 +26,7 @@ NORM_MAX = 16384
 ROUTE_EXPERTS, ROUTE_MOST = 1024, 64                # most experts, and most of them for a token
 ADAMW_BLOCK = 256                   # elements of 8-bit states that share a scale, and what a tensor's states start on a multiple of
 ADAMW_WORKSPACE = 256
+TOP_MOST = 64                       # most alternatives of a row
 MAX_LD = (1 << 22) - (1 << 14)      # a product's operands have their rows closer than this many elements
 
 
@@ -82,6 +83,13 @@ class _AdamwArgs(C.Structure):
                 + [("scale_by", C.c_void_p), ("seed", C.c_uint64), ("tensors", C.c_void_p), ("n_tensors", C.c_int64), ("total", C.c_int64)]
                 + [(n, C.c_void_p) for n in ("count", "m", "v", "m_scale", "v_scale", "master", "workspace")]
                 + [("workspace_bytes", C.c_uint64)])
+
+
+class _LogprobArgs(C.Structure):
+    _fields_ = ([("dtype", C.c_int32), ("token_bits", C.c_int32), ("temperature", C.c_float), ("top", C.c_int32), ("rows", C.c_int64), ("vocab", C.c_int64)]
+                + [(n, C.c_void_p) for n in ("logits", "tokens", "logp", "entropy", "lse", "top_ids", "top_logp", "dlogp", "dentropy", "dlogits")]
+                + [(n, C.c_int64) for n in ("ldlogits", "lddlogits", "dlogp_stride", "dentropy_stride")]
+                + [("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)])
 
 
 # ---- the calls from native code ---
@@ -558,6 +566,83 @@ class VocabLoss(torch.autograd.Function):
         h, w, labels, lse = ctx.saved_tensors
         dh, dw = vocab_loss_grad(dloss, h, w, labels, lse, need_dh=ctx.needs_input_grad[0], need_dw=ctx.needs_input_grad[1])
         return dh, dw, None
+
+
+# ---- log probabilities of given tokens ------------------------------------------------------------------------------------
+def _logprob_inputs(logits, tokens, temperature, *others):
+    _tensor(logits, "logits", (None, None), NORM_DTYPES)
+    rows, v = logits.shape
+    _require(v > 0, "logits has no columns")
+    _tensor(tokens, "tokens", (rows,), INTEGERS)
+    _require(isinstance(temperature, (int, float)) and 2.0 ** -64 <= temperature <= 2.0 ** 64, f"temperature is {temperature!r}: 2^-64 to 2^64 are possible")
+    for name, t in zip(("dlogp", "dentropy", "lse", "entropy"), others):
+        if t is not None or name in ("lse", "entropy"):
+            _tensor(t, name, (rows,), (torch.float32,))
+    return _on_gpu(logits, tokens, *others), _rows(logits), _vector(tokens)
+
+
+def token_logprobs(logits, tokens, temperature: float = 1.0, top: int = 0):
+    """Log probabilities of one token of every row under softmax(logits / temperature), and what else is read off such rows.
+
+    logits [rows, vocab] in bfloat16, float16 or float32, tokens [rows] in int32 or int64 -> (logp [rows], entropy [rows], lse [rows],
+    top_ids [rows, top] int32, top_logp [rows, top]), in float32: the token's log probability, the entropy of the row's distribution, the logarithm of its
+    sum of exponentials, and the `top` largest logits in descending order, equal ones by the lower word, with their log probabilities.
+
+    A token outside [0, vocab) is none: its logp is zero.  Logits of -infinity are ruled out; where fewer than `top` are left, the rest are
+    word -1 with -infinity, and a row of nothing has lse -infinity and entropy 0.  A NaN or +infinity makes its row's values NaN."""
+    out = _native().token_logprobs(logits, tokens, temperature, top)
+    if out is not None:
+        return out
+    device, logits, tokens = _logprob_inputs(logits, tokens, temperature)
+    _integer(top, "top", 0, TOP_MOST)
+    rows, v = logits.shape
+    L = lib()
+    with _current(device):
+        logp, entropy, lse = (torch.empty(rows, dtype=torch.float32, device=device) for _ in range(3))
+        top_ids = torch.empty(rows, top, dtype=torch.int32, device=device)
+        top_logp = torch.empty(rows, top, dtype=torch.float32, device=device)
+        a = _LogprobArgs(NORM_DTYPES[logits.dtype], 8 * tokens.element_size(), temperature, top, rows, v, logits.data_ptr(), tokens.data_ptr(), logp.data_ptr(),
+                         entropy.data_ptr(), lse.data_ptr(), top_ids.data_ptr(), top_logp.data_ptr(), None, None, None, _ld(logits), v, 0, 0, None, 0)
+        ws = _workspace(L.ccld_logprob_workspace, a, device)
+        _call(L.ccld_token_logprobs, a, device)
+    del ws
+    return logp, entropy, lse, top_ids, top_logp
+
+
+def token_logprobs_grad(dlogp, dentropy, logits, tokens, lse, entropy, temperature: float = 1.0):
+    """Gradient of token_logprobs for those of logp and entropy (either may be None: zero) and the lse and entropy that it returned: dlogits [rows, vocab] in
+    the type of logits.  A row of nothing has none, and the dlogp of a token that is none does not matter."""
+    out = _native().token_logprobs_grad(dlogp, dentropy, logits, tokens, lse, entropy, temperature)
+    if out is not None:
+        return out
+    device, logits, tokens = _logprob_inputs(logits, tokens, temperature, dlogp, dentropy, lse, entropy)
+    dlogp, dentropy = (None if t is None else _plain(t) for t in (dlogp, dentropy))
+    lse, entropy = _vector(lse), _vector(entropy)
+    rows, v = logits.shape
+    stride = lambda t: 0 if t is None else t.stride(0)
+    with _current(device):
+        dlogits = torch.empty(rows, v, dtype=logits.dtype, device=device)
+        a = _LogprobArgs(NORM_DTYPES[logits.dtype], 8 * tokens.element_size(), temperature, 0, rows, v, logits.data_ptr(), tokens.data_ptr(), None, entropy.data_ptr(),
+                         lse.data_ptr(), None, None, _ptr(dlogp), _ptr(dentropy), dlogits.data_ptr(), _ld(logits), v, stride(dlogp), stride(dentropy), None, 0)
+        _call(lib().ccld_token_logprobs_grad, a, device)
+    return dlogits
+
+
+class TokenLogprobs(torch.autograd.Function):
+    """token_logprobs with its gradient: TokenLogprobs.apply(logits, tokens, temperature) -> (logp [rows], entropy [rows])."""
+
+    @staticmethod
+    def forward(ctx, logits, tokens, temperature):
+        logp, entropy, lse, _, _ = token_logprobs(logits, tokens, temperature)
+        ctx.set_materialize_grads(False)
+        ctx.temperature = temperature
+        ctx.save_for_backward(logits, tokens, lse, entropy)
+        return logp, entropy
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dlogp, dentropy):
+        return token_logprobs_grad(dlogp, dentropy, *ctx.saved_tensors, ctx.temperature), None, None
 
 
 # ---- the norms around a block, its gate and the residual scale -----------------------------------------------------------
