@@ -72,9 +72,9 @@ __global__ void k_adamw_begin(BeginJob j) {
 template <int BITS, int LEAST, int TOP>
 struct Format {
   static constexpr int CUT = 23 - BITS;
-  // the code of |x| by `random`, 16 bits; inverse: 1 / scale
-  static __device__ __forceinline__ u32 code(float x, float inverse, u32 random) {
-    const float q = fabsf(x) * inverse * __builtin_ldexpf(1.0f, -126 - LEAST);
+  // the code of |x| by `random`, 16 bits; inverse: 1 / scale, whose rounding a step of the division's remainder takes out again
+  static __device__ __forceinline__ u32 code(float x, float scale, float inverse, u32 random) {
+    const float a = fabsf(x), first = a * inverse, q = fmaf(fmaf(-first, scale, a), inverse, first) * __builtin_ldexpf(1.0f, -126 - LEAST);
     return min((__builtin_bit_cast(u32, q) + (random << (CUT - 16)) + (1u << (CUT - 17))) >> CUT, (u32)TOP);
   }
   static __device__ __forceinline__ float value(u32 code, float scale) {
@@ -95,6 +95,13 @@ __device__ __forceinline__ u32 half_max(u32 v) {
 __device__ __forceinline__ float scale_of(u32 largest, float most) {
   if (largest >= 0x7F800000u) return __builtin_nanf("");
   return fmaxf(__builtin_bit_cast(float, largest), __builtin_ldexpf(1.0f, -80)) * (1.0f / most);
+}
+
+// each operation rounded by itself, as a program that takes them one after another has them: 8-bit values next to one of the random borders then go the same way
+__device__ __forceinline__ void next_moments(float& m, float& v, float g, const AdamwJob& j) {
+#pragma clang fp contract(off)
+  m = j.b1 * m + j.c1 * g;
+  v = j.b2 * v + j.c2 * g * g;
 }
 
 template <class T, class G, int BITS, bool MASTERS>
@@ -156,8 +163,7 @@ __global__ __launch_bounds__(ADAMW_THREADS) void k_adamw(AdamwJob j) {
     u32 most_m = 0, most_v = 0;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-      m[i] = j.b1 * m[i] + j.c1 * g[i];
-      v[i] = j.b2 * v[i] + j.c2 * (g[i] * g[i]);
+      next_moments(m[i], v[i], g[i], j);
       most_m = max(most_m, __builtin_bit_cast(u32, m[i]) & 0x7FFFFFFFu);
       most_v = max(most_v, __builtin_bit_cast(u32, v[i]) & 0x7FFFFFFFu);
       const float ratio = m[i] / (sqrtf(v[i]) * s.root + j.eps);
@@ -194,7 +200,7 @@ __global__ __launch_bounds__(ADAMW_THREADS) void k_adamw(AdamwJob j) {
 #pragma unroll
       for (int i = 0; i < EACH; ++i) {
         const u32 r = mix(key + (u32)state + i);
-        const u32 a = FirstFormat::code(m[i], im, r & 0xFFFF), b = SecondFormat::code(v[i], iv, r >> 16);
+        const u32 a = FirstFormat::code(m[i], sm, im, r & 0xFFFF), b = SecondFormat::code(v[i], sv, iv, r >> 16);
         qm[i] = (uint8_t)(a | (__builtin_bit_cast(u32, m[i]) >> 24 & 0x80));
         qv[i] = (uint8_t)(v[i] > 0 ? max(b, 1u) : 0u);
       }

@@ -3,14 +3,19 @@
 //   z = logits / T      S = sum exp(z - m)      lse = m + log S      logp = z[token] - lse      entropy = log S + sum exp(z - m) (m - z) / S
 //   dlogits = (dlogp ([v = token] - p) - dentropy p (log p + entropy)) / T,  p = exp(z - lse)
 //
-// Memory bounds both: a row is read once (again for the alternatives, which the caches answer), a few operations and one exponential to a logit.  Largest logit, sum and
-// entropy's sum are taken in one pass: every thread takes a batch of values, moves to the batch's maximum if that is larger than its own, and
-// adds up relative to it.  The entropy's terms all have one sign, so nothing cancels.
+// Memory bounds both, the exponentials and their dozen of operations to a logit come next.  Largest logit, sum and entropy's sum are taken in one pass: a thread moves to a
+// vector's maximum if that is larger than its own, and adds up relative to it.  The entropy's terms all have one sign, so nothing cancels.  Few
+// long rows are cut into parts, one to a workgroup, which a second launch joins in their order.
 //
-// Alternatives: the `top` largest of 64 maxima of a row's parts are each at least as large as the smallest of them, which therefore bounds the row's `top` largest
-// logits from below; a second pass collects what reaches the bound (a few more than `top`, as a rule) and ranks it.  Rows of which more reaches it than there is room for, equal
-// logits by the thousand, are searched once for each alternative.
+// Alternatives: of 64 maxima of a row's disjoint shares the `top` largest are as many different logits, so the smallest of them bounds the row's `top` largest logits from
+// below.  A second pass, over a row that the caches still hold, collects what reaches the bound (a few more than `top`, as a rule) and ranks it.  Rows of which more reaches it than
+// there is room for, equal logits by the thousand, are searched once for each alternative.
+//
+// Gradient: 1 - p of a sure target needs more bits than lse has, so the sum is taken again.  Rows are held in registers in between, where they fit (131,072 values of
+// 16 bits: half of a compute unit's registers), and the next row's vectors are asked for as this row's are written, so that a row is read once and loads do
+// not stop while it is computed.
 #include <algorithm>
+#include <type_traits>
 
 #include "ccld_internal.h"
 #include "operators.h"
@@ -28,9 +33,12 @@ struct LogprobJob {
   i64 ld, ldd, dlogp_stride, dentropy_stride, rows, vocab;
   float temperature;
   int top, token_bits;
-  u32 parts;                     // workgroups to a row (gradient)
+  i64 parts, span;               // of a row, and their columns
+  float *part_sums, *part_values;        // [rows][parts][3], [rows][parts][top]
+  int* part_ids;
 };
 
+constexpr int JOIN_THREADS = 256;
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 // below 2^-200 of the largest nothing is left of a value (and a masked one stays finite)
 constexpr float NOTHING = -200.0f;
@@ -38,6 +46,14 @@ constexpr float NOTHING = -200.0f;
 __device__ __forceinline__ i64 token_of(const LogprobJob& j, i64 row) {
   const i64 t = j.token_bits == 32 ? static_cast<const int32_t*>(j.tokens)[row] : static_cast<const i64*>(j.tokens)[row];
   return t >= 0 && t < j.vocab ? t : -1;
+}
+
+template <int N>
+__device__ __forceinline__ float largest_of(const float (&z)[N]) {
+  float m = z[0];
+#pragma unroll
+  for (int i = 1; i < N; ++i) m = fmaxf(m, z[i]);
+  return m;
 }
 
 // Sums of exp2((z - m) c) and of exp2((z - m) c) (m - z) c.
@@ -52,12 +68,7 @@ struct Sums {
     m = to;
   }
   template <int N>
-  __device__ __forceinline__ void add(const float (&z)[N], float c) {
-    float most = m;
-#pragma unroll
-    for (int i = 0; i < N; ++i) most = fmaxf(most, z[i]);
-    if (most > m) move(most, c);
-    const float from = m == LOWEST ? 0.0f : m;
+  __device__ __forceinline__ void terms(const float (&z)[N], float from, float c) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const float d = (z[i] - from) * c, e = __builtin_amdgcn_exp2f(d);
@@ -65,106 +76,187 @@ struct Sums {
       b -= e * fmaxf(d, NOTHING);
     }
   }
-  __device__ __forceinline__ void join(const Sums& o, float c) {
-    const float to = fmaxf(m, o.m);
-    Sums other = o;
-    move(to, c);
-    other.move(to, c);
-    s += other.s;
-    b += other.b;
+  template <int N>
+  __device__ __forceinline__ void add(const float (&z)[N], float c) {
+    float most = m;
+#pragma unroll
+    for (int i = 0; i < N; ++i) most = fmaxf(most, z[i]);
+    if (most > m) move(most, c);
+    terms(z, m == LOWEST ? 0.0f : m, c);
   }
 };
 
-// The row's values that belong to this thread of so many, in batches: f(values, first column of each vector).
-template <class T, int THREADS, class F>
-__device__ __forceinline__ void each_batch(const T* row, i64 vocab, int me, F f) {
-  constexpr int N = 16 / sizeof(T), BATCH = 4;
-  i64 at = (i64)me * N;
-  for (; at + (i64)(BATCH - 1) * THREADS * N + N <= vocab; at += (i64)BATCH * THREADS * N) {
-    Vec<T, N> v[BATCH];
+// Rows that are read as often as they are gone through, BATCH vectors of 16 bytes to a thread at a time.  each(f) calls f(values, first column).
+template <class T, int THREADS>
+struct Streamed {
+  static constexpr int N = 16 / sizeof(T), BATCH = 4;
+  const T* row;
+  i64 vocab;
+  __device__ __forceinline__ Streamed(const T* row_, i64 vocab_) : row(row_), vocab(vocab_) {}
+  template <class F>
+  __device__ __forceinline__ void each(F f) const {
+    i64 at = (i64)threadIdx.x * N;
+    for (; at + (i64)(BATCH - 1) * THREADS * N + N <= vocab; at += (i64)BATCH * THREADS * N) {
+      Vec<T, N> v[BATCH];
 #pragma unroll
-    for (int i = 0; i < BATCH; ++i) v[i] = load_vec<N>(row + at + (i64)i * THREADS * N);
+      for (int i = 0; i < BATCH; ++i) v[i] = load_vec<N>(row + at + (i64)i * THREADS * N);
 #pragma unroll
-    for (int i = 0; i < BATCH; ++i) {
+      for (int i = 0; i < BATCH; ++i) {
+        float z[N];
+#pragma unroll
+        for (int n = 0; n < N; ++n) z[n] = (float)v[i][n];
+        f(z, at + (i64)i * THREADS * N);
+      }
+    }
+    for (; at + N <= vocab; at += (i64)THREADS * N) {
+      const Vec<T, N> v = load_vec<N>(row + at);
       float z[N];
 #pragma unroll
-      for (int n = 0; n < N; ++n) z[n] = (float)v[i][n];
-      f(z, at + (i64)i * THREADS * N);
-    }
-  }
-  for (; at < vocab; at += (i64)THREADS * N) {
-    float z[N];
-    if (at + N <= vocab) {
-      const Vec<T, N> v = load_vec<N>(row + at);
-#pragma unroll
       for (int n = 0; n < N; ++n) z[n] = (float)v[n];
-    } else {
-#pragma unroll
-      for (int n = 0; n < N; ++n) z[n] = at + n < vocab ? (float)row[at + n] : LOWEST;
+      f(z, at);
     }
-    f(z, at);
+    // (one thread has what is left of the row)
+    for (; at < vocab; ++at) {
+      const float z[1] = {(float)row[at]};
+      f(z, at);
+    }
   }
-}
+  // each(f) with the results stored to the same columns of `out`; `next` is not needed
+  template <class F>
+  __device__ __forceinline__ void write(T* out, const T*, F f) const {
+    each([&](const auto& z, i64 at) {
+      constexpr int S = sizeof(z) / sizeof(float);
+      Vec<T, S> o;
+      f(z, o);
+      store_vec<S>(out + at, o);
+    });
+  }
+  // the thread that stores a column
+  __device__ __forceinline__ int owner(int at) const { return at / N % THREADS; }
+};
 
-template <int THREADS>
-__device__ __forceinline__ Sums join_all(Sums x, float c, float (&place)[THREADS / CCLD_WAVE][3]) {
-  const float m = wave_max(x.m);
-  x.move(m, c);
-  x.s = wave_total(x.s);
-  x.b = wave_total(x.b);
-  x.m = m;
-  constexpr int WAVES = THREADS / CCLD_WAVE;
-  const int wave = threadIdx.x / CCLD_WAVE;
-  if (lane_id() == 0) { place[wave][0] = x.m; place[wave][1] = x.s; place[wave][2] = x.b; }
-  __syncthreads();
-  Sums all;
+// Rows that stay in registers.  Vectors and values behind the row's end are the lowest.
+typedef u32 words4 __attribute__((ext_vector_type(4)));
+template <class T, int THREADS, int VECS>
+struct Held {
+  static constexpr int N = 16 / sizeof(T);
+  words4 v[VECS];
+  float rest;                       // one of the values that do not fill a vector
+  int vocab;
+  __device__ __forceinline__ int whole() const { return vocab - vocab % N; }
+  __device__ __forceinline__ bool inside(int i) const {
+    return (i + 1) * THREADS * N <= vocab || (i * THREADS + (int)threadIdx.x) * N < whole();       // (the first is known to the whole workgroup)
+  }
+  // (a scalar base and 32 bits of offset: with a pointer to each vector the registers would not suffice)
+  template <class P>
+  static __device__ __forceinline__ auto place(P* row, int i) {
+    typedef typename std::conditional<std::is_const<P>::value, const char, char>::type byte;
+    return reinterpret_cast<P*>(reinterpret_cast<byte*>(row) + i * THREADS * 16 + (u32)(threadIdx.x * 16));
+  }
+  __device__ __forceinline__ void load(const T* row, int i) {
+    if (inside(i)) v[i] = __builtin_bit_cast(words4, load_vec<N>(place(row, i)));
+  }
+  __device__ __forceinline__ void load_rest(const T* row) {
+    if ((int)threadIdx.x < vocab - whole()) rest = (float)row[whole() + threadIdx.x];
+  }
+  __device__ __forceinline__ Held(const T* row, i64 vocab_) : rest(LOWEST), vocab((int)vocab_) {
 #pragma unroll
-  for (int w = 0; w < WAVES; ++w) {
-    Sums o;
-    o.m = place[w][0]; o.s = place[w][1]; o.b = place[w][2];
-    all.join(o, c);
+    for (int i = 0; i < VECS; ++i) {
+      Vec<T, N> x;
+#pragma unroll
+      for (int n = 0; n < N; ++n) x[n] = (T)LOWEST;
+      v[i] = __builtin_bit_cast(words4, x);
+      load(row, i);
+    }
+    load_rest(row);
   }
-  return all;
+  // The values of vector i.  (They stay packed from one time to the next: the compiler would unpack them once for all, into twice the registers.)
+  __device__ __forceinline__ void values(int i, float (&z)[N]) {
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      u32 x = v[i][w];
+      asm volatile("" : "+v"(x));
+      v[i][w] = x;
+    }
+    const Vec<T, N> x = __builtin_bit_cast(Vec<T, N>, v[i]);
+#pragma unroll
+    for (int n = 0; n < N; ++n) z[n] = (float)x[n];
+  }
+  template <class F>
+  __device__ __forceinline__ void each(F f) {
+#pragma unroll
+    for (int i = 0; i < VECS; ++i) {
+      float z[N];
+      values(i, z);
+      f(z, (i * THREADS + (int)threadIdx.x) * N);
+      __builtin_amdgcn_sched_barrier(0);          // one vector after another: what they need together would not fit
+    }
+    const float z[1] = {rest};
+    f(z, (int)threadIdx.x < vocab - whole() ? whole() + (int)threadIdx.x : vocab);
+  }
+  // Results stored to the same columns of `out`; each vector makes room for the next row's, if there is one.
+  template <class F>
+  __device__ __forceinline__ void write(T* out, const T* next, F f) {
+#pragma unroll
+    for (int i = 0; i < VECS; ++i) {
+      float z[N];
+      values(i, z);
+      Vec<T, N> o;
+      f(z, o);
+      if (inside(i)) store_vec<N>(place(out, i), o);
+      if (next) load(next, i);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    const float z[1] = {rest};
+    Vec<T, 1> o;
+    f(z, o);
+    if ((int)threadIdx.x < vocab - whole()) out[whole() + threadIdx.x] = o[0];
+    if (next) load_rest(next);
+  }
+  __device__ __forceinline__ int owner(int at) const { return at < whole() ? at / N % THREADS : at - whole(); }
+};
+template <class T, int THREADS, int VECS>
+struct RowOf { typedef Held<T, THREADS, VECS> type; };
+template <class T, int THREADS>
+struct RowOf<T, THREADS, 0> { typedef Streamed<T, THREADS> type; };
+
+// The largest of the workgroup's values and their sum.  place: of this call alone between two barriers of the caller's.
+template <int THREADS>
+__device__ __forceinline__ float max_of_all(float v, float (&place)[16]) {
+  v = wave_max(v);
+  if (lane_id() == 0) place[threadIdx.x / CCLD_WAVE] = v;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < THREADS / CCLD_WAVE; ++w) v = fmaxf(v, place[w]);
+  return v;
+}
+template <int THREADS>
+__device__ __forceinline__ float sum_of_all(float v, float (&place)[16]) {
+  v = wave_total(v);
+  if (lane_id() == 0) place[threadIdx.x / CCLD_WAVE] = v;
+  __syncthreads();
+  v = 0;
+#pragma unroll
+  for (int w = 0; w < THREADS / CCLD_WAVE; ++w) v += place[w];
+  return v;
 }
 
-constexpr int ROOM = 1024;
+// The `top` largest values of a row, equal ones by the lower column: put(rank, value, column), column -1 for what is not there.
+template <int THREADS, int ROOM>
+struct Alternatives {
+  float maxima[THREADS], value[ROOM];
+  int id[ROOM > THREADS ? ROOM : THREADS];
+  u32 found;
+  float bound;
 
-template <class T, int THREADS>
-__global__ __launch_bounds__(THREADS) void k_logprobs(LogprobJob j) {
-  __shared__ float place[THREADS / CCLD_WAVE][3];
-  __shared__ float maxima[THREADS], value[ROOM];
-  __shared__ int id[ROOM];
-  __shared__ u32 found;
-  __shared__ float bound;
-  const float c = LOG2E / j.temperature;
-  const int me = threadIdx.x;
-  for (i64 r = blockIdx.x; r < j.rows; r += gridDim.x) {
-    const T* const row = static_cast<const T*>(j.logits) + r * j.ld;
-    Sums x;
-    float most = LOWEST;
-    each_batch<T, THREADS>(row, j.vocab, me, [&](const auto& z, i64) { x.add(z, c); });
-    most = x.m;
+  // all threads call this; most: the largest of the thread's values
+  template <class ROW, class PUT>
+  __device__ __forceinline__ void find(ROW row, float most, int top, PUT put) {
+    const int me = threadIdx.x;
     __syncthreads();                        // the row before is done with
     if (me == 0) found = 0;
     maxima[me] = most;
-    const Sums all = join_all<THREADS>(x, c, place);
-    const bool none = all.m == LOWEST && all.s == 0;
-    // (a row that is not empty has a finite lse, at a low temperature too, by which the gradient knows it; NaN stays)
-    const float log_s = logf(all.s);
-    float lse = none ? LOWEST : all.m / j.temperature + log_s;
-    if (!none && fabsf(lse) > __FLT_MAX__) lse = copysignf(__FLT_MAX__, lse);
-    if (me == 0) {
-      const i64 t = token_of(j, r);
-      float logp = 0;
-      if (t >= 0) {
-        const float z = (float)row[t];
-        logp = z == LOWEST && all.s == all.s ? LOWEST : (z - all.m) / j.temperature - log_s;
-      }
-      j.logp[r] = logp;
-      j.lse[r] = lse;
-      j.entropy[r] = none ? 0.0f : log_s + all.b * LN2 / all.s;
-    }
-    if (j.top == 0) continue;
+    __syncthreads();
     // 64 maxima: the bound is the one with top - 1 before it
     if (me < CCLD_WAVE) {
       float mine = LOWEST;
@@ -174,57 +266,51 @@ __global__ __launch_bounds__(THREADS) void k_logprobs(LogprobJob j) {
         const float o = read_lane(mine, l);
         before += o > mine || (o == mine && l < me);
       }
-      if (before == j.top - 1) bound = mine;
+      if (before == top - 1) bound = mine;
     }
     __syncthreads();
     const float least = bound;
-    each_batch<T, THREADS>(row, j.vocab, me, [&](const auto& z, i64 at) {
-      constexpr int N = 16 / sizeof(T);
-      float most = z[0];
+    if (most >= least && most > LOWEST)
+      row.each([&](const auto& z, i64 at) {
+        const float largest = largest_of(z);
+        if (largest >= least && largest > LOWEST) {
 #pragma unroll
-      for (int n = 1; n < N; ++n) most = fmaxf(most, z[n]);
-      if (most >= least && most > LOWEST) {
-        for (int n = 0; n < N; ++n)
-          if (z[n] >= least && z[n] > LOWEST) {
-            const u32 to = atomicAdd(&found, 1u);
-            if (to < ROOM) { value[to] = z[n]; id[to] = (int)(at + n); }
-          }
-      }
-    });
+          for (int n = 0; n < (int)(sizeof(z) / sizeof(float)); ++n)
+            if (z[n] >= least && z[n] > LOWEST) {
+              const u32 to = atomicAdd(&found, 1u);
+              if (to < ROOM) { value[to] = z[n]; id[to] = (int)at + n; }
+            }
+        }
+      });
     __syncthreads();
     const u32 n = found;
-    int32_t* const ids = j.top_ids + r * j.top;
-    float* const logps = j.top_logp + r * j.top;
-    auto put = [&](int rank, float z, int at) {
-      ids[rank] = at;
-      logps[rank] = at < 0 ? LOWEST : (z - all.m) / j.temperature - log_s;
-    };
     if (n <= ROOM) {
       for (u32 i = me; i < n; i += THREADS) {
         const float z = value[i];
         const int at = id[i];
         int rank = 0;
         for (u32 o = 0; o < n; ++o) rank += value[o] > z || (value[o] == z && id[o] < at);
-        if (rank < j.top) put(rank, z, at);
+        if (rank < top) put(rank, z, at);
       }
-      for (int i = me; i < j.top; i += THREADS)
-        if (i >= (int)n) put(i, 0, -1);
+      for (int i = me; i < top; i += THREADS)
+        if (i >= (int)n) put(i, LOWEST, -1);
     } else {
       // one after another: the largest of those that come after the one before
       float last = __builtin_huge_valf();
-      i64 last_at = -1;
-      for (int k = 0; k < j.top; ++k) {
+      int last_at = -1;
+      for (int k = 0; k < top; ++k) {
         float best = LOWEST;
-        i64 best_at = j.vocab;
-        each_batch<T, THREADS>(row, j.vocab, me, [&](const auto& z, i64 at) {
-          constexpr int N = 16 / sizeof(T);
+        int best_at = 0x7FFFFFFF;
+        row.each([&](const auto& z, i64 at) {
 #pragma unroll
-          for (int n = 0; n < N; ++n)
-            if ((z[n] < last || (z[n] == last && at + n > last_at)) && z[n] > best) { best = z[n]; best_at = at + n; }
+          for (int n = 0; n < (int)(sizeof(z) / sizeof(float)); ++n) {
+            const int c = (int)at + n;
+            if ((z[n] < last || (z[n] == last && c > last_at)) && (z[n] > best || (z[n] == best && c < best_at))) { best = z[n]; best_at = c; }
+          }
         });
         __syncthreads();
         maxima[me] = best;
-        id[me] = (int)best_at;
+        id[me] = best_at;
         __syncthreads();
         for (int half = THREADS / 2; half >= 1; half /= 2) {
           if (me < half) {
@@ -236,58 +322,159 @@ __global__ __launch_bounds__(THREADS) void k_logprobs(LogprobJob j) {
         }
         last = maxima[0];
         last_at = id[0];
-        if (me == 0) put(k, last, last == LOWEST ? -1 : (int)last_at);
+        if (me == 0) put(k, last, last == LOWEST ? -1 : last_at);
       }
+    }
+  }
+};
+
+// what a row's sums say
+struct Values {
+  float m, per, log_s, lse, entropy;
+  bool nan;
+  __device__ __forceinline__ Values(const Sums& x, float temperature) : m(x.m), nan(x.s != x.s) {
+    const bool none = x.m == LOWEST && x.s == 0;
+    per = temperature;
+    log_s = logf(x.s);
+    // (a row that is not empty has a finite lse, at a low temperature too, by which the gradient knows it; NaN stays)
+    lse = none ? LOWEST : m / temperature + log_s;
+    if (!none && fabsf(lse) > __FLT_MAX__) lse = copysignf(__FLT_MAX__, lse);
+    entropy = none ? 0.0f : log_s + x.b * LN2 / x.s;
+  }
+  __device__ __forceinline__ float logp(float z) const { return z == LOWEST && !nan ? LOWEST : (z - m) / per - log_s; }
+};
+template <class T>
+__device__ __forceinline__ void put_values(const LogprobJob& j, i64 r, const Values& v) {
+  const i64 t = token_of(j, r);
+  j.logp[r] = t < 0 ? 0.0f : v.logp((float)static_cast<const T*>(j.logits)[r * j.ld + t]);
+  j.lse[r] = v.lse;
+  j.entropy[r] = v.entropy;
+}
+
+// A row, or (j.parts > 1) a part of one, to a workgroup.
+constexpr int ROOM = 1024;
+template <class T, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_logprobs(LogprobJob j) {
+  __shared__ float places[3][16];
+  __shared__ Alternatives<THREADS, ROOM> alternatives;
+  const float c = LOG2E / j.temperature;
+  for (i64 b = blockIdx.x; b < j.rows * j.parts; b += gridDim.x) {
+    const i64 r = b / j.parts, start = (b - r * j.parts) * j.span;
+    const Streamed<T, THREADS> row(static_cast<const T*>(j.logits) + r * j.ld + start, min(j.span, j.vocab - start));
+    Sums x;
+    row.each([&](const auto& z, i64) { x.add(z, c); });
+    const float most = x.m;
+    __syncthreads();                        // the row before is done with
+    x.move(max_of_all<THREADS>(most, places[0]), c);
+    x.s = sum_of_all<THREADS>(x.s, places[1]);
+    x.b = sum_of_all<THREADS>(x.b, places[2]);
+    if (j.parts > 1) {
+      if (threadIdx.x == 0) { j.part_sums[3 * b] = x.m; j.part_sums[3 * b + 1] = x.s; j.part_sums[3 * b + 2] = x.b; }
+      if (j.top)
+        alternatives.find(row, most, j.top, [&](int rank, float z, int at) {
+          j.part_values[b * j.top + rank] = z;
+          j.part_ids[b * j.top + rank] = at < 0 ? -1 : (int)start + at;
+        });
+    } else {
+      const Values v(x, j.temperature);
+      if (threadIdx.x == 0) put_values<T>(j, r, v);
+      if (j.top)
+        alternatives.find(row, most, j.top, [&](int rank, float z, int at) {
+          j.top_ids[r * j.top + rank] = at;
+          j.top_logp[r * j.top + rank] = at < 0 ? LOWEST : v.logp(z);
+        });
     }
   }
 }
 
-// lse of a row far from zero has too few bits behind the point to take exp(z - lse) with (at 64 p is off by 2^-18): the row's maximum and sum are taken
-// again there.
-constexpr float FAR = 64.0f;
+// The alternatives of a row's parts, as a row.
+struct Candidates {
+  const float* value;
+  const int* id;
+  int n;
+  template <class F>
+  __device__ __forceinline__ void each(F f) const {
+    for (int i = threadIdx.x; i < n; i += JOIN_THREADS) {
+      const float z[1] = {value[i]};
+      f(z, (i64)id[i]);
+    }
+  }
+};
+template <class T>
+__global__ __launch_bounds__(JOIN_THREADS) void k_logprobs_join(LogprobJob j) {
+  __shared__ Alternatives<JOIN_THREADS, ROOM> alternatives;
+  const float c = LOG2E / j.temperature;
+  for (i64 r = blockIdx.x; r < j.rows; r += gridDim.x) {
+    // every wavefront by itself: a part to a lane
+    Sums x;
+    const u32 part = lane_id();
+    if (part < j.parts) {
+      const float* const at = j.part_sums + 3 * (r * j.parts + part);
+      x.m = at[0]; x.s = at[1]; x.b = at[2];
+    }
+    x.move(wave_max(x.m), c);
+    x.s = wave_total(x.s);
+    x.b = wave_total(x.b);
+    const Values v(x, j.temperature);
+    if (threadIdx.x == 0) put_values<T>(j, r, v);
+    if (!j.top) continue;
+    const i64 first = r * j.parts * j.top;
+    const Candidates row{j.part_values + first, j.part_ids + first, (int)j.parts * j.top};
+    float most = LOWEST;
+    row.each([&](const auto& z, i64) { most = fmaxf(most, z[0]); });
+    alternatives.find(row, most, j.top, [&](int rank, float z, int at) {
+      j.top_ids[r * j.top + rank] = at;
+      j.top_logp[r * j.top + rank] = at < 0 ? LOWEST : v.logp(z);
+    });
+  }
+}
 
-template <class T, int THREADS>
+// lse says where to measure from.  Beyond 2^20 it does not say it well enough and the largest logit is looked for.
+constexpr float FAR = 0x1p20f;
+
+template <class T, int THREADS, int VECS>
 __global__ __launch_bounds__(THREADS) void k_logprobs_grad(LogprobJob j) {
-  constexpr int N = 16 / sizeof(T);
-  __shared__ float place[THREADS / CCLD_WAVE][3];
+  __shared__ float places[2][2][16];
   const float c = LOG2E / j.temperature, per = 1.0f / j.temperature;
-  const i64 all = j.rows * j.parts;
-  for (i64 b = blockIdx.x; b < all; b += gridDim.x) {
-    const i64 r = b / j.parts;
-    const u32 part = (u32)(b - r * j.parts);
-    const T* const row = static_cast<const T*>(j.logits) + r * j.ld;
+  int turn = 0;
+  i64 r = blockIdx.x;
+  const T* logits = static_cast<const T*>(j.logits) + r * j.ld;
+  typename RowOf<T, THREADS, VECS>::type held(logits, j.vocab);
+  for (; r < j.rows; r += gridDim.x) {
+    const T* const next = r + gridDim.x < j.rows ? logits + gridDim.x * j.ld : nullptr;
     T* const out = static_cast<T*>(j.dlogits) + r * j.ldd;
     const float lse = j.lse[r], entropy = j.entropy[r];
-    const i64 t = token_of(j, r);
-    const float dl = t >= 0 && j.dlogp ? j.dlogp[r * j.dlogp_stride] : 0.0f, de = j.dentropy ? j.dentropy[r * j.dentropy_stride] : 0.0f;
-    // log p = (z - base) c2 - rest, in powers of two
-    float base = 0, rest = lse * LOG2E;
+    const int t = (int)token_of(j, r);
     const bool none = lse == LOWEST;
-    if (fabsf(lse) >= FAR && !none) {
-      Sums x;
-      each_batch<T, THREADS>(row, j.vocab, threadIdx.x, [&](const auto& z, i64) { x.add(z, c); });
-      __syncthreads();
-      const Sums sums = join_all<THREADS>(x, c, place);
-      base = sums.m;
-      rest = log2f(sums.s);
-    }
-    auto gradient = [&](float z, bool target) {
-      if (none) return 0.0f;
-      const float d = (z - base) * c - rest, p = __builtin_amdgcn_exp2f(d);
-      const float g = (target ? dl : 0.0f) - p * (dl + de * (fmaxf(d, NOTHING) * LN2 + entropy));
-      return g * per;
-    };
-    for (i64 at = ((i64)part * THREADS + threadIdx.x) * N; at < j.vocab; at += (i64)j.parts * THREADS * N) {
-      if (at + N <= j.vocab) {
-        const Vec<T, N> v = load_vec<N>(row + at);
-        Vec<T, N> o;
-#pragma unroll
-        for (int n = 0; n < N; ++n) o[n] = (T)gradient((float)v[n], at + n == t);
-        store_vec<N>(out + at, o);
-      } else {
-        for (i64 k = at; k < j.vocab; ++k) out[k] = (T)gradient((float)row[k], k == t);
+    const float dl = !none && t >= 0 && j.dlogp ? j.dlogp[r * j.dlogp_stride] : 0.0f, de = !none && j.dentropy ? j.dentropy[r * j.dentropy_stride] : 0.0f;
+    float from = none ? 0.0f : lse * j.temperature, s = 0, rest = 0;
+    if (!none) {
+      if (!(fabsf(lse) < FAR)) {
+        float m = LOWEST;
+        held.each([&](const auto& z, auto) { m = fmaxf(m, largest_of(z)); });
+        from = max_of_all<THREADS>(m, places[turn][1]);
       }
+      held.each([&](const auto& z, auto) {
+#pragma unroll
+        for (int n = 0; n < (int)(sizeof(z) / sizeof(float)); ++n) s += __builtin_amdgcn_exp2f((z[n] - from) * c);
+      });
+      rest = log2f(sum_of_all<THREADS>(s, places[turn][0]));
+      turn ^= 1;                            // (a place is written again behind the next row's barrier)
     }
+    // dlogits without the target's own: -p (k0 + k1 log2 p)
+    const float k0 = -(none ? 0.0f : dl + de * entropy) * per, k1 = -de * LN2 * per;
+    auto gradient = [&](float z) {
+      const float d = (z - from) * c - rest;
+      return __builtin_amdgcn_exp2f(d) * (k1 * fmaxf(d, NOTHING) + k0);
+    };
+    held.write(out, next, [&](const auto& z, auto& o) {
+#pragma unroll
+      for (int n = 0; n < (int)(sizeof(z) / sizeof(float)); ++n) o[n] = (T)gradient(z[n]);
+    });
+    // (behind the same thread's store to the same place)
+    if (t >= 0 && (int)threadIdx.x == held.owner(t)) out[t] = (T)(dl * per + gradient((float)logits[t]));
+    if constexpr (VECS == 0) held.row = next;
+    logits = next;
   }
 }
 
@@ -300,8 +487,49 @@ ccld_status check(const ccld_logprob_args* a) {
 }
 LogprobJob make_job(const ccld_logprob_args* a) {
   return LogprobJob{a->logits, a->tokens, a->logp, a->entropy, a->lse, a->top_logp, a->top_ids, a->dlogp, a->dentropy, a->dlogits, a->ldlogits, a->lddlogits,
-                    a->dlogp_stride, a->dentropy_stride, a->rows, a->vocab, a->temperature, a->top, a->token_bits, 1};
+                    a->dlogp_stride, a->dentropy_stride, a->rows, a->vocab, a->temperature, a->top, a->token_bits, 1, a->vocab};
 }
+// Few rows are cut into parts of two vectors to a thread and more, so that there are two workgroups to a compute unit.
+constexpr i64 MOST_PARTS = CCLD_WAVE;
+constexpr int THREADS = 256;
+void cut_rows(LogprobJob& j, int32_t dtype, uint8_t* workspace, uint64_t* bytes) {
+  const i64 n = 16 / size_of(dtype), vectors = blocks_for(j.vocab, n);
+  j.parts = std::max<i64>(1, std::min({MOST_PARTS, vectors / (2 * THREADS), 2 * (i64)COMPUTE_UNITS / std::max<i64>(j.rows, 1)}));
+  *bytes = 0;
+  if (j.parts == 1) return;
+  j.span = blocks_for(vectors, j.parts) * n;
+  j.parts = blocks_for(j.vocab, j.span);
+  auto take = [&](i64 each) {
+    uint8_t* const at = workspace ? workspace + *bytes : nullptr;
+    *bytes += ((uint64_t)(j.rows * j.parts * each) + 255) & ~(uint64_t)255;
+    return at;
+  };
+  j.part_sums = reinterpret_cast<float*>(take(12));
+  j.part_values = reinterpret_cast<float*>(take(4 * j.top));
+  j.part_ids = reinterpret_cast<int*>(take(4 * j.top));
+}
+
+template <class T, int THREADS, int VECS>
+void launch_grad(const LogprobJob& j, hipStream_t stream) {
+  // 16 wavefronts to a compute unit, each workgroup with rows one after another
+  const i64 most = VECS >= 8 ? (i64)COMPUTE_UNITS * 1024 / THREADS : 1 << 20;
+  k_logprobs_grad<T, THREADS, VECS><<<(u32)std::min(j.rows, most), THREADS, 0, stream>>>(j);
+}
+// the smallest form that holds a row
+template <class T>
+void launch_grad(const LogprobJob& j, hipStream_t stream) {
+  constexpr i64 N = 16 / sizeof(T);
+  const i64 vectors = blocks_for(j.vocab, N);
+  if (vectors <= 256) launch_grad<T, 256, 1>(j, stream);
+  else if (vectors <= 256 * 4) launch_grad<T, 256, 4>(j, stream);
+  else if (vectors <= 256 * 8) launch_grad<T, 256, 8>(j, stream);
+  else if (vectors <= 256 * 16) launch_grad<T, 256, 16>(j, stream);
+  else if (vectors <= 512 * 16) launch_grad<T, 512, 16>(j, stream);
+  else if (vectors <= 1024 * 16) launch_grad<T, 1024, 16>(j, stream);
+  else if (j.rows < 2 * (i64)COMPUTE_UNITS) launch_grad<T, 1024, 0>(j, stream);
+  else launch_grad<T, 256, 0>(j, stream);
+}
+
 bool all_aligned(const ccld_logprob_args* a) {
   for (const void* p : {static_cast<const void*>(a->logp), static_cast<const void*>(a->entropy), static_cast<const void*>(a->lse), static_cast<const void*>(a->top_ids),
                         static_cast<const void*>(a->top_logp), static_cast<const void*>(a->dlogp), static_cast<const void*>(a->dentropy)})
@@ -313,8 +541,11 @@ bool all_aligned(const ccld_logprob_args* a) {
 
 extern "C" ccld_status ccld_logprob_workspace(const ccld_logprob_args* a, uint64_t* bytes) {
   if (!bytes) return CCLD_E_NULL;
-  *bytes = 0;
-  return check(a);
+  const ccld_status s = check(a);
+  if (s != CCLD_OK) return s;
+  LogprobJob j = make_job(a);
+  cut_rows(j, a->dtype, nullptr, bytes);
+  return CCLD_OK;
 }
 
 extern "C" ccld_status ccld_token_logprobs(const ccld_logprob_args* a, void* stream) {
@@ -323,12 +554,16 @@ extern "C" ccld_status ccld_token_logprobs(const ccld_logprob_args* a, void* str
   if (a->rows && (!a->logits || !a->tokens || !a->logp || !a->entropy || !a->lse || (a->top && (!a->top_ids || !a->top_logp)))) return CCLD_E_NULL;
   if (a->ldlogits < a->vocab || !all_aligned(a)) return CCLD_E_BAD_ARG;
   if (a->rows == 0) return CCLD_OK;
-  const LogprobJob j = make_job(a);
-  const u32 grid = (u32)std::min<i64>(a->rows, 1 << 20);
+  LogprobJob j = make_job(a);
+  uint64_t need;
+  cut_rows(j, a->dtype, static_cast<uint8_t*>(a->workspace), &need);
+  if (need && (need > a->workspace_bytes || !a->workspace || !aligned(a->workspace, 256))) return CCLD_E_WORKSPACE;
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  const u32 grid = (u32)std::min<i64>(j.rows * j.parts, 1 << 20);
   with_type(a->dtype, [&](auto zero) {
     using T = decltype(zero);
-    if (a->rows < (i64)2 * COMPUTE_UNITS) k_logprobs<T, 1024><<<grid, 1024, 0, static_cast<hipStream_t>(stream)>>>(j);
-    else k_logprobs<T, 256><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(j);
+    k_logprobs<T, THREADS><<<grid, THREADS, 0, st>>>(j);
+    if (j.parts > 1) k_logprobs_join<T><<<(u32)j.rows, JOIN_THREADS, 0, st>>>(j);
   });
   return launched();
 }
@@ -339,12 +574,6 @@ extern "C" ccld_status ccld_token_logprobs_grad(const ccld_logprob_args* a, void
   if (a->rows && (!a->logits || !a->tokens || !a->entropy || !a->lse || !a->dlogits)) return CCLD_E_NULL;
   if (a->ldlogits < a->vocab || a->lddlogits < a->vocab || !all_aligned(a)) return CCLD_E_BAD_ARG;
   if (a->rows == 0) return CCLD_OK;
-  LogprobJob j = make_job(a);
-  constexpr int THREADS = 256;
-  // eight workgroups to a compute unit, and two vectors to a thread at least
-  const i64 vectors = blocks_for(a->vocab, 16 / size_of(a->dtype));
-  j.parts = (u32)std::max<i64>(1, std::min<i64>(blocks_for(8 * COMPUTE_UNITS, a->rows), vectors / (2 * THREADS)));
-  const u32 grid = (u32)std::min<i64>(a->rows * j.parts, 1 << 20);
-  with_type(a->dtype, [&](auto zero) { k_logprobs_grad<decltype(zero), THREADS><<<grid, THREADS, 0, static_cast<hipStream_t>(stream)>>>(j); });
+  with_type(a->dtype, [&](auto zero) { launch_grad<decltype(zero)>(make_job(a), static_cast<hipStream_t>(stream)); });
   return launched();
 }
