@@ -7,7 +7,7 @@
 // vector's maximum if that is larger than its own, and adds up relative to it.  The entropy's terms all have one sign, so nothing cancels.  Few
 // long rows are cut into parts, one to a workgroup, which a second launch joins in their order.
 //
-// Alternatives: of 64 maxima of a row's disjoint shares the `top` largest are as many different logits, so the smallest of them bounds the row's `top` largest logits from
+// Alternatives: of the threads' maxima the `top` largest are as many different logits, so the smallest of them bounds the row's `top` largest logits from
 // below.  A second pass, over a row that the caches still hold, collects what reaches the bound (a few more than `top`, as a rule) and ranks it.  Rows of which more reaches it than
 // there is room for, equal logits by the thousand, are searched once for each alternative.
 //
@@ -241,35 +241,45 @@ __device__ __forceinline__ float sum_of_all(float v, float (&place)[16]) {
   return v;
 }
 
+// A value and its column as a number that is larger for larger values and, where these are equal, for lower columns.
+__device__ __forceinline__ u64 key_of(float z, int at) {
+  const u32 bits = __builtin_bit_cast(u32, z + 0.0f);           // one zero
+  return (u64)(bits ^ (bits >> 31 ? ~0u : 0x80000000u)) << 32 | (u32)~at;
+}
+__device__ __forceinline__ float value_of(u64 key) {
+  const u32 bits = (u32)(key >> 32);
+  return __builtin_bit_cast(float, bits ^ (bits >> 31 ? 0x80000000u : ~0u));
+}
+__device__ __forceinline__ int column_of(u64 key) { return (int)~(u32)key; }
+
 // The `top` largest values of a row, equal ones by the lower column: put(rank, value, column), column -1 for what is not there.
-template <int THREADS, int ROOM>
+template <int THREADS>
 struct Alternatives {
-  float maxima[THREADS], value[ROOM];
-  int id[ROOM > THREADS ? ROOM : THREADS];
+  static constexpr int ROOM = 1024;
+  uint4 maxima[THREADS / 4];
+  u64 key[ROOM], best[THREADS / CCLD_WAVE];
   u32 found;
-  float bound;
 
   // all threads call this; most: the largest of the thread's values
   template <class ROW, class PUT>
   __device__ __forceinline__ void find(ROW row, float most, int top, PUT put) {
+    static_assert(THREADS == 4 * CCLD_WAVE && THREADS >= CCLD_TOP_MOST, "four maxima to a lane, as many as alternatives");
     const int me = threadIdx.x;
     __syncthreads();                        // the row before is done with
     if (me == 0) found = 0;
-    maxima[me] = most;
+    reinterpret_cast<u32*>(maxima)[me] = (u32)(key_of(most, 0) >> 32);
     __syncthreads();
-    // 64 maxima: the bound is the one with top - 1 before it
-    if (me < CCLD_WAVE) {
-      float mine = LOWEST;
-      for (int i = me; i < THREADS; i += CCLD_WAVE) mine = fmaxf(mine, maxima[i]);
-      int before = 0;
-      for (int l = 0; l < CCLD_WAVE; ++l) {
-        const float o = read_lane(mine, l);
-        before += o > mine || (o == mine && l < me);
-      }
-      if (before == top - 1) bound = mine;
+    // The largest number of 16 bits that at least `top` maxima reach, bit by bit, in every wavefront by itself (counting for each maximum those before it took 3 us).
+    const uint4 o = maxima[lane_id()];
+    u32 reached = 0;
+#pragma unroll
+    for (int bit = 31; bit >= 16; --bit) {
+      const u32 more = reached | 1u << bit;
+      const int n = __builtin_popcountll(ballot64(o.x >= more)) + __builtin_popcountll(ballot64(o.y >= more)) +
+                    __builtin_popcountll(ballot64(o.z >= more)) + __builtin_popcountll(ballot64(o.w >= more));
+      reached = n >= top ? more : reached;
     }
-    __syncthreads();
-    const float least = bound;
+    const float least = reached <= (u32)(key_of(LOWEST, 0) >> 32) ? LOWEST : value_of((u64)reached << 32);
     if (most >= least && most > LOWEST)
       row.each([&](const auto& z, i64 at) {
         const float largest = largest_of(z);
@@ -278,7 +288,7 @@ struct Alternatives {
           for (int n = 0; n < (int)(sizeof(z) / sizeof(float)); ++n)
             if (z[n] >= least && z[n] > LOWEST) {
               const u32 to = atomicAdd(&found, 1u);
-              if (to < ROOM) { value[to] = z[n]; id[to] = (int)at + n; }
+              if (to < ROOM) key[to] = key_of(z[n], (int)at + n);
             }
         }
       });
@@ -286,43 +296,33 @@ struct Alternatives {
     const u32 n = found;
     if (n <= ROOM) {
       for (u32 i = me; i < n; i += THREADS) {
-        const float z = value[i];
-        const int at = id[i];
+        const u64 mine = key[i];
         int rank = 0;
-        for (u32 o = 0; o < n; ++o) rank += value[o] > z || (value[o] == z && id[o] < at);
-        if (rank < top) put(rank, z, at);
+#pragma unroll 8
+        for (u32 o = 0; o < n; ++o) rank += key[o] > mine;
+        if (rank < top) put(rank, value_of(mine), column_of(mine));
       }
       for (int i = me; i < top; i += THREADS)
         if (i >= (int)n) put(i, LOWEST, -1);
     } else {
       // one after another: the largest of those that come after the one before
-      float last = __builtin_huge_valf();
-      int last_at = -1;
+      u64 last = ~0ull;
       for (int k = 0; k < top; ++k) {
-        float best = LOWEST;
-        int best_at = 0x7FFFFFFF;
+        u64 next = 0;
         row.each([&](const auto& z, i64 at) {
 #pragma unroll
           for (int n = 0; n < (int)(sizeof(z) / sizeof(float)); ++n) {
-            const int c = (int)at + n;
-            if ((z[n] < last || (z[n] == last && c > last_at)) && (z[n] > best || (z[n] == best && c < best_at))) { best = z[n]; best_at = c; }
+            const u64 x = key_of(z[n], (int)at + n);
+            if (z[n] > LOWEST && x < last && x > next) next = x;
           }
         });
+        next = wave_max_u64(next);
         __syncthreads();
-        maxima[me] = best;
-        id[me] = best_at;
+        if (lane_id() == 0) best[me / CCLD_WAVE] = next;
         __syncthreads();
-        for (int half = THREADS / 2; half >= 1; half /= 2) {
-          if (me < half) {
-            const float o = maxima[me + half];
-            const int at = id[me + half];
-            if (o > maxima[me] || (o == maxima[me] && at < id[me])) { maxima[me] = o; id[me] = at; }
-          }
-          __syncthreads();
-        }
-        last = maxima[0];
-        last_at = id[0];
-        if (me == 0) put(k, last, last == LOWEST ? -1 : last_at);
+        for (int w = 0; w < THREADS / CCLD_WAVE; ++w) next = max(next, best[w]);
+        last = next;
+        if (me == 0) put(k, next ? value_of(next) : LOWEST, next ? column_of(next) : -1);
       }
     }
   }
@@ -352,11 +352,10 @@ __device__ __forceinline__ void put_values(const LogprobJob& j, i64 r, const Val
 }
 
 // A row, or (j.parts > 1) a part of one, to a workgroup.
-constexpr int ROOM = 1024;
 template <class T, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_logprobs(LogprobJob j) {
   __shared__ float places[3][16];
-  __shared__ Alternatives<THREADS, ROOM> alternatives;
+  __shared__ Alternatives<THREADS> alternatives;
   const float c = LOG2E / j.temperature;
   for (i64 b = blockIdx.x; b < j.rows * j.parts; b += gridDim.x) {
     const i64 r = b / j.parts, start = (b - r * j.parts) * j.span;
@@ -402,7 +401,7 @@ struct Candidates {
 };
 template <class T>
 __global__ __launch_bounds__(JOIN_THREADS) void k_logprobs_join(LogprobJob j) {
-  __shared__ Alternatives<JOIN_THREADS, ROOM> alternatives;
+  __shared__ Alternatives<JOIN_THREADS> alternatives;
   const float c = LOG2E / j.temperature;
   for (i64 r = blockIdx.x; r < j.rows; r += gridDim.x) {
     // every wavefront by itself: a part to a lane
