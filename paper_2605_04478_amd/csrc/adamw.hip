@@ -10,8 +10,7 @@
 // States in 8 bits: blocks of 256 elements (32 lanes with 8 each) share a scale.  m is an e4m3, v an e5m2 number: a block in which one gradient is
 // thousands of times the others' must not lift the others' v, for which its 32 powers of two matter more than a bit of precision.  Rounding to nearest would not
 // follow b2 = 0.999, whose steps are a hundredth of what two or three bits tell apart; values are rounded up or down at random, with the odds that keep
-// the mean.  Both formats' values are those of 32-bit floats whose exponents and mantissas are cut, once they are scaled so that the formats' smallest exponent
-// is that of a float: numbers below it are subnormal in both, and an addition of random bits below the cut rounds.
+// the mean.  The card converts and rounds both formats.
 #include <algorithm>
 
 #include <math.h>
@@ -26,6 +25,7 @@ namespace {
 constexpr int BLOCK = CCLD_ADAMW_BLOCK, ADAMW_THREADS = 256;
 constexpr int EACH = 8;                                  // neighbouring elements of a thread
 constexpr int PASSES = 2, CHUNK = ADAMW_THREADS * EACH * PASSES;
+typedef u32 Words __attribute__((ext_vector_type(EACH / 4), aligned(4)));      // 8-bit values
 constexpr int LISTED = 112;                              // tensors of a launch: its arguments have 4 KB
 
 // What a step's elements share.
@@ -38,6 +38,7 @@ struct AdamwJob {
   void *m, *v;
   float *m_scale, *v_scale, *master;
   float b1, b2, c1, c2, eps;
+  float up;                      // v is multiplied by it before the root is taken
   int n_tensors;
 };
 static_assert(sizeof(AdamwJob) <= 4096, "arguments of a launch");
@@ -53,14 +54,14 @@ struct BeginJob {
   i64* count;
   const float* scale_by;
   Step* step;
-  double lr, b1, b2, weight_decay, scale;
+  double lr, b1, b2, weight_decay, scale, up;
   u64 seed;
 };
 __global__ void k_adamw_begin(BeginJob j) {
   const i64 t = ++*j.count;
   Step s;
   s.step_size = (float)(j.lr / (1.0 - pow(j.b1, (double)t)));
-  s.root = (float)(1.0 / sqrt(1.0 - pow(j.b2, (double)t)));
+  s.root = (float)(1.0 / sqrt(j.up * (1.0 - pow(j.b2, (double)t))));
   // (1 - lr wd would lose most of lr wd's bits in 32 of them)
   s.decay = (float)(j.lr * j.weight_decay);
   s.scale = (float)(j.scale_by ? j.scale * (double)*j.scale_by : j.scale);
@@ -68,28 +69,32 @@ __global__ void k_adamw_begin(BeginJob j) {
   *j.step = s;
 }
 
-// One of the two formats: BITS of mantissa, the smallest normal value 2^LEAST, the largest MOST with code TOP.
-template <int BITS, int LEAST, int TOP>
-struct Format {
-  static constexpr int CUT = 23 - BITS;
-  // the code of |x| by `random`, 16 bits; inverse: 1 / scale, whose rounding a step of the division's remainder takes out again
-  static __device__ __forceinline__ u32 code(float x, float scale, float inverse, u32 random) {
-    const float a = fabsf(x), first = a * inverse, q = fmaf(fmaf(-first, scale, a), inverse, first) * __builtin_ldexpf(1.0f, -126 - LEAST);
-    return min((__builtin_bit_cast(u32, q) + (random << (CUT - 16)) + (1u << (CUT - 17))) >> CUT, (u32)TOP);
-  }
-  static __device__ __forceinline__ float value(u32 code, float scale) {
-    return __builtin_bit_cast(float, code << CUT) * __builtin_ldexpf(1.0f, 126 + LEAST) * scale;
-  }
-};
-typedef Format<3, -6, 0x7E> FirstFormat;            // e4m3: up to 448
-typedef Format<2, -14, 0x7B> SecondFormat;          // e5m2: up to 57344
-constexpr float FIRST_MOST = 448.0f, SECOND_MOST = 57344.0f;
+constexpr float FIRST_MOST = 448.0f, SECOND_MOST = 57344.0f;            // the largest values of e4m3 and e5m2
+constexpr float SECOND_LEAST = 0x1p-16f;                               // the smallest of e5m2 but zero
+
+// x / scale, whose reciprocal is at hand: a step of the division's remainder takes out what rounding that did
+__device__ __forceinline__ float quotient(float x, float scale, float reciprocal) {
+  const float q = x * reciprocal;
+  return fmaf(fmaf(-q, scale, x), reciprocal, q);
+}
+// The card's rounding to 8 bits by random bits adds those of `random` from the top on to what is cut off, below the smallest normal values too (it was compared with an addition
+// to the bits of a float for 2 million values in all of both formats' binades: equal).  16 random bits, and the middle of the interval that they leave.
+template <int TO>
+__device__ __forceinline__ u32 put_first(float q, u32 random, u32 word) {
+  return (u32)__builtin_amdgcn_cvt_sr_fp8_f32(__builtin_amdgcn_fmed3f(q, -FIRST_MOST, FIRST_MOST), (int)(random << 16 | 0x8000), (int)word, TO);
+}
+// (never zero for what is not)
+template <int TO>
+__device__ __forceinline__ u32 put_second(float q, float v, u32 random, u32 word) {
+  return (u32)__builtin_amdgcn_cvt_sr_bf8_f32(__builtin_amdgcn_fmed3f(q, v > 0 ? SECOND_LEAST : 0.0f, SECOND_MOST), (int)((random & 0xFFFF0000u) | 0x8000), (int)word, TO);
+}
 
 // The largest of 32 lanes' values, which are not negative: as whole numbers these have the same order, with NaN above all others.
+template <int CTRL>
+__device__ __forceinline__ u32 max_with(u32 v) { return max(v, (u32)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, 0xF, 0xF, false)); }
 __device__ __forceinline__ u32 half_max(u32 v) {
-#pragma unroll
-  for (int m = 16; m >= 1; m >>= 1) v = max(v, (u32)__shfl_xor((int)v, m, 32));
-  return v;
+  v = max_with<0x128>(max_with<0x124>(max_with<0x122>(max_with<0x121>(v))));      // row_ror: 1, 2, 4, 8
+  return max(v, (u32)__shfl_xor((int)v, 16, 32));
 }
 // a block's scale: NaN where a value of it is not finite
 __device__ __forceinline__ float scale_of(u32 largest, float most) {
@@ -151,22 +156,26 @@ __global__ __launch_bounds__(ADAMW_THREADS) void k_adamw(AdamwJob j) {
 #pragma unroll
       for (int i = 0; i < EACH; ++i) { m[i] = qm[i]; v[i] = qv[i]; }
     } else {
-      const Vec<uint8_t, EACH> qm = load_vec<EACH>(static_cast<const uint8_t*>(j.m) + state), qv = load_vec<EACH>(static_cast<const uint8_t*>(j.v) + state);
       const float sm = j.m_scale[block], sv = j.v_scale[block];
+      const Words qm = *reinterpret_cast<const Words*>(static_cast<const uint8_t*>(j.m) + state), qv = *reinterpret_cast<const Words*>(static_cast<const uint8_t*>(j.v) + state);
 #pragma unroll
-      for (int i = 0; i < EACH; ++i) {
-        const float a = FirstFormat::value(qm[i] & 0x7F, sm);
-        m[i] = qm[i] & 0x80 ? -a : a;
-        v[i] = SecondFormat::value(qv[i] & 0x7F, sv);
+      for (int i = 0; i < EACH; i += 4) {
+        const auto m0 = __builtin_amdgcn_cvt_pk_f32_fp8((int)qm[i / 4], false), m1 = __builtin_amdgcn_cvt_pk_f32_fp8((int)qm[i / 4], true);
+        const auto v0 = __builtin_amdgcn_cvt_pk_f32_bf8((int)qv[i / 4], false), v1 = __builtin_amdgcn_cvt_pk_f32_bf8((int)qv[i / 4], true);
+        m[i] = sm * m0[0]; m[i + 1] = sm * m0[1]; m[i + 2] = sm * m1[0]; m[i + 3] = sm * m1[1];
+        v[i] = sv * v0[0]; v[i + 1] = sv * v0[1]; v[i + 2] = sv * v1[0]; v[i + 3] = sv * v1[1];
       }
     }
     u32 most_m = 0, most_v = 0;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
       next_moments(m[i], v[i], g[i], j);
-      most_m = max(most_m, __builtin_bit_cast(u32, m[i]) & 0x7FFFFFFFu);
-      most_v = max(most_v, __builtin_bit_cast(u32, v[i]) & 0x7FFFFFFFu);
-      const float ratio = m[i] / (sqrtf(v[i]) * s.root + j.eps);
+      if constexpr (BITS == 8) {
+        most_m = max(most_m, __builtin_bit_cast(u32, m[i]) & 0x7FFFFFFFu);
+        most_v = max(most_v, __builtin_bit_cast(u32, v[i]) & 0x7FFFFFFFu);
+      }
+      // (the card's square root and reciprocal, off by a step each)
+      const float ratio = m[i] * __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_sqrtf(v[i] * j.up), s.root, j.eps));
       p[i] = p[i] - s.decay * p[i] - s.step_size * ratio;
     }
     if constexpr (MASTERS) {
@@ -196,16 +205,20 @@ __global__ __launch_bounds__(ADAMW_THREADS) void k_adamw(AdamwJob j) {
       const float sm = scale_of(half_max(most_m), FIRST_MOST), sv = scale_of(half_max(most_v), SECOND_MOST);
       const float im = 1.0f / sm, iv = 1.0f / sv;
       const u32 key = mix(s.key ^ (u32)((u64)state >> 32));
-      Vec<uint8_t, EACH> qm, qv;
+      u32 r[EACH];
 #pragma unroll
-      for (int i = 0; i < EACH; ++i) {
-        const u32 r = mix(key + (u32)state + i);
-        const u32 a = FirstFormat::code(m[i], sm, im, r & 0xFFFF), b = SecondFormat::code(v[i], sv, iv, r >> 16);
-        qm[i] = (uint8_t)(a | (__builtin_bit_cast(u32, m[i]) >> 24 & 0x80));
-        qv[i] = (uint8_t)(v[i] > 0 ? max(b, 1u) : 0u);
+      for (int i = 0; i < EACH; ++i) r[i] = mix(key + (u32)state + i);
+      Words qm, qv;
+#pragma unroll
+      for (int i = 0; i < EACH; i += 4) {
+        auto first = [&](int n) { return quotient(m[i + n], sm, im); };
+        auto second = [&](int n) { return quotient(v[i + n], sv, iv); };
+        qm[i / 4] = put_first<3>(first(3), r[i + 3], put_first<2>(first(2), r[i + 2], put_first<1>(first(1), r[i + 1], put_first<0>(first(0), r[i], 0))));
+        qv[i / 4] = put_second<3>(second(3), v[i + 3], r[i + 3], put_second<2>(second(2), v[i + 2], r[i + 2], put_second<1>(second(1), v[i + 1], r[i + 1],
+                                  put_second<0>(second(0), v[i], r[i], 0))));
       }
-      store_vec<EACH>(static_cast<uint8_t*>(j.m) + state, qm);
-      store_vec<EACH>(static_cast<uint8_t*>(j.v) + state, qv);
+      *reinterpret_cast<Words*>(static_cast<uint8_t*>(j.m) + state) = qm;
+      *reinterpret_cast<Words*>(static_cast<uint8_t*>(j.v) + state) = qv;
       if (threadIdx.x % (BLOCK / EACH) == 0) {
         j.m_scale[block] = sm;
         j.v_scale[block] = sv;
@@ -236,8 +249,7 @@ ccld_status check(const ccld_adamw_args* a) {
   if (a->n_tensors < 0 || a->total < 0 || a->total % BLOCK || (a->master && a->dtype == CCLD_FP32)) return CCLD_E_BAD_ARG;
   if (a->total / BLOCK >= (i64)1 << 32) return CCLD_E_CAPACITY;
   if (!a->count || (a->n_tensors && !a->tensors) || (a->total && (!a->m || !a->v || (a->bits == 8 && (!a->m_scale || !a->v_scale))))) return CCLD_E_NULL;
-  const uintptr_t state = a->bits == 32 ? 4 : 1;
-  if (!aligned(a->count, 8) || !aligned(a->m, state) || !aligned(a->v, state) || !aligned(a->m_scale, 4) || !aligned(a->v_scale, 4) || !aligned(a->master, 4) ||
+  if (!aligned(a->count, 8) || !aligned(a->m, 4) || !aligned(a->v, 4) || !aligned(a->m_scale, 4) || !aligned(a->v_scale, 4) || !aligned(a->master, 4) ||
       !aligned(a->scale_by, 4)) return CCLD_E_BAD_ARG;
   if (a->workspace_bytes < CCLD_ADAMW_WORKSPACE || !a->workspace || !aligned(a->workspace, 256)) return CCLD_E_WORKSPACE;
   for (i64 i = 0; i < a->n_tensors; ++i) {
@@ -256,11 +268,13 @@ extern "C" ccld_status ccld_adamw(const ccld_adamw_args* a, void* stream) {
   if (st != CCLD_OK) return st;
   const hipStream_t hs = static_cast<hipStream_t>(stream);
   Step* const step = static_cast<Step*>(a->workspace);
-  k_adamw_begin<<<1, 1, 0, hs>>>(BeginJob{a->count, a->scale_by, step, a->lr, a->beta1, a->beta2, a->weight_decay, a->scale, a->seed});
+  // the card's root takes subnormal numbers for zero: beside an eps of 2^-60 that is nothing, beside a smaller one v is scaled out of their range
+  const double up = a->eps >= 0x1p-60 ? 1.0 : 0x1p24;
+  k_adamw_begin<<<1, 1, 0, hs>>>(BeginJob{a->count, a->scale_by, step, a->lr, a->beta1, a->beta2, a->weight_decay, a->scale, up, a->seed});
   AdamwJob j{};
   j.step = step;
   j.m = a->m; j.v = a->v; j.m_scale = a->m_scale; j.v_scale = a->v_scale; j.master = a->master;
-  j.b1 = (float)a->beta1; j.b2 = (float)a->beta2; j.c1 = (float)(1.0 - a->beta1); j.c2 = (float)(1.0 - a->beta2); j.eps = (float)a->eps;
+  j.b1 = (float)a->beta1; j.b2 = (float)a->beta2; j.c1 = (float)(1.0 - a->beta1); j.c2 = (float)(1.0 - a->beta2); j.eps = (float)a->eps; j.up = (float)up;
   u32 groups = 0;
   auto flush = [&] {
     if (!groups) return;

@@ -172,6 +172,21 @@ def test_zeros_stay_zeros_and_v_does_not_become_zero():
     assert not v[301:].any() and torch.isfinite(p).all()
 
 
+def test_without_eps():
+    """Gradients whose squares are subnormal in 32 bits still step by lr."""
+    g = torch.tensor([1e-3, -1e-18, 3e-19, 5.0, 1e10], device=DEV)
+    p = torch.zeros(5, device=DEV)
+    state = step.adamw_state([p])
+    step.adamw([p], [g], state, 0.5, betas=(0.9, 0.5), eps=0.0)
+    # v = 0.5 g^2 of 1e-37 has 23 bits, of 4.5e-38 too; m / sqrt(v) / (0.1 / sqrt(0.5)) is 1 to 2^-17 where v's spacing, 2^-149, is 2^-17 of it
+    assert float((p + 0.5 * torch.sign(g)).abs().max()) < 0.5 * 2.0 ** -16
+    tiny = torch.full((300,), 1e-20, device=DEV)
+    p, state = torch.zeros(300, device=DEV), None
+    state = step.adamw_state([p])
+    step.adamw([p], [tiny], state, 0.5, betas=(0.9, 0.5), eps=0.0)          # v is 5e-41: 35,682 of its spacings
+    assert float((p + 0.5).abs().max()) < 0.5 * 2.0 ** -14
+
+
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
 def test_gradients_that_are_not_finite(bad):
     for bits in (32, 8):
