@@ -23,9 +23,10 @@ using namespace ccld;
 namespace {
 
 constexpr int BLOCK = CCLD_ADAMW_BLOCK, ADAMW_THREADS = 256;
-constexpr int EACH = 8;                                  // neighbouring elements of a thread
-constexpr int PASSES = 2, CHUNK = ADAMW_THREADS * EACH * PASSES;
-typedef u32 Words __attribute__((ext_vector_type(EACH / 4), aligned(4)));      // 8-bit values
+// neighbouring elements of a thread: 16 bytes of a 32-bit state, 8 of one in 8 bits
+constexpr int each_of(int bits) { return bits == 32 ? 4 : 8; }
+constexpr int CHUNK = 4096;                              // elements of a workgroup
+typedef u32 Words __attribute__((ext_vector_type(2), aligned(4)));      // 8-bit values
 constexpr int LISTED = 112;                              // tensors of a launch: its arguments have 4 KB
 
 // What a step's elements share.
@@ -111,6 +112,7 @@ __device__ __forceinline__ void next_moments(float& m, float& v, float g, const 
 
 template <class T, class G, int BITS, bool MASTERS>
 __global__ __launch_bounds__(ADAMW_THREADS) void k_adamw(AdamwJob j) {
+  constexpr int EACH = each_of(BITS), PASSES = CHUNK / (ADAMW_THREADS * EACH);
   // the last tensor that starts at or before this workgroup
   int mine = -1;
   for (int i = 0; i < j.n_tensors; i += CCLD_WAVE) {
