@@ -133,7 +133,7 @@ __global__ __launch_bounds__(ADAMW_THREADS) void k_adamw(AdamwJob j) {
     const G* const from = static_cast<const G*>(x.g) + at;
     const bool whole = at + EACH <= x.n;
     if (whole) {
-      const Vec<G, EACH> q = load_vec<EACH>(from);
+      const Vec<G, EACH> q = load_once<EACH>(from);
 #pragma unroll
       for (int i = 0; i < EACH; ++i) g[i] = s.scale * (float)q[i];
     } else {
@@ -141,11 +141,11 @@ __global__ __launch_bounds__(ADAMW_THREADS) void k_adamw(AdamwJob j) {
       for (int i = 0; i < EACH; ++i) g[i] = at + i < x.n ? s.scale * (float)from[i] : 0.0f;
     }
     if constexpr (MASTERS) {
-      const Vec<float, EACH> q = load_vec<EACH>(j.master + state);
+      const Vec<float, EACH> q = load_once<EACH>(j.master + state);
 #pragma unroll
       for (int i = 0; i < EACH; ++i) p[i] = q[i];
     } else if (whole) {
-      const Vec<T, EACH> q = load_vec<EACH>(to);
+      const Vec<T, EACH> q = load_once<EACH>(to);
 #pragma unroll
       for (int i = 0; i < EACH; ++i) p[i] = (float)q[i];
     } else {
@@ -154,12 +154,13 @@ __global__ __launch_bounds__(ADAMW_THREADS) void k_adamw(AdamwJob j) {
     }
     const i64 block = state / BLOCK;
     if constexpr (BITS == 32) {
-      const Vec<float, EACH> qm = load_vec<EACH>(static_cast<const float*>(j.m) + state), qv = load_vec<EACH>(static_cast<const float*>(j.v) + state);
+      const Vec<float, EACH> qm = load_once<EACH>(static_cast<const float*>(j.m) + state), qv = load_once<EACH>(static_cast<const float*>(j.v) + state);
 #pragma unroll
       for (int i = 0; i < EACH; ++i) { m[i] = qm[i]; v[i] = qv[i]; }
     } else {
       const float sm = j.m_scale[block], sv = j.v_scale[block];
-      const Words qm = *reinterpret_cast<const Words*>(static_cast<const uint8_t*>(j.m) + state), qv = *reinterpret_cast<const Words*>(static_cast<const uint8_t*>(j.v) + state);
+      const Words qm = __builtin_nontemporal_load(reinterpret_cast<const Words*>(static_cast<const uint8_t*>(j.m) + state)),
+                  qv = __builtin_nontemporal_load(reinterpret_cast<const Words*>(static_cast<const uint8_t*>(j.v) + state));
 #pragma unroll
       for (int i = 0; i < EACH; i += 4) {
         const auto m0 = __builtin_amdgcn_cvt_pk_f32_fp8((int)qm[i / 4], false), m1 = __builtin_amdgcn_cvt_pk_f32_fp8((int)qm[i / 4], true);
@@ -185,13 +186,13 @@ __global__ __launch_bounds__(ADAMW_THREADS) void k_adamw(AdamwJob j) {
       Vec<float, EACH> q;
 #pragma unroll
       for (int i = 0; i < EACH; ++i) q[i] = at + i < x.n ? p[i] : 0.0f;
-      store_vec<EACH>(j.master + state, q);
+      store_once<EACH>(j.master + state, q);
     }
     if (whole) {
       Vec<T, EACH> q;
 #pragma unroll
       for (int i = 0; i < EACH; ++i) q[i] = (T)p[i];
-      store_vec<EACH>(to, q);
+      store_once<EACH>(to, q);
     } else {
 #pragma unroll
       for (int i = 0; i < EACH; ++i)
@@ -201,8 +202,8 @@ __global__ __launch_bounds__(ADAMW_THREADS) void k_adamw(AdamwJob j) {
       Vec<float, EACH> qm, qv;
 #pragma unroll
       for (int i = 0; i < EACH; ++i) { qm[i] = m[i]; qv[i] = v[i]; }
-      store_vec<EACH>(static_cast<float*>(j.m) + state, qm);
-      store_vec<EACH>(static_cast<float*>(j.v) + state, qv);
+      store_once<EACH>(static_cast<float*>(j.m) + state, qm);
+      store_once<EACH>(static_cast<float*>(j.v) + state, qv);
     } else {
       const float sm = scale_of(half_max(most_m), FIRST_MOST), sv = scale_of(half_max(most_v), SECOND_MOST);
       const float im = 1.0f / sm, iv = 1.0f / sv;
@@ -219,8 +220,8 @@ __global__ __launch_bounds__(ADAMW_THREADS) void k_adamw(AdamwJob j) {
         qv[i / 4] = put_second<3>(second(3), v[i + 3], r[i + 3], put_second<2>(second(2), v[i + 2], r[i + 2], put_second<1>(second(1), v[i + 1], r[i + 1],
                                   put_second<0>(second(0), v[i], r[i], 0))));
       }
-      *reinterpret_cast<Words*>(static_cast<uint8_t*>(j.m) + state) = qm;
-      *reinterpret_cast<Words*>(static_cast<uint8_t*>(j.v) + state) = qv;
+      __builtin_nontemporal_store(qm, reinterpret_cast<Words*>(static_cast<uint8_t*>(j.m) + state));
+      __builtin_nontemporal_store(qv, reinterpret_cast<Words*>(static_cast<uint8_t*>(j.v) + state));
       if (threadIdx.x % (BLOCK / EACH) == 0) {
         j.m_scale[block] = sm;
         j.v_scale[block] = sv;

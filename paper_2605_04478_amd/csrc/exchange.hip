@@ -15,6 +15,10 @@ using namespace ccld;
 
 namespace {
 
+// Entries of a token that are on their way at once.  Two are enough, with as many tokens to a compute unit as its wavefronts hold; eight ask for six
+// rows in vain where there are two (8,192 x 2,048 with 2 experts: combine 18 and 20 us).
+constexpr int AT_ONCE = 2;
+
 struct ExchangeJob {
   const int32_t *places, *used;
   const float* weights;
@@ -26,7 +30,8 @@ struct ExchangeJob {
   int k, d;
 };
 
-constexpr int EXCHANGE_THREADS = 256;
+// a team is a workgroup, or one of the four wavefronts of one
+constexpr int threads_of(int team) { return team == CCLD_WAVE ? 256 : team; }
 
 // A token's places and weights.  A team's token is the same for all of its lanes, so these are scalar loads, which no lane has to be active for.
 struct Places {
@@ -47,15 +52,15 @@ __device__ __forceinline__ void clear_unused(const ExchangeJob& j, i64 t, int me
   for (u32 r = max((u32)(t * j.k), used); r < (u32)(t * j.k) + (u32)j.k; ++r) {
     T* const row = static_cast<T*>(j.y_out) + (i64)r * j.ldy_out;
     int c = me * N;
-    for (; c + N <= j.d; c += TEAM * N) store_vec<N>(row + c, Vec<T, N>{});
+    for (; c + N <= j.d; c += TEAM * N) store_once<N>(row + c, Vec<T, N>{});
     for (; c < j.d; ++c) row[c] = (T)0.0f;
   }
 }
 
 // (a thread that the end of the row falls on takes what is left of it value by value)
 template <class T, int TEAM>
-__global__ __launch_bounds__(EXCHANGE_THREADS) void k_dispatch(ExchangeJob j) {
-  constexpr int N = 16 / sizeof(T), TEAMS = EXCHANGE_THREADS / TEAM;
+__global__ __launch_bounds__(threads_of(TEAM)) void k_dispatch(ExchangeJob j) {
+  constexpr int N = 16 / sizeof(T), TEAMS = threads_of(TEAM) / TEAM;
   const int me = threadIdx.x % TEAM;
   const u32 used = (u32)max(*j.used, 0);
   i64 t = (i64)blockIdx.x * TEAMS + (TEAMS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / TEAM) : 0);
@@ -68,7 +73,7 @@ __global__ __launch_bounds__(EXCHANGE_THREADS) void k_dispatch(ExchangeJob j) {
       const Vec<T, N> v = load_vec<N>(x + c);
       for (int i = 0; i < j.k; ++i) {
         const int at = p.at(i);
-        if (at >= 0) store_vec<N>(y + at * j.ldy_out + c, v);
+        if (at >= 0) store_once<N>(y + at * j.ldy_out + c, v);
       }
     }
     for (; c < j.d; ++c) {
@@ -83,8 +88,8 @@ __global__ __launch_bounds__(EXCHANGE_THREADS) void k_dispatch(ExchangeJob j) {
 
 // WEIGHTED: combine, else the gradient of dispatch
 template <class T, int TEAM, bool WEIGHTED>
-__global__ __launch_bounds__(EXCHANGE_THREADS) void k_gather(ExchangeJob j) {
-  constexpr int N = 16 / sizeof(T), TEAMS = EXCHANGE_THREADS / TEAM, AT_ONCE = 4;
+__global__ __launch_bounds__(threads_of(TEAM)) void k_gather(ExchangeJob j) {
+  constexpr int N = 16 / sizeof(T), TEAMS = threads_of(TEAM) / TEAM;
   const int me = threadIdx.x % TEAM;
   i64 t = (i64)blockIdx.x * TEAMS + (TEAMS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / TEAM) : 0);
   for (; t < j.tokens; t += (i64)gridDim.x * TEAMS) {
@@ -114,7 +119,7 @@ __global__ __launch_bounds__(EXCHANGE_THREADS) void k_gather(ExchangeJob j) {
       Vec<T, N> o;
 #pragma unroll
       for (int n = 0; n < N; ++n) o[n] = (T)sum[n];
-      store_vec<N>(out + c, o);
+      store_once<N>(out + c, o);
     }
     for (; c < j.d; ++c) {
       float sum = 0;
@@ -129,9 +134,9 @@ __global__ __launch_bounds__(EXCHANGE_THREADS) void k_gather(ExchangeJob j) {
 
 // The gradient of combine: AT_ONCE entries in a pass over the row, their products with y summed over the team.
 template <class T, int TEAM>
-__global__ __launch_bounds__(EXCHANGE_THREADS) void k_combine_grad(ExchangeJob j) {
-  constexpr int N = 16 / sizeof(T), TEAMS = EXCHANGE_THREADS / TEAM, AT_ONCE = 8, WAVES = TEAM / CCLD_WAVE;
-  __shared__ float sums[2][EXCHANGE_THREADS / CCLD_WAVE][AT_ONCE];
+__global__ __launch_bounds__(threads_of(TEAM)) void k_combine_grad(ExchangeJob j) {
+  constexpr int N = 16 / sizeof(T), TEAMS = threads_of(TEAM) / TEAM, WAVES = TEAM / CCLD_WAVE;
+  __shared__ float sums[2][WAVES][AT_ONCE];
   const int me = threadIdx.x % TEAM;
   const u32 used = (u32)max(*j.used, 0);
   int turn = 0;
@@ -157,7 +162,7 @@ __global__ __launch_bounds__(EXCHANGE_THREADS) void k_combine_grad(ExchangeJob j
           Vec<T, N> o;
 #pragma unroll
           for (int n = 0; n < N; ++n) o[n] = (T)(w * (float)v[n]);
-          store_vec<N>(dy + p.at(i0 + i) * j.ldy_out + c, o);
+          store_once<N>(dy + p.at(i0 + i) * j.ldy_out + c, o);
           if (j.dweights)
 #pragma unroll
             for (int n = 0; n < N; ++n) dot[i] += (float)v[n] * (float)q[i][n];
@@ -201,11 +206,12 @@ enum Way { DISPATCH, DISPATCH_GRAD, COMBINE, COMBINE_GRAD };
 
 template <class T, int TEAM>
 void launch(const ExchangeJob& j, Way way, hipStream_t stream) {
-  const u32 grid = (u32)std::min<i64>(blocks_for(j.tokens, EXCHANGE_THREADS / TEAM), 64 * COMPUTE_UNITS);
-  if (way == DISPATCH) k_dispatch<T, TEAM><<<grid, EXCHANGE_THREADS, 0, stream>>>(j);
-  else if (way == DISPATCH_GRAD) k_gather<T, TEAM, false><<<grid, EXCHANGE_THREADS, 0, stream>>>(j);
-  else if (way == COMBINE) k_gather<T, TEAM, true><<<grid, EXCHANGE_THREADS, 0, stream>>>(j);
-  else k_combine_grad<T, TEAM><<<grid, EXCHANGE_THREADS, 0, stream>>>(j);
+  constexpr int THREADS = threads_of(TEAM);
+  const u32 grid = (u32)std::min<i64>(blocks_for(j.tokens, THREADS / TEAM), 64 * COMPUTE_UNITS);
+  if (way == DISPATCH) k_dispatch<T, TEAM><<<grid, THREADS, 0, stream>>>(j);
+  else if (way == DISPATCH_GRAD) k_gather<T, TEAM, false><<<grid, THREADS, 0, stream>>>(j);
+  else if (way == COMBINE) k_gather<T, TEAM, true><<<grid, THREADS, 0, stream>>>(j);
+  else k_combine_grad<T, TEAM><<<grid, THREADS, 0, stream>>>(j);
 }
 
 ccld_status exchange(const ccld_exchange_args* a, Way way, void* stream) {
@@ -226,9 +232,13 @@ ccld_status exchange(const ccld_exchange_args* a, Way way, void* stream) {
   const hipStream_t st = static_cast<hipStream_t>(stream);
   with_type(a->dtype, [&](auto zero) {
     using T = decltype(zero);
-    // a wavefront to a row of two vectors a lane and less
-    if (a->d <= 2 * CCLD_WAVE * 16 / (i64)sizeof(T)) launch<T, CCLD_WAVE>(j, way, st);
-    else launch<T, EXCHANGE_THREADS>(j, way, st);
+    // a vector to a thread: dispatch, combine, its gradient and dispatch's of 8,192 x 4,096 in bfloat16 with 8 experts each take 104, 112, 223 and 111 us in teams of 512 threads, 108, 118, 233
+    // and 118 in teams of 256, 118, 137, 272 and 135 in wavefronts; of 8,192 x 1,024 with 2 experts 9.6, 10.4, 25 and 10 in teams of 512 and 9.0, 9.0, 15 and 9.2 in teams of 128
+    const i64 vectors = blocks_for(a->d, 16 / (i64)sizeof(T));
+    if (vectors <= 64) launch<T, CCLD_WAVE>(j, way, st);
+    else if (vectors <= 128) launch<T, 128>(j, way, st);
+    else if (vectors <= 256) launch<T, 256>(j, way, st);
+    else launch<T, 512>(j, way, st);
   });
   return launched();
 }

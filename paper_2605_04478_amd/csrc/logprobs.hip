@@ -128,7 +128,7 @@ struct Streamed {
       constexpr int S = sizeof(z) / sizeof(float);
       Vec<T, S> o;
       f(z, o);
-      store_vec<S>(out + at, o);
+      store_once<S>(out + at, o);
     });
   }
   // the thread that stores a column
@@ -154,7 +154,7 @@ struct Held {
     return reinterpret_cast<P*>(reinterpret_cast<byte*>(row) + i * THREADS * 16 + (u32)(threadIdx.x * 16));
   }
   __device__ __forceinline__ void load(const T* row, int i) {
-    if (inside(i)) v[i] = __builtin_bit_cast(words4, load_vec<N>(place(row, i)));
+    if (inside(i)) v[i] = __builtin_bit_cast(words4, load_once<N>(place(row, i)));
   }
   __device__ __forceinline__ void load_rest(const T* row) {
     if ((int)threadIdx.x < vocab - whole()) rest = (float)row[whole() + threadIdx.x];
@@ -203,7 +203,7 @@ struct Held {
       values(i, z);
       Vec<T, N> o;
       f(z, o);
-      if (inside(i)) store_vec<N>(place(out, i), o);
+      if (inside(i)) store_once<N>(place(out, i), o);
       if (next) load(next, i);
       __builtin_amdgcn_sched_barrier(0);
     }

@@ -27,6 +27,18 @@ __device__ __forceinline__ void store_vec(T* p, Vec<T, N> v) {
   else *reinterpret_cast<typename Vector<T, N>::loose*>(p) = v;
 }
 
+// The same past the caches where they can: for what is not read again before much else has been.
+template <int N, class T>
+__device__ __forceinline__ Vec<T, N> load_once(const T* p) {
+  if constexpr (N == 1) return Vec<T, 1>{*p};
+  else return __builtin_nontemporal_load(reinterpret_cast<const typename Vector<T, N>::loose*>(p));
+}
+template <int N, class T>
+__device__ __forceinline__ void store_once(T* p, Vec<T, N> v) {
+  if constexpr (N == 1) *p = v[0];
+  else __builtin_nontemporal_store(v, reinterpret_cast<typename Vector<T, N>::loose*>(p));
+}
+
 // Maxima and sums over a wavefront's lanes, in all of them.  Neighbours by DPP shifts within rows of 16 lanes, then the rows' results (a shuffle
 // through the LDS crossbar takes many times as long).
 template <int CTRL>

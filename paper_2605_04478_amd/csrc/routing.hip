@@ -4,9 +4,11 @@
 //   ds[e_j] = w_j dw_j (of each chosen one)  -  p_e sum_j w_j dw_j      p: the same softmax
 //   place[n] = entries of lower experts + earlier entries of the same expert: a stable counting sort
 //
-// A row of scores belongs to one wavefront and stays in its registers: lane l holds the experts from l V on, so that the lowest
-// lane with the largest value has the lowest expert.  A choice is a maximum over the lanes, a ballot and its removal.
+// The choice is bound by its instructions, not by memory: k times a maximum over a row and its removal.  A row therefore belongs to as few lanes as hold it in 16 registers
+// each, 16 lanes for up to 256 experts, so that a wavefront's instructions serve four tokens; maxima over 16 lanes take four instructions.  (A wavefront to a token: 57 us for 65,536 x 256 in
+// 32 bits, 8 of them, with weights over all.)
 #include <algorithm>
+#include <type_traits>
 
 #include "ccld_internal.h"
 #include "operators.h"
@@ -25,77 +27,126 @@ struct RouteJob {
   int n, k, over_all;
 };
 
-constexpr int ROUTE_THREADS = 256, ROUTE_TOKENS = ROUTE_THREADS / CCLD_WAVE;
+constexpr int ROUTE_THREADS = 256;
 
-// scores that cannot be chosen (switched off, NaN, behind the last expert) are the lowest value
-template <int V, class T>
-__device__ __forceinline__ void load_scores(float (&z)[V], const T* row, int lane, int n) {
-  const int first = lane * V;
-  if (first + V <= n) {
-    const Vec<T, V> v = load_vec<V>(row + first);
+// A token's scores in L lanes, V to each, in pieces of up to 4 neighbours: index(i) is the expert of value i.
+template <int L, int V>
+struct Scores {
+  static constexpr int P = V < 4 ? V : 4;
+  float z[V];
+  static __device__ __forceinline__ int index(int lane, int i) { return (i / P * L + lane) * P + i % P; }
+  // scores that cannot be chosen (switched off, NaN, behind the last expert) are the lowest value
+  template <class T>
+  __device__ __forceinline__ Scores(const T* row, int lane, int n, bool there) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) z[i] = (float)v[i];
-  } else {
+    for (int i = 0; i < V; i += P) {
+      const int first = index(lane, i);
+      if (there && first + P <= n) {
+        const Vec<T, P> v = load_vec<P>(row + first);
 #pragma unroll
-    for (int i = 0; i < V; ++i) z[i] = first + i < n ? (float)row[first + i] : LOWEST;
+        for (int p = 0; p < P; ++p) z[i + p] = (float)v[p];
+      } else {
+#pragma unroll
+        for (int p = 0; p < P; ++p) z[i + p] = there && first + p < n ? (float)row[first + p] : LOWEST;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) z[i] = z[i] != z[i] ? LOWEST : z[i];
   }
+  __device__ __forceinline__ float largest() const {
+    float m = z[0];
 #pragma unroll
-  for (int i = 0; i < V; ++i) z[i] = z[i] != z[i] ? LOWEST : z[i];
-}
-template <int V>
-__device__ __forceinline__ float largest_of(const float (&z)[V]) {
-  float m = z[0];
-#pragma unroll
-  for (int i = 1; i < V; ++i) m = fmaxf(m, z[i]);
-  return m;
-}
-// (the largest counts one also where it is infinite)
-__device__ __forceinline__ float share(float z, float m) { return z == m ? 1.0f : expf(z - m); }
+    for (int i = 1; i < V; ++i) m = fmaxf(m, z[i]);
+    return m;
+  }
+};
 
-template <class T, int V>
+// over the L lanes of a token, in all of them
+template <int L, class T, class F>
+__device__ __forceinline__ T over_lanes(T v, F f) {
+  auto with = [&](auto ctrl) {
+    const int x = __builtin_bit_cast(int, v);
+    v = f(v, __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(x, x, decltype(ctrl)::value, 0xF, 0xF, false)));
+  };
+  with(std::integral_constant<int, 0x121>());          // row_ror: 1, 2, 4, 8
+  with(std::integral_constant<int, 0x122>());
+  with(std::integral_constant<int, 0x124>());
+  with(std::integral_constant<int, 0x128>());
+  if constexpr (L > 16) v = f(v, __shfl_xor(v, 16, CCLD_WAVE));
+  if constexpr (L > 32) v = f(v, __shfl_xor(v, 32, CCLD_WAVE));
+  return v;
+}
+template <int L>
+__device__ __forceinline__ float max_over(float v) { return over_lanes<L>(v, [](float a, float b) { return fmaxf(a, b); }); }
+template <int L>
+__device__ __forceinline__ float sum_over(float v) { return over_lanes<L>(v, [](float a, float b) { return a + b; }); }
+template <int L>
+__device__ __forceinline__ int min_over(int v) { return over_lanes<L>(v, [](int a, int b) { return a < b ? a : b; }); }
+
+// exp(z - m) by the card's power of two, whose argument's rounding is made good; the largest counts one also where it is infinite
+__device__ __forceinline__ float share(float z, float m) {
+  const float d = z - m, t = d * 0x1.715476p+0f, r = fmaf(d, 0x1.715476p+0f, -t) + d * 0x1.4ae0c0p-26f;
+  const float e = __builtin_amdgcn_exp2f(t);
+  return z == m ? 1.0f : d < -150.0f ? 0.0f : fmaf(e, r * 0x1.62e430p-1f, e);
+}
+
+template <class T, int L, int V>
 __global__ __launch_bounds__(ROUTE_THREADS) void k_route(RouteJob j) {
-  const int lane = (int)lane_id();
-  const i64 first = (i64)blockIdx.x * ROUTE_TOKENS + __builtin_amdgcn_readfirstlane(threadIdx.x / CCLD_WAVE);
-  for (i64 t = first; t < j.tokens; t += (i64)gridDim.x * ROUTE_TOKENS) {
-    float z[V];
-    load_scores<V>(z, static_cast<const T*>(j.scores) + t * j.ld, lane, j.n);
-    float total = 0, m0 = LOWEST, value = LOWEST;
-    int mine = -1;
+  constexpr int TOKENS = ROUTE_THREADS / L;
+  struct Pick { float value; int expert; };
+  __shared__ Pick picks[TOKENS][CCLD_ROUTE_MOST];
+  const int lane = threadIdx.x % L, mine = threadIdx.x / L;
+  for (i64 t0 = (i64)blockIdx.x * TOKENS; t0 < j.tokens; t0 += (i64)gridDim.x * TOKENS) {
+    const i64 t = t0 + mine;
+    const bool there = t < j.tokens;                   // (lanes without a token go along)
+    Scores<L, V> s(static_cast<const T*>(j.scores) + t * j.ld, lane, j.n, there);
+    float total = 0, m0 = LOWEST;
     for (int c = 0; c < j.k; ++c) {
-      const float best = largest_of(z), m = wave_max(best);
-      if (m == LOWEST) break;
+      const float m = max_over<L>(s.largest());
       if (c == 0) {
         m0 = m;
         if (j.over_all) {
           float e = 0;
 #pragma unroll
-          for (int i = 0; i < V; ++i) e += share(z[i], m0);
-          total = wave_total(e);
+          for (int i = 0; i < V; ++i) e += s.z[i] == LOWEST ? 0.0f : share(s.z[i], m0);
+          total = sum_over<L>(e);
         }
       }
-      const int who = (int)__builtin_ctzll(ballot64(best == m));
-      int at = V;
+      // the lowest expert with this score, and its removal
+      int at = 0x7FFFFFFF;
 #pragma unroll
-      for (int i = V - 1; i >= 0; --i) at = z[i] == m ? i : at;
+      for (int i = V - 1; i >= 0; --i) at = s.z[i] == m ? s.index(lane, i) : at;
+      const int expert = min_over<L>(at);
 #pragma unroll
-      for (int i = 0; i < V; ++i) z[i] = lane == who && i == at ? LOWEST : z[i];
-      const int expert = who * V + __builtin_amdgcn_readlane(at, who);
-      if (lane == c) { mine = expert; value = m; }
+      for (int i = 0; i < V; ++i) s.z[i] = s.index(lane, i) == expert ? LOWEST : s.z[i];
+      if (lane == 0) picks[mine][c] = Pick{m, m == LOWEST ? -1 : expert};
     }
-    const float e = mine < 0 ? 0.0f : share(value, m0);
-    if (!j.over_all) total = wave_total(e);
-    if (lane < j.k) {
-      j.experts[t * j.k + lane] = mine;
-      j.weights[t * j.k + lane] = mine < 0 ? 0.0f : e / total;
+    // (a token's lanes are of one wavefront, whose accesses to LDS are in order)
+    __builtin_amdgcn_wave_barrier();
+    float sum = 0;
+    for (int c = lane; c < j.k; c += L) {
+      const Pick p = picks[mine][c];
+      sum += p.expert < 0 ? 0.0f : share(p.value, m0);
     }
+    if (!j.over_all) total = sum_over<L>(sum);
+    for (int c = lane; there && c < j.k; c += L) {
+      const Pick p = picks[mine][c];
+      j.experts[t * j.k + c] = p.expert;
+      j.weights[t * j.k + c] = p.expert < 0 ? 0.0f : share(p.value, m0) / total;
+    }
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
+// One wavefront to a token: memory bounds the gradient.
 template <class T, int V>
 __global__ __launch_bounds__(ROUTE_THREADS) void k_route_grad(RouteJob j) {
+  constexpr int TOKENS = ROUTE_THREADS / CCLD_WAVE;
+  typedef Scores<CCLD_WAVE, V> S;
+  constexpr int P = S::P;
   const int lane = (int)lane_id();
-  const i64 first = (i64)blockIdx.x * ROUTE_TOKENS + __builtin_amdgcn_readfirstlane(threadIdx.x / CCLD_WAVE);
-  for (i64 t = first; t < j.tokens; t += (i64)gridDim.x * ROUTE_TOKENS) {
+  const i64 first = (i64)blockIdx.x * TOKENS + __builtin_amdgcn_readfirstlane(threadIdx.x / CCLD_WAVE);
+  for (i64 t = first; t < j.tokens; t += (i64)gridDim.x * TOKENS) {
     int expert = -1;
     float w = 0, each = 0;
     if (lane < j.k) {
@@ -108,12 +159,12 @@ __global__ __launch_bounds__(ROUTE_THREADS) void k_route_grad(RouteJob j) {
     float d[V] = {};
     const float common = wave_total(each);
     if (j.over_all) {
-      load_scores<V>(d, static_cast<const T*>(j.scores) + t * j.ld, lane, j.n);
-      const float m = wave_max(largest_of(d));
+      const S s(static_cast<const T*>(j.scores) + t * j.ld, lane, j.n, true);
+      const float m = wave_max(s.largest());
       float sum = 0;
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        d[i] = m == LOWEST ? 0.0f : share(d[i], m);
+        d[i] = s.z[i] == LOWEST ? 0.0f : share(s.z[i], m);
         sum += d[i];
       }
       const float scale = m == LOWEST ? 0.0f : common / wave_total(sum);
@@ -127,37 +178,52 @@ __global__ __launch_bounds__(ROUTE_THREADS) void k_route_grad(RouteJob j) {
       if ((u32)e >= (u32)j.n) continue;
       const float more = read_lane(each, c);
 #pragma unroll
-      for (int i = 0; i < V; ++i) d[i] = lane * V + i == e ? d[i] + more : d[i];
+      for (int i = 0; i < V; ++i) d[i] = S::index(lane, i) == e ? d[i] + more : d[i];
     }
-    T* const row = static_cast<T*>(j.dscores) + t * j.ldd + lane * V;
-    if (lane * V + V <= j.n) {
-      Vec<T, V> v;
+    T* const row = static_cast<T*>(j.dscores) + t * j.ldd;
 #pragma unroll
-      for (int i = 0; i < V; ++i) v[i] = (T)d[i];
-      store_vec<V>(row, v);
-    } else {
+    for (int i = 0; i < V; i += P) {
+      const int at = S::index(lane, i);
+      if (at + P <= j.n) {
+        Vec<T, P> v;
 #pragma unroll
-      for (int i = 0; i < V; ++i)
-        if (lane * V + i < j.n) row[i] = (T)d[i];
+        for (int p = 0; p < P; ++p) v[p] = (T)d[i + p];
+        store_once<P>(row + at, v);
+      } else {
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+          if (at + p < j.n) row[at + p] = (T)d[i + p];
+      }
     }
   }
 }
 
-template <bool GRAD, class T, int V>
-void launch_route(const RouteJob& j, hipStream_t stream) {
-  const u32 grid = (u32)std::min<i64>(blocks_for(j.tokens, ROUTE_TOKENS), 64 * COMPUTE_UNITS);
-  if constexpr (GRAD) k_route_grad<T, V><<<grid, ROUTE_THREADS, 0, stream>>>(j);
-  else k_route<T, V><<<grid, ROUTE_THREADS, 0, stream>>>(j);
+template <class T, int L, int V>
+void launch_choice(const RouteJob& j, hipStream_t stream) {
+  k_route<T, L, V><<<(u32)std::min<i64>(blocks_for(j.tokens, ROUTE_THREADS / L), 64 * COMPUTE_UNITS), ROUTE_THREADS, 0, stream>>>(j);
+}
+template <class T, int V>
+void launch_gradient(const RouteJob& j, hipStream_t stream) {
+  k_route_grad<T, V><<<(u32)std::min<i64>(blocks_for(j.tokens, ROUTE_THREADS / CCLD_WAVE), 64 * COMPUTE_UNITS), ROUTE_THREADS, 0, stream>>>(j);
 }
 template <bool GRAD>
 ccld_status launch_route(const RouteJob& j, int32_t dtype, hipStream_t stream) {
   with_type(dtype, [&](auto zero) {
     using T = decltype(zero);
-    if (j.n <= 64) launch_route<GRAD, T, 1>(j, stream);
-    else if (j.n <= 128) launch_route<GRAD, T, 2>(j, stream);
-    else if (j.n <= 256) launch_route<GRAD, T, 4>(j, stream);
-    else if (j.n <= 512) launch_route<GRAD, T, 8>(j, stream);
-    else launch_route<GRAD, T, 16>(j, stream);
+    if constexpr (GRAD) {
+      if (j.n <= 64) launch_gradient<T, 1>(j, stream);
+      else if (j.n <= 128) launch_gradient<T, 2>(j, stream);
+      else if (j.n <= 256) launch_gradient<T, 4>(j, stream);
+      else if (j.n <= 512) launch_gradient<T, 8>(j, stream);
+      else launch_gradient<T, 16>(j, stream);
+    } else {
+      if (j.n <= 16) launch_choice<T, 16, 1>(j, stream);
+      else if (j.n <= 64) launch_choice<T, 16, 4>(j, stream);
+      else if (j.n <= 128) launch_choice<T, 16, 8>(j, stream);
+      else if (j.n <= 256) launch_choice<T, 16, 16>(j, stream);
+      else if (j.n <= 512) launch_choice<T, 32, 16>(j, stream);
+      else launch_choice<T, 64, 16>(j, stream);
+    }
   });
   return launched();
 }
@@ -180,23 +246,30 @@ RouteJob route_job(const ccld_route_args* a) {
 
 // ---- entries by expert ---------------------------------------------------------------------------------------------
 // Chunks of entries, one to a workgroup, whose wavefronts take a stretch of it each.  Counts per chunk first (where there is more than one), then every workgroup
-// finds what lies before its own entries of each expert, and a wavefront ranks 64 entries at a time: those of one expert are found by ballots over the bits
+// finds what lies before its own entries of each expert, from all chunks' counts or, where there are many, from a scan of them, and a wavefront ranks 64 entries at a time: those of one expert are found by ballots over the bits
 // of its number, the lowest of their lanes takes as many places from the wavefront's counter.
 struct OrderJob {
   const void* experts;
   int32_t *places, *offsets;
-  u32* counts;                   // [chunks][n]
+  u32 *counts, *totals;          // [chunks][n]; [n], where counts are turned into what lies before
   u32 entries, chunks, stretch;  // stretch: a wavefront's entries
   int n;
 };
 constexpr int ORDER_THREADS = 256;
-constexpr u32 MOST_CHUNKS = 256, LEAST_STRETCH = 512, SINGLE_CHUNK = 8192;
+// Stretches of 256 entries, all of which are on their way at once; longer ones where there would be more than 256 chunks.
+constexpr int AT_ONCE = 4;
+constexpr u32 MOST_CHUNKS = 256, LEAST_STRETCH = AT_ONCE * CCLD_WAVE, SINGLE_CHUNK = 16 * LEAST_STRETCH;
 
+// the experts of a wavefront's next entries, n for those that have none
 template <class I>
-__device__ __forceinline__ u32 expert_at(const OrderJob& j, u32 at, u32 end) {
-  if (at >= end) return (u32)j.n;
-  const I e = static_cast<const I*>(j.experts)[at];
-  return e >= 0 && e < (I)j.n ? (u32)e : (u32)j.n;
+__device__ __forceinline__ void next_experts(const OrderJob& j, u64 at0, u32 end, u32 (&e)[AT_ONCE]) {
+#pragma unroll
+  for (int i = 0; i < AT_ONCE; ++i) {
+    const u64 at = at0 + i * CCLD_WAVE + lane_id();
+    I x = -1;
+    if (at < end) x = static_cast<const I*>(j.experts)[at];
+    e[i] = x >= 0 && x < (I)j.n ? (u32)x : (u32)j.n;
+  }
 }
 
 template <class I>
@@ -204,49 +277,99 @@ __global__ __launch_bounds__(ORDER_THREADS) void k_order_count(OrderJob j) {
   __shared__ u32 counts[CCLD_ROUTE_EXPERTS];
   for (int e = threadIdx.x; e < j.n; e += ORDER_THREADS) counts[e] = 0;
   __syncthreads();
-  const u64 chunk = (u64)j.stretch * (ORDER_THREADS / CCLD_WAVE), start = blockIdx.x * chunk;
-  const u32 end = (u32)min((u64)j.entries, start + chunk);
-  for (u64 at = start + threadIdx.x; at < end; at += ORDER_THREADS) {
-    const u32 e = expert_at<I>(j, (u32)at, end);
-    if (e < (u32)j.n) atomicAdd(&counts[e], 1u);
+  const u64 start = ((u64)blockIdx.x * (ORDER_THREADS / CCLD_WAVE) + threadIdx.x / CCLD_WAVE) * j.stretch;
+  const u32 end = (u32)min((u64)j.entries, start + j.stretch);
+  for (u64 at = start; at < end; at += LEAST_STRETCH) {
+    u32 e[AT_ONCE];
+    next_experts<I>(j, at, end, e);
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i)
+      if (e[i] < (u32)j.n) atomicAdd(&counts[e[i]], 1u);
   }
   __syncthreads();
   for (int e = threadIdx.x; e < j.n; e += ORDER_THREADS) j.counts[(u64)blockIdx.x * j.n + e] = counts[e];
 }
 
+// Where there are many chunks: each expert's counts become what lies before them, by one wavefront.
+constexpr u32 MANY_CHUNKS = 32;
+__global__ __launch_bounds__(ORDER_THREADS) void k_order_scan(OrderJob j) {
+  constexpr int EACH = MOST_CHUNKS / CCLD_WAVE;
+  const int e = blockIdx.x * (ORDER_THREADS / CCLD_WAVE) + threadIdx.x / CCLD_WAVE;
+  if (e >= j.n) return;
+  const u32 first = lane_id() * EACH;
+  u32 x[EACH], sum = 0;
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) x[i] = first + i < j.chunks ? j.counts[(u64)(first + i) * j.n + e] : 0;
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) sum += x[i];
+  const u32 upto = wave_inclusive_sum(sum);
+  u32 before = upto - sum;
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) {
+    if (first + i < j.chunks) j.counts[(u64)(first + i) * j.n + e] = before;
+    before += x[i];
+  }
+  if (lane_id() == CCLD_WAVE - 1) j.totals[e] = upto;
+}
+
 template <class I, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_order_place(OrderJob j) {
   constexpr int WAVES = THREADS / CCLD_WAVE, EACH = CCLD_ROUTE_EXPERTS / THREADS;
-  __shared__ u32 counter[WAVES][CCLD_ROUTE_EXPERTS], all[CCLD_ROUTE_EXPERTS], s_wave[WAVES];
+  __shared__ u32 counter[WAVES][CCLD_ROUTE_EXPERTS], all[CCLD_ROUTE_EXPERTS], earlier[CCLD_ROUTE_EXPERTS], s_wave[WAVES];
   const u32 lane = lane_id();
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / CCLD_WAVE), n = j.n;
   const u64 start = ((u64)blockIdx.x * WAVES + wave) * j.stretch;
   const u32 end = (u32)min((u64)j.entries, start + j.stretch);
   for (int e = lane; e < n; e += CCLD_WAVE) counter[wave][e] = 0;
-  for (u64 at = start + lane; at < end; at += CCLD_WAVE) {
-    const u32 e = expert_at<I>(j, (u32)at, end);
-    if (e < (u32)n) atomicAdd(&counter[wave][e], 1u);
+  for (int e = threadIdx.x; e < n; e += THREADS) all[e] = earlier[e] = 0;
+  u32 first[AT_ONCE];
+  next_experts<I>(j, start, end, first);
+  for (u64 at = start; at < end; at += LEAST_STRETCH) {
+    u32 e[AT_ONCE];
+    if (at == start) __builtin_memcpy(e, first, sizeof e);
+    else next_experts<I>(j, at, end, e);
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i)
+      if (e[i] < (u32)n) atomicAdd(&counter[wave][e[i]], 1u);
   }
   __syncthreads();
   // what lies before this chunk's entries of an expert, and how many there are in all
-  for (int e = threadIdx.x; e < n; e += THREADS) {
-    u32 before = 0, sum = 0;
-    if (j.chunks == 1) {
-      for (int w = 0; w < WAVES; ++w) sum += counter[w][e];
-    } else {
-#pragma unroll 8
-      for (u32 c = 0; c < j.chunks; ++c) {
-        const u32 x = j.counts[(u64)c * n + e];
-        sum += x;
-        before += c < blockIdx.x ? x : 0;
-      }
+  if (j.totals) {
+    for (int e = threadIdx.x; e < n; e += THREADS) {
+      all[e] = j.totals[e];
+      earlier[e] = j.counts[(u64)blockIdx.x * n + e];
     }
-    all[e] = sum;
+    __syncthreads();
+  } else if (j.chunks > 1) {
+    // the chunks shared by as many threads to an expert as there are, eight at a time
+    const int parts = max(THREADS / n, 1);
+    for (int i = threadIdx.x; i < n * parts; i += THREADS) {
+      const int e = i % n;
+      u32 sum = 0, before = 0;
+      for (u32 c = i / n; c < j.chunks; c += 8 * parts) {
+        u32 x[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) x[q] = j.counts[(u64)min(c + q * parts, j.chunks - 1) * n + e];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          const u32 at = c + q * parts;
+          sum += at < j.chunks ? x[q] : 0;
+          before += at < min(j.chunks, blockIdx.x) ? x[q] : 0;
+        }
+      }
+      atomicAdd(&all[e], sum);
+      atomicAdd(&earlier[e], before);
+    }
+    __syncthreads();
+  }
+  for (int e = threadIdx.x; e < n; e += THREADS) {
+    u32 before = earlier[e];
     for (int w = 0; w < WAVES; ++w) {
       const u32 x = counter[w][e];
       counter[w][e] = before;
       before += x;
     }
+    if (j.chunks == 1) all[e] = before;
   }
   __syncthreads();
   u32 own[EACH], sum = 0, total;
@@ -269,25 +392,30 @@ __global__ __launch_bounds__(THREADS) void k_order_place(OrderJob j) {
   if (blockIdx.x == 0 && threadIdx.x == 0) j.offsets[n] = (int32_t)total;
   __syncthreads();
   const int bits = 32 - __builtin_clz((u32)n);
-  for (u64 at0 = start; at0 < end; at0 += CCLD_WAVE) {
-    const u64 at = at0 + lane;
-    const u32 e = at < end ? expert_at<I>(j, (u32)at, end) : (u32)n;
-    u64 same = ~0ull;
-    for (int b = 0; b < bits; ++b) {
-      const bool set = e >> b & 1;
-      const u64 m = ballot64(set);
-      same &= set ? m : ~m;
+  for (u64 at0 = start; at0 < end; at0 += LEAST_STRETCH) {
+    u32 e[AT_ONCE];
+    if (at0 == start) __builtin_memcpy(e, first, sizeof e);
+    else next_experts<I>(j, at0, end, e);
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      u64 same = ~0ull;
+      for (int b = 0; b < bits; ++b) {
+        const bool set = e[i] >> b & 1;
+        const u64 m = ballot64(set);
+        same &= set ? m : ~m;
+      }
+      const u32 rank = mbcnt64(same);
+      u32 taken = 0;
+      if (rank == 0 && e[i] < (u32)n) taken = atomicAdd(&counter[wave][e[i]], (u32)__builtin_popcountll(same));
+      taken = lane_read(taken, (u32)__builtin_ctzll(same));
+      const u64 at = at0 + i * CCLD_WAVE + lane;
+      if (at < end) j.places[at] = e[i] < (u32)n ? (int32_t)(all[e[i]] + taken + rank) : -1;
     }
-    const u32 rank = mbcnt64(same);
-    u32 taken = 0;
-    if (rank == 0 && e < (u32)n) taken = atomicAdd(&counter[wave][e], (u32)__builtin_popcountll(same));
-    taken = lane_read(taken, (u32)__builtin_ctzll(same));
-    if (at < end) j.places[at] = e < (u32)n ? (int32_t)(all[e] + taken + rank) : -1;
   }
 }
 
 OrderJob order_job(const ccld_order_args* a, uint64_t* bytes) {
-  OrderJob j{a->experts, a->places, a->offsets, static_cast<u32*>(a->workspace), (u32)(a->tokens * a->k), 1, 0, (int)a->n_experts};
+  OrderJob j{a->experts, a->places, a->offsets, static_cast<u32*>(a->workspace), nullptr, (u32)(a->tokens * a->k), 1, 0, (int)a->n_experts};
   if (j.entries <= SINGLE_CHUNK) {
     j.stretch = (u32)blocks_for(std::max<u32>(j.entries, 1), 1024) * CCLD_WAVE;
     *bytes = 0;
@@ -295,7 +423,10 @@ OrderJob order_job(const ccld_order_args* a, uint64_t* bytes) {
     const u64 waves = MOST_CHUNKS * (ORDER_THREADS / CCLD_WAVE);
     j.stretch = std::max<u32>(LEAST_STRETCH, (u32)((((u64)j.entries + waves - 1) / waves + CCLD_WAVE - 1) / CCLD_WAVE * CCLD_WAVE));
     j.chunks = (u32)blocks_for(j.entries, (i64)j.stretch * (ORDER_THREADS / CCLD_WAVE));
-    *bytes = (uint64_t)j.chunks * (uint64_t)a->n_experts * 4;
+    const uint64_t counts = (uint64_t)j.chunks * (uint64_t)a->n_experts;
+    const bool many = j.chunks > MANY_CHUNKS;
+    if (many && j.counts) j.totals = j.counts + counts;
+    *bytes = 4 * (counts + (many ? (uint64_t)a->n_experts : 0));
   }
   return j;
 }
@@ -305,6 +436,7 @@ void launch_order(const OrderJob& j, hipStream_t stream) {
     k_order_place<I, 1024><<<1, 1024, 0, stream>>>(j);
   } else {
     k_order_count<I><<<j.chunks, ORDER_THREADS, 0, stream>>>(j);
+    if (j.totals) k_order_scan<<<(u32)blocks_for(j.n, ORDER_THREADS / CCLD_WAVE), ORDER_THREADS, 0, stream>>>(j);
     k_order_place<I, ORDER_THREADS><<<j.chunks, ORDER_THREADS, 0, stream>>>(j);
   }
 }
