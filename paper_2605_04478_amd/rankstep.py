@@ -2,10 +2,12 @@
 
 The analysis names a rank whose computation is slow (Section 2.2, S1).  Its card may be slow, or it was given more work: what its work takes on a
 card that is known to be sound tells, beside what it took in the job.  `RankStep` is a step's computation (experts, norms with gate and
-residual scale, the vocabulary's loss; forward and backward) with the operators of `step`, `measure` times it on this card for given loads, and
+residual scale, the vocabulary's loss; forward and backward) with the operators of `step`, `RoutedStep` a whole step, in which each token's experts are chosen, its
+rows go to them and back, and the optimizer follows.  `measure` times either on this card for given loads, and
 `trace` lets the ranks of a job compute for so long between their collectives, so that the analyzer sees what these times would do to a job.
 
     python -m paper_2605_04478_amd.rankstep --ranks 16 --busy-rank 5 --took-us 9000
+    python -m paper_2605_04478_amd.rankstep --choices 2
 """
 from __future__ import annotations
 
@@ -83,6 +85,10 @@ class RankStep:
         loss = self.loss(h, offsets, labels)
         return loss.detach(), torch.autograd.grad(loss, self.weights())
 
+    def take(self, *batch):
+        """What measure times: the gradients."""
+        return self.gradients(*batch)
+
     def measure(self, loads: Sequence[Sequence[int]], repeats: int = 5) -> np.ndarray:
         """Nanoseconds that a step takes with each of the loads: the median of `repeats`, after one that does not count."""
         out = []
@@ -93,13 +99,64 @@ class RankStep:
                 for k in range(repeats + 1):
                     begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
                     begin.record()
-                    self.gradients(*batch)
+                    self.take(*batch)
                     end.record()
                     end.synchronize()
                     if k:
                         times.append(begin.elapsed_time(end))
                 out.append(int(np.median(times) * 1e6))
         return np.asarray(out, dtype=np.int64)
+
+
+class RoutedStep(RankStep):
+    """A whole step of one rank: a router chooses `choices` experts for every token, and AdamW takes the gradients."""
+
+    def __init__(self, spec: StepSpec = StepSpec(), choices: int = 2, dtype=torch.bfloat16, device: str = "cuda:0", lr: float = 1e-3, weight_decay: float = 0.1,
+                 bits: int = 32):
+        super().__init__(spec, dtype, device)
+        g = torch.Generator(device=self.device).manual_seed(spec.seed + 1)
+        for layer in self.layers:
+            router = torch.empty(spec.experts, spec.d, dtype=dtype, device=self.device).normal_(0.0, spec.d ** -0.5, generator=g)
+            layer["router"] = router.requires_grad_()
+        self.choices = choices
+        self.optimizer = step.AdamW(self.weights(), lr, weight_decay=weight_decay, bits=bits, masters=dtype != torch.float32, seed=spec.seed)
+
+    def batch(self, load: Sequence[int], seed: int = 0, masked: float = 0.0):
+        """As many tokens as the load has rows, which the router spreads, and their labels: (h [tokens, d], labels)."""
+        h, _, labels = super().batch(load, seed, masked)
+        return h, labels
+
+    def _forward(self, h):
+        u = h
+        for w in self.layers:
+            experts, weights = step.Route.apply(u @ w["router"].t(), self.choices, False)
+            places, offsets = step.expert_order(experts, self.spec.experts)
+            rows = step.Dispatch.apply(u, places, offsets)
+            inner = torch.nn.functional.silu(step.ExpertProduct.apply(rows, w["up"], offsets))
+            block = step.Combine.apply(step.ExpertProduct.apply(inner, w["down"], offsets), places, weights, offsets)
+            h, u = step.NormResidual.apply(h, block, w["gate"], w["post"], w["pre"], self.spec.scale, self.spec.eps)
+        return u
+
+    def loss(self, h, labels) -> torch.Tensor:
+        """The mean loss of the tokens that have a target."""
+        loss = step.VocabLoss.apply(self._forward(h), self.vocabulary, labels)
+        return loss.sum() / ((labels >= 0) & (labels < self.spec.vocab)).sum().clamp(min=1)
+
+    def gradients(self, h, labels):
+        """One step without the optimizer: (loss, gradients of weights())."""
+        loss = self.loss(h, labels)
+        return loss.detach(), torch.autograd.grad(loss, self.weights())
+
+    def take(self, h, labels) -> torch.Tensor:
+        """One whole step: the loss before it."""
+        loss, grads = self.gradients(h, labels)
+        self.optimizer.step(grads)
+        return loss
+
+    @torch.no_grad()
+    def evaluate(self, h, labels, top: int = 0, temperature: float = 1.0):
+        """What token_logprobs says of the labels under the model's logits."""
+        return step.token_logprobs(self._forward(h) @ self.vocabulary.t(), labels, temperature, top)
 
 
 def trace(compute_ns: np.ndarray, n_slots: int = 200, seed: int = 0) -> tg.Trace:
@@ -120,13 +177,16 @@ def main(argv=None) -> int:
     p.add_argument("--times", type=float, default=2.0, help="how many times the rows of the others")
     p.add_argument("--slots", type=int, default=200, help="collectives of the trace")
     p.add_argument("--took-us", type=float, help="what the busy rank's step took in its job, on its own card")
+    p.add_argument("--choices", type=int, default=0, help="experts that are chosen for every token, in a whole step with its optimizer (0: rows come sorted)")
     a = p.parse_args(argv)
     if a.ranks < 3 or not 0 <= a.busy_rank < a.ranks or a.rows < 1:
         p.error("at least 3 ranks, one of them busy, and a row")
     if a.took_us is not None and not a.took_us > 0:
         p.error("a step takes more than no time")
+    if not 0 <= a.choices <= StepSpec().experts:
+        p.error(f"a step has {StepSpec().experts} experts to choose from")
     from . import ccld
-    work = RankStep()
+    work = RoutedStep(choices=a.choices) if a.choices else RankStep()
     usual, busy = even_load(a.rows, work.spec.experts), even_load(int(a.rows * a.times), work.spec.experts)
     usual_ns, busy_ns = work.measure([usual, busy])
     compute_ns = np.full(a.ranks, usual_ns, dtype=np.int64)
