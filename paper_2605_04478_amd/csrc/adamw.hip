@@ -73,21 +73,23 @@ __global__ void k_adamw_begin(BeginJob j) {
 constexpr float FIRST_MOST = 448.0f, SECOND_MOST = 57344.0f;            // the largest values of e4m3 and e5m2
 constexpr float SECOND_LEAST = 0x1p-16f;                               // the smallest of e5m2 but zero
 
-// x / scale, whose reciprocal is at hand: a step of the division's remainder takes out what rounding that did
+// |x| / scale rounded towards zero, whose reciprocal is at hand: a step of the division's remainder makes it the nearest quotient, the sign of what then remains says whether that is
+// too large.  What random bits are added to is then not rounded before: a value goes up or down as the exact quotient says.
 __device__ __forceinline__ float quotient(float x, float scale, float reciprocal) {
-  const float q = x * reciprocal;
-  return fmaf(fmaf(-q, scale, x), reciprocal, q);
+  const float a = fabsf(x), first = a * reciprocal, q = fmaf(fmaf(-first, scale, a), reciprocal, first);
+  return __builtin_bit_cast(float, __builtin_bit_cast(u32, q) - (fmaf(-q, scale, a) < 0 ? 1u : 0u));
 }
 // The card's rounding to 8 bits by random bits adds those of `random` from the top on to what is cut off, below the smallest normal values too (it was compared with an addition
-// to the bits of a float for 2 million values in all of both formats' binades: equal).  16 random bits, and the middle of the interval that they leave.
+// to the bits of a float for 2 million values in all of both formats' binades: equal).  16 random bits, and the middle of the interval that they leave: at most 8 (16) short of a step, so that the block's largest
+// value, which the scale's rounding may leave 2 units in the last place above the format's, stays.
 template <int TO>
 __device__ __forceinline__ u32 put_first(float q, u32 random, u32 word) {
-  return (u32)__builtin_amdgcn_cvt_sr_fp8_f32(__builtin_amdgcn_fmed3f(q, -FIRST_MOST, FIRST_MOST), (int)(random << 16 | 0x8000), (int)word, TO);
+  return (u32)__builtin_amdgcn_cvt_sr_fp8_f32(q, (int)(random << 16 | 0x8000), (int)word, TO);
 }
 // (never zero for what is not)
 template <int TO>
 __device__ __forceinline__ u32 put_second(float q, float v, u32 random, u32 word) {
-  return (u32)__builtin_amdgcn_cvt_sr_bf8_f32(__builtin_amdgcn_fmed3f(q, v > 0 ? SECOND_LEAST : 0.0f, SECOND_MOST), (int)((random & 0xFFFF0000u) | 0x8000), (int)word, TO);
+  return (u32)__builtin_amdgcn_cvt_sr_bf8_f32(fmaxf(q, v > 0 ? SECOND_LEAST : 0.0f), (int)((random & 0xFFFF0000u) | 0x8000), (int)word, TO);
 }
 
 // The largest of 32 lanes' values, which are not negative: as whole numbers these have the same order, with NaN above all others.
@@ -97,11 +99,7 @@ __device__ __forceinline__ u32 half_max(u32 v) {
   v = max_with<0x128>(max_with<0x124>(max_with<0x122>(max_with<0x121>(v))));      // row_ror: 1, 2, 4, 8
   return max(v, (u32)__shfl_xor((int)v, 16, 32));
 }
-// a block's scale: NaN where a value of it is not finite
-__device__ __forceinline__ float scale_of(u32 largest, float most) {
-  if (largest >= 0x7F800000u) return __builtin_nanf("");
-  return fmaxf(__builtin_bit_cast(float, largest), __builtin_ldexpf(1.0f, -80)) * (1.0f / most);
-}
+__device__ __forceinline__ float scale_of(u32 largest, float most) { return fmaxf(__builtin_bit_cast(float, largest), 0x1p-80f) * (1.0f / most); }
 
 // each operation rounded by itself, as a program that takes them one after another has them: 8-bit values next to one of the random borders then go the same way
 __device__ __forceinline__ void next_moments(float& m, float& v, float g, const AdamwJob& j) {
@@ -169,13 +167,14 @@ __global__ __launch_bounds__(ADAMW_THREADS) void k_adamw(AdamwJob j) {
         v[i] = sv * v0[0]; v[i + 1] = sv * v0[1]; v[i + 2] = sv * v1[0]; v[i + 3] = sv * v1[1];
       }
     }
-    u32 most_m = 0, most_v = 0;
+    float most_m = 0;
+    u32 most_v = 0;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
       next_moments(m[i], v[i], g[i], j);
       if constexpr (BITS == 8) {
-        most_m = max(most_m, __builtin_bit_cast(u32, m[i]) & 0x7FFFFFFFu);
-        most_v = max(most_v, __builtin_bit_cast(u32, v[i]) & 0x7FFFFFFFu);
+        most_m = fmaxf(most_m, fabsf(m[i]));
+        most_v = max(most_v, __builtin_bit_cast(u32, v[i]));
       }
       // (the card's square root and reciprocal, off by a step each)
       const float ratio = m[i] * __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_sqrtf(v[i] * j.up), s.root, j.eps));
@@ -205,7 +204,11 @@ __global__ __launch_bounds__(ADAMW_THREADS) void k_adamw(AdamwJob j) {
       store_once<EACH>(static_cast<float*>(j.m) + state, qm);
       store_once<EACH>(static_cast<float*>(j.v) + state, qv);
     } else {
-      const float sm = scale_of(half_max(most_m), FIRST_MOST), sv = scale_of(half_max(most_v), SECOND_MOST);
+      // a gradient that is not finite leaves a v that is not, which is larger as a whole number than all that are (m's largest may hide one): NaN for the block
+      const u32 largest = half_max(most_v);
+      const bool finite = largest < 0x7F800000u;
+      const float sm = finite ? scale_of(half_max(__builtin_bit_cast(u32, most_m)), FIRST_MOST) : __builtin_nanf("");
+      const float sv = finite ? scale_of(largest, SECOND_MOST) : __builtin_nanf("");
       const float im = 1.0f / sm, iv = 1.0f / sv;
       const u32 key = mix(s.key ^ (u32)((u64)state >> 32));
       u32 r[EACH];
@@ -214,7 +217,7 @@ __global__ __launch_bounds__(ADAMW_THREADS) void k_adamw(AdamwJob j) {
       Words qm, qv;
 #pragma unroll
       for (int i = 0; i < EACH; i += 4) {
-        auto first = [&](int n) { return quotient(m[i + n], sm, im); };
+        auto first = [&](int n) { return copysignf(quotient(m[i + n], sm, im), m[i + n]); };
         auto second = [&](int n) { return quotient(v[i + n], sv, iv); };
         qm[i / 4] = put_first<3>(first(3), r[i + 3], put_first<2>(first(2), r[i + 2], put_first<1>(first(1), r[i + 1], put_first<0>(first(0), r[i], 0))));
         qv[i / 4] = put_second<3>(second(3), v[i + 3], r[i + 3], put_second<2>(second(2), v[i + 2], r[i + 2], put_second<1>(second(1), v[i + 1], r[i + 1],

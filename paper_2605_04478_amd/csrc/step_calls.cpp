@@ -588,10 +588,11 @@ PyObject* adamw(PyObject* const* args) {
   ccld_adamw_args a{};
   a.dtype = a.grad_dtype = type_of(first, true);
   std::vector<ccld_adamw_tensor> tensors;
-  std::vector<Tensor> stepped;
+  std::vector<Tensor> stepped, kept_grads;               // (held while the interpreter is left)
   std::vector<std::pair<uintptr_t, uintptr_t>> ranges;
   tensors.reserve(params.n);
   stepped.reserve(params.n);
+  kept_grads.reserve(params.n);
   ranges.reserve(params.n);
   at::ScalarType grad_type = at::ScalarType::Undefined;
   for (Py_ssize_t i = 0; i < params.n; ++i) {
@@ -608,6 +609,7 @@ PyObject* adamw(PyObject* const* args) {
       grad_type = g.scalar_type();
       tensors.push_back({p.data_ptr(), in(g), n, a.total});
       stepped.push_back(p);
+      kept_grads.push_back(g);
     }
     a.total += (n + CCLD_ADAMW_BLOCK - 1) / CCLD_ADAMW_BLOCK * CCLD_ADAMW_BLOCK;
   }
