@@ -22,10 +22,12 @@ using namespace ccld;
 
 namespace {
 
-constexpr int BLOCK = CCLD_ADAMW_BLOCK, ADAMW_THREADS = 256;
+constexpr int BLOCK = CCLD_ADAMW_BLOCK, ADAMW_THREADS = 128;
 // neighbouring elements of a thread: 16 bytes of a 32-bit state, 8 of one in 8 bits
 constexpr int each_of(int bits) { return bits == 32 ? 4 : 8; }
-constexpr int CHUNK = 4096;                              // elements of a workgroup
+// elements of a workgroup: one vector to a thread, or two of 8 bits, which have more to compute.  (90M elements with masters: 406 us; 413 in workgroups of 256 threads, 444 with two vectors to
+// a thread, 465 with four, 491 with eight.  320M with 8-bit states: 561; 577 with one vector, 586 with four.)
+constexpr int chunk_of(int bits) { return bits == 32 ? 512 : 2048; }
 typedef u32 Words __attribute__((ext_vector_type(2), aligned(4)));      // 8-bit values
 constexpr int LISTED = 112;                              // tensors of a launch: its arguments have 4 KB
 
@@ -110,7 +112,7 @@ __device__ __forceinline__ void next_moments(float& m, float& v, float g, const 
 
 template <class T, class G, int BITS, bool MASTERS>
 __global__ __launch_bounds__(ADAMW_THREADS) void k_adamw(AdamwJob j) {
-  constexpr int EACH = each_of(BITS), PASSES = CHUNK / (ADAMW_THREADS * EACH);
+  constexpr int EACH = each_of(BITS), CHUNK = chunk_of(BITS), PASSES = CHUNK / (ADAMW_THREADS * EACH);
   // the last tensor that starts at or before this workgroup
   int mine = -1;
   for (int i = 0; i < j.n_tensors; i += CCLD_WAVE) {
@@ -290,16 +292,16 @@ extern "C" ccld_status ccld_adamw(const ccld_adamw_args* a, void* stream) {
     groups = 0;
     j.n_tensors = 0;
   };
-  const i64 most = most_groups(ADAMW_THREADS);
+  const i64 most = most_groups(ADAMW_THREADS), chunk = chunk_of(a->bits);
   for (i64 i = 0; i < a->n_tensors; ++i) {
     const ccld_adamw_tensor& t = a->tensors[i];
     // (a tensor that is too long for a launch is taken in pieces)
     for (i64 done = 0; done < t.n;) {
       if (j.n_tensors == LISTED || groups == (u32)most) flush();
-      const i64 n = std::min(t.n - done, (most - groups) * CHUNK);
+      const i64 n = std::min(t.n - done, (most - groups) * chunk);
       j.tensors[j.n_tensors++] = Tensor{static_cast<uint8_t*>(t.p) + done * size_of(a->dtype), static_cast<const uint8_t*>(t.g) + done * size_of(a->grad_dtype), n,
                                         (u32)((t.start + done) / BLOCK), groups};
-      groups += (u32)blocks_for(n, CHUNK);
+      groups += (u32)blocks_for(n, chunk);
       done += n;
     }
   }
