@@ -3,8 +3,8 @@
 //   z = logits / T      S = sum exp(z - m)      lse = m + log S      logp = z[token] - lse      entropy = log S + sum exp(z - m) (m - z) / S
 //   dlogits = (dlogp ([v = token] - p) - dentropy p (log p + entropy)) / T,  p = exp(z - lse)
 //
-// Memory bounds both, the exponentials and their dozen of operations to a logit come next.  Largest logit, sum and entropy's sum are taken in one pass: a thread moves to a
-// vector's maximum if that is larger than its own, and adds up relative to it.  The entropy's terms all have one sign, so nothing cancels.  Few
+// Memory bounds both, the exponentials and their dozen of operations to a logit come next.  Largest logit, sum and entropy's sum are taken in one pass: a thread
+// adds up relative to a value next to the largest that it has seen, so that the entropy's terms do not cancel.  Few
 // long rows are cut into parts, one to a workgroup, which a second launch joins in their order.
 //
 // Alternatives: of the threads' maxima the `top` largest are as many different logits, so the smallest of them bounds the row's `top` largest logits from
@@ -56,19 +56,24 @@ __device__ __forceinline__ float largest_of(const float (&z)[N]) {
   return m;
 }
 
-// Sums of exp2((z - m) c) and of exp2((z - m) c) (m - z) c.
+// Sums of exp2((z - m) c) and of exp2((z - m) c) (m - z) c.  m follows the largest value seen where that is more than 2^8 times as large: a wavefront then moves a few times in a
+// row and not with almost every vector.  The second sum's terms below zero are at most 8 of the first's, which cost the entropy 2^-21 at most.
+constexpr float LEEWAY = 8.0f;
 struct Sums {
-  float m = LOWEST, s = 0, b = 0;
-  // the same relative to a maximum that is at least as large
+  float m = LOWEST, s = 0, b = 0, most = LOWEST;
+  // the same relative to another value, above m or some way below
   __device__ __forceinline__ void move(float to, float c) {
     if (to == LOWEST) return;
-    const float d = m == LOWEST ? 0.0f : (m - to) * c, f = exp2f(d);
+    const float d = m == LOWEST ? 0.0f : (m - to) * c, f = __builtin_amdgcn_exp2f(d);
     b = f * (b - s * fmaxf(d, NOTHING));
     s *= f;
     m = to;
   }
   template <int N>
-  __device__ __forceinline__ void terms(const float (&z)[N], float from, float c) {
+  __device__ __forceinline__ void add(const float (&z)[N], float c) {
+    most = fmaxf(most, largest_of(z));
+    if ((most - m) * c > LEEWAY) move(most, c);
+    const float from = m == LOWEST ? 0.0f : m;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const float d = (z[i] - from) * c, e = __builtin_amdgcn_exp2f(d);
@@ -76,49 +81,54 @@ struct Sums {
       b -= e * fmaxf(d, NOTHING);
     }
   }
-  template <int N>
-  __device__ __forceinline__ void add(const float (&z)[N], float c) {
-    float most = m;
-#pragma unroll
-    for (int i = 0; i < N; ++i) most = fmaxf(most, z[i]);
-    if (most > m) move(most, c);
-    terms(z, m == LOWEST ? 0.0f : m, c);
-  }
 };
 
-// Rows that are read as often as they are gone through, BATCH vectors of 16 bytes to a thread at a time.  each(f) calls f(values, first column).
+// Rows that are read as often as they are gone through, BATCH vectors of 16 bytes to a thread at a time, with the next ones on their way.
+// each(f) calls f(values, first column); values that do not fill a vector go to the first threads, one each.
 template <class T, int THREADS>
 struct Streamed {
   static constexpr int N = 16 / sizeof(T), BATCH = 4;
+  static constexpr u32 STEP = BATCH * THREADS * N;
   const T* row;
-  i64 vocab;
-  __device__ __forceinline__ Streamed(const T* row_, i64 vocab_) : row(row_), vocab(vocab_) {}
+  u32 vocab;
+  __device__ __forceinline__ Streamed(const T* row_, i64 vocab_) : row(row_), vocab((u32)vocab_) {}
+  __device__ __forceinline__ u32 whole() const { return vocab - vocab % N; }
+  // (columns behind the last vector load that one: without a branch the loads of a batch are all on their way at once)
+  __device__ __forceinline__ void load(Vec<T, N> (&v)[BATCH], u32 at) const {
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) v[i] = load_vec<N>(row + min(at + i * THREADS * N, vocab - N));
+  }
   template <class F>
   __device__ __forceinline__ void each(F f) const {
-    i64 at = (i64)threadIdx.x * N;
-    for (; at + (i64)(BATCH - 1) * THREADS * N + N <= vocab; at += (i64)BATCH * THREADS * N) {
-      Vec<T, N> v[BATCH];
+    const u32 end = whole();
+    if (end) {
+      u32 at = threadIdx.x * N;
+      Vec<T, N> now[BATCH];
+      load(now, at);
+      for (u32 done = 0; done < end; done += STEP, at += STEP) {
+        Vec<T, N> next[BATCH];
+        if (done + STEP < end) load(next, at + STEP);
+        auto use = [&](int i) {
+          float z[N];
 #pragma unroll
-      for (int i = 0; i < BATCH; ++i) v[i] = load_vec<N>(row + at + (i64)i * THREADS * N);
+          for (int n = 0; n < N; ++n) z[n] = (float)now[i][n];
+          f(z, (i64)(at + i * THREADS * N));
+        };
+        if (end - done >= STEP) {
 #pragma unroll
-      for (int i = 0; i < BATCH; ++i) {
-        float z[N];
+          for (int i = 0; i < BATCH; ++i) use(i);
+        } else {
 #pragma unroll
-        for (int n = 0; n < N; ++n) z[n] = (float)v[i][n];
-        f(z, at + (i64)i * THREADS * N);
+          for (int i = 0; i < BATCH; ++i)
+            if (at + i * THREADS * N < end) use(i);
+        }
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) now[i] = next[i];
       }
     }
-    for (; at + N <= vocab; at += (i64)THREADS * N) {
-      const Vec<T, N> v = load_vec<N>(row + at);
-      float z[N];
-#pragma unroll
-      for (int n = 0; n < N; ++n) z[n] = (float)v[n];
-      f(z, at);
-    }
-    // (one thread has what is left of the row)
-    for (; at < vocab; ++at) {
-      const float z[1] = {(float)row[at]};
-      f(z, at);
+    if (threadIdx.x < vocab - end) {
+      const float z[1] = {(float)row[end + threadIdx.x]};
+      f(z, (i64)(end + threadIdx.x));
     }
   }
   // each(f) with the results stored to the same columns of `out`; `next` is not needed
@@ -132,7 +142,7 @@ struct Streamed {
     });
   }
   // the thread that stores a column
-  __device__ __forceinline__ int owner(int at) const { return at / N % THREADS; }
+  __device__ __forceinline__ int owner(int at) const { return (u32)at < whole() ? at / N % THREADS : at - (int)whole(); }
 };
 
 // Rows that stay in registers.  Vectors and values behind the row's end are the lowest.
@@ -362,7 +372,7 @@ __global__ __launch_bounds__(THREADS) void k_logprobs(LogprobJob j) {
     const Streamed<T, THREADS> row(static_cast<const T*>(j.logits) + r * j.ld + start, min(j.span, j.vocab - start));
     Sums x;
     row.each([&](const auto& z, i64) { x.add(z, c); });
-    const float most = x.m;
+    const float most = x.most;
     __syncthreads();                        // the row before is done with
     x.move(max_of_all<THREADS>(most, places[0]), c);
     x.s = sum_of_all<THREADS>(x.s, places[1]);
