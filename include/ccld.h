@@ -407,6 +407,9 @@ ccld_status ccld_profile_read(ccld_ctx *ctx, double *ms, uint64_t *launches, uin
  * was given more work, and these are the kinds of work that are uneven by design (experts with different
  * numbers of rows, the loss that only the last pipeline stage has) or that only memory bounds (norms).
  *
+ * What a step needs around these is below: the choice of experts, tokens sorted by expert and back, the optimizer, log
+ * probabilities of given tokens.
+ *
  * They need no context.  Arguments are checked before anything is enqueued; work goes to `stream` (a
  * hipStream_t) of the current device and the call returns before it is done.  Nothing is allocated: where a
  * workspace is needed its size comes from the query beside the call, and it may be reused as soon as the

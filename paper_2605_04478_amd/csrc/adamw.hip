@@ -3,7 +3,7 @@
 //   t = ++count      g' = scale g      m = b1 m + (1 - b1) g'      v = b2 v + (1 - b2) g'^2
 //   p = p - lr wd p - lr / (1 - b1^t) m / (sqrt(v) / sqrt(1 - b2^t) + eps)
 //
-// Memory bounds it: some thirty operations to the 10 to 30 bytes of an element.  The tensors of a launch are listed in its arguments, so that nothing has to
+// Memory bounds it: thirty operations, or sixty with states in 8 bits, to the 10 to 30 bytes of an element.  The tensors of a launch are listed in its arguments, so that nothing has to
 // be copied to the device and a captured launch keeps its list; a workgroup finds its tensor by a ballot over the list.  What depends on
 // the count is computed once, on the device, by a launch of one thread: a replayed graph counts on.
 //
@@ -11,6 +11,9 @@
 // thousands of times the others' must not lift the others' v, for which its 32 powers of two matter more than a bit of precision.  Rounding to nearest would not
 // follow b2 = 0.999, whose steps are a hundredth of what two or three bits tell apart; values are rounded up or down at random, with the odds that keep
 // the mean.  The card converts and rounds both formats.
+//
+// Measured (a copy of 2 GB moves 4.9 TB/s here, x + 1 6.1): 200 tensors, 90M elements in bfloat16 with masters 406 us = 6.2 TB/s; 320M in bfloat16 with 8-bit states 561 us = 5.7 TB/s, where the sixty operations
+// of an element take nearly as long (732 with conversions and rounding by hand, exact root and quotient); six small tensors 2 + 4 us of a call's 8.7.
 #include <algorithm>
 
 #include <math.h>

@@ -6,6 +6,9 @@
 // Memory bounds all four.  A token belongs to a team of threads, so that its own row is moved once however many experts it has: spreading writes
 // one loaded vector to k rows, gathering adds k rows up in registers in the order of j, rounded once.  A place outside the rows is
 // never followed.
+//
+// Measured (a copy of 2 GB moves 4.9 TB/s here, x + 1 6.1): 32,768 x 4,096 in bfloat16 with 8 experts: dispatch 462 us = 5.2 TB/s, combine and dispatch's gradient 445 = 5.4, combine's gradient 899 =
+// 5.1; 8,192 x 2,048 with 2: 15 to 17 and 26; 3,001 x 1,001 in half precision with 3, whose rows start anywhere: 5 to 7 and 10.  5 tokens: 3 us each.
 #include <algorithm>
 
 #include "ccld_internal.h"

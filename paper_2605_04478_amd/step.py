@@ -2,7 +2,8 @@
 
 A rank that the analysis calls computation-slow (Section 2.2, S1) has a slow card, or was given more work than its peers.
 These operators are the work to run on such a card, and the kinds of work that are uneven by design: the products of
-a rank's experts, whose rows routing decides, and the loss over the vocabulary, which the last pipeline stage alone has; and the norms around a block, which only memory bounds.  The HIP library computes them; this module checks arguments and marshals them
+a rank's experts, whose rows routing decides, and the loss over the vocabulary, which the last pipeline stage alone has; and the norms around a block, which only memory bounds.  Beside them
+stands what a step needs around its products: the choice of experts, tokens sorted by expert and back, log probabilities of given tokens, and the optimizer.  The HIP library computes them; this module checks arguments and marshals them
 (for ordinary tensors in native code), PyTorch supplies memory and the stream.  Every call goes to the current stream of its tensors' device and returns before it is
 done; outputs and workspaces come from torch's allocator, so calls may be captured into a graph.  (Who captures a backward pass of
 the classes below captures its forward pass with it, while no eager result of the same leaves is alive: torch would have the
