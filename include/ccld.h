@@ -584,7 +584,7 @@ typedef struct {
   const ccld_adamw_tensor *tensors;  /* host memory, read before the call returns                       */
   int64_t n_tensors, total;
   int64_t *count;                    /* on the device: steps taken, in and out                          */
-  void *m, *v;                       /* [total]                                                         */
+  void *m, *v;                       /* [total], aligned to 4 bytes                                     */
   float *m_scale, *v_scale;          /* [total / CCLD_ADAMW_BLOCK] (8 bits)                             */
   float *master;                     /* [total] or NULL                                                 */
   void *workspace;                   /* CCLD_ADAMW_WORKSPACE bytes                                      */

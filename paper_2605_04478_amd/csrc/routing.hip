@@ -254,6 +254,7 @@ constexpr int ORDER_THREADS = 256;
 // Stretches of 256 entries, all of which are on their way at once; longer ones where there would be more than 256 chunks.
 constexpr int AT_ONCE = 4;
 constexpr u32 MOST_CHUNKS = 256, LEAST_STRETCH = AT_ONCE * CCLD_WAVE, SINGLE_CHUNK = 16 * LEAST_STRETCH;
+constexpr u32 FEW_ENTRIES = 4 * LEAST_STRETCH;          // one workgroup of four wavefronts, up to SINGLE_CHUNK one of sixteen
 
 // the experts of a wavefront's next entries, n for those that have none
 template <class I>
@@ -412,7 +413,7 @@ __global__ __launch_bounds__(THREADS) void k_order_place(OrderJob j) {
 OrderJob order_job(const ccld_order_args* a, uint64_t* bytes) {
   OrderJob j{a->experts, a->places, a->offsets, static_cast<u32*>(a->workspace), nullptr, (u32)(a->tokens * a->k), 1, 0, (int)a->n_experts};
   if (j.entries <= SINGLE_CHUNK) {
-    j.stretch = (u32)blocks_for(std::max<u32>(j.entries, 1), 1024) * CCLD_WAVE;
+    j.stretch = (u32)blocks_for(std::max<u32>(j.entries, 1), j.entries <= FEW_ENTRIES ? ORDER_THREADS : 1024) * CCLD_WAVE;
     *bytes = 0;
   } else {
     const u64 waves = MOST_CHUNKS * (ORDER_THREADS / CCLD_WAVE);
@@ -427,7 +428,9 @@ OrderJob order_job(const ccld_order_args* a, uint64_t* bytes) {
 }
 template <class I>
 void launch_order(const OrderJob& j, hipStream_t stream) {
-  if (j.chunks == 1) {
+  if (j.entries <= FEW_ENTRIES) {
+    k_order_place<I, ORDER_THREADS><<<1, ORDER_THREADS, 0, stream>>>(j);
+  } else if (j.chunks == 1) {
     k_order_place<I, 1024><<<1, 1024, 0, stream>>>(j);
   } else {
     k_order_count<I><<<j.chunks, ORDER_THREADS, 0, stream>>>(j);

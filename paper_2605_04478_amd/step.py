@@ -830,7 +830,8 @@ def adamw(params, grads, state, lr: float, betas=(0.9, 0.999), eps: float = 1e-8
 
     params are contiguous and of one type, bfloat16, float16 or float32; grads of that type or float32, all of one.  A tensor whose
     gradient is None is left as it is, with its state.  scale is a number, or a tensor of one float32 on the GPU (a clipping that was
-    computed there).  The count is kept on the GPU: a captured step counts on when it is replayed.  8-bit states are rounded up or down
+    computed there).  The count is kept on the GPU: a captured step counts on when it is replayed (with
+    the rates that it was captured with).  8-bit states are rounded up or down
     at random, by `seed`, the count and the element.  A gradient that is not finite leaves NaN: in 8-bit states, in its whole block."""
     if _native().adamw(params, grads, state, lr, betas, eps, weight_decay, scale, seed) is not None:
         return
@@ -853,7 +854,7 @@ def adamw(params, grads, state, lr: float, betas=(0.9, 0.999), eps: float = 1e-8
                        _ptr(state.get("master")), ws.data_ptr(), ADAMW_WORKSPACE)
         _call(lib().ccld_adamw, a, device)
     del ws
-    torch.autograd.graph.increment_version([p for p, g in zip(params, grads) if g is not None])
+    torch.autograd.graph.increment_version([p for p, g in zip(params, grads) if g is not None and not p.is_inference()])
 
 
 class AdamW:

@@ -285,6 +285,16 @@ def test_a_saved_parameter_is_known_to_have_changed():
             y.backward()
 
 
+def test_parameters_of_inference_mode():
+    with torch.inference_mode():
+        p, g = torch.ones(10, device=DEV), torch.ones(10, device=DEV)
+        for grad in (g, torch.stack([g, g], -1)[..., 0]):
+            state = step.adamw_state([p])
+            step.adamw([p], [grad], state, 0.5)
+        # two first steps of 0.5, each by a ratio of 1 that passes 16 roundings of 2^-24 (and eps, 2^-26): off by 2 (0.5 (16 + 1) + 1) 2^-24 < 2^-19
+        assert float(p.abs().max()) < 2.0 ** -19
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 def test_captured_and_replayed(bits):
     make = lambda: _tensors([(3000,), (77, 13), (5,)], torch.bfloat16, None, seed=4)

@@ -103,7 +103,7 @@ def test_lowest_values_are_scores():
 
 
 @pytest.mark.parametrize("bits", [torch.int32, torch.int64], ids=str)
-@pytest.mark.parametrize("tokens,k,n", [(0, 2, 3), (1, 1, 1), (5, 4, 16), (63, 1, 7), (100, 3, 12), (2048, 4, 64), (8193, 1, 5), (3001, 3, 1024), (40000, 8, 128), (300001, 1, 256),
+@pytest.mark.parametrize("tokens,k,n", [(0, 2, 3), (1, 1, 1), (5, 4, 16), (63, 1, 7), (100, 3, 12), (1024, 1, 40), (1025, 1, 40), (4096, 1, 9), (4097, 1, 9), (2048, 4, 64), (8193, 1, 5), (3001, 3, 1024), (40000, 8, 128), (300001, 1, 256),
                                         (150000, 2, 2)])
 def test_expert_order(tokens, k, n, bits):
     rng = np.random.default_rng(tokens + n)
