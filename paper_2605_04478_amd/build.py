@@ -30,7 +30,7 @@ def _step_commands():
            "-isystem", ROCM_INCLUDE, "-isystem", os.path.join(at, "include"), "-isystem", os.path.join(at, "include", "torch", "csrc", "api", "include"),
            "-isystem", sysconfig.get_paths()["include"], "-c", STEP_SOURCE, "-o", obj]
     yield [HIPCC, "-shared", "-fPIC", "-o", STEP, obj, LIB, "-Wl,-rpath,$ORIGIN", "-L", os.path.join(at, "lib"),
-           "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip"]
+           "-ltorch_python", "-ltorch_cpu", "-ltorch_hip", "-lc10", "-lc10_hip"]
 
 
 def build_lib(verbose: bool = False) -> str:

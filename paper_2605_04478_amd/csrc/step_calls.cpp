@@ -11,7 +11,7 @@
 
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
-#include <ATen/ops/empty.h>
+#include <ATen/hip/EmptyTensor.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 
@@ -73,7 +73,8 @@ struct Device {
     has(t);
     require(t.dim() == 1 && t.scalar_type() == type && t.size(0) == n && t.is_contiguous());
   }
-  Tensor empty(at::IntArrayRef shape, at::ScalarType type) const { return at::empty(shape, at::TensorOptions().dtype(type).device(device)); }
+  // (straight from the GPU's allocator: torch::empty takes 0.2 us longer to get there)
+  Tensor empty(at::IntArrayRef shape, at::ScalarType type) const { return at::detail::empty_cuda(shape, type, device, std::nullopt); }
   void* stream() const { return c10::hip::getCurrentHIPStream(device.index()).stream(); }
 };
 
