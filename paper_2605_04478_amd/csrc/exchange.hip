@@ -74,6 +74,7 @@ __global__ __launch_bounds__(threads_of(TEAM)) void k_dispatch(ExchangeJob j) {
     int c = me * N;
     for (; c + N <= j.d; c += TEAM * N) {
       const Vec<T, N> v = load_vec<N>(x + c);
+#pragma unroll 4
       for (int i = 0; i < j.k; ++i) {
         const int at = p.at(i);
         if (at >= 0) store_once<N>(y + at * j.ldy_out + c, v);
@@ -236,12 +237,14 @@ ccld_status exchange(const ccld_exchange_args* a, Way way, void* stream) {
   with_type(a->dtype, [&](auto zero) {
     using T = decltype(zero);
     // a vector to a thread: dispatch, combine, its gradient and dispatch's of 8,192 x 4,096 in bfloat16 with 8 experts each take 104, 112, 223 and 111 us in teams of 512 threads, 108, 118, 233
-    // and 118 in teams of 256, 118, 137, 272 and 135 in wavefronts; of 8,192 x 1,024 with 2 experts 9.6, 10.4, 25 and 10 in teams of 512 and 9.0, 9.0, 15 and 9.2 in teams of 128
+    // and 118 in teams of 256, 118, 137, 272 and 135 in wavefronts; of 8,192 x 1,024 with 2 experts 9.6, 10.4, 25 and 10 in teams of 512 and 9.0, 9.0, 15 and 9.2 in teams of 128; of 8,192 x 4,096 in 32 bits with 2 experts 73, 70, 123 and 70 in teams of 1,024 and
+    // 75, 74, 129 and 74 in teams of 512
     const i64 vectors = blocks_for(a->d, 16 / (i64)sizeof(T));
     if (vectors <= 64) launch<T, CCLD_WAVE>(j, way, st);
     else if (vectors <= 128) launch<T, 128>(j, way, st);
     else if (vectors <= 256) launch<T, 256>(j, way, st);
-    else launch<T, 512>(j, way, st);
+    else if (vectors <= 512) launch<T, 512>(j, way, st);
+    else launch<T, 1024>(j, way, st);
   });
   return launched();
 }
