@@ -37,6 +37,7 @@ struct LogprobJob {
   float temperature;
   int top, token_bits;
   i64 parts, span;               // of a row, and their columns
+  int held;                      // vectors of a thread, where a row is cut into parts
   float *part_sums, *part_values;        // [rows][parts][3], [rows][parts][top]
   int* part_ids;
 };
@@ -275,7 +276,7 @@ struct Alternatives {
 
   // all threads call this; most: the largest of the thread's values
   template <class ROW, class PUT>
-  __device__ __forceinline__ void find(ROW row, float most, int top, PUT put) {
+  __device__ __forceinline__ void find(ROW& row, float most, int top, PUT put) {
     static_assert(THREADS == 4 * CCLD_WAVE && THREADS >= CCLD_TOP_MOST, "four maxima to a lane, as many as alternatives");
     const int me = threadIdx.x;
     __syncthreads();                        // the row before is done with
@@ -365,16 +366,17 @@ __device__ __forceinline__ void put_values(const LogprobJob& j, i64 r, const Val
 }
 
 // A row, or (j.parts > 1) a part of one, to a workgroup.
-template <class T, int THREADS>
+// VECS: the parts are held in registers; 0: read as often as they are gone through
+template <class T, int THREADS, int VECS>
 __global__ __launch_bounds__(THREADS) void k_logprobs(LogprobJob j) {
   __shared__ float places[3][16];
   __shared__ Alternatives<THREADS> alternatives;
   const float c = LOG2E / j.temperature;
   for (i64 b = blockIdx.x; b < j.rows * j.parts; b += gridDim.x) {
     const i64 r = b / j.parts, start = (b - r * j.parts) * j.span;
-    const Streamed<T, THREADS> row(static_cast<const T*>(j.logits) + r * j.ld + start, min(j.span, j.vocab - start));
+    typename RowOf<T, THREADS, VECS>::type row(static_cast<const T*>(j.logits) + r * j.ld + start, min(j.span, j.vocab - start));
     Sums x;
-    row.each([&](const auto& z, i64) { x.add(z, c); });
+    row.each([&](const auto& z, auto) { x.add(z, c); });
     const float most = x.most;
     __syncthreads();                        // the row before is done with
     x.move(max_of_all<THREADS>(most, places[0]), c);
@@ -431,7 +433,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_logprobs_join(LogprobJob j) {
     if (threadIdx.x == 0) put_values<T>(j, r, v);
     if (!j.top) continue;
     const i64 first = r * j.parts * j.top;
-    const Candidates row{j.part_values + first, j.part_ids + first, (int)j.parts * j.top};
+    Candidates row{j.part_values + first, j.part_ids + first, (int)j.parts * j.top};
     float most = LOWEST;
     row.each([&](const auto& z, i64) { most = fmaxf(most, z[0]); });
     alternatives.find(row, most, j.top, [&](int rank, float z, int at) {
@@ -499,18 +501,24 @@ ccld_status check(const ccld_logprob_args* a) {
 }
 LogprobJob make_job(const ccld_logprob_args* a) {
   return LogprobJob{a->logits, a->tokens, a->logp, a->entropy, a->lse, a->top_logp, a->top_ids, a->dlogp, a->dentropy, a->dlogits, a->ldlogits, a->lddlogits,
-                    a->dlogp_stride, a->dentropy_stride, a->rows, a->vocab, a->temperature, a->top, a->token_bits, 1, a->vocab};
+                    a->dlogp_stride, a->dentropy_stride, a->rows, a->vocab, a->temperature, a->top, a->token_bits, 1, a->vocab, 0};
 }
-// Few rows are cut into parts of two vectors to a thread and more, so that there are two workgroups to a compute unit.
-constexpr i64 MOST_PARTS = CCLD_WAVE;
+// Few long rows are cut into parts of 4 or 8 vectors to a thread, which stay in registers (longer ones, where there would be more than MOST_PARTS, do not).  With 20 alternatives,
+// in parts of 4, of 8, and whole, bfloat16: 3 x 128,000 13.0, 14.3 and 23 us; 64 x 128,000 16.5, 16.5 and 32.6; 256 x 128,000 33.9, 29.1 and 38.1; 400 x 128,000 46.9, 40.1 and 44.6; 600 x 128,000 64.8, 53.0 and 54.1;
+// 64 x 20,000 13.3, 15.0 and 12.5; 128 x 32,000 14.0, 15.2 and 15.1; 600 x 32,000 24.7, 24.3 and 19.9.
+constexpr i64 MOST_PARTS = CCLD_WAVE, LEAST_PARTS = 5;
 constexpr int THREADS = 256;
 void cut_rows(LogprobJob& j, int32_t dtype, uint8_t* workspace, uint64_t* bytes) {
-  const i64 n = 16 / size_of(dtype), vectors = blocks_for(j.vocab, n);
-  j.parts = std::max<i64>(1, std::min({MOST_PARTS, vectors / (2 * THREADS), 2 * (i64)COMPUTE_UNITS / std::max<i64>(j.rows, 1)}));
+  const i64 n = 16 / size_of(dtype);
+  auto parts = [&](int vecs) { return blocks_for(j.vocab, vecs * THREADS * n); };
+  auto fits = [&](int vecs, i64 groups) { return parts(vecs) <= MOST_PARTS && j.rows * parts(vecs) <= groups * (i64)COMPUTE_UNITS; };
   *bytes = 0;
-  if (j.parts == 1) return;
-  j.span = blocks_for(vectors, j.parts) * n;
+  if (parts(4) < LEAST_PARTS) return;
+  j.held = fits(4, 4) ? 4 : fits(8, 16) ? 8 : 0;
+  if (j.held) j.span = j.held * THREADS * n;
+  else if (parts(8) > MOST_PARTS) j.span = blocks_for(blocks_for(j.vocab, n), std::max<i64>(1, std::min(MOST_PARTS, 2 * (i64)COMPUTE_UNITS / std::max<i64>(j.rows, 1)))) * n;
   j.parts = blocks_for(j.vocab, j.span);
+  if (j.parts == 1) return;
   auto take = [&](i64 each) {
     uint8_t* const at = workspace ? workspace + *bytes : nullptr;
     *bytes += ((uint64_t)(j.rows * j.parts * each) + 255) & ~(uint64_t)255;
@@ -574,7 +582,9 @@ extern "C" ccld_status ccld_token_logprobs(const ccld_logprob_args* a, void* str
   const u32 grid = (u32)std::min<i64>(j.rows * j.parts, 1 << 20);
   with_type(a->dtype, [&](auto zero) {
     using T = decltype(zero);
-    k_logprobs<T, THREADS><<<grid, THREADS, 0, st>>>(j);
+    if (j.held == 4) k_logprobs<T, THREADS, 4><<<grid, THREADS, 0, st>>>(j);
+    else if (j.held == 8) k_logprobs<T, THREADS, 8><<<grid, THREADS, 0, st>>>(j);
+    else k_logprobs<T, THREADS, 0><<<grid, THREADS, 0, st>>>(j);
     if (j.parts > 1) k_logprobs_join<T><<<(u32)j.rows, JOIN_THREADS, 0, st>>>(j);
   });
   return launched();

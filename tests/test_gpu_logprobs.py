@@ -88,7 +88,7 @@ def _check(logits, tokens, temperature, top, gradient=True):
 
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
 @pytest.mark.parametrize("rows,v,top,temperature", [(1, 1, 1, 1.0), (3, 7, 7, 0.7), (4, 5, 9, 1.0), (5, 1000, 20, 2.0), (2, 1025, 64, 1.0), (9, 4099, 5, 0.3), (511, 2000, 3, 1.0),
-                                                    (700, 1537, 10, 1.0), (513, 64, 64, 1.5), (4, 128000, 20, 1.0), (3, 50021, 1, 0.7), (2, 300001, 0, 1.0)])
+                                                    (700, 1537, 10, 1.0), (513, 64, 64, 1.5), (4, 128000, 20, 1.0), (3, 50021, 1, 0.7), (2, 300001, 0, 1.0), (2, 1200007, 5, 1.0), (90, 40000, 20, 1.0), (300, 33001, 2, 0.6)])
 def test_rows(rows, v, top, temperature, dtype):
     g = torch.Generator(device=DEV).manual_seed(rows + v)
     z = torch.randn(rows, v, device=DEV, generator=g) * (0.2 + 6 * torch.rand(rows, 1, device=DEV, generator=g))

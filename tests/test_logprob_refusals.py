@@ -6,7 +6,7 @@ import torch
 
 from paper_2605_04478_amd import ccld, step
 
-BAD_ARG, NULL, CAPACITY = -6, -7, -8
+BAD_ARG, NULL, CAPACITY, WORKSPACE = -6, -7, -8, -12
 NAN, INF = float("nan"), float("inf")
 
 
@@ -58,6 +58,19 @@ def test_token_logprobs_status(change, status):
 @pytest.mark.parametrize("change,status", BOTH + [(dict(dlogits=None), NULL), (dict(lddlogits=7), BAD_ARG), (dict(dlogits=1), BAD_ARG), (dict(dlogp=2), BAD_ARG)])
 def test_gradient_status(change, status):
     assert ccld.lib().ccld_token_logprobs_grad(C.addressof(_args(**change)), None) == status
+
+
+@pytest.mark.parametrize("rows", [0, 1, 3, 100, 513, 5000, (1 << 31) - 1])
+@pytest.mark.parametrize("vocab", [1, 1000, 50021, 128000, 1 << 20, (1 << 31) - 1])
+@pytest.mark.parametrize("dtype", [0, 2])
+def test_workspace_is_small(rows, vocab, dtype):
+    """64 parts of a row at most, each with three sums and `top` numbers and words, in as many as 4,096 workgroups."""
+    need = C.c_uint64(9)
+    assert ccld.lib().ccld_logprob_workspace(C.addressof(_args(rows=rows, vocab=vocab, ldlogits=vocab, dtype=dtype, top=64)), C.addressof(need)) == 0
+    assert need.value <= min(64 * rows, 4096) * (12 + 8 * 64) + 3 * 256
+    if need.value:
+        a = _args(rows=rows, vocab=vocab, ldlogits=vocab, dtype=dtype, top=64, workspace=1 << 20, workspace_bytes=need.value - 1)
+        assert ccld.lib().ccld_token_logprobs(C.addressof(a), None) == WORKSPACE
 
 
 def test_top_is_checked():
