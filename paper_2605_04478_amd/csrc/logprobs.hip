@@ -16,7 +16,7 @@
 // not stop while it is computed.
 //
 // Measured (a copy of 2 GB moves 4.9 TB/s here, x + 1 6.1): 8,192 x 128,000 in bfloat16 356 us = 5.9 TB/s, with 20 alternatives 462, the gradient 775 = 5.4 (951 without the next row's loads, 1,160 with rows
-// read twice); 1,003 x 50,021 in 32 bits 47 and 64; 3 x 128,000 with 20 alternatives 8 + 6 us, without 4.5 + 2.7.
+// read twice); 1,003 x 50,021 in 32 bits 47 and 64; 3 x 128,000 with 20 alternatives 8 + 5 us, without 4.5 + 2.7.
 #include <algorithm>
 #include <type_traits>
 

@@ -13,7 +13,7 @@
 //
 // Measured (a copy of 2 GB moves 4.9 TB/s here, an elementwise sum 6.0): 32,768 x 8,192 in bfloat16 372 us = 5.8 TB/s; 16,384 x 4,096 92 us = 5.8 TB/s
 // forward and 163 us = 5.0 TB/s of the bytes that the gradient needs (6 reads and writes of a row), with 6 us for the join; 3,003 x 2,500 in 32 bits 21, 35
-// and 6 us.  One row: 3 us of a call's 7.
+// and 6 us.  One row: 3 us of a call's 6.
 #include <algorithm>
 
 #include "ccld_internal.h"

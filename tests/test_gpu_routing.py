@@ -147,7 +147,7 @@ def _both_ways(tokens, k, n, d, dtype, dropped, seed=0, spread=0):
 
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
 @pytest.mark.parametrize("tokens,k,n,d,dropped,spread", [(1, 1, 1, 1, 0, 0), (1, 4, 16, 2048, 0, 0), (3, 2, 4, 7, 0.5, 0), (5, 64, 64, 130, 0.2, 3), (40, 9, 12, 1001, 0.1, 0),
-                                                         (33, 3, 8, 1024, 1.0, 0), (70, 8, 16, 4096, 0, 8), (9, 3, 4, 5003, 0.1, 1), (4, 2, 3, 20011, 0, 0), (257, 2, 5, 515, 0.3, 1), (18000, 1, 4, 24, 0.05, 0)])
+                                                         (33, 3, 8, 1024, 1.0, 0), (70, 8, 16, 4096, 0, 8), (9, 3, 4, 5003, 0.1, 1), (50, 3, 4, 1000, 0.1, 0), (50, 3, 4, 72, 0.1, 8), (4, 2, 3, 20011, 0, 0), (257, 2, 5, 515, 0.3, 1), (18000, 1, 4, 24, 0.05, 0)])
 def test_dispatch_and_combine(tokens, k, n, d, dropped, spread, dtype):
     places, offsets, x, y, dout, drows, weights = _both_ways(tokens, k, n, d, dtype, dropped, spread=spread)
     used, at = int(offsets[-1]), places.long().cpu()
