@@ -88,7 +88,8 @@ def _check(logits, tokens, temperature, top, gradient=True):
 
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
 @pytest.mark.parametrize("rows,v,top,temperature", [(1, 1, 1, 1.0), (3, 7, 7, 0.7), (4, 5, 9, 1.0), (5, 1000, 20, 2.0), (2, 1025, 64, 1.0), (9, 4099, 5, 0.3), (511, 2000, 3, 1.0),
-                                                    (700, 1537, 10, 1.0), (513, 64, 64, 1.5), (4, 128000, 20, 1.0), (3, 50021, 1, 0.7), (2, 300001, 0, 1.0), (2, 1200007, 5, 1.0), (90, 40000, 20, 1.0), (300, 33001, 2, 0.6)])
+                                                    (700, 1537, 10, 1.0), (513, 64, 64, 1.5), (4, 128000, 20, 1.0), (3, 50021, 1, 0.7), (2, 300001, 0, 1.0), (2, 1200007, 5, 1.0), (90, 40000, 20, 1.0), (300, 33001, 2, 0.6),
+                                                    (1500, 9001, 2, 1.0), (280, 70003, 1, 1.0)])
 def test_rows(rows, v, top, temperature, dtype):
     g = torch.Generator(device=DEV).manual_seed(rows + v)
     z = torch.randn(rows, v, device=DEV, generator=g) * (0.2 + 6 * torch.rand(rows, 1, device=DEV, generator=g))
@@ -100,10 +101,11 @@ def test_rows(rows, v, top, temperature, dtype):
     _check(z.to(dtype), tokens if rows % 2 else tokens.int(), temperature, top)
 
 
+@pytest.mark.parametrize("v", [9000, 45003])                       # whole rows; parts
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
-def test_masks(dtype):
+def test_masks(dtype, v):
     """Rows of nothing, of one word, of the type's lowest value, with it as a mask, far from zero, with more equal logits than the candidates have room for."""
-    v, low = 9000, torch.finfo(dtype).min
+    low = torch.finfo(dtype).min
     g = torch.Generator(device=DEV).manual_seed(1)
     z = torch.randn(12, v, device=DEV, generator=g)
     z[0] = -INF
@@ -123,8 +125,9 @@ def test_masks(dtype):
     for top in (0, 1, 5, 64):
         for temperature in (1.0, 0.25):
             _check(z.to(dtype), tokens, temperature, top)
-    many = z.repeat(60, 1).to(dtype)                              # the form for many rows
-    _check(many, tokens.repeat(60), 1.0, 20)
+    if v == 9000:
+        many = z.repeat(60, 1).to(dtype)
+        _check(many, tokens.repeat(60), 1.0, 20)
 
 
 def test_a_token_that_is_ruled_out():
@@ -138,9 +141,9 @@ def test_a_token_that_is_ruled_out():
 
 
 @pytest.mark.parametrize("bad", [NAN, INF])
-@pytest.mark.parametrize("rows", [2, 600])
-def test_rows_that_are_not_finite_are_nan_and_alone(rows, bad):
-    z = torch.randn(rows, 3000, device=DEV)
+@pytest.mark.parametrize("rows,v", [(2, 3000), (600, 3000), (2, 60000)])
+def test_rows_that_are_not_finite_are_nan_and_alone(rows, v, bad):
+    z = torch.randn(rows, v, device=DEV)
     z[1, 2000] = bad
     z[1, 4] = 50.0
     tokens = torch.full((rows,), 7, device=DEV)
@@ -247,6 +250,22 @@ def test_captured_and_replayed():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(kept, want))
+
+
+def test_more_rows_than_workgroups():
+    rows = (1 << 20) + 70001
+    z = (torch.arange(rows * 8, device=DEV).view(rows, 8) * 2654435761 % 1009).float() / 128
+    tokens = torch.arange(rows, device=DEV) % 8
+    logp, entropy, lse, ids, best = step.token_logprobs(z, tokens, 1.0, 2)
+    q = torch.log_softmax(z.double(), 1)
+    # 8 terms: a dozen roundings of values below 8 + log 8
+    assert float((logp - q.gather(1, tokens[:, None])[:, 0]).abs().max()) < 12 * 16 * F32
+    assert float((entropy + (q.exp() * q).sum(1)).abs().max()) < 24 * 16 * F32
+    assert torch.equal(ids[:, 0].long(), z.argmax(1)) or float((best[:, 0] - q.amax(1)).abs().max()) < 12 * 16 * F32
+    got = step.token_logprobs_grad(torch.ones(rows, device=DEV), None, z, tokens, lse, entropy)
+    want = -q.exp()
+    want.scatter_add_(1, tokens[:, None], torch.ones(rows, 1, device=DEV, dtype=torch.float64))
+    assert float((got - want).abs().max()) < 24 * 16 * F32
 
 
 def test_logits_beyond_32_bits():

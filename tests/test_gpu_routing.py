@@ -321,6 +321,43 @@ def test_both_ways_of_calling_give_the_same(monkeypatch):
     assert all(torch.equal(a, b) for a, b in zip(native, calls()))
 
 
+@pytest.mark.parametrize("n", [10, 200])
+def test_more_tokens_than_workgroups(n):
+    """300,001 tokens: every workgroup takes several."""
+    t, k = 300001, 3
+    z = (torch.arange(t, device=DEV)[:, None] * 7919 + torch.arange(n, device=DEV) * 104729) % 8191 / 1024.0
+    experts, weights = step.route(z, k)
+    top, want = z.sort(dim=1, descending=True, stable=True)
+    assert torch.equal(experts.long(), want[:, :k])
+    w = torch.softmax(top[:, :k].double(), 1)
+    assert float((weights - w).abs().max()) < 64 * F32               # differences below 8, three terms
+    dw = torch.randn(t, k, device=DEV)
+    each = w * dw
+    full = torch.zeros(t, n, device=DEV, dtype=torch.float64).scatter_(1, want[:, :k], each - w * each.sum(1, keepdim=True))
+    assert float((step.route_grad(dw, z, experts, weights) - full).abs().max()) < 256 * F32 * float(dw.abs().max())
+
+
+@pytest.mark.parametrize("d", [20, 520])
+def test_more_rows_than_workgroups(d):
+    """70,001 tokens of whole numbers, whose sums are exact."""
+    t, k, n = 70001, 2, 7
+    experts = (torch.arange(t * k, device=DEV) * 48271 % (n + 1)).view(t, k).int()          # n: dropped
+    places, offsets = step.expert_order(experts, n)
+    used, there, at = int(offsets[-1]), places >= 0, places.long().clamp(min=0)
+    number = lambda rows: (torch.arange(rows, device=DEV)[:, None] * 31 + torch.arange(d, device=DEV) * 17) % 61 - 30.0
+    x, y, w = number(t), number(t * k), (torch.arange(t * k, device=DEV).view(t, k) % 5).float()
+    rows = step.dispatch(x, places, offsets)
+    want = torch.zeros_like(rows)
+    want[at[there]] = x.repeat_interleave(k, 0)[there.view(-1)]
+    assert torch.equal(rows, want) and not rows[used:].any()
+    keep = there[..., None]
+    assert torch.equal(step.combine(y, places, w), (torch.where(keep, y[at], 0.0) * w[..., None]).sum(1))
+    assert torch.equal(step.dispatch_grad(y, places), torch.where(keep, y[at], 0.0).sum(1))
+    dy, dw = step.combine_grad(x, y, places, w, offsets)
+    want[at[there]] = (x[:, None, :] * w[..., None])[there]
+    assert torch.equal(dy, want) and torch.equal(dw, (torch.where(keep, y[at], 0.0) * x[:, None, :]).sum(2))
+
+
 def test_rows_beyond_32_bits():
     """Rows whose elements lie beyond 2^31 of the first."""
     t, d = 70000, 32768                                     # 2.3 G values
