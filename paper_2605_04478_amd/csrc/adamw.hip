@@ -44,8 +44,8 @@ struct AdamwJob {
   void *m, *v;
   float *m_scale, *v_scale, *master;
   float b1, b2, c1, c2, eps;
-  float up;                      // v is multiplied by it before the root is taken
   int n_tensors;
+  bool small_eps;                // roots of subnormal numbers count
 };
 static_assert(sizeof(AdamwJob) <= 4096, "arguments of a launch");
 
@@ -60,14 +60,14 @@ struct BeginJob {
   i64* count;
   const float* scale_by;
   Step* step;
-  double lr, b1, b2, weight_decay, scale, up;
+  double lr, b1, b2, weight_decay, scale;
   u64 seed;
 };
 __global__ void k_adamw_begin(BeginJob j) {
   const i64 t = ++*j.count;
   Step s;
   s.step_size = (float)(j.lr / (1.0 - pow(j.b1, (double)t)));
-  s.root = (float)(1.0 / sqrt(j.up * (1.0 - pow(j.b2, (double)t))));
+  s.root = (float)(1.0 / sqrt(1.0 - pow(j.b2, (double)t)));
   // (1 - lr wd would lose most of lr wd's bits in 32 of them)
   s.decay = (float)(j.lr * j.weight_decay);
   s.scale = (float)(j.scale_by ? j.scale * (double)*j.scale_by : j.scale);
@@ -181,10 +181,21 @@ __global__ __launch_bounds__(ADAMW_THREADS) void k_adamw(AdamwJob j) {
         most_m = fmaxf(most_m, fabsf(m[i]));
         most_v = max(most_v, __builtin_bit_cast(u32, v[i]));
       }
-      // (the card's square root and reciprocal, off by a step each)
-      const float ratio = m[i] * __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_sqrtf(v[i] * j.up), s.root, j.eps));
-      p[i] = p[i] - s.decay * p[i] - s.step_size * ratio;
     }
+    auto step_by = [&](auto root) {
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) {
+        // (the card's reciprocal, off by a step)
+        const float ratio = m[i] * __builtin_amdgcn_rcpf(fmaf(root(v[i]), s.root, j.eps));
+        p[i] = p[i] - s.decay * p[i] - s.step_size * ratio;
+      }
+    };
+    // the card's square root, off by a step, takes subnormal numbers for zero: what is next to them is moved up for it
+    if (j.small_eps) step_by([](float x) {
+      const bool low = x < 0x1p-96f;
+      return __builtin_amdgcn_sqrtf(x * (low ? 0x1p32f : 1.0f)) * (low ? 0x1p-16f : 1.0f);
+    });
+    else step_by([](float x) { return __builtin_amdgcn_sqrtf(x); });
     if constexpr (MASTERS) {
       // (behind the last element: zeros stay)
       Vec<float, EACH> q;
@@ -279,13 +290,13 @@ extern "C" ccld_status ccld_adamw(const ccld_adamw_args* a, void* stream) {
   if (st != CCLD_OK) return st;
   const hipStream_t hs = static_cast<hipStream_t>(stream);
   Step* const step = static_cast<Step*>(a->workspace);
-  // the card's root takes subnormal numbers for zero: beside an eps of 2^-60 that is nothing, beside a smaller one v is scaled out of their range
-  const double up = a->eps >= 0x1p-60 ? 1.0 : 0x1p24;
-  k_adamw_begin<<<1, 1, 0, hs>>>(BeginJob{a->count, a->scale_by, step, a->lr, a->beta1, a->beta2, a->weight_decay, a->scale, up, a->seed});
+  k_adamw_begin<<<1, 1, 0, hs>>>(BeginJob{a->count, a->scale_by, step, a->lr, a->beta1, a->beta2, a->weight_decay, a->scale, a->seed});
   AdamwJob j{};
   j.step = step;
   j.m = a->m; j.v = a->v; j.m_scale = a->m_scale; j.v_scale = a->v_scale; j.master = a->master;
-  j.b1 = (float)a->beta1; j.b2 = (float)a->beta2; j.c1 = (float)(1.0 - a->beta1); j.c2 = (float)(1.0 - a->beta2); j.eps = (float)a->eps; j.up = (float)up;
+  j.b1 = (float)a->beta1; j.b2 = (float)a->beta2; j.c1 = (float)(1.0 - a->beta1); j.c2 = (float)(1.0 - a->beta2); j.eps = (float)a->eps;
+  // What stands beside eps is the root over sqrt(1 - b2^t), at least sqrt(1 - b2): of a subnormal v up to 2^-63 / sqrt(1 - b2).  From here on that is at most a 2^-25th of eps.
+  j.small_eps = a->eps * sqrt(1.0 - a->beta2) < 0x1p-38;
   u32 groups = 0;
   auto flush = [&] {
     if (!groups) return;
