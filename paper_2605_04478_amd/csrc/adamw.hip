@@ -45,7 +45,7 @@ struct AdamwJob {
   float *m_scale, *v_scale, *master;
   float b1, b2, c1, c2, eps;
   int n_tensors;
-  bool small_eps;                // roots of subnormal numbers count
+  bool small_eps, far_eps;       // roots of subnormal numbers count; the card has no reciprocal of eps
 };
 static_assert(sizeof(AdamwJob) <= 4096, "arguments of a launch");
 
@@ -182,20 +182,20 @@ __global__ __launch_bounds__(ADAMW_THREADS) void k_adamw(AdamwJob j) {
         most_v = max(most_v, __builtin_bit_cast(u32, v[i]));
       }
     }
-    auto step_by = [&](auto root) {
+    auto step_by = [&](auto root, auto over) {
 #pragma unroll
-      for (int i = 0; i < EACH; ++i) {
-        // (the card's reciprocal, off by a step)
-        const float ratio = m[i] * __builtin_amdgcn_rcpf(fmaf(root(v[i]), s.root, j.eps));
-        p[i] = p[i] - s.decay * p[i] - s.step_size * ratio;
-      }
+      for (int i = 0; i < EACH; ++i) p[i] = p[i] - s.decay * p[i] - s.step_size * over(m[i], fmaf(root(v[i]), s.root, j.eps));
     };
-    // the card's square root, off by a step, takes subnormal numbers for zero: what is next to them is moved up for it
-    if (j.small_eps) step_by([](float x) {
+    // The card's square root and reciprocal, off by a step each, take subnormal numbers for zero and give none: where those count, what is next to them is moved up for the root, and
+    // quotients are divisions.
+    auto root = [](float x) { return __builtin_amdgcn_sqrtf(x); };
+    auto over = [](float x, float by) { return x * __builtin_amdgcn_rcpf(by); };
+    if (j.far_eps) step_by([](float x) { return sqrtf(x); }, [](float x, float by) { return x / by; });
+    else if (j.small_eps) step_by([&](float x) {
       const bool low = x < 0x1p-96f;
-      return __builtin_amdgcn_sqrtf(x * (low ? 0x1p32f : 1.0f)) * (low ? 0x1p-16f : 1.0f);
-    });
-    else step_by([](float x) { return __builtin_amdgcn_sqrtf(x); });
+      return root(x * (low ? 0x1p32f : 1.0f)) * (low ? 0x1p-16f : 1.0f);
+    }, over);
+    else step_by(root, over);
     if constexpr (MASTERS) {
       // (behind the last element: zeros stay)
       Vec<float, EACH> q;
@@ -295,8 +295,12 @@ extern "C" ccld_status ccld_adamw(const ccld_adamw_args* a, void* stream) {
   j.step = step;
   j.m = a->m; j.v = a->v; j.m_scale = a->m_scale; j.v_scale = a->v_scale; j.master = a->master;
   j.b1 = (float)a->beta1; j.b2 = (float)a->beta2; j.c1 = (float)(1.0 - a->beta1); j.c2 = (float)(1.0 - a->beta2); j.eps = (float)a->eps;
+  // an eps that 32 bits do not have is still no zero: what never had a gradient stays where it is
+  if (a->eps > 0) j.eps = std::max(j.eps, 0x1p-149f);
   // What stands beside eps is the root over sqrt(1 - b2^t), at least sqrt(1 - b2): of a subnormal v up to 2^-63 / sqrt(1 - b2).  From here on that is at most a 2^-25th of eps.
   j.small_eps = a->eps * sqrt(1.0 - a->beta2) < 0x1p-38;
+  // (the root of the smallest v is 2^-74.5, of the largest over sqrt(1 - b2) below 2^91: by themselves these have reciprocals)
+  j.far_eps = (a->eps > 0 && a->eps < 0x1p-126) || a->eps > 0x1p125;
   u32 groups = 0;
   auto flush = [&] {
     if (!groups) return;

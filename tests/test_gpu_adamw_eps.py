@@ -32,7 +32,8 @@ def _check(g, m0, v0, count, eps, betas, bits=32, lr=0.5):
     er = (em / (1 - b1 ** t) + ratio.abs() / (1 - b1 ** t) * eden) / (den - eden).clamp(min=1e-300) + 16 * F32 * ratio.abs() / (1 - b1 ** t)
     want = -lr * ratio / (1 - b1 ** t)
     er = torch.where((m0 == 0) & (g == 0), torch.zeros_like(er), er)         # a parameter that never had a gradient stays
-    close(p, want, lr * er + 4 * F32 * want.abs(), (eps, betas, bits))
+    # (the parameter itself is a 32-bit number)
+    close(p, want, lr * er + 4 * F32 * want.abs() + LEAST, (eps, betas, bits))
 
 
 def _first(g, eps, betas, bits, lr=0.5):
@@ -64,3 +65,22 @@ def test_later_steps(eps):
     v0[:20] = torch.ldexp(torch.ones(20, device=DEV), torch.arange(-148, -128, device=DEV).int())
     m0 = v0.sqrt() * torch.randn(300, device=DEV)
     _check(torch.zeros(300, device=DEV), m0, v0, 10 ** 6, eps, (0.9, 0.999))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("eps", [1e-30, 1e-38, 1e-40, 1e-45, 1e-60, 5e-324])
+def test_what_never_had_a_gradient_stays(eps, bits):
+    """m = v = 0: the ratio is 0 / eps, whatever 32 bits have of eps and its reciprocal."""
+    _first([0.0, -0.0, 1.0, 1e-18, 0.0, -1e10], eps, (0.9, 0.999), bits)
+
+
+@pytest.mark.parametrize("eps", [1e-37, 1e-38, 1e-39, 1e-40])
+def test_quotients_by_a_subnormal_eps(eps):
+    m0 = torch.tensor([1e-33, -1e-36, 1e-38, 0.0, 3e-35], device=DEV)
+    _check(torch.zeros_like(m0), m0, torch.zeros_like(m0), 10 ** 6, eps, (0.9, 0.999))
+
+
+@pytest.mark.parametrize("eps", [1e20, 1e38, 1.5e38, 1e300])
+def test_a_large_eps(eps):
+    """A step of 10^18 by ratios of 10^-18: a reciprocal that is subnormal is no zero."""
+    _first([1e18, -3e18, 1.0], eps, (0.0, 0.999), 32, lr=1e20)
