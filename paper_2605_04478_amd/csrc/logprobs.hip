@@ -60,17 +60,28 @@ __device__ __forceinline__ float largest_of(const float (&z)[N]) {
   return m;
 }
 
+// sum += x, where sum is `over` above what was added to it: with the rounding of one addition made good by the next, a sum of any length is off by two roundings
+__device__ __forceinline__ void add_to(float& sum, float& over, float x) {
+  const float y = x - over, t = sum + y;
+  over = (t - sum) - y;
+  sum = t;
+}
+
 // Sums of exp2((z - m) c) and of exp2((z - m) c) (m - z) c.  m follows the largest value seen where that is more than 2^8 times as large: a wavefront then moves a few times in a
-// row and not with almost every vector.  The second sum's terms below zero are at most 8 of the first's, which cost the entropy 2^-21 at most.
+// row and not with almost every vector.  The second sum's terms below zero are at most 8 times the first's, and its roundings with them: additions one after another, whose roundings may
+// all go one way, would cost the entropy up to 0.0002 with 1,024 values to a thread (and lse 0.00002).  A vector is therefore summed by itself and added to a sum that knows its
+// rounding: a vector's eight roundings and three more are left, 2^-18 in the entropy where all terms are at the far end (0.000002 was the most in either length, 512 or 1,024 values).
 constexpr float LEEWAY = 8.0f;
 struct Sums {
-  float m = LOWEST, s = 0, b = 0, most = LOWEST;
+  float m = LOWEST, s = 0, b = 0, s_over = 0, b_over = 0, most = LOWEST;
   // the same relative to another value, above m or some way below
   __device__ __forceinline__ void move(float to, float c) {
     if (to == LOWEST) return;
-    const float d = m == LOWEST ? 0.0f : (m - to) * c, f = __builtin_amdgcn_exp2f(d);
-    b = f * (b - s * fmaxf(d, NOTHING));
+    const float d = m == LOWEST ? 0.0f : (m - to) * c, f = __builtin_amdgcn_exp2f(d), by = fmaxf(d, NOTHING);
+    b = f * fmaf(-by, s, b);
+    b_over = f * fmaf(-by, s_over, b_over);
     s *= f;
+    s_over *= f;
     m = to;
   }
   template <int N>
@@ -78,12 +89,15 @@ struct Sums {
     most = fmaxf(most, largest_of(z));
     if ((most - m) * c > LEEWAY) move(most, c);
     const float from = m == LOWEST ? 0.0f : m;
+    float own_s = 0, own_b = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const float d = (z[i] - from) * c, e = __builtin_amdgcn_exp2f(d);
-      s += e;
-      b -= e * fmaxf(d, NOTHING);
+      own_s += e;
+      own_b -= e * fmaxf(d, NOTHING);
     }
+    add_to(s, s_over, own_s);
+    add_to(b, b_over, own_b);
   }
 };
 
@@ -380,8 +394,8 @@ __global__ __launch_bounds__(THREADS) void k_logprobs(LogprobJob j) {
     const float most = x.most;
     __syncthreads();                        // the row before is done with
     x.move(max_of_all<THREADS>(most, places[0]), c);
-    x.s = sum_of_all<THREADS>(x.s, places[1]);
-    x.b = sum_of_all<THREADS>(x.b, places[2]);
+    x.s = sum_of_all<THREADS>(x.s - x.s_over, places[1]);
+    x.b = sum_of_all<THREADS>(x.b - x.b_over, places[2]);
     if (j.parts > 1) {
       if (threadIdx.x == 0) { j.part_sums[3 * b] = x.m; j.part_sums[3 * b + 1] = x.s; j.part_sums[3 * b + 2] = x.b; }
       if (j.top)
@@ -461,7 +475,7 @@ __global__ __launch_bounds__(THREADS) void k_logprobs_grad(LogprobJob j) {
     const int t = (int)token_of(j, r);
     const bool none = lse == LOWEST;
     const float dl = !none && t >= 0 && j.dlogp ? j.dlogp[r * j.dlogp_stride] : 0.0f, de = !none && j.dentropy ? j.dentropy[r * j.dentropy_stride] : 0.0f;
-    float from = none ? 0.0f : lse * j.temperature, s = 0, rest = 0;
+    float from = none ? 0.0f : lse * j.temperature, s = 0, over = 0, rest = 0;
     if (!none) {
       if (!(fabsf(lse) < FAR)) {
         float m = LOWEST;
@@ -469,10 +483,13 @@ __global__ __launch_bounds__(THREADS) void k_logprobs_grad(LogprobJob j) {
         from = max_of_all<THREADS>(m, places[turn][1]);
       }
       held.each([&](const auto& z, auto) {
+        float own = 0;
 #pragma unroll
-        for (int n = 0; n < (int)(sizeof(z) / sizeof(float)); ++n) s += __builtin_amdgcn_exp2f((z[n] - from) * c);
+        for (int n = 0; n < (int)(sizeof(z) / sizeof(float)); ++n) own += __builtin_amdgcn_exp2f((z[n] - from) * c);
+        if constexpr (VECS == 0) add_to(s, over, own);
+        else s += own;                      // (17 of them at most)
       });
-      rest = log2f(sum_of_all<THREADS>(s, places[turn][0]));
+      rest = log2f(sum_of_all<THREADS>(s - over, places[turn][0]));
       turn ^= 1;                            // (a place is written again behind the next row's barrier)
     }
     // dlogits without the target's own: -p (k0 + k1 log2 p)
