@@ -63,17 +63,17 @@ struct Scores {
   }
 };
 
-// over the L lanes of a token, in all of them
+// Over the L lanes of a token, in all of them: pairs, fours, eights and so on exchange what they have, so that every lane adds the same two numbers and all have the same bits.
 template <int L, class T, class F>
 __device__ __forceinline__ T over_lanes(T v, F f) {
   auto with = [&](auto ctrl) {
     const int x = __builtin_bit_cast(int, v);
     v = f(v, __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(x, x, decltype(ctrl)::value, 0xF, 0xF, false)));
   };
-  with(std::integral_constant<int, 0x121>());          // row_ror: 1, 2, 4, 8
-  with(std::integral_constant<int, 0x122>());
-  with(std::integral_constant<int, 0x124>());
-  with(std::integral_constant<int, 0x128>());
+  with(std::integral_constant<int, 0xB1>());           // quad_perm: 1, 0, 3, 2
+  with(std::integral_constant<int, 0x4E>());           // quad_perm: 2, 3, 0, 1
+  with(std::integral_constant<int, 0x141>());          // row_half_mirror: 7 - i of eight
+  with(std::integral_constant<int, 0x140>());          // row_mirror: 15 - i
   if constexpr (L > 16) v = f(v, __shfl_xor(v, 16, CCLD_WAVE));
   if constexpr (L > 32) v = f(v, __shfl_xor(v, 32, CCLD_WAVE));
   return v;
