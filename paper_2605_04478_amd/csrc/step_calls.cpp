@@ -589,11 +589,12 @@ PyObject* adamw(PyObject* const* args) {
   ccld_adamw_args a{};
   a.dtype = a.grad_dtype = type_of(first, true);
   std::vector<ccld_adamw_tensor> tensors;
-  std::vector<Tensor> stepped, kept_grads;               // (held while the interpreter is left)
+  std::vector<Tensor> stepped, kept_grads, kept_states;  // (held while the interpreter is left: another thread may change the lists and the dict)
   std::vector<std::pair<uintptr_t, uintptr_t>> ranges;
   tensors.reserve(params.n);
   stepped.reserve(params.n);
   kept_grads.reserve(params.n);
+  kept_states.reserve(6);
   ranges.reserve(params.n);
   at::ScalarType grad_type = at::ScalarType::Undefined;
   for (Py_ssize_t i = 0; i < params.n; ++i) {
@@ -622,6 +623,7 @@ PyObject* adamw(PyObject* const* args) {
     require(o);
     const Tensor& t = tensor(o);
     d.vector(t, n, type);
+    kept_states.push_back(t);
     return t.data_ptr();
   };
   PyObject* const m = PyDict_GetItemString(state, "m");

@@ -835,6 +835,9 @@ def adamw(params, grads, state, lr: float, betas=(0.9, 0.999), eps: float = 1e-8
     at random, by `seed`, the count and the element.  A gradient that is not finite leaves NaN: in 8-bit states, in its whole block."""
     if _native().adamw(params, grads, state, lr, betas, eps, weight_decay, scale, seed) is not None:
         return
+    # (their own copies: another thread may change the caller's while this one is between its checks and the call)
+    params, grads = (list(x) if isinstance(x, (list, tuple)) else x for x in (params, grads))
+    state = dict(state) if isinstance(state, dict) else state
     device, grads, grad_dtype, bits, total = _adamw_inputs(params, grads, state, lr, betas, eps, weight_decay, scale, seed)
     if not params:
         return
