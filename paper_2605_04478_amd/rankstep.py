@@ -109,7 +109,10 @@ class RankStep:
 
 
 class RoutedStep(RankStep):
-    """A whole step of one rank: a router chooses `choices` experts for every token, and AdamW takes the gradients."""
+    """A whole step of one rank: a router chooses `choices` experts for every token, and AdamW takes the gradients.
+
+    With one choice the loss says nothing of the router: its only weight is one, and what another weight multiplied would be undone by the norm that
+    follows.  Its gradient is zero then, and the optimizer leaves it as it is.  All other weights decay alike, those of norms too."""
 
     def __init__(self, spec: StepSpec = StepSpec(), choices: int = 2, dtype=torch.bfloat16, device: str = "cuda:0", lr: float = 1e-3, weight_decay: float = 0.1,
                  bits: int = 32):
@@ -150,7 +153,8 @@ class RoutedStep(RankStep):
     def take(self, h, labels) -> torch.Tensor:
         """One whole step: the loss before it."""
         loss, grads = self.gradients(h, labels)
-        self.optimizer.step(grads)
+        routers = {id(layer["router"]) for layer in self.layers} if self.choices == 1 else ()
+        self.optimizer.step([None if id(w) in routers else g for w, g in zip(self.weights(), grads)])
         return loss
 
     @torch.no_grad()
