@@ -12,8 +12,9 @@
 // follow b2 = 0.999, whose steps are a hundredth of what two or three bits tell apart; values are rounded up or down at random, with the odds that keep
 // the mean.  The card converts and rounds both formats.
 //
-// Measured (a copy of 2 GB moves 4.9 TB/s here, x + 1 6.1): 200 tensors, 90M elements in bfloat16 with masters 406 us = 6.2 TB/s; 320M in bfloat16 with 8-bit states 561 us = 5.7 TB/s, where the sixty operations
-// of an element take nearly as long (732 with conversions and rounding by hand, exact root and quotient); six small tensors 2 + 4 us of a call's 8.7.
+// Measured (a copy of 2 GB moves 4.9 TB/s here, x + 1 6.1): 200 tensors, 90M elements in bfloat16 with masters 408 us = 6.2 TB/s; 320M in bfloat16 with 8-bit states 560 us = 5.7 TB/s, where the 61 instructions
+// of an element take 532 by themselves (575 where an eps is so small that roots of subnormal numbers count; 732 with conversions and rounding by hand, exact root and quotient), with 32-bit states 1,094 = 6.4, with
+// masters and 8-bit states 986, and gradients in 32 bits 1,120; six small tensors 2 + 4 us of a call's 8.8.
 #include <algorithm>
 
 #include <math.h>

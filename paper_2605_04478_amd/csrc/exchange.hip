@@ -9,6 +9,8 @@
 //
 // Measured (a copy of 2 GB moves 4.9 TB/s here, x + 1 6.1): 32,768 x 4,096 in bfloat16 with 8 experts: dispatch 462 us = 5.2 TB/s, combine and dispatch's gradient 445 = 5.4, combine's gradient 899 =
 // 5.1; 8,192 x 2,048 with 2: 15 to 17 and 26; 3,001 x 1,001 in half precision with 3, whose rows start anywhere: 5 to 7 and 10.  5 tokens: 3 us each.
+// Rows at odd addresses that the caches do not hold: every vector lies across two lines (18,289 x 997 in bfloat16 with 7 experts, other data each time: dispatch, combine, its gradient and dispatch's 76, 92, 188 and 89 us; x 1,000 69, 54, 118 and 54; a copy's rate
+// would be 60 and 112 for the gradient).
 #include <algorithm>
 
 #include "ccld_internal.h"
@@ -215,8 +217,9 @@ void launch(const ExchangeJob& j, Way way, hipStream_t stream) {
   constexpr int THREADS = threads_of(TEAM);
   const u32 grid = (u32)std::min<i64>(blocks_for(j.tokens, THREADS / TEAM), 64 * COMPUTE_UNITS);
   if (way == DISPATCH) {
-    // past the caches, but for rows of whole vectors that share lines with their neighbours: a line then goes to memory in two pieces (18,289 x 1,000 in bfloat16 with 7 experts 73 us, 52 through the
-    // caches; x 1,024 51 and 49; x 997, whose vectors lie across lines, 76 and 87; 32,768 x 4,096 with 8 460 and 470)
+    // Past the caches, but for rows of whole vectors that share lines with their neighbours: a line then goes to memory in two pieces.  What is left in the caches is there for who reads the rows next, or
+    // is written back while another kernel runs: 18,289 x 1,000 in bfloat16 with 7 experts, past and through the caches, takes 73 and 69 us call after call, 128 and 103 with a gather of the same rows behind it, 88 and 99 beside an addition to 256 MB;
+    // 4,000 x 1,000 17 and 12, 29 and 24, 20 and 32; 30,000 x 2,056 with 8 284 and 250, 486 and 479, 314 and 287.  (x 1,024 51 and 49; x 997, whose vectors lie across lines, 76 and 87; 32,768 x 4,096 with 8 460 and 470.)
     auto made_of = [&](i64 bytes) { return aligned(j.y_out, bytes) && j.ldy_out * (i64)sizeof(T) % bytes == 0; };
     if (made_of(128) || !made_of(16)) k_dispatch<T, TEAM, true><<<grid, THREADS, 0, stream>>>(j);
     else k_dispatch<T, TEAM, false><<<grid, THREADS, 0, stream>>>(j);

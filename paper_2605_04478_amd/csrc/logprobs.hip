@@ -15,8 +15,8 @@
 // 16 bits: half of a compute unit's registers), and the next row's vectors are asked for as this row's are written, so that a row is read once and loads do
 // not stop while it is computed.
 //
-// Measured (a copy of 2 GB moves 4.9 TB/s here, x + 1 6.1): 8,192 x 128,000 in bfloat16 356 us = 5.9 TB/s, with 20 alternatives 462, the gradient 775 = 5.4 (951 without the next row's loads, 1,160 with rows
-// read twice); 1,003 x 50,021 in 32 bits 47 and 64; 3 x 128,000 with 20 alternatives 8 + 5 us, without 4.5 + 2.7.
+// Measured (a copy of 2 GB moves 4.9 TB/s here, x + 1 6.1): 8,192 x 128,000 in bfloat16 356 us = 5.9 TB/s, with 20 alternatives 462, the gradient 775 = 5.4 (951 without the next row's loads); 1,003 x 50,021 in 32 bits 48 and
+// 65; rows that registers do not hold are read twice: 8,192 x 151,936 in bfloat16 425 and 1,430, 4,096 x 262,144 364 and 1,210, 2,000 x 128,000 in 32 bits 177 and 605; 3 x 128,000 with 20 alternatives 8 + 5 us, without 4.5 + 2.7.
 #include <algorithm>
 #include <type_traits>
 

@@ -7,8 +7,8 @@
 // The choice is bound by its instructions, not by memory: k times a maximum over a row and its removal.  A row therefore belongs to as few lanes as hold it in 16 registers
 // each, 16 lanes for up to 256 experts, so that a wavefront's instructions serve four tokens; maxima over 16 lanes take four instructions.
 //
-// Measured (a copy of 2 GB moves 4.9 TB/s here, x + 1 6.1): 65,536 x 256 in 32 bits, 8 experts, weights over all: 34 us (57 with a wavefront to a token; the scores are 67 MB, 14 us), gradient 24 us = 5.5
-// TB/s.  7 tokens: 3 us of a call's 5.  262,144 entries of 128 experts in order: 3 + 3 + 5 us; 16,384 of 8: 2.5 + 4.5; 20: 3.3.
+// Measured (a copy of 2 GB moves 4.9 TB/s here, x + 1 6.1): 65,536 x 256 in 32 bits, 8 experts, weights over all: 34 us (57 with a wavefront to a token; the scores are 67 MB, 14 us), of which the 1,241 instructions to four tokens
+// take 33; gradient 24 us = 5.5 TB/s.  In bfloat16 31 and 18, over the chosen 27 and 10 (8 us of bytes each way); 32,768 x 512 with 16 in 32 bits 51 and 24, in bfloat16 49 and 19.  7 tokens: 3 us of a call's 5.  262,144 entries of 128 experts in order: 3 + 3 + 5 us; 16,384 of 8: 2.5 + 4.5; 20: 3.3.
 #include <algorithm>
 #include <type_traits>
 

@@ -831,7 +831,8 @@ def adamw(params, grads, state, lr: float, betas=(0.9, 0.999), eps: float = 1e-8
     params are contiguous and of one type, bfloat16, float16 or float32; grads of that type or float32, all of one.  A tensor whose
     gradient is None is left as it is, with its state.  scale is a number, or a tensor of one float32 on the GPU (a clipping that was
     computed there).  The count is kept on the GPU: a captured step counts on when it is replayed (with
-    the rates that it was captured with).  8-bit states are rounded up or down
+    the rates that it was captured with).  It is one for all tensors, those without a gradient too: one whose first gradient comes late is corrected
+    with the count of the others, and its first step may be larger than lr.  With eps 0 a parameter that never had a gradient becomes NaN, as the formula has it.  8-bit states are rounded up or down
     at random, by `seed`, the count and the element.  A gradient that is not finite leaves NaN: in 8-bit states, in its whole block."""
     if _native().adamw(params, grads, state, lr, betas, eps, weight_decay, scale, seed) is not None:
         return
@@ -861,7 +862,8 @@ def adamw(params, grads, state, lr: float, betas=(0.9, 0.999), eps: float = 1e-8
 
 
 class AdamW:
-    """adamw with the state that it keeps: AdamW(params, lr), then step() after every backward pass."""
+    """adamw with the state that it keeps: AdamW(params, lr), then step() after every backward pass.  All of params have one weight decay: where some are to have another, there are
+    two of these."""
 
     def __init__(self, params, lr: float, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.0, bits: int = 32, masters: bool = False,
                  seed: int = 0):
